@@ -307,6 +307,79 @@ int pvq_decode_static_table(const uint32_t* d_codes, const uint8_t* d_scale_idx,
                             const float* d_levels, void* d_out, int64_t ld_out, uint32_t* d_status,
                             pvq_stream_t stream);
 
+/* ---- 8-bit floating point with a scale for each block of 128 ------------------------------ */
+
+/* Operators for what a model does with decoded weights and quantised activations: products of
+ * 8-bit matrices, and a backward pass whose activations were kept in 8 bits.  (The paper has no
+ * counterpart; it compares with formats of this kind.)
+ *
+ * The format: one e4m3 code a value (sign, 4 bits of exponent, 3 of mantissa, largest value 448)
+ * and one scale a block, a power of two 2^(byte - 127) kept as its byte (e8m0; 255 is NaN).  A
+ * block is 128 values of a row (the last of a row may be shorter), or, with `tile`, 128 x 128
+ * values (cut off at the matrix's ends).  A value is code * scale, exactly.
+ *   d_codes    rows x cols bytes, leading dimension ld_codes; 16-byte aligned, ld_codes a
+ *              multiple of 16.  Bytes behind a row's end are not read as values and not written.
+ *   d_scales   ceil(cols / 128) bytes a row of blocks, leading dimension ld_scales; 4-byte
+ *              aligned, ld_scales a multiple of 4 (pvq_fp8_scale_row_stride is the smallest).
+ *              The bytes behind a row's end up to the next multiple of 4 are read (and ignored),
+ *              so they have to be readable; they are not written.
+ * Every size is at least 1, rows and columns below 2^31, rows * ceil(cols / 128) below 2^31.
+ * Other matrices are row-major fp32 or bf16 (PVQ_DTYPE_*), 16-byte aligned, with a leading
+ * dimension that is a multiple of 4 (fp32) or 8 (bf16) elements.  Outputs may not overlap
+ * inputs or one another.  No call keeps anything, or needs a workspace; all can be captured into
+ * graphs.  Results do not depend on launch order: the same inputs give the same bits. */
+typedef struct {
+    uint8_t* d_codes;
+    uint8_t* d_scales;
+    int64_t rows, cols, ld_codes, ld_scales;
+    int tile; /* 0: blocks of 128 along a row; 1: blocks of 128 x 128 */
+} pvq_fp8_matrix;
+
+/* Bytes from one row of scales to the next: ceil(cols / 128) rounded up to 4; 0 if cols < 1. */
+size_t pvq_fp8_scale_row_stride(int64_t cols);
+
+/* Quantise the q->rows x q->cols matrix d_x (leading dimension ld) into q.  A block's scale is the
+ * smallest power of two s, at least 2^-126, with |x| <= 448 s for its finite values (1 if they are
+ * all zero); a code is x / s rounded to nearest even.  NaN and infinities become the code NaN
+ * (e4m3 has no infinity) and do not count for the scale. */
+int pvq_fp8_quantize(const void* d_x, int dtype, int64_t ld, const pvq_fp8_matrix* q, pvq_stream_t stream);
+
+/* The values of q: fp32 (exact), or bf16 (exact too unless they leave its range). */
+int pvq_fp8_dequantize(const pvq_fp8_matrix* q, void* d_out, int dtype, int64_t ld_out, pvq_stream_t stream);
+
+/* out[i][j] = sum_k a[i][k] b[j][k], or with transposed = 1  sum_k a[i][k] b[k][j]: activations
+ * times a weight [outputs][inputs], and a gradient times the same weight.  Sums are held in fp32
+ * and rounded once to the type of d_out.  Either matrix may be in blocks along rows or in tiles;
+ * a transposed b has to be in tiles (its scales have to be constant along k within a block;
+ * PVQ_ERR_UNSUPPORTED).  a->cols must be b's k.
+ *   d_status   optional device word; PVQ_STATUS_STAGING_TIMEOUT is OR-ed into it when a thread
+ *              block gave up waiting for its copies (a bounded wait; not expected to happen; its
+ *              part of the output is then not valid).  May be NULL. */
+int pvq_fp8_matmul(const pvq_fp8_matrix* a, const pvq_fp8_matrix* b, int transposed, void* d_out, int dtype, int64_t ld_out,
+                   uint32_t* d_status, pvq_stream_t stream);
+
+#define PVQ_ACT_SILU 0 /* g / (1 + e^-g) */
+#define PVQ_ACT_GELU 1 /* g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2 */
+
+/* The middle of a gated feed-forward block: h = act(gate) * up, computed in fp32 and quantised as by
+ * pvq_fp8_quantize, ready for the next product.  `gate` and `up`, if given, receive the two inputs
+ * in the same format, for pvq_fp8_gated_backward; NULL (both) in inference.  All three are in
+ * blocks along rows and of the same shape. */
+int pvq_fp8_gated(const void* d_gate, int64_t ld_gate, const void* d_up, int64_t ld_up, int dtype, int act, const pvq_fp8_matrix* h,
+                  const pvq_fp8_matrix* gate, const pvq_fp8_matrix* up, pvq_stream_t stream);
+
+/* Its backward pass from the values g, u that were kept: dgate = dh u act'(g), dup = dh act(g), of
+ * dh's type, computed in fp32 and rounded once. */
+int pvq_fp8_gated_backward(const void* d_dh, int64_t ld_dh, int dtype, const pvq_fp8_matrix* gate, const pvq_fp8_matrix* up, int act,
+                           void* d_dgate, int64_t ld_dgate, void* d_dup, int64_t ld_dup, pvq_stream_t stream);
+
+/* The gradient of a projection's weight from the 8-bit input that was kept:
+ * out[o][i] = sum_t dy[t][o] x[t][i], dy bf16 with x->rows rows and `outer` columns.  Sums are held in
+ * fp32 and rounded once to the type of d_out.  The values of x are taken as bf16 (exact unless
+ * they leave its range).  d_status as in pvq_fp8_matmul. */
+int pvq_fp8_weight_grad(const void* d_dy, int64_t outer, int64_t ld_dy, const pvq_fp8_matrix* x, void* d_out, int dtype, int64_t ld_out,
+                        uint32_t* d_status, pvq_stream_t stream);
+
 /* ---- bounds-checked build -------------------------------------------------------------- */
 
 /* Bits of the word of pvq_debug_status. */

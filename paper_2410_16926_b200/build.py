@@ -27,11 +27,15 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 
 
 def _sources():
-    return sorted(f for f in os.listdir(CSRC) if f.endswith(".cu"))
+    """The translation units, relative to CSRC: the codec's, and those of the 8-bit floating-point operators in fp8/."""
+    names = os.listdir(CSRC) + [os.path.join("fp8", f) for f in os.listdir(os.path.join(CSRC, "fp8"))]
+    return sorted(f for f in names if f.endswith(".cu"))
 
 
-def _headers_mtime():
-    paths = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
+def _headers_mtime(src):
+    """Of the headers that a translation unit may include: pvq.h and those of its own folder."""
+    d = os.path.dirname(os.path.join(CSRC, src))
+    paths = [os.path.join(d, f) for f in os.listdir(d) if f.endswith((".cuh", ".h"))]
     paths.append(os.path.join(ROOT, "include", "pvq.h"))
     return max(os.path.getmtime(p) for p in paths)
 
@@ -64,21 +68,20 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     objdir = os.path.join(OBJDIR, "debug") if debug else OBJDIR
     lib = DEBUG_LIB if debug else LIB
     os.makedirs(objdir, exist_ok=True)
-    hdr = _headers_mtime()
     jobs, objs = [], []
     sources = _sources()
     extra = []
     if debug:  # the shared-memory kernels only; the rest of the launchers answer "unsupported"
         sources = [f for f in sources if not f.startswith(("pvq_big", "pvq_wide"))]
         extra = ["-DPVQ_DEBUG"]
-    newest = max([hdr] + [os.path.getmtime(os.path.join(CSRC, f)) for f in sources])
+    newest = max(max(_headers_mtime(f), os.path.getmtime(os.path.join(CSRC, f))) for f in sources)
     if not force and os.path.exists(lib) and os.path.getmtime(lib) >= newest:
         return lib  # also where the objects are not at hand
     for src in sources:
         s = os.path.join(CSRC, src)
-        o = os.path.join(objdir, src[:-3] + ".o")
+        o = os.path.join(objdir, os.path.basename(src)[:-3] + ".o")
         objs.append(o)
-        if force or not os.path.exists(o) or os.path.getmtime(o) < max(os.path.getmtime(s), hdr):
+        if force or not os.path.exists(o) or os.path.getmtime(o) < max(os.path.getmtime(s), _headers_mtime(src)):
             cmd = ["nvcc"] + NVCC_FLAGS + extra + (["-Xptxas", "-v"] if verbose else []) + ["-c", s, "-o", o]
             jobs.append(cmd)
 

@@ -9,12 +9,14 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
+#include <optional>
 #include <vector>
 
 #include "pvq.h"
@@ -33,6 +35,13 @@ struct Entries {
     decltype(&pvq_decode_batched) decode_batched;
     decltype(&pvq_code_words) code_words;
     decltype(&pvq_scale_row_stride) scale_row_stride;
+    decltype(&pvq_fp8_quantize) fp8_quantize;
+    decltype(&pvq_fp8_dequantize) fp8_dequantize;
+    decltype(&pvq_fp8_matmul) fp8_matmul;
+    decltype(&pvq_fp8_gated) fp8_gated;
+    decltype(&pvq_fp8_gated_backward) fp8_gated_backward;
+    decltype(&pvq_fp8_weight_grad) fp8_weight_grad;
+    decltype(&pvq_fp8_scale_row_stride) fp8_scale_row_stride;
 } lib;
 PyObject* raise_error = nullptr;  // raise_error(status, where) raises PvqError
 PyObject *k_get, *k_x, *k_out, *k_codes, *k_scale_idx, *k_row_norm, *k_edges, *k_levels, *k_cols;
@@ -439,6 +448,331 @@ PyObject* bind_decode_batched(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the 8-bit floating-point operators
+
+// The device of a call's tensors: the first one's, which has to be the current one (the library launches there).
+struct Place {
+    std::optional<c10::Device> dev;
+};
+bool at_place(const at::Tensor& t, Place* p) {
+    if (!t.is_cuda()) {
+        PyErr_SetString(PyExc_ValueError, "expected a CUDA tensor");
+        return false;
+    }
+    if (p->dev ? t.device() != *p->dev : t.device().index() != c10::cuda::current_device()) {
+        PyErr_SetString(PyExc_ValueError, "expected tensors on the current device");
+        return false;
+    }
+    p->dev = t.device();
+    return true;
+}
+
+// A matrix with unit steps along its rows; *ld is its leading dimension, for a single row the smallest multiple of `unit`.
+const at::Tensor* matrix(PyObject* o, Place* place, int64_t unit, int64_t* ld) {
+    const at::Tensor* t = tensor_of(o);
+    if (!t || !at_place(*t, place)) return nullptr;
+    if (t->dim() != 2) {
+        PyErr_SetString(PyExc_ValueError, "expected a matrix");
+        return nullptr;
+    }
+    if (t->size(1) > 1 && t->stride(1) != 1) {
+        PyErr_SetString(PyExc_ValueError, "expected a row-major tensor");
+        return nullptr;
+    }
+    *ld = t->size(0) > 1 ? t->stride(0) : (t->size(1) + unit - 1) / unit * unit;
+    return t;
+}
+
+bool typed(const at::Tensor& t, at::ScalarType type) {
+    if (t.scalar_type() == type) return true;
+    PyErr_Format(PyExc_TypeError, "expected dtype %s, got %s", c10::toString(type), c10::toString(t.scalar_type()));
+    return false;
+}
+
+struct Values {  // an fp32 or bf16 matrix
+    const at::Tensor* t;
+    void* p;
+    int dtype;
+    int64_t rows, cols, ld;
+};
+bool values(PyObject* o, Place* place, Values* v) {
+    v->t = tensor_of(o);
+    if (!v->t) return false;
+    if (v->t->scalar_type() == at::kFloat)
+        v->dtype = PVQ_DTYPE_F32;
+    else if (v->t->scalar_type() == at::kBFloat16)
+        v->dtype = PVQ_DTYPE_BF16;
+    else {
+        PyErr_SetString(PyExc_TypeError, "input must be float32 or bfloat16");
+        return false;
+    }
+    if (!matrix(o, place, v->dtype == PVQ_DTYPE_BF16 ? 8 : 4, &v->ld)) return false;
+    v->p = v->t->data_ptr();
+    v->rows = v->t->size(0);
+    v->cols = v->t->size(1);
+    return true;
+}
+
+bool shaped(const Values& v, int64_t rows, int64_t cols) {
+    if (v.rows == rows && v.cols == cols) return true;
+    PyErr_Format(PyExc_ValueError, "expected a matrix of %lld x %lld", static_cast<long long>(rows), static_cast<long long>(cols));
+    return false;
+}
+
+// An output of the given type: the caller's, or a new one whose rows start on 16-byte boundaries.  *result is a new reference.
+bool values_out(PyObject* o, Place* place, int dtype, int64_t rows, int64_t cols, Values* v, PyObject** result) {
+    if (o != Py_None) {
+        if (!values(o, place, v)) return false;
+        if (v->dtype != dtype) {
+            PyErr_SetString(PyExc_TypeError, "the output is of another type");
+            return false;
+        }
+        if (!shaped(*v, rows, cols)) return false;
+        Py_INCREF(o);
+        *result = o;
+        return true;
+    }
+    const int64_t unit = dtype == PVQ_DTYPE_BF16 ? 8 : 4;
+    v->dtype = dtype, v->rows = rows, v->cols = cols, v->ld = (cols + unit - 1) / unit * unit;
+    at::Tensor t = at::detail::empty_cuda({rows, v->ld}, dtype == PVQ_DTYPE_BF16 ? at::kBFloat16 : at::kFloat, *place->dev, std::nullopt);
+    v->p = t.data_ptr();
+    if (v->ld != cols) t = t.narrow(1, 0, cols);
+    *result = THPVariable_Wrap(std::move(t));
+    return *result != nullptr;
+}
+
+// A matrix of the format from its codes, scales and kind.
+bool fp8_matrix(PyObject* codes, PyObject* scales, PyObject* tile, Place* place, pvq_fp8_matrix* m) {
+    const at::Tensor* c = matrix(codes, place, 16, &m->ld_codes);
+    if (!c || !typed(*c, at::kFloat8_e4m3fn)) return false;
+    const at::Tensor* s = matrix(scales, place, 4, &m->ld_scales);
+    if (!s || !typed(*s, at::kFloat8_e8m0fnu)) return false;
+    const int t = PyObject_IsTrue(tile);
+    if (t < 0) return false;
+    m->tile = t;
+    m->rows = c->size(0);
+    m->cols = c->size(1);
+    if (s->size(0) != (t ? (m->rows + 127) / 128 : m->rows) || s->size(1) != (m->cols + 127) / 128) {
+        PyErr_SetString(PyExc_ValueError, "the scales are not those of these codes");
+        return false;
+    }
+    m->d_codes = static_cast<uint8_t*>(c->data_ptr());
+    m->d_scales = static_cast<uint8_t*>(s->data_ptr());
+    return true;
+}
+
+// A new matrix of the format: codes and scales go to *first and *second (new references).
+bool fp8_new(const Place& place, int64_t rows, int64_t cols, bool tile, pvq_fp8_matrix* m, PyObject** first, PyObject** second) {
+    const int64_t blocks = (cols + 127) / 128, down = tile ? (rows + 127) / 128 : rows;
+    m->rows = rows, m->cols = cols, m->tile = tile;
+    m->ld_codes = (cols + 15) / 16 * 16;
+    m->ld_scales = static_cast<int64_t>(lib.fp8_scale_row_stride(cols));
+    at::Tensor c = at::detail::empty_cuda({rows, m->ld_codes}, at::kFloat8_e4m3fn, *place.dev, std::nullopt);
+    at::Tensor s = at::detail::empty_cuda({down, m->ld_scales}, at::kFloat8_e8m0fnu, *place.dev, std::nullopt);
+    m->d_codes = static_cast<uint8_t*>(c.data_ptr());
+    m->d_scales = static_cast<uint8_t*>(s.data_ptr());
+    if (m->ld_codes != cols) c = c.narrow(1, 0, cols);
+    if (m->ld_scales != blocks) s = s.narrow(1, 0, blocks);
+    *first = THPVariable_Wrap(std::move(c));
+    *second = THPVariable_Wrap(std::move(s));
+    return *first && *second;
+}
+// ... or the caller's, a pair of tensors
+bool fp8_out(PyObject* o, Place* place, int64_t rows, int64_t cols, PyObject* tile, pvq_fp8_matrix* m, PyObject** first, PyObject** second) {
+    const int t = PyObject_IsTrue(tile);
+    if (t < 0) return false;
+    if (o == Py_None) return fp8_new(*place, rows, cols, t, m, first, second);
+    PyObject* seq = PySequence_Tuple(o);
+    if (!seq) return false;
+    bool ok = PyTuple_GET_SIZE(seq) >= 2;
+    if (!ok) PyErr_SetString(PyExc_ValueError, "expected codes and scales");
+    ok = ok && fp8_matrix(PyTuple_GET_ITEM(seq, 0), PyTuple_GET_ITEM(seq, 1), tile, place, m);
+    if (ok && (m->rows != rows || m->cols != cols)) {
+        PyErr_SetString(PyExc_ValueError, "the output has another shape");
+        ok = false;
+    }
+    if (ok) {
+        *first = PyTuple_GET_ITEM(seq, 0);
+        *second = PyTuple_GET_ITEM(seq, 1);
+        Py_INCREF(*first);
+        Py_INCREF(*second);
+    }
+    Py_DECREF(seq);
+    return ok;
+}
+
+bool status_word(PyObject* o, Place* place, void** out) {
+    *out = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = tensor_of(o);
+    if (!t || !at_place(*t, place) || !typed(*t, at::kInt)) return false;
+    if (t->numel() < 1) {
+        PyErr_SetString(PyExc_ValueError, "expected a status word");
+        return false;
+    }
+    *out = t->data_ptr();
+    return true;
+}
+
+struct Refs {  // results that a failed call drops
+    PyObject* r[6] = {};
+    PyObject* tuple(int n) {
+        PyObject* t = PyTuple_New(n);
+        for (int i = 0; t && i < n; ++i) {
+            PyTuple_SET_ITEM(t, i, r[i]);
+            r[i] = nullptr;
+        }
+        return t;
+    }
+    PyObject* one() {
+        PyObject* o = r[0];
+        r[0] = nullptr;
+        return o;
+    }
+    ~Refs() {
+        for (PyObject* o : r) Py_XDECREF(o);
+    }
+};
+
+// fp8_quantize(x, tile, out) -> (codes, scales)
+PyObject* bind_fp8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Place place;
+    Values x;
+    pvq_fp8_matrix q;
+    Refs refs;
+    if (!want_args(n, 3) || !values(a[0], &place, &x) || !fp8_out(a[2], &place, x.rows, x.cols, a[1], &q, &refs.r[0], &refs.r[1])) return nullptr;
+    void* s = stream();
+    if (failed(unlocked([&] { return lib.fp8_quantize(x.p, x.dtype, x.ld, &q, s); }), "pvq_fp8_quantize")) return nullptr;
+    return refs.tuple(2);
+    END_HANDLE_TH_ERRORS
+}
+
+// fp8_dequantize(codes, scales, tile, dtype, out)
+PyObject* bind_fp8_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Place place;
+    Values out;
+    pvq_fp8_matrix q;
+    Refs refs;
+    long long dtype;
+    if (!want_args(n, 5) || !fp8_matrix(a[0], a[1], a[2], &place, &q) || !integer(a[3], &dtype) ||
+        !values_out(a[4], &place, static_cast<int>(dtype), q.rows, q.cols, &out, &refs.r[0]))
+        return nullptr;
+    void* s = stream();
+    if (failed(unlocked([&] { return lib.fp8_dequantize(&q, out.p, out.dtype, out.ld, s); }), "pvq_fp8_dequantize")) return nullptr;
+    return refs.one();
+    END_HANDLE_TH_ERRORS
+}
+
+// fp8_matmul(codes a, scales a, tile a, codes b, scales b, tile b, transposed, dtype, out, status)
+PyObject* bind_fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Place place;
+    Values out;
+    pvq_fp8_matrix ma, mb;
+    Refs refs;
+    long long dtype;
+    void* status;
+    if (!want_args(n, 10) || !fp8_matrix(a[0], a[1], a[2], &place, &ma) || !fp8_matrix(a[3], a[4], a[5], &place, &mb)) return nullptr;
+    const int transposed = PyObject_IsTrue(a[6]);
+    if (transposed < 0 || !integer(a[7], &dtype)) return nullptr;
+    if (ma.cols != (transposed ? mb.rows : mb.cols)) {
+        PyErr_SetString(PyExc_ValueError, "the matrices do not fit one another");
+        return nullptr;
+    }
+    if (!values_out(a[8], &place, static_cast<int>(dtype), ma.rows, transposed ? mb.cols : mb.rows, &out, &refs.r[0]) ||
+        !status_word(a[9], &place, &status))
+        return nullptr;
+    void* s = stream();
+    if (failed(unlocked([&] { return lib.fp8_matmul(&ma, &mb, transposed, out.p, out.dtype, out.ld, static_cast<uint32_t*>(status), s); }), "pvq_fp8_matmul"))
+        return nullptr;
+    return refs.one();
+    END_HANDLE_TH_ERRORS
+}
+
+// fp8_gated(gate, up, act, checkpoint) -> (h codes, h scales) or with the two checkpoints' behind
+PyObject* bind_fp8_gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Place place;
+    Values gate, up;
+    pvq_fp8_matrix q[3];
+    Refs refs;
+    long long act;
+    if (!want_args(n, 4) || !values(a[0], &place, &gate) || !values(a[1], &place, &up) || !integer(a[2], &act)) return nullptr;
+    const int keep = PyObject_IsTrue(a[3]);
+    if (keep < 0 || !shaped(up, gate.rows, gate.cols)) return nullptr;
+    if (up.dtype != gate.dtype) {
+        PyErr_SetString(PyExc_TypeError, "gate and up are of different types");
+        return nullptr;
+    }
+    for (int i = 0; i < (keep ? 3 : 1); ++i)
+        if (!fp8_new(place, gate.rows, gate.cols, false, &q[i], &refs.r[2 * i], &refs.r[2 * i + 1])) return nullptr;
+    void* s = stream();
+    if (failed(unlocked([&] {
+                   return lib.fp8_gated(gate.p, gate.ld, up.p, up.ld, gate.dtype, static_cast<int>(act), &q[0], keep ? &q[1] : nullptr,
+                                        keep ? &q[2] : nullptr, s);
+               }),
+               "pvq_fp8_gated"))
+        return nullptr;
+    return refs.tuple(keep ? 6 : 2);
+    END_HANDLE_TH_ERRORS
+}
+
+// fp8_gated_backward(dh, codes gate, scales gate, codes up, scales up, act, dgate or None, dup or None) -> (dgate, dup)
+PyObject* bind_fp8_gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Place place;
+    Values dh, dgate, dup;
+    pvq_fp8_matrix gate, up;
+    Refs refs;
+    long long act;
+    if (!want_args(n, 8) || !values(a[0], &place, &dh) || !fp8_matrix(a[1], a[2], Py_False, &place, &gate) ||
+        !fp8_matrix(a[3], a[4], Py_False, &place, &up) || !integer(a[5], &act))
+        return nullptr;
+    if (gate.rows != up.rows || gate.cols != up.cols || !shaped(dh, gate.rows, gate.cols)) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "gate and up have different shapes");
+        return nullptr;
+    }
+    if (!values_out(a[6], &place, dh.dtype, dh.rows, dh.cols, &dgate, &refs.r[0]) || !values_out(a[7], &place, dh.dtype, dh.rows, dh.cols, &dup, &refs.r[1]))
+        return nullptr;
+    void* s = stream();
+    if (failed(unlocked([&] {
+                   return lib.fp8_gated_backward(dh.p, dh.ld, dh.dtype, &gate, &up, static_cast<int>(act), dgate.p, dgate.ld, dup.p, dup.ld, s);
+               }),
+               "pvq_fp8_gated_backward"))
+        return nullptr;
+    return refs.tuple(2);
+    END_HANDLE_TH_ERRORS
+}
+
+// fp8_weight_grad(dy, codes x, scales x, tile x, dtype, out, status)
+PyObject* bind_fp8_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Place place;
+    Values dy, out;
+    pvq_fp8_matrix x;
+    Refs refs;
+    long long dtype;
+    void* status;
+    if (!want_args(n, 7) || !values(a[0], &place, &dy) || !typed(*dy.t, at::kBFloat16) || !fp8_matrix(a[1], a[2], a[3], &place, &x) ||
+        !integer(a[4], &dtype))
+        return nullptr;
+    if (dy.rows != x.rows) {
+        PyErr_SetString(PyExc_ValueError, "dy and x have different numbers of rows");
+        return nullptr;
+    }
+    if (!values_out(a[5], &place, static_cast<int>(dtype), dy.cols, x.cols, &out, &refs.r[0]) || !status_word(a[6], &place, &status)) return nullptr;
+    void* s = stream();
+    if (failed(unlocked([&] {
+                   return lib.fp8_weight_grad(dy.p, dy.cols, dy.ld, &x, out.p, out.dtype, out.ld, static_cast<uint32_t*>(status), s);
+               }),
+               "pvq_fp8_weight_grad"))
+        return nullptr;
+    return refs.one();
+    END_HANDLE_TH_ERRORS
+}
+
 // init(raise_error, address of every entry of `Entries`, in its order)
 PyObject* bind_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     constexpr Py_ssize_t count = sizeof(Entries) / sizeof(void*);
@@ -466,6 +800,12 @@ PyMethodDef methods[] = {method<bind_init>("init"),
                          method<bind_rotate_roundtrip>("rotate_roundtrip"),
                          method<bind_encode_batched>("encode_batched"),
                          method<bind_decode_batched>("decode_batched"),
+                         method<bind_fp8_quantize>("fp8_quantize"),
+                         method<bind_fp8_dequantize>("fp8_dequantize"),
+                         method<bind_fp8_matmul>("fp8_matmul"),
+                         method<bind_fp8_gated>("fp8_gated"),
+                         method<bind_fp8_gated_backward>("fp8_gated_backward"),
+                         method<bind_fp8_weight_grad>("fp8_weight_grad"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods};
 

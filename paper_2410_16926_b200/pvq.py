@@ -7,6 +7,7 @@ of the codec happens here, and there is no fallback: a missing library is an
 error.  The set-up calls go through ctypes; the hot calls do the same work in a
 CPython extension (csrc/bind/pvq_bind.cpp), handed the library's entry points.
 """
+import collections
 import ctypes as C
 import importlib.machinery
 import importlib.util
@@ -47,6 +48,12 @@ class MatrixDesc(C.Structure):
                 ("ld_out", C.c_int64)]
 
 
+class Fp8Desc(C.Structure):
+    """Mirror of pvq_fp8_matrix."""
+    _fields_ = [("d_codes", C.c_void_p), ("d_scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ld_codes", C.c_int64), ("ld_scales", C.c_int64), ("tile", C.c_int)]
+
+
 def lib():
     """The loaded C library; raises if it has not been built."""
     global _lib
@@ -78,6 +85,15 @@ def lib():
         L.pvq_rotate_encode.argtypes = [vp, i32, i64, i64, i64, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
         L.pvq_rotate_roundtrip.argtypes = [vp, i32, i64, i64, i64, i32, vp, i32, i32, i32, vp, vp, vp, vp, i64, vp]
         L.pvq_decode_static_table.argtypes = [vp, vp, vp, i64, i64, i32, i32, i32, vp, vp, i64, vp, vp]
+        fp8 = C.POINTER(Fp8Desc)
+        L.pvq_fp8_scale_row_stride.argtypes = [i64]
+        L.pvq_fp8_scale_row_stride.restype = sz
+        L.pvq_fp8_quantize.argtypes = [vp, i32, i64, fp8, vp]
+        L.pvq_fp8_dequantize.argtypes = [fp8, vp, i32, i64, vp]
+        L.pvq_fp8_matmul.argtypes = [fp8, fp8, i32, vp, i32, i64, vp, vp]
+        L.pvq_fp8_gated.argtypes = [vp, i64, vp, i64, i32, i32, fp8, fp8, fp8, vp]
+        L.pvq_fp8_gated_backward.argtypes = [vp, i64, i32, fp8, fp8, i32, vp, i64, vp, i64, vp]
+        L.pvq_fp8_weight_grad.argtypes = [vp, i64, i64, fp8, vp, i32, i64, vp, vp]
         L.pvq_debug_status.argtypes = [vp]
         L.pvq_encode_status.argtypes = [vp]
         _lib = L
@@ -88,7 +104,8 @@ EXPORTS = ["pvq_strerror", "pvq_last_cuda_error", "pvq_index_bits", "pvq_max_pul
            "pvq_count_table_bytes", "pvq_scale_row_stride", "pvq_build_count_table",
            "pvq_build_scale_codebook", "pvq_encode", "pvq_decode", "pvq_roundtrip", "pvq_encode_batched",
            "pvq_decode_batched", "pvq_decode_static_table", "pvq_rotate_encode", "pvq_rotate_roundtrip", "pvq_encode_amp",
-           "pvq_debug_status", "pvq_encode_status"]
+           "pvq_debug_status", "pvq_encode_status", "pvq_fp8_scale_row_stride", "pvq_fp8_quantize", "pvq_fp8_dequantize",
+           "pvq_fp8_matmul", "pvq_fp8_gated", "pvq_fp8_gated_backward", "pvq_fp8_weight_grad"]
 
 
 def _check(status, where):
@@ -110,7 +127,8 @@ def _load_native():
     m = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_bind", BIND_PATH, loader=loader))
     loader.exec_module(m)
     names = ("encode", "encode_amp", "decode", "roundtrip", "rotate_encode", "rotate_roundtrip", "encode_batched",
-             "decode_batched", "code_words", "scale_row_stride")
+             "decode_batched", "code_words", "scale_row_stride", "fp8_quantize", "fp8_dequantize", "fp8_matmul", "fp8_gated",
+             "fp8_gated_backward", "fp8_weight_grad", "fp8_scale_row_stride")
     m.init(_raise, *(C.cast(getattr(L, "pvq_" + n), C.c_void_p).value for n in names))
     _native = m
     return m
@@ -260,3 +278,71 @@ def encode_batched(items, dtype, N, K, scale_bits, table):
 def decode_batched(items, N, K, scale_bits, table, status=None):
     """items: dicts with out, codes, scale_idx, row_norm, levels, cols.  One launch."""
     (_native or _load_native()).decode_batched(items, N, K, scale_bits, table, status)
+
+
+# ---- 8-bit floating point with a scale for each block of 128 ------------------------
+
+# codes: float8_e4m3fn [rows][cols]; scales: float8_e8m0fnu [rows][ceil(cols / 128)], or, where `tile` is true,
+# [ceil(rows / 128)][ceil(cols / 128)].  Rows of codes start on 16-byte boundaries, rows of scales on 4-byte boundaries
+# (the calls' results do; where the widths are no such multiples, they are views of wider tensors).
+Fp8Matrix = collections.namedtuple("Fp8Matrix", "codes scales tile")
+
+ACTIVATIONS = {"silu": 0, "gelu": 1}
+
+
+def _value_type(dtype):
+    if dtype == torch.bfloat16:
+        return DTYPE_BF16
+    if dtype == torch.float32:
+        return DTYPE_F32
+    raise TypeError("expected float32 or bfloat16, got %s" % dtype)
+
+
+def _activation(act):
+    try:
+        return ACTIVATIONS[act]
+    except KeyError:
+        raise ValueError("unknown activation %r (one of %s)" % (act, ", ".join(sorted(ACTIVATIONS)))) from None
+
+
+def fp8_quantize(x, tile=False, out=None):
+    """x [rows][cols] float32 / bfloat16 -> Fp8Matrix, in blocks of 128 along the rows or, with `tile`, of 128 x 128.
+    `out`: an Fp8Matrix of the same shape and kind to write into."""
+    tile = bool(tile)
+    if out is not None and len(out) > 2 and bool(out[2]) != tile:
+        raise ValueError("the output is of the other kind of blocks")
+    codes, scales = (_native or _load_native()).fp8_quantize(x, tile, out)
+    return Fp8Matrix(codes, scales, tile)
+
+
+def fp8_dequantize(q, dtype=torch.bfloat16, out=None):
+    """The values of an Fp8Matrix, as bfloat16 or float32."""
+    return (_native or _load_native()).fp8_dequantize(q[0], q[1], q[2], _value_type(dtype), out)
+
+
+def fp8_matmul(a, b, transposed=False, dtype=torch.bfloat16, out=None, status=None):
+    """a [M][K] times b [N][K] transposed (activations times a weight), or, with `transposed`, a [M][K] times b [K][N] (a
+    gradient times the same weight; b in tiles) -> [M][N].  `status`: optional int32 device tensor of one element."""
+    return (_native or _load_native()).fp8_matmul(a[0], a[1], a[2], b[0], b[1], b[2], transposed, _value_type(dtype), out, status)
+
+
+def fp8_gated(gate, up, act="silu", checkpoint=False):
+    """act(gate) * up of a gated feed-forward block -> Fp8Matrix; with `checkpoint` also gate and up in 8 bits, for
+    fp8_gated_backward.  act: "silu" or "gelu" (the form with tanh)."""
+    r = (_native or _load_native()).fp8_gated(gate, up, _activation(act), checkpoint)
+    if len(r) == 2:
+        return Fp8Matrix(r[0], r[1], False)
+    return Fp8Matrix(r[0], r[1], False), Fp8Matrix(r[2], r[3], False), Fp8Matrix(r[4], r[5], False)
+
+
+def fp8_gated_backward(dh, gate, up, act="silu", out=(None, None)):
+    """The gradients (dgate, dup) from dh and the checkpoints of fp8_gated, of dh's type.  `out`: tensors to write them
+    into, for instance the two halves of one matrix."""
+    if gate[2] or up[2]:
+        raise ValueError("expected blocks along rows")
+    return (_native or _load_native()).fp8_gated_backward(dh, gate[0], gate[1], up[0], up[1], _activation(act), *out)
+
+
+def fp8_weight_grad(dy, x, dtype=torch.float32, out=None, status=None):
+    """dy [tokens][outputs] bfloat16 transposed, times the values of x [tokens][inputs] -> [outputs][inputs]."""
+    return (_native or _load_native()).fp8_weight_grad(dy, x[0], x[1], x[2], _value_type(dtype), out, status)
