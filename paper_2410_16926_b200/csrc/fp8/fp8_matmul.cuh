@@ -1,0 +1,20 @@
+// The two kernels of the 8-bit product and what they take.
+#pragma once
+#include "fp8_mma.cuh"
+
+namespace pvq {
+namespace fp8 {
+
+struct MatmulArgs {
+    Matrix a, b;
+    void* out;
+    int64_t rows, outs, inner, ld;  // a.rows, columns of the result, k
+    uint32_t* status;
+};
+// Few rows: 128 columns of the result by up to 128 rows a thread block, k split over `split` blocks of a cluster.
+int matmul_few(const MatmulArgs& p, bool transposed, bool bf16, int split, cudaStream_t s);
+// Many rows: 256 x 256 of the result a pair of thread blocks.
+int matmul_many(const MatmulArgs& p, bool transposed, bool bf16, cudaStream_t s);
+
+}  // namespace fp8
+}  // namespace pvq

@@ -1,0 +1,229 @@
+// The 8-bit product of few rows, or of little work: out[i][j] = sum_k a(i,k) b(j,k), bound by reading b.
+//
+// The operands change places: 128 columns of the result (rows of b, the weight) are the product's 128 lanes, ROWS rows of a
+// (16 to 128) its columns, so that a token costs 1/16 of a tile's width and not 1/128 of its height.  k is split over the
+// blocks of a cluster where there are few tiles: each sums its part in tensor memory, puts it into its shared memory, and
+// then every block adds the parts of its share of the columns, in the order of the ranks (no atomics: the same bits every
+// time), reading the others' shared memory.
+//
+// Warps: one issues the copies, one the products, one allocates tensor memory, four bring the scales there (double-buffered,
+// four blocks along k at a time) and then read the result.
+#include "fp8_matmul.cuh"
+
+namespace pvq {
+namespace fp8 {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <int ROWS>
+struct Shape {
+    static constexpr int kStageBytes = (128 + ROWS) * kBlock;
+    static constexpr int kStages = ROWS <= 32 ? 5 : (ROWS == 64 ? 4 : 6);  // two blocks an SM up to 64 rows
+    static constexpr int kWordsB = ROWS <= 32 ? 1 : ROWS / 32;             // of scales, a lane
+    static constexpr int kScales = ROWS < 32 ? 32 : ROWS;                  // columns before them
+    static constexpr int kColumns = ROWS == 128 ? 256 : (ROWS == 64 ? 128 : 64);  // of tensor memory: ROWS + 2 * (4 + 4) at most, a power of two
+    static constexpr size_t kShared = 1024 + kStages * kStageBytes + 256;
+    static_assert(kStages * kStageBytes >= ROWS * 512, "the result takes the stages' place");
+    static_assert(kScales + 16 <= kColumns, "tensor memory");
+};
+
+struct Maps {
+    CUtensorMap a, b;
+};
+
+template <int ROWS, bool ACROSS, class T>
+__global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_constant__ Maps maps, const __grid_constant__ MatmulArgs p, int split) {
+    using S = Shape<ROWS>;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
+    const uint32_t full = base + S::kStages * S::kStageBytes, empty = full + 8 * S::kStages, scales_full = empty + 8 * S::kStages,
+                   scales_empty = scales_full + 16, sum_full = scales_empty + 16;
+    __shared__ uint32_t tensor_base;
+    __shared__ int over;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = blockIdx.x % split;  // in the cluster
+    if (threadIdx.x == 0) {
+        over = 0;
+        for (int i = 0; i < S::kStages; ++i) barrier_init(full + 8 * i, 1), barrier_init(empty + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) barrier_init(scales_full + 8 * i, 4), barrier_init(scales_empty + 8 * i, 1);
+        barrier_init(sum_full, 1);
+        barrier_init_fence();
+        prefetch_map(&maps.a), prefetch_map(&maps.b);
+    }
+    if (warp == 2) tensor_alloc<false>(shared_address(&tensor_base), S::kColumns);
+    tensor_fence_before();
+    __syncthreads();
+    tensor_fence_after();
+    const uint32_t tensor = tensor_base;
+    const Bounds bounds{&over, p.status};
+    const int64_t col0 = int64_t(blockIdx.x / split) * 128, row0 = int64_t(blockIdx.y) * ROWS;
+    const int blocks = static_cast<int>((p.inner + kBlock - 1) / kBlock);
+    const int first = static_cast<int>(int64_t(blocks) * rank / split), last = static_cast<int>(int64_t(blocks) * (rank + 1) / split);  // (split <= blocks)
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (int kb = first; kb < last; ++kb, ++it) {
+                const uint32_t s = it % S::kStages, at = base + s * S::kStageBytes;
+                if (it >= S::kStages && !barrier_wait(empty + 8 * s, (it / S::kStages - 1) & 1, bounds)) {
+                    ok = false;
+                    break;
+                }
+                barrier_expect(full + 8 * s, S::kStageBytes);
+                if (ACROSS) load_tile<false>(at, &maps.b, static_cast<int>(col0), kb * kBlock, full + 8 * s);
+                else load_tile<false>(at, &maps.b, kb * kBlock, static_cast<int>(col0), full + 8 * s);
+                load_tile<false>(at + 128 * kBlock, &maps.a, kb * kBlock, static_cast<int>(row0), full + 8 * s);
+            }
+            if (!ok)  // copies in flight have to land before the block ends
+                for (uint32_t i = it > S::kStages ? it - S::kStages : 0; i < it; ++i)
+                    for (int polls = 0; polls < 64 && !barrier_wait(full + 8 * (i % S::kStages), (i / S::kStages) & 1, bounds); ++polls) {}
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t product = product_e4m3(128, ROWS, ACROSS, false);
+            uint32_t it = 0, four = 0;
+            for (int kb = first; kb < last; ++kb, ++it) {
+                const uint32_t s = it % S::kStages, buffer = four & 1;
+                if ((kb == first || kb % 4 == 0) && !barrier_wait(scales_full + 8 * buffer, (four >> 1) & 1, bounds)) break;
+                if (!barrier_wait(full + 8 * s, (it / S::kStages) & 1, bounds)) break;
+                tensor_fence_after();
+                const uint32_t w = base + s * S::kStageBytes, x = w + 128 * kBlock;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    multiply_e4m3<false>(tensor, operand(w + (ACROSS ? 32 * kBlock : 32) * k, ACROSS ? 128 * kBlock : 16), operand(x + 32 * k),
+                                         with_part(product, kb % 4), tensor + S::kScales + 8 * buffer, tensor + S::kScales + 8 * buffer + 4,
+                                         it > 0 || k > 0);
+                products_done<false>(empty + 8 * s);
+                if (kb % 4 == 3) {
+                    products_done<false>(scales_empty + 8 * buffer);
+                    ++four;
+                }
+            }
+            products_done<false>(sum_full);
+            if (over)
+                for (int polls = 0; polls < 64 && !barrier_wait(sum_full, 0, bounds); ++polls) {}
+        }
+    } else if (warp >= 4) {
+        const uint32_t mine = tensor + ((warp & 3) << 21);
+        uint32_t four = 0;
+        bool ok = true;
+        for (int f = first / 4; f <= (last - 1) / 4; ++f, ++four) {
+            const uint32_t buffer = four & 1;
+            uint32_t w[4], x[S::kWordsB];
+            scale_words<ACROSS>(p.b, col0, f, w);
+            if (p.a.shift && ROWS < 128) {  // (the rows do not begin at a tile of its scales)
+#pragma unroll
+                for (int j = 0; j < S::kWordsB; ++j) x[j] = scale_word<false>(p.a, row0 + 32 * j + lane, f);
+            } else {
+                scale_words<false>(p.a, row0, f, x);
+            }
+            if (four >= 2) {
+                ok = __all_sync(0xffffffffu, barrier_wait(scales_empty + 8 * buffer, ((four >> 1) - 1) & 1, bounds));
+                if (!ok) break;
+                tensor_fence_after();
+            }
+            tensor_store(mine + S::kScales + 8 * buffer, w);
+            tensor_store(mine + S::kScales + 8 * buffer + 4, x);
+            tensor_wait_stores();
+            tensor_fence_before();
+            __syncwarp();
+            if (lane == 0) barrier_arrive(scales_full + 8 * buffer);
+        }
+        ok = ok && __all_sync(0xffffffffu, barrier_wait(sum_full, 0, bounds));
+        ok = ok && !over;
+        if (__all_sync(0xffffffffu, ok)) {  // the part of the sum, in shared memory: [row][128]
+            tensor_fence_after();
+            const uint32_t to = base + ((warp & 3) * 32 + lane) * 4;
+#pragma unroll
+            for (int c = 0; c < ROWS; c += 16) {
+                float v[16];
+                tensor_load(mine + c, v);
+                tensor_wait_loads();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + (c + i) * 512), "f"(v[i]) : "memory");
+            }
+        }
+        tensor_fence_before();
+    }
+    __syncwarp();
+    cluster_barrier();
+    if (warp >= 4) {
+        // this block's share of the columns: 128 / split, eight a thread
+        const int share = 128 / split, across = share / 8, thread = threadIdx.x - 128;
+        const int col = rank * share + thread % across * 8;
+        T* out = static_cast<T*>(p.out) + row0 * p.ld + col0 + col;
+        const int rows = static_cast<int>(min(int64_t(ROWS), p.rows - row0));
+        const int64_t left = p.outs - col0 - col;
+        for (int r = thread / across; r < rows && left > 0; r += 128 / across) {
+            float v[8] = {};
+            for (int s = 0; s < split; ++s) {
+                const uint32_t from = address_in(base + r * 512 + col * 4, s);
+                float4 lo, hi;
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(lo.x), "=f"(lo.y), "=f"(lo.z), "=f"(lo.w) : "r"(from));
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(hi.x), "=f"(hi.y), "=f"(hi.z), "=f"(hi.w) : "r"(from + 16));
+                v[0] += lo.x, v[1] += lo.y, v[2] += lo.z, v[3] += lo.w, v[4] += hi.x, v[5] += hi.y, v[6] += hi.z, v[7] += hi.w;
+            }
+            T* to = out + r * p.ld;
+            if (left >= 8) {
+                if constexpr (sizeof(T) == 2) {
+                    *reinterpret_cast<uint4*>(to) = make_uint4(bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3]), bf16x2_of(v[4], v[5]), bf16x2_of(v[6], v[7]));
+                } else {
+                    reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                    reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < left) to[i] = T(v[i]);
+            }
+        }
+    }
+    __syncwarp();
+    cluster_barrier();  // the others have read this block's part
+    if (warp == 2) {
+        tensor_fence_after();
+        tensor_free<false>(tensor, S::kColumns);
+    }
+}
+
+template <int ROWS, bool ACROSS, class T>
+int launch(const MatmulArgs& p, int split, cudaStream_t s) {
+    Maps maps;
+    int st = tile_map(&maps.a, p.a.codes, Element::kByte, p.a.rows, p.a.cols, p.a.ld_codes, kBlock, ROWS);
+    if (st == PVQ_OK) st = tile_map(&maps.b, p.b.codes, Element::kByte, p.b.rows, p.b.cols, p.b.ld_codes, kBlock, 128);
+    const auto kernel = matmul_few_kernel<ROWS, ACROSS, T>;
+    if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), Shape<ROWS>::kShared);
+    if (st != PVQ_OK) return st;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(static_cast<unsigned>((p.outs + 127) / 128 * split), static_cast<unsigned>((p.rows + ROWS - 1) / ROWS));
+    config.blockDim = dim3(kThreads);
+    config.dynamicSmemBytes = Shape<ROWS>::kShared;
+    config.stream = s;
+    cudaLaunchAttribute cluster;
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = split, cluster.val.clusterDim.y = 1, cluster.val.clusterDim.z = 1;
+    config.attrs = &cluster;
+    config.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&config, kernel, maps, p, split);
+    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
+}
+
+template <int ROWS>
+int launch_rows(const MatmulArgs& p, bool transposed, bool bf16, int split, cudaStream_t s) {
+    if (transposed) return bf16 ? launch<ROWS, true, __nv_bfloat16>(p, split, s) : launch<ROWS, true, float>(p, split, s);
+    return bf16 ? launch<ROWS, false, __nv_bfloat16>(p, split, s) : launch<ROWS, false, float>(p, split, s);
+}
+
+}  // namespace
+
+int matmul_few(const MatmulArgs& p, bool transposed, bool bf16, int split, cudaStream_t s) {
+    if (p.rows <= 16) return launch_rows<16>(p, transposed, bf16, split, s);
+    if (p.rows <= 32) return launch_rows<32>(p, transposed, bf16, split, s);
+    if (p.rows <= 64) return launch_rows<64>(p, transposed, bf16, split, s);
+    return launch_rows<128>(p, transposed, bf16, split, s);
+}
+
+}  // namespace fp8
+}  // namespace pvq

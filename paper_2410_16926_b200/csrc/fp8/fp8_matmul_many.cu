@@ -1,0 +1,261 @@
+// The 8-bit product where there is enough of it to fill the GPU: out[i][j] = sum_k a(i,k) b(j,k).
+//
+// A pair of thread blocks on two neighbouring SMs makes tiles of 256 x 256, each block 128 of the rows; each loads its 128
+// rows of a and half of the 256 of b (32 KB a block of 128 along k), and the product reads both halves.  The scales are
+// powers of two, which the tensor cores apply to the products of a step (32 values of k) before they add them, so that a
+// tile's sum stays in tensor memory from the first to the last k, and is read once.
+//
+// Warps of a block: one issues the copies, one (of the pair's first block) the products, four bring the scales to tensor
+// memory - four blocks along k at a time, double-buffered, a lane the words of its rows, the same in each quarter of the
+// lanes as the product wants it -, eight read the result, round it and store it by tiled copies, a warp its own 32 rows.
+// The 256 columns of the result and the scales leave no room for a second result (512 columns): the next tile's products
+// begin when the result has been read into registers.
+#include "fp8_matmul.cuh"
+
+namespace pvq {
+namespace fp8 {
+namespace {
+
+constexpr int kStages = 5, kStageBytes = 2 * 128 * kBlock, kThreads = 512;
+constexpr int kStoreBytes = 4096;  // 32 rows of 128 bytes
+constexpr int kScalesA = 256, kScalesB = 264;  // columns, two buffers of 4 and of 8
+constexpr int kGroup = 8;  // tiles down that are taken together across
+constexpr size_t kShared = 1024 + kStages * kStageBytes + 8 * 2 * kStoreBytes + 256;
+
+struct Maps {
+    CUtensorMap a, b, out;
+};
+
+struct Tiles {
+    int down, across;
+    __device__ __forceinline__ int count() const { return down * across; }
+    // Tiles of kGroup rows of tiles go down first, so that those of one moment share what they read.
+    __device__ __forceinline__ void at(int t, int* m, int* n) const {
+        const int group = t / (kGroup * across), first = group * kGroup, rest = t - group * kGroup * across;
+        const int high = min(kGroup, down - first);
+        *m = first + rest % high;
+        *n = rest / high;
+    }
+};
+
+template <bool ACROSS, class T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_constant__ Maps maps, const __grid_constant__ MatmulArgs p) {
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
+    const uint32_t stores = base + kStages * kStageBytes, bars = stores + 8 * 2 * kStoreBytes;
+    const uint32_t full = bars, empty = full + 8 * kStages, scales_full = empty + 8 * kStages, scales_empty = scales_full + 16, sum_full = scales_empty + 16,
+                   sum_empty = sum_full + 8, drained = sum_empty + 8;
+    __shared__ uint32_t tensor_base;
+    __shared__ int over;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    if (threadIdx.x == 0) {
+        over = 0;
+        for (int i = 0; i < kStages; ++i) barrier_init(full + 8 * i, 1), barrier_init(empty + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) barrier_init(scales_full + 8 * i, 8), barrier_init(scales_empty + 8 * i, 1);
+        barrier_init(sum_full, 1), barrier_init(sum_empty, 16), barrier_init(drained, 1);
+        barrier_init_fence();
+        prefetch_map(&maps.a), prefetch_map(&maps.b), prefetch_map(&maps.out);
+    }
+    if (warp == 2) tensor_alloc<true>(shared_address(&tensor_base), 512);
+    tensor_fence_before();
+    __syncthreads();
+    cluster_barrier();
+    tensor_fence_after();
+    const uint32_t tensor = tensor_base;
+    const Bounds bounds{&over, p.status};
+    const Tiles tiles{static_cast<int>((p.rows + 255) / 256), static_cast<int>((p.outs + 255) / 256)};
+    const int blocks = static_cast<int>((p.inner + kBlock - 1) / kBlock), first = blockIdx.x / 2, step = gridDim.x / 2;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            const uint32_t full_there = address_in(full, 0);
+            for (int t = first; t < tiles.count() && ok; t += step) {
+                int m, n;
+                tiles.at(t, &m, &n);
+                const int row = m * 256 + rank * 128, col = n * 256 + rank * 128;
+                for (int kb = 0; kb < blocks; ++kb, ++it) {
+                    const uint32_t s = it % kStages, at = base + s * kStageBytes;
+                    if (it >= kStages && !barrier_wait(empty + 8 * s, (it / kStages - 1) & 1, bounds)) {
+                        ok = false;
+                        break;
+                    }
+                    if (rank == 0) barrier_expect(full + 8 * s, 2 * kStageBytes);  // both blocks' tiles
+                    load_tile<true>(at, &maps.a, kb * kBlock, row, full_there + 8 * s);
+                    if (ACROSS) load_tile<true>(at + kStageBytes / 2, &maps.b, col, kb * kBlock, full_there + 8 * s);
+                    else load_tile<true>(at + kStageBytes / 2, &maps.b, kb * kBlock, col, full_there + 8 * s);
+                }
+            }
+            if (!ok && rank == 0) {  // copies in flight have to land before the block ends
+                const Bounds alone{&over, p.status};
+                for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
+                    for (int polls = 0; polls < 64 && !barrier_wait(full + 8 * (i % kStages), (i / kStages) & 1, alone); ++polls) {}
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t product = product_e4m3(256, 256, false, ACROSS);
+            uint32_t it = 0, four = 0, tile = 0;
+            bool ok = true;
+            for (int t = first; t < tiles.count() && ok; t += step, ++tile) {
+                if (tile > 0 && !barrier_wait(sum_empty, (tile - 1) & 1, bounds)) break;
+                tensor_fence_after();
+                for (int kb = 0; kb < blocks; ++kb, ++it) {
+                    const uint32_t s = it % kStages, buffer = four & 1;
+                    if (kb % 4 == 0 && !barrier_wait(scales_full + 8 * buffer, (four >> 1) & 1, bounds)) {
+                        ok = false;
+                        break;
+                    }
+                    if (!barrier_wait(full + 8 * s, (it / kStages) & 1, bounds)) {
+                        ok = false;
+                        break;
+                    }
+                    tensor_fence_after();
+                    const uint32_t a = base + s * kStageBytes, b = a + kStageBytes / 2;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        multiply_e4m3<true>(tensor, operand(a + 32 * k), operand(b + (ACROSS ? 32 * kBlock : 32) * k, ACROSS ? kStageBytes / 2 : 16),
+                                            with_part(product, kb % 4), tensor + kScalesA + 4 * buffer, tensor + kScalesB + 8 * buffer, kb > 0 || k > 0);
+                    products_done<true>(empty + 8 * s);
+                    if (kb % 4 == 3 || kb == blocks - 1) {
+                        products_done<true>(scales_empty + 8 * buffer);
+                        ++four;
+                    }
+                }
+                if (ok) products_done<true>(sum_full);
+            }
+            if (!ok) {
+                products_done<true>(drained);
+                for (int polls = 0; polls < 64 && !barrier_wait(drained, 0, bounds); ++polls) {}
+            }
+        }
+    } else if (warp >= 4 && warp < 8) {
+        const uint32_t mine = tensor + ((warp & 3) << 21);
+        const uint32_t full_there = address_in(scales_full, 0);
+        uint32_t four = 0;
+        bool ok = true;
+        for (int t = first; t < tiles.count() && ok; t += step) {
+            int m, n;
+            tiles.at(t, &m, &n);
+            for (int kb = 0; kb < blocks; kb += 4, ++four) {
+                const uint32_t buffer = four & 1;
+                uint32_t a[4], b[8];
+                scale_words<false>(p.a, int64_t(m) * 256 + rank * 128, kb / 4, a);
+                scale_words<ACROSS>(p.b, int64_t(n) * 256, kb / 4, b);
+                if (four >= 2) {
+                    ok = __all_sync(0xffffffffu, barrier_wait(scales_empty + 8 * buffer, ((four >> 1) - 1) & 1, bounds));
+                    if (!ok) break;
+                    tensor_fence_after();
+                }
+                tensor_store(mine + kScalesA + 4 * buffer, a);
+                tensor_store(mine + kScalesB + 8 * buffer, b);
+                tensor_wait_stores();
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive_in(full_there + 8 * buffer);
+            }
+        }
+    } else if (warp >= 8) {
+        constexpr int kColumns = 128 / sizeof(T);  // of a stored tile
+        const int quarter = warp & 3, half = (warp - 8) >> 2;
+        const uint32_t buffers = stores + (warp - 8) * 2 * kStoreBytes, empty_there = address_in(sum_empty, 0);
+        uint32_t tile = 0;
+        for (int t = first; t < tiles.count(); t += step, ++tile) {
+            int m, n;
+            tiles.at(t, &m, &n);
+            if (!__all_sync(0xffffffffu, barrier_wait(sum_full, tile & 1, bounds))) break;
+            tensor_fence_after();
+            const int64_t row = int64_t(m) * 256 + rank * 128 + quarter * 32;
+#pragma unroll
+            for (int c = 0; c < 128 / kColumns; ++c) {
+                const uint32_t to = buffers + (c & 1) * kStoreBytes + lane * 128;
+                const int64_t col = int64_t(n) * 256 + half * 128 + c * kColumns;
+                uint32_t w[32];
+                float v[32];
+                const uint32_t from = tensor + (quarter << 21) + half * 128 + c * kColumns;
+                tensor_load(from, v);
+                tensor_wait_loads();
+                if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = bf16x2_of(v[2 * i], v[2 * i + 1]);
+                    tensor_load(from + 32, v);
+                    tensor_wait_loads();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[16 + i] = bf16x2_of(v[2 * i], v[2 * i + 1]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i]);
+                }
+                if (c == 128 / kColumns - 1) {
+                    tensor_fence_before();
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive_in(empty_there);
+                }
+                // A tiled store ends at a multiple of 16 bytes behind the last column: where that is not the row's end, and
+                // might be another matrix's, the last tile is stored by values.
+                if (col + kColumns > p.outs && p.outs * sizeof(T) % 16 != 0) {
+                    if (row + lane < p.rows) {
+                        T* to_row = static_cast<T*>(p.out) + (row + lane) * p.ld + col;
+#pragma unroll
+                        for (int i = 0; i < kColumns; ++i)
+                            if (col + i < p.outs) {
+                                if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(to_row)[i] = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));
+                                else reinterpret_cast<uint32_t*>(to_row)[i] = w[i];
+                            }
+                    }
+                    if (lane == 0) store_commit();  // (an empty group: the buffers' turns go on)
+                    continue;
+                }
+                if (lane == 0) store_wait_read<1>();
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((j ^ (lane & 7)) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
+                                 "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
+                                 : "memory");
+                async_fence();
+                __syncwarp();
+                if (lane == 0) {
+                    if (row < p.rows && col < p.outs) store_tile(&maps.out, static_cast<int>(col), static_cast<int>(row), to);
+                    store_commit();
+                }
+            }
+        }
+        if (lane == 0) store_wait_all();
+    }
+    __syncwarp();
+    tensor_fence_before();
+    __syncthreads();
+    cluster_barrier();
+    if (warp == 2) tensor_free<true>(tensor, 512);
+}
+
+template <bool ACROSS, class T>
+int launch(const MatmulArgs& p, cudaStream_t s) {
+    Maps maps;
+    const Element out = sizeof(T) == 2 ? Element::kBf16 : Element::kF32;
+    int st = tile_map(&maps.a, p.a.codes, Element::kByte, p.a.rows, p.a.cols, p.a.ld_codes, kBlock, 128);
+    if (st == PVQ_OK) st = tile_map(&maps.b, p.b.codes, Element::kByte, p.b.rows, p.b.cols, p.b.ld_codes, kBlock, 128);
+    if (st == PVQ_OK) st = tile_map(&maps.out, p.out, out, p.rows, p.outs, p.ld, 128 / sizeof(T), 32);
+    const auto kernel = matmul_many_kernel<ACROSS, T>;
+    if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), kShared);
+    if (st != PVQ_OK) return st;
+    const int64_t tiles = ((p.rows + 255) / 256) * ((p.outs + 255) / 256);
+    if (tiles >= int64_t(1) << 30) return PVQ_ERR_UNSUPPORTED;
+    const unsigned pairs = static_cast<unsigned>(tiles < kSms / 2 ? tiles : kSms / 2);
+    kernel<<<2 * pairs, kThreads, kShared, s>>>(maps, p);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
+}
+
+}  // namespace
+
+int matmul_many(const MatmulArgs& p, bool transposed, bool bf16, cudaStream_t s) {
+    if (transposed) return bf16 ? launch<true, __nv_bfloat16>(p, s) : launch<true, float>(p, s);
+    return bf16 ? launch<false, __nv_bfloat16>(p, s) : launch<false, float>(p, s);
+}
+
+}  // namespace fp8
+}  // namespace pvq

@@ -1,0 +1,390 @@
+// The gradient of a weight from the 8-bit input that was kept: out[o][i] = sum_t dy[t][o] x[t][i].
+//
+// The scales of x lie along t, inside the sum, so x is made bf16 (a code times a power of two: exact) on its way to the
+// tensor cores: tiles of codes arrive by tiled copies, four warps convert them into the operand's layout, and the product
+// takes both operands across k, as they lie in memory.  The tensor cores cut off what an addition to a running sum loses
+// instead of rounding it: over 16384 values of t a sum in tensor memory ends 1.9e-5 of itself too small.  So after every
+// 512 values of t the sum is read and added to one in registers (fp32, rounded to nearest), while the products go on in
+// a second buffer.
+//
+// PAIR: two blocks on neighbouring SMs make 256 x 256 of the result, each 128 rows of it and half of the other operand.
+// Otherwise a block makes 128 x 128, and where there are few tiles the blocks of a cluster split t, and add their sums
+// through one another's shared memory in the order of the ranks.
+//
+// Warps of a block: one issues the copies, one the products, four convert, eight hold and store the sums.
+#include "fp8_mma.cuh"
+
+namespace pvq {
+namespace fp8 {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kDepth = 64;                    // values of t a stage
+constexpr int kStages = 6, kStageBytes = 128 * kDepth * 3;  // 128 columns of dy (bf16), 128 of x (codes)
+constexpr int kConverted = 3, kConvertedBytes = 128 * kDepth * 2;
+constexpr int kRun = 512 / kDepth;            // stages that are added in tensor memory
+constexpr int kStoreBytes = 4096;             // 32 rows of 128 bytes
+constexpr int kAtom = kDepth * 128;           // bytes from 64 bf16 columns to the next 64
+constexpr size_t kShared = 1024 + kStages * kStageBytes + kConverted * kConvertedBytes + 8 * kStoreBytes + 256;
+constexpr int kGroup = 8;                     // tiles down that are taken together across
+
+struct Maps {
+    CUtensorMap dy, x, out;
+};
+struct Args {
+    Matrix x;
+    void* out;
+    int64_t outer, ld;
+    uint32_t* status;
+    int split;
+};
+
+// Registers a thread of the four warpgroups of a pair's block: what all are launched with, shared out anew.  A sum of 128
+// columns takes 128 of them.
+constexpr int kRegisters = 128, kFew = 48, kSome = 64, kMany = 200;
+static_assert(kFew + kSome + 2 * kMany <= 4 * kRegisters, "a share beyond these would be waited for without end");
+
+template <int REGISTERS>
+__device__ __forceinline__ void more_registers() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGISTERS));
+}
+template <int REGISTERS>
+__device__ __forceinline__ void fewer_registers() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGISTERS));
+}
+
+template <bool PAIR, class T>
+__global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args p) {
+    constexpr int kSide = PAIR ? 256 : 128;   // of a tile
+    constexpr int kHeld = kSide / 2;          // columns of the sum a warp holds
+    constexpr uint32_t kBlocks = PAIR ? 2 : 1;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
+    const uint32_t converted = base + kStages * kStageBytes, stores = converted + kConverted * kConvertedBytes, bars = stores + 8 * kStoreBytes;
+    const uint32_t full_dy = bars, full_x = full_dy + 8 * kStages, empty = full_x + 8 * kStages, converted_full = empty + 8 * kStages,
+                   converted_empty = converted_full + 8 * kConverted, sum_full = converted_empty + 8 * kConverted, sum_empty = sum_full + 16,
+                   drained = sum_empty + 16;
+    __shared__ uint32_t tensor_base;
+    __shared__ int over;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR ? cluster_rank() : 0;              // in the pair
+    const int part = PAIR ? 0 : static_cast<int>(cluster_rank());  // of t
+    if (threadIdx.x == 0) {
+        over = 0;
+        for (int i = 0; i < kStages; ++i) barrier_init(full_dy + 8 * i, 1), barrier_init(full_x + 8 * i, 1), barrier_init(empty + 8 * i, 1);
+        for (int i = 0; i < kConverted; ++i) barrier_init(converted_full + 8 * i, 4 * kBlocks), barrier_init(converted_empty + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) barrier_init(sum_full + 8 * i, 1), barrier_init(sum_empty + 8 * i, 8 * kBlocks);
+        barrier_init(drained, 1);
+        barrier_init_fence();
+        prefetch_map(&maps.dy), prefetch_map(&maps.x), prefetch_map(&maps.out);
+    }
+    if (warp == 2) tensor_alloc<PAIR>(shared_address(&tensor_base), 2 * kSide);
+    tensor_fence_before();
+    __syncthreads();
+    cluster_barrier();
+    tensor_fence_after();
+    const uint32_t tensor = tensor_base;
+    const Bounds bounds{&over, p.status};
+    const int down = static_cast<int>((p.outer + kSide - 1) / kSide), across = static_cast<int>((p.x.cols + kSide - 1) / kSide), tiles = down * across;
+    const int team = PAIR ? 2 : p.split, step = gridDim.x / team;
+    const int stages = static_cast<int>((p.x.rows + kDepth - 1) / kDepth);
+    const int begin = static_cast<int>(int64_t(stages) * part / p.split), end = static_cast<int>(int64_t(stages) * (part + 1) / p.split);
+
+    // Tiles of kGroup rows of tiles go down first, so that those of one moment share what they read.
+    const auto tile_at = [&](int t, int* m, int* n) {
+        const int group = t / (kGroup * across), first = group * kGroup, rest = t - group * kGroup * across, high = min(kGroup, down - first);
+        *m = first + rest % high;
+        *n = rest / high;
+    };
+
+    if (warp < 4) {
+        if (PAIR) fewer_registers<kFew>();
+        if (warp == 0 && lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            const uint32_t full_there = PAIR ? address_in(full_dy, 0) : full_dy;
+            for (int t = blockIdx.x / team; t < tiles && ok; t += step) {
+                int m, n;
+                tile_at(t, &m, &n);
+                const int row = m * kSide + rank * 128, col = n * kSide + rank * 128;
+                for (int kb = begin; kb < end; ++kb, ++it) {
+                    const uint32_t s = it % kStages, at = base + s * kStageBytes;
+                    if (it >= kStages && !barrier_wait(empty + 8 * s, (it / kStages - 1) & 1, bounds)) {
+                        ok = false;
+                        break;
+                    }
+                    if (rank == 0) barrier_expect(full_dy + 8 * s, kBlocks * 2 * kAtom);
+                    load_tile<PAIR>(at, &maps.dy, row, kb * kDepth, full_there + 8 * s);
+                    load_tile<PAIR>(at + kAtom, &maps.dy, row + 64, kb * kDepth, full_there + 8 * s);
+                    barrier_expect(full_x + 8 * s, kAtom);
+                    load_tile<false>(at + 2 * kAtom, &maps.x, col, kb * kDepth, full_x + 8 * s);
+                }
+            }
+            if (!ok)  // copies in flight have to land before the block ends
+                for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
+                    for (int polls = 0; polls < 64 && !((rank != 0 || barrier_wait(full_dy + 8 * (i % kStages), (i / kStages) & 1, bounds)) &&
+                                                        barrier_wait(full_x + 8 * (i % kStages), (i / kStages) & 1, bounds));
+                         ++polls) {}
+        } else if (warp == 1 && lane == 0 && rank == 0) {
+            constexpr uint32_t product = product_bf16(kSide, kSide, true, true);
+            uint32_t it = 0, run = 0;
+            bool ok = true;
+            for (int t = blockIdx.x / team; t < tiles && ok; t += step)
+                for (int kb = begin; kb < end; ++kb, ++it) {
+                    const uint32_t s = it % kStages, c = it % kConverted, buffer = run & 1;
+                    const int within = (kb - begin) % kRun;
+                    if (within == 0) {
+                        if (run >= 2 && !barrier_wait(sum_empty + 8 * buffer, ((run >> 1) - 1) & 1, bounds)) {
+                            ok = false;
+                            break;
+                        }
+                    }
+                    if (!barrier_wait(full_dy + 8 * s, (it / kStages) & 1, bounds) || !barrier_wait(converted_full + 8 * c, (it / kConverted) & 1, bounds)) {
+                        ok = false;
+                        break;
+                    }
+                    tensor_fence_after();
+                    const uint32_t a = base + s * kStageBytes, b = converted + c * kConvertedBytes;
+#pragma unroll
+                    for (int k = 0; k < kDepth / 16; ++k)
+                        multiply_bf16<PAIR>(tensor + buffer * kSide, operand(a + 2048 * k, kAtom), operand(b + 2048 * k, kAtom), product, within > 0 || k > 0);
+                    products_done<PAIR>(empty + 8 * s);
+                    products_done<PAIR>(converted_empty + 8 * c);
+                    if (within == kRun - 1 || kb == end - 1) {
+                        products_done<PAIR>(sum_full + 8 * buffer);
+                        ++run;
+                    }
+                }
+            if (!ok) {
+                products_done<PAIR>(drained);
+                for (int polls = 0; polls < 64 && !barrier_wait(drained, 0, bounds); ++polls) {}
+            }
+        }
+    } else if (warp < 8) {
+        if (PAIR) fewer_registers<kSome>();
+        // a thread takes 64 codes of one t: a row of the tile, eight neighbouring rows in eight different places
+        const int row = lane + 32 * (warp & 1), half = (warp >> 1) & 1;
+        const uint32_t full_there = PAIR ? address_in(converted_full, 0) : converted_full;
+        uint32_t it = 0;
+        bool ok = true;
+        for (int t = blockIdx.x / team; t < tiles && ok; t += step) {
+            int m, n;
+            tile_at(t, &m, &n);
+            const int block = n * (kSide / kBlock) + rank;
+            const uint8_t* scales = p.x.scales + block;
+            const auto scale_at = [&](int kb) -> uint32_t {  // (rows behind the end: codes of zero)
+                const int64_t r = int64_t(kb) * kDepth + row;
+                return kb < end && r < p.x.rows && block < p.x.blocks ? __ldg(scales + (r >> p.x.shift) * p.x.ld_scales) : 127u;
+            };
+            uint32_t ahead[3] = {scale_at(begin), scale_at(begin + 1), scale_at(begin + 2)};
+            for (int kb = begin; kb < end; ++kb, ++it) {
+                const uint32_t s = it % kStages, c = it % kConverted;
+                const float scale = scale_of(ahead[0]);
+                ahead[0] = ahead[1], ahead[1] = ahead[2], ahead[2] = scale_at(kb + 3);
+                ok = barrier_wait(full_x + 8 * s, (it / kStages) & 1, bounds) &&
+                     (it < kConverted || barrier_wait(converted_empty + 8 * c, (it / kConverted - 1) & 1, bounds));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t from = base + s * kStageBytes + 2 * kAtom + row * 128, to = converted + c * kConvertedBytes + half * kAtom + row * 128;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t w[4], v[8];
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                                 : "r"(from + (((half * 4 + j) ^ (row & 7)) << 4)));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 lo = values_of(w[i] & 0xffffu), hi = values_of(w[i] >> 16);
+                        v[2 * i] = bf16x2_of(lo.x * scale, lo.y * scale);
+                        v[2 * i + 1] = bf16x2_of(hi.x * scale, hi.y * scale);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((2 * j + i) ^ (row & 7)) << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]),
+                                     "r"(v[4 * i + 2]), "r"(v[4 * i + 3])
+                                     : "memory");
+                }
+                async_fence();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR) barrier_arrive_in(full_there + 8 * c);
+                    else barrier_arrive(full_there + 8 * c);
+                }
+            }
+        }
+    } else {
+        if (PAIR) more_registers<kMany>();
+        constexpr int kColumns = 128 / sizeof(T);  // of a stored tile
+        const int quarter = warp & 3, half = (warp - 8) >> 2;
+        const uint32_t buffer_at = stores + (warp - 8) * kStoreBytes, empty_there = PAIR ? address_in(sum_empty, 0) : sum_empty;
+        const uint32_t mine = tensor + (quarter << 21) + half * kHeld;
+        uint32_t run = 0;
+        bool ok = true;
+        for (int t = blockIdx.x / team; t < tiles && ok; t += step) {
+            int m, n;
+            tile_at(t, &m, &n);
+            float sum[kHeld];
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) sum[i] = 0.0f;
+            for (int kb = begin; kb < end; kb += kRun, ++run) {
+                const uint32_t buffer = run & 1;
+                ok = __all_sync(0xffffffffu, barrier_wait(sum_full + 8 * buffer, (run >> 1) & 1, bounds));
+                if (!ok) break;
+                tensor_fence_after();
+#pragma unroll
+                for (int c = 0; c < kHeld; c += 32) {
+                    float v[32];
+                    tensor_load(mine + buffer * kSide + c, v);
+                    tensor_wait_loads();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) sum[c + i] += v[i];
+                }
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR) barrier_arrive_in(empty_there + 8 * buffer);
+                    else barrier_arrive(empty_there + 8 * buffer);
+                }
+            }
+            if (!ok) break;
+            if (!PAIR && p.split > 1) {  // the part of the sum, in shared memory: [row][128], in places turned by the row
+                const uint32_t to = base + (quarter * 32 + lane) * 512;
+#pragma unroll
+                for (int c = 0; c < kHeld / 4; ++c)
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((half * (kHeld / 4) + c) ^ (lane & 7)) << 4)), "f"(sum[4 * c]),
+                                 "f"(sum[4 * c + 1]), "f"(sum[4 * c + 2]), "f"(sum[4 * c + 3])
+                                 : "memory");
+                continue;  // (the only tile)
+            }
+            const int64_t row = int64_t(m) * kSide + rank * 128 + quarter * 32;
+#pragma unroll
+            for (int c = 0; c < kHeld / kColumns; ++c) {
+                const int64_t col = int64_t(n) * kSide + half * kHeld + c * kColumns;
+                uint32_t w[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    if constexpr (sizeof(T) == 2) w[i] = bf16x2_of(sum[c * kColumns + 2 * i], sum[c * kColumns + 2 * i + 1]);
+                    else w[i] = __float_as_uint(sum[c * kColumns + i]);
+                }
+                // A tiled store ends at a multiple of 16 bytes behind the last column: where that is not the row's end, and
+                // might be another matrix's, the last tile is stored by values.
+                if (col + kColumns > p.x.cols && p.x.cols * sizeof(T) % 16 != 0) {
+                    if (row + lane < p.outer) {
+                        T* to_row = static_cast<T*>(p.out) + (row + lane) * p.ld + col;
+#pragma unroll
+                        for (int i = 0; i < kColumns; ++i)
+                            if (col + i < p.x.cols) {
+                                if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(to_row)[i] = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));
+                                else reinterpret_cast<uint32_t*>(to_row)[i] = w[i];
+                            }
+                    }
+                    continue;
+                }
+                if (lane == 0) store_wait_read<0>();
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffer_at + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(w[4 * j]),
+                                 "r"(w[4 * j + 1]), "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
+                                 : "memory");
+                async_fence();
+                __syncwarp();
+                if (lane == 0) {
+                    if (row < p.outer && col < p.x.cols) store_tile(&maps.out, static_cast<int>(col), static_cast<int>(row), buffer_at);
+                    store_commit();
+                }
+            }
+        }
+        if (lane == 0) store_wait_all();
+    }
+    __syncwarp();
+    tensor_fence_before();
+    __syncthreads();
+    cluster_barrier();
+    if (!PAIR && p.split > 1) {
+        if (warp >= 8) {  // this block's share of the rows, eight columns a thread
+            int m, n;
+            tile_at(blockIdx.x / team, &m, &n);
+            const int thread = threadIdx.x - 256, share = 128 / p.split, col = thread % 16 * 8;
+            const int64_t left = p.x.cols - int64_t(n) * 128 - col;
+            for (int r = part * share + thread / 16; r < (part + 1) * share; r += 16) {
+                const int64_t row = int64_t(m) * 128 + r;
+                if (row >= p.outer || left <= 0) break;
+                float v[8] = {};
+                for (int s = 0; s < p.split; ++s) {
+                    float4 lo, hi;
+                    const uint32_t lo_at = address_in(base + r * 512 + (((col / 4) ^ (r & 7)) << 4), s);
+                    const uint32_t hi_at = address_in(base + r * 512 + (((col / 4 + 1) ^ (r & 7)) << 4), s);
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(lo.x), "=f"(lo.y), "=f"(lo.z), "=f"(lo.w) : "r"(lo_at));
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(hi.x), "=f"(hi.y), "=f"(hi.z), "=f"(hi.w) : "r"(hi_at));
+                    v[0] += lo.x, v[1] += lo.y, v[2] += lo.z, v[3] += lo.w, v[4] += hi.x, v[5] += hi.y, v[6] += hi.z, v[7] += hi.w;
+                }
+                T* to = static_cast<T*>(p.out) + row * p.ld + int64_t(n) * 128 + col;
+                if (left >= 8) {
+                    if constexpr (sizeof(T) == 2) {
+                        *reinterpret_cast<uint4*>(to) = make_uint4(bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3]), bf16x2_of(v[4], v[5]), bf16x2_of(v[6], v[7]));
+                    } else {
+                        reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                        reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i < left) to[i] = T(v[i]);
+                }
+            }
+        }
+        __syncwarp();
+        cluster_barrier();  // the others have read this block's part
+    }
+    if (warp == 2) {
+        tensor_fence_after();
+        tensor_free<PAIR>(tensor, 2 * kSide);
+    }
+}
+
+template <bool PAIR, class T>
+int launch(const Args& p, const void* dy, int64_t ld_dy, int64_t tiles, cudaStream_t s) {
+    Maps maps;
+    const Element out = sizeof(T) == 2 ? Element::kBf16 : Element::kF32;
+    int st = tile_map(&maps.dy, dy, Element::kBf16, p.x.rows, p.outer, ld_dy, 64, kDepth);
+    if (st == PVQ_OK) st = tile_map(&maps.x, p.x.codes, Element::kByte, p.x.rows, p.x.cols, p.x.ld_codes, 128, kDepth);
+    if (st == PVQ_OK) st = tile_map(&maps.out, p.out, out, p.outer, p.x.cols, p.ld, 128 / sizeof(T), 32);
+    const auto kernel = weight_grad_kernel<PAIR, T>;
+    if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), kShared);
+    if (st == PVQ_OK && PAIR) {
+        int registers = 0;
+        st = registers_of(reinterpret_cast<const void*>(kernel), &registers);
+        if (st == PVQ_OK && registers < kRegisters) st = PVQ_ERR_UNSUPPORTED;
+    }
+    if (st != PVQ_OK) return st;
+    const int team = PAIR ? 2 : p.split;
+    const int64_t teams = p.split > 1 || tiles < kSms / team ? tiles : kSms / team;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(static_cast<unsigned>(teams * team));
+    config.blockDim = dim3(kThreads);
+    config.dynamicSmemBytes = kShared;
+    config.stream = s;
+    cudaLaunchAttribute cluster;
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = team, cluster.val.clusterDim.y = 1, cluster.val.clusterDim.z = 1;
+    config.attrs = &cluster;
+    config.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&config, kernel, maps, p);
+    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
+}
+
+}  // namespace
+
+int weight_grad(const void* dy, int64_t outer, int64_t ld_dy, const Matrix& x, void* out, bool bf16, int64_t ld, uint32_t* status, cudaStream_t s) {
+    Args p{x, out, outer, ld, status, 1};
+    const int64_t pairs = ((outer + 255) / 256) * ((x.cols + 255) / 256), tiles = ((outer + 127) / 128) * ((x.cols + 127) / 128);
+    if (tiles >= int64_t(1) << 30) return PVQ_ERR_UNSUPPORTED;
+    if (pairs >= 48) return bf16 ? launch<true, __nv_bfloat16>(p, dy, ld_dy, pairs, s) : launch<true, float>(p, dy, ld_dy, pairs, s);
+    const int64_t stages = (x.rows + kDepth - 1) / kDepth;
+    while (p.split < 8 && tiles * p.split * 2 <= kSms && stages >= kRun * p.split * 2) p.split *= 2;
+    return bf16 ? launch<false, __nv_bfloat16>(p, dy, ld_dy, tiles, s) : launch<false, float>(p, dy, ld_dy, tiles, s);
+}
+
+}  // namespace fp8
+}  // namespace pvq

@@ -149,7 +149,7 @@ def check_matmul(a, b, transposed, dtype, out=None):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,inner,outer", [(1, 1, 1), (1, 128, 128), (2, 130, 7), (1, 4096, 1024), (5, 1000, 333), (8, 512, 4096), (16, 300, 136),
                                               (17, 257, 129), (33, 2048, 512), (64, 640, 200), (65, 127, 640), (128, 1024, 384), (129, 4096, 257),
-                                              (300, 513, 1000), (513, 900, 770), (1024, 256, 2048)])
+                                              (300, 513, 1000), (513, 900, 770), (1024, 256, 2048), (1281, 1400, 2100), (2100, 260, 2600)])
 def test_matmul(rows, inner, outer, dtype, transposed):
     a = random_held(rows, inner, False, rows + inner, pad=16)
     shape = (inner, outer) if transposed else (outer, inner)
@@ -160,13 +160,13 @@ def test_matmul(rows, inner, outer, dtype, transposed):
 
 
 @pytest.mark.parametrize("tiles", [(False, False), (True, True), (True, False)])
-@pytest.mark.parametrize("rows,inner,outer", [(3, 300, 200), (200, 640, 300), (700, 384, 520)])
+@pytest.mark.parametrize("rows,inner,outer", [(3, 300, 200), (200, 640, 300), (700, 384, 520), (1300, 700, 2050)])
 def test_matmul_of_other_blocks(rows, inner, outer, tiles):
     a, b = random_held(rows, inner, tiles[0], 1), random_held(outer, inner, tiles[1], 2)
     check_matmul(a, b, False, BF16)
 
 
-@pytest.mark.parametrize("rows,outer", [(2, 256), (300, 512), (600, 1024)])
+@pytest.mark.parametrize("rows,outer", [(2, 256), (300, 512), (600, 1024), (1700, 1800)])
 def test_matmul_of_nan_and_of_scales_behind_the_end(rows, outer):
     """A NaN reaches its own row or column alone; what lies behind a row's end (scales of NaN, codes) reaches nothing."""
     inner = 300
@@ -183,7 +183,7 @@ def test_matmul_of_nan_and_of_scales_behind_the_end(rows, outer):
     assert np.array_equal(nan, want)
 
 
-@pytest.mark.parametrize("rows", [1, 40, 300])
+@pytest.mark.parametrize("rows", [1, 40, 300, 12300])
 def test_matmul_of_far_apart_scales(rows):
     """Blocks whose scales are at the ends of the range: products that cancel their scales, and ones that vanish."""
     rng = np.random.default_rng(8)
@@ -207,7 +207,8 @@ def check_weight_grad(dy, x, dtype, out=None):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,inner,outer,tile", [(1, 1, 1, False), (1, 300, 200, False), (7, 130, 7, False), (64, 128, 128, False),
                                                    (65, 256, 264, True), (1000, 513, 257, False), (1001, 1024, 520, True), (2500, 300, 1000, False),
-                                                   (4096, 128, 64, False), (129, 2048, 1024, False)])
+                                                   (4096, 128, 64, False), (129, 2048, 1024, False),
+                                                   (1500, 1500, 2100, False), (700, 2600, 2060, True), (3000, 250, 130, False)])
 def test_weight_grad(rows, inner, outer, tile, dtype):
     dy = normal(rows, outer, BF16, rows, pad=16)
     x = random_held(rows, inner, tile, rows + 1, pad=16)
