@@ -23,8 +23,11 @@ __device__ __forceinline__ uint32_t address_in(uint32_t a, uint32_t rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
     return r;
 }
+// (Released to the block's scope, not the cluster's, whose fence waits for every access of the thread, a thousand cycles with
+// global loads in flight.  What the other block's products read by this is in tensor memory, or written to shared memory
+// through async_fence: both are complete, by tensor_wait_stores and that fence, before the arrival is sent.)
 __device__ __forceinline__ void barrier_arrive_in(uint32_t cluster_address) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_address) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_address) : "memory");
 }
 
 constexpr int kPolls = 1 << 20;  // of a wait; a poll itself may wait for some time
@@ -41,7 +44,7 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, cons
         asm volatile(
             "{\n\t"
             ".reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
             "selp.u32 %0, 1, 0, p;\n\t"
             "}"
             : "=r"(done)

@@ -53,6 +53,54 @@ __device__ __forceinline__ void fewer_registers() {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGISTERS));
 }
 
+// Column j of four neighbouring ones lies in place turned(j) of the converted operand, and so of the sums: two codes of a word
+// are made two values where they are, bytes 0 and 2, 1 and 3.
+__host__ __device__ constexpr int turned(int j) { return (j & ~3) | (j & 1) << 1 | (j & 2) >> 1; }
+
+// 64 codes of a row to bf16, by integer instructions (the conversion instructions run at a sixteenth of their rate, and took
+// three times as long as the product): a code's exponent and mantissa, in the places of bf16's, are its value times 2^-120,
+// subnormal ones too, and a product with 2^120 times the scale is exact.  False where that is not enough: a NaN among the
+// codes (magnitude 0x7f), a scale above 2^7, or NaN.
+__device__ __forceinline__ bool convert_row(uint32_t from, uint32_t to, int half, int row, uint32_t byte) {
+    const uint32_t one = (byte + 120u) << 7, factor = one | one << 16;
+    uint32_t most = 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t w[4], v[8];
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                     : "r"(from + (((half * 4 + j) ^ (row & 7)) << 4)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t even = (w[i] << 4) & 0x07f007f0u, odd = (w[i] >> 4) & 0x07f007f0u;
+            asm("max.u16x2 %0, %0, %1;" : "+r"(most) : "r"(even));
+            asm("max.u16x2 %0, %0, %1;" : "+r"(most) : "r"(odd));
+            asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(v[2 * i]) : "r"(((w[i] << 8) & 0x80008000u) | even), "r"(factor));
+            asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(v[2 * i + 1]) : "r"((w[i] & 0x80008000u) | odd), "r"(factor));
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((2 * j + i) ^ (row & 7)) << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]),
+                         "r"(v[4 * i + 2]), "r"(v[4 * i + 3])
+                         : "memory");
+    }
+    return byte <= 134u && (most & 0xffffu) != 0x07f0u && (most >> 16) != 0x07f0u;
+}
+// ... any codes and scale, by fp32.
+__device__ __noinline__ void convert_row_any(uint32_t from, uint32_t to, int half, int row, uint32_t byte) {
+    const float scale = scale_of(byte);
+    for (int j = 0; j < 8; ++j) {  // eight codes
+        uint32_t w[2], v[4];
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(from + (((half * 4 + j / 2) ^ (row & 7)) << 4) + j % 2 * 8));
+        for (int i = 0; i < 2; ++i) {
+            const float2 lo = values_of(w[i] & 0xffffu), hi = values_of(w[i] >> 16);
+            v[2 * i] = bf16x2_of(lo.x * scale, hi.x * scale);
+            v[2 * i + 1] = bf16x2_of(lo.y * scale, hi.y * scale);
+        }
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((j ^ (row & 7)) << 4)), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+    }
+}
+
 template <bool PAIR, class T>
 __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args p) {
     constexpr int kSide = PAIR ? 256 : 128;   // of a tile
@@ -176,39 +224,32 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                 const int64_t r = int64_t(kb) * kDepth + row;
                 return kb < end && r < p.x.rows && block < p.x.blocks ? __ldg(scales + (r >> p.x.shift) * p.x.ld_scales) : 127u;
             };
-            uint32_t ahead[3] = {scale_at(begin), scale_at(begin + 1), scale_at(begin + 2)};
-            for (int kb = begin; kb < end; ++kb, ++it) {
-                const uint32_t s = it % kStages, c = it % kConverted;
-                const float scale = scale_of(ahead[0]);
-                ahead[0] = ahead[1], ahead[1] = ahead[2], ahead[2] = scale_at(kb + 3);
-                ok = barrier_wait(full_x + 8 * s, (it / kStages) & 1, bounds) &&
-                     (it < kConverted || barrier_wait(converted_empty + 8 * c, (it / kConverted - 1) & 1, bounds));
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                const uint32_t from = base + s * kStageBytes + 2 * kAtom + row * 128, to = converted + c * kConvertedBytes + half * kAtom + row * 128;
+            // (loaded four stages at a time, four ahead: to hand a loaded value on is to wait for it)
+            uint32_t bytes[4], next[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t w[4], v[8];
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                                 : "r"(from + (((half * 4 + j) ^ (row & 7)) << 4)));
+            for (int i = 0; i < 4; ++i) next[i] = scale_at(begin + i);
+            for (int four = begin; four < end && ok; four += 4) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 lo = values_of(w[i] & 0xffffu), hi = values_of(w[i] >> 16);
-                        v[2 * i] = bf16x2_of(lo.x * scale, lo.y * scale);
-                        v[2 * i + 1] = bf16x2_of(hi.x * scale, hi.y * scale);
+                for (int i = 0; i < 4; ++i) bytes[i] = next[i];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) next[i] = scale_at(four + 4 + i);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (four + i >= end) break;
+                    const uint32_t s = it % kStages, c = it % kConverted;
+                    ok = barrier_wait(full_x + 8 * s, (it / kStages) & 1, bounds) &&
+                         (it < kConverted || barrier_wait(converted_empty + 8 * c, (it / kConverted - 1) & 1, bounds));
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    const uint32_t from = base + s * kStageBytes + 2 * kAtom + row * 128, to = converted + c * kConvertedBytes + half * kAtom + row * 128;
+                    if (!convert_row(from, to, half, row, bytes[i])) convert_row_any(from, to, half, row, bytes[i]);
+                    async_fence();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (PAIR) barrier_arrive_in(full_there + 8 * c);
+                        else barrier_arrive(full_there + 8 * c);
                     }
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((2 * j + i) ^ (row & 7)) << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]),
-                                     "r"(v[4 * i + 2]), "r"(v[4 * i + 3])
-                                     : "memory");
-                }
-                async_fence();
-                __syncwarp();
-                if (lane == 0) {
-                    if (PAIR) barrier_arrive_in(full_there + 8 * c);
-                    else barrier_arrive(full_there + 8 * c);
+                    ++it;
                 }
             }
         }
@@ -252,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
 #pragma unroll
                 for (int c = 0; c < kHeld / 4; ++c)
                     asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((half * (kHeld / 4) + c) ^ (lane & 7)) << 4)), "f"(sum[4 * c]),
-                                 "f"(sum[4 * c + 1]), "f"(sum[4 * c + 2]), "f"(sum[4 * c + 3])
+                                 "f"(sum[4 * c + 2]), "f"(sum[4 * c + 1]), "f"(sum[4 * c + 3])
                                  : "memory");
                 continue;  // (the only tile)
             }
@@ -263,8 +304,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                 uint32_t w[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
-                    if constexpr (sizeof(T) == 2) w[i] = bf16x2_of(sum[c * kColumns + 2 * i], sum[c * kColumns + 2 * i + 1]);
-                    else w[i] = __float_as_uint(sum[c * kColumns + i]);
+                    if constexpr (sizeof(T) == 2) w[i] = bf16x2_of(sum[c * kColumns + turned(2 * i)], sum[c * kColumns + turned(2 * i + 1)]);
+                    else w[i] = __float_as_uint(sum[c * kColumns + turned(i)]);
                 }
                 // A tiled store ends at a multiple of 16 bytes behind the last column: where that is not the row's end, and
                 // might be another matrix's, the last tile is stored by values.

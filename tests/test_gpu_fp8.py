@@ -426,3 +426,24 @@ def test_tensors_of_different_devices_are_refused():
         pvq.fp8_quantize(x[:, 1:])  # rows that do not start on 16-byte boundaries
     with pytest.raises(pvq.PvqError):
         pvq.fp8_quantize(x[:0])
+
+
+@pytest.mark.parametrize("rows,inner,outer", [(130, 300, 200), (200, 2000, 1800)])
+def test_weight_grad_of_every_code_at_the_ends_of_the_scales(rows, inner, outer):
+    """All codes but NaN, subnormal ones among them, under scales from 2^-100 to 2^100; one row of x a row of dy, so that a
+    sum has one product alone and is exact."""
+    rng = np.random.default_rng(9)
+    codes = rng.integers(0, 256, size=(rows, inner)).astype(np.uint8)
+    codes[(codes & 0x7f) == 0x7f] = 0x80
+    blocks = -(-inner // 128)
+    scales = np.full((rows, -(-blocks // 4) * 4), 255, dtype=np.uint8)
+    scales[:, :blocks] = rng.integers(27, 228, size=(rows, blocks))
+    padded = np.zeros((rows, -(-inner // 16) * 16), dtype=np.uint8)
+    padded[:, :inner] = codes
+    x = pvq.Fp8Matrix(torch.from_numpy(padded).cuda()[:, :inner].view(torch.float8_e4m3fn),
+                      torch.from_numpy(scales).cuda()[:, :blocks].view(torch.float8_e8m0fnu), False)
+    dy = np.zeros((rows, outer), dtype=np.float32)
+    where = rng.integers(0, rows, size=outer)
+    dy[where, np.arange(outer)] = np.where(np.arange(outer) % 2 == 0, 1.0, -2.0)
+    got = ref.to64(pvq.fp8_weight_grad(torch.from_numpy(dy).to(BF16).cuda(), x))
+    assert np.array_equal(got, ref.values(x)[where] * np.where(np.arange(outer) % 2 == 0, 1.0, -2.0)[:, None])
