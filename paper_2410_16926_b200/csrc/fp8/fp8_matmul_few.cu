@@ -6,8 +6,8 @@
 // then every block adds the parts of its share of the columns, in the order of the ranks (no atomics: the same bits every
 // time), reading the others' shared memory.
 //
-// Warps: one issues the copies, one the products, one allocates tensor memory, four bring the scales there (double-buffered,
-// four blocks along k at a time) and then read the result.
+// Warps: one issues the copies, one the products, one allocates tensor memory, four bring the scales there (four
+// blocks along k at a time, in four sets of columns) and then read the result.
 #include "fp8_matmul.cuh"
 
 namespace pvq {
@@ -22,10 +22,11 @@ struct Shape {
     static constexpr int kStages = ROWS <= 32 ? 5 : (ROWS == 64 ? 4 : 6);  // two blocks an SM up to 64 rows
     static constexpr int kWordsB = ROWS <= 32 ? 1 : ROWS / 32;             // of scales, a lane
     static constexpr int kScales = ROWS < 32 ? 32 : ROWS;                  // columns before them
-    static constexpr int kColumns = ROWS == 128 ? 256 : (ROWS == 64 ? 128 : 64);  // of tensor memory: ROWS + 2 * (4 + 4) at most, a power of two
+    static constexpr int kScaleSets = 4;
+    static constexpr int kColumns = ROWS == 128 ? 256 : (ROWS == 64 ? 128 : 64);  // of tensor memory, a power of two
     static constexpr size_t kShared = 1024 + kStages * kStageBytes + 256;
     static_assert(kStages * kStageBytes >= ROWS * 512, "the result takes the stages' place");
-    static_assert(kScales + 16 <= kColumns, "tensor memory");
+    static_assert(kScales + 8 * kScaleSets <= kColumns, "tensor memory");
 };
 
 struct Maps {
@@ -38,7 +39,7 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
     extern __shared__ uint8_t raw[];
     const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
     const uint32_t full = base + S::kStages * S::kStageBytes, empty = full + 8 * S::kStages, scales_full = empty + 8 * S::kStages,
-                   scales_empty = scales_full + 16, sum_full = scales_empty + 16;
+                   scales_empty = scales_full + 8 * S::kScaleSets, sum_full = scales_empty + 8 * S::kScaleSets;
     __shared__ uint32_t tensor_base;
     __shared__ int over;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -46,7 +47,7 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
     if (threadIdx.x == 0) {
         over = 0;
         for (int i = 0; i < S::kStages; ++i) barrier_init(full + 8 * i, 1), barrier_init(empty + 8 * i, 1);
-        for (int i = 0; i < 2; ++i) barrier_init(scales_full + 8 * i, 4), barrier_init(scales_empty + 8 * i, 1);
+        for (int i = 0; i < S::kScaleSets; ++i) barrier_init(scales_full + 8 * i, 4), barrier_init(scales_empty + 8 * i, 1);
         barrier_init(sum_full, 1);
         barrier_init_fence();
         prefetch_map(&maps.a), prefetch_map(&maps.b);
@@ -62,74 +63,85 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
     const int first = static_cast<int>(int64_t(blocks) * rank / split), last = static_cast<int>(int64_t(blocks) * (rank + 1) / split);  // (split <= blocks)
 
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t it = 0;
+        if (elected()) {
+            Turn<S::kStages> turn;
+            uint32_t issued = 0;
             bool ok = true;
-            for (int kb = first; kb < last; ++kb, ++it) {
-                const uint32_t s = it % S::kStages, at = base + s * S::kStageBytes;
-                if (it >= S::kStages && !barrier_wait(empty + 8 * s, (it / S::kStages - 1) & 1, bounds)) {
-                    ok = false;
-                    break;
-                }
-                barrier_expect(full + 8 * s, S::kStageBytes);
-                if (ACROSS) load_tile<false>(at, &maps.b, static_cast<int>(col0), kb * kBlock, full + 8 * s);
-                else load_tile<false>(at, &maps.b, kb * kBlock, static_cast<int>(col0), full + 8 * s);
-                load_tile<false>(at + 128 * kBlock, &maps.a, kb * kBlock, static_cast<int>(row0), full + 8 * s);
+            for (int kb = first; kb < last; ++kb) {
+                const uint32_t at = base + turn.at * S::kStageBytes;
+                ok = barrier_wait(empty + 8 * turn.at, turn.parity ^ 1, bounds);
+                if (!ok) break;
+                barrier_expect(full + 8 * turn.at, S::kStageBytes);
+                if (ACROSS) load_tile<false>(at, &maps.b, static_cast<int>(col0), kb * kBlock, full + 8 * turn.at);
+                else load_tile<false>(at, &maps.b, kb * kBlock, static_cast<int>(col0), full + 8 * turn.at);
+                load_tile<false>(at + 128 * kBlock, &maps.a, kb * kBlock, static_cast<int>(row0), full + 8 * turn.at);
+                turn.next();
+                ++issued;
             }
             if (!ok)  // copies in flight have to land before the block ends
-                for (uint32_t i = it > S::kStages ? it - S::kStages : 0; i < it; ++i)
-                    for (int polls = 0; polls < 64 && !barrier_wait(full + 8 * (i % S::kStages), (i / S::kStages) & 1, bounds); ++polls) {}
+                for (uint32_t i = issued > S::kStages ? issued - S::kStages : 0; i < issued; ++i)
+                    for (int polls = 0; polls < kLandings && !barrier_passed(full + 8 * (i % S::kStages), (i / S::kStages) & 1); ++polls) {}
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (elected()) {
             constexpr uint32_t product = product_e4m3(128, ROWS, ACROSS, false);
-            uint32_t it = 0, four = 0;
-            for (int kb = first; kb < last; ++kb, ++it) {
-                const uint32_t s = it % S::kStages, buffer = four & 1;
-                if ((kb == first || kb % 4 == 0) && !barrier_wait(scales_full + 8 * buffer, (four >> 1) & 1, bounds)) break;
-                if (!barrier_wait(full + 8 * s, (it / S::kStages) & 1, bounds)) break;
+            constexpr uint32_t kAlongW = (ACROSS ? 32 * kBlock : 32) >> 4;
+            const uint64_t w0 = operand(base, ACROSS ? 128 * kBlock : 16), x0 = operand(base + 128 * kBlock);
+            Turn<S::kStages> turn;
+            Turn<S::kScaleSets> scales;
+            bool ok = true;
+            for (int kb = first; kb < last; ++kb) {
+                const uint32_t part = kb & 3;
+                if (part == 0 || kb == first) ok = barrier_wait(scales_full + 8 * scales.at, scales.parity, bounds);
+                ok = ok && barrier_wait(full + 8 * turn.at, turn.parity, bounds);
+                if (!ok) break;
                 tensor_fence_after();
-                const uint32_t w = base + s * S::kStageBytes, x = w + 128 * kBlock;
+                const uint64_t w = w0 + turn.at * (S::kStageBytes >> 4), x = x0 + turn.at * (S::kStageBytes >> 4);
+                const uint32_t sw = tensor + S::kScales + 8 * scales.at, with = with_part(product, part);
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    multiply_e4m3<false>(tensor, operand(w + (ACROSS ? 32 * kBlock : 32) * k, ACROSS ? 128 * kBlock : 16), operand(x + 32 * k),
-                                         with_part(product, kb % 4), tensor + S::kScales + 8 * buffer, tensor + S::kScales + 8 * buffer + 4,
-                                         it > 0 || k > 0);
-                products_done<false>(empty + 8 * s);
-                if (kb % 4 == 3) {
-                    products_done<false>(scales_empty + 8 * buffer);
-                    ++four;
+                for (int k = 0; k < 4; ++k) multiply_e4m3<false>(tensor, w + kAlongW * k, x + 2 * k, with, sw, sw + 4, kb > first || k > 0);
+                products_done<false>(empty + 8 * turn.at);
+                turn.next();
+                if (part == 3) {
+                    products_done<false>(scales_empty + 8 * scales.at);
+                    scales.next();
                 }
             }
             products_done<false>(sum_full);
-            if (over)
-                for (int polls = 0; polls < 64 && !barrier_wait(sum_full, 0, bounds); ++polls) {}
+            for (int polls = 0; !ok && polls < kLandings && !barrier_passed(sum_full, 0); ++polls) {}
         }
     } else if (warp >= 4) {
         const uint32_t mine = tensor + ((warp & 3) << 21);
-        uint32_t four = 0;
+        Turn<S::kScaleSets> turn;
         bool ok = true;
-        for (int f = first / 4; f <= (last - 1) / 4; ++f, ++four) {
-            const uint32_t buffer = four & 1;
-            uint32_t w[4], x[S::kWordsB];
-            scale_words<ACROSS>(p.b, col0, f, w);
-            if (p.a.shift && ROWS < 128) {  // (the rows do not begin at a tile of its scales)
+        // asked for as many steps at once as there are sets of columns: to wait for one before the next is a microsecond each
+        for (int f0 = first / 4; f0 <= (last - 1) / 4 && ok; f0 += S::kScaleSets) {
+            uint32_t w[S::kScaleSets][4], x[S::kScaleSets][S::kWordsB];
 #pragma unroll
-                for (int j = 0; j < S::kWordsB; ++j) x[j] = scale_word<false>(p.a, row0 + 32 * j + lane, f);
-            } else {
-                scale_words<false>(p.a, row0, f, x);
+            for (int i = 0; i < S::kScaleSets; ++i) {
+                if (f0 + i > (last - 1) / 4) break;
+                scale_words<ACROSS>(p.b, col0, f0 + i, w[i]);
+                if (p.a.shift && ROWS < 128) {  // (the rows do not begin at a tile of its scales)
+#pragma unroll
+                    for (int j = 0; j < S::kWordsB; ++j) x[i][j] = scale_word<false>(p.a, row0 + 32 * j + lane, f0 + i);
+                } else {
+                    scale_words<false>(p.a, row0, f0 + i, x[i]);
+                }
             }
-            if (four >= 2) {
-                ok = __all_sync(0xffffffffu, barrier_wait(scales_empty + 8 * buffer, ((four >> 1) - 1) & 1, bounds));
+#pragma unroll
+            for (int i = 0; i < S::kScaleSets; ++i) {
+                if (f0 + i > (last - 1) / 4) break;
+                ok = __all_sync(0xffffffffu, barrier_wait(scales_empty + 8 * turn.at, turn.parity ^ 1, bounds));
                 if (!ok) break;
                 tensor_fence_after();
+                tensor_store(mine + S::kScales + 8 * turn.at, w[i]);
+                tensor_store(mine + S::kScales + 8 * turn.at + 4, x[i]);
+                tensor_wait_stores();
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(scales_full + 8 * turn.at);
+                turn.next();
             }
-            tensor_store(mine + S::kScales + 8 * buffer, w);
-            tensor_store(mine + S::kScales + 8 * buffer + 4, x);
-            tensor_wait_stores();
-            tensor_fence_before();
-            __syncwarp();
-            if (lane == 0) barrier_arrive(scales_full + 8 * buffer);
         }
         ok = ok && __all_sync(0xffffffffu, barrier_wait(sum_full, 0, bounds));
         ok = ok && !over;

@@ -68,94 +68,110 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) matmul_
     const int blocks = static_cast<int>((p.inner + kBlock - 1) / kBlock), first = blockIdx.x / 2, step = gridDim.x / 2;
 
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t it = 0;
+        if (elected()) {
+            Turn<kStages> turn;
+            uint32_t issued = 0;
             bool ok = true;
             const uint32_t full_there = address_in(full, 0);
             for (int t = first; t < tiles.count() && ok; t += step) {
                 int m, n;
                 tiles.at(t, &m, &n);
                 const int row = m * 256 + rank * 128, col = n * 256 + rank * 128;
-                for (int kb = 0; kb < blocks; ++kb, ++it) {
-                    const uint32_t s = it % kStages, at = base + s * kStageBytes;
-                    if (it >= kStages && !barrier_wait(empty + 8 * s, (it / kStages - 1) & 1, bounds)) {
-                        ok = false;
-                        break;
-                    }
-                    if (rank == 0) barrier_expect(full + 8 * s, 2 * kStageBytes);  // both blocks' tiles
-                    load_tile<true>(at, &maps.a, kb * kBlock, row, full_there + 8 * s);
-                    if (ACROSS) load_tile<true>(at + kStageBytes / 2, &maps.b, col, kb * kBlock, full_there + 8 * s);
-                    else load_tile<true>(at + kStageBytes / 2, &maps.b, kb * kBlock, col, full_there + 8 * s);
+                for (int kb = 0; kb < blocks; ++kb) {
+                    const uint32_t at = base + turn.at * kStageBytes;
+                    ok = barrier_wait(empty + 8 * turn.at, turn.parity ^ 1, bounds);
+                    if (!ok) break;
+                    if (rank == 0) barrier_expect(full + 8 * turn.at, 2 * kStageBytes);  // both blocks' tiles
+                    load_tile<true>(at, &maps.a, kb * kBlock, row, full_there + 8 * turn.at);
+                    if (ACROSS) load_tile<true>(at + kStageBytes / 2, &maps.b, col, kb * kBlock, full_there + 8 * turn.at);
+                    else load_tile<true>(at + kStageBytes / 2, &maps.b, kb * kBlock, col, full_there + 8 * turn.at);
+                    turn.next();
+                    ++issued;
                 }
             }
-            if (!ok && rank == 0) {  // copies in flight have to land before the block ends
-                const Bounds alone{&over, p.status};
-                for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
-                    for (int polls = 0; polls < 64 && !barrier_wait(full + 8 * (i % kStages), (i / kStages) & 1, alone); ++polls) {}
-            }
+            if (!ok && rank == 0)  // copies in flight have to land before the block ends
+                for (uint32_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
+                    for (int polls = 0; polls < kLandings && !barrier_passed(full + 8 * (i % kStages), (i / kStages) & 1); ++polls) {}
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elected()) {
             constexpr uint32_t product = product_e4m3(256, 256, false, ACROSS);
-            uint32_t it = 0, four = 0, tile = 0;
+            constexpr uint32_t kAlongB = (ACROSS ? 32 * kBlock : 32) >> 4;
+            const uint64_t a0 = operand(base), b0 = operand(base + kStageBytes / 2, ACROSS ? kStageBytes / 2 : 16);
+            Turn<kStages> turn;
+            Turn<2> scales;
+            uint32_t sum_parity = 1;
             bool ok = true;
-            for (int t = first; t < tiles.count() && ok; t += step, ++tile) {
-                if (tile > 0 && !barrier_wait(sum_empty, (tile - 1) & 1, bounds)) break;
+            for (int t = first; t < tiles.count() && ok; t += step, sum_parity ^= 1) {
+                ok = barrier_wait(sum_empty, sum_parity, bounds);
+                if (!ok) break;
                 tensor_fence_after();
-                for (int kb = 0; kb < blocks; ++kb, ++it) {
-                    const uint32_t s = it % kStages, buffer = four & 1;
-                    if (kb % 4 == 0 && !barrier_wait(scales_full + 8 * buffer, (four >> 1) & 1, bounds)) {
-                        ok = false;
-                        break;
-                    }
-                    if (!barrier_wait(full + 8 * s, (it / kStages) & 1, bounds)) {
-                        ok = false;
-                        break;
-                    }
+                for (int kb = 0; kb < blocks; ++kb) {
+                    const uint32_t part = kb & 3;
+                    if (part == 0) ok = barrier_wait(scales_full + 8 * scales.at, scales.parity, bounds);
+                    ok = ok && barrier_wait(full + 8 * turn.at, turn.parity, bounds);
+                    if (!ok) break;
                     tensor_fence_after();
-                    const uint32_t a = base + s * kStageBytes, b = a + kStageBytes / 2;
+                    const uint64_t a = a0 + turn.at * (kStageBytes >> 4), b = b0 + turn.at * (kStageBytes >> 4);
+                    const uint32_t sa = tensor + kScalesA + 4 * scales.at, sb = tensor + kScalesB + 8 * scales.at, with = with_part(product, part);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        multiply_e4m3<true>(tensor, operand(a + 32 * k), operand(b + (ACROSS ? 32 * kBlock : 32) * k, ACROSS ? kStageBytes / 2 : 16),
-                                            with_part(product, kb % 4), tensor + kScalesA + 4 * buffer, tensor + kScalesB + 8 * buffer, kb > 0 || k > 0);
-                    products_done<true>(empty + 8 * s);
-                    if (kb % 4 == 3 || kb == blocks - 1) {
-                        products_done<true>(scales_empty + 8 * buffer);
-                        ++four;
+                    for (int k = 0; k < 4; ++k) multiply_e4m3<true>(tensor, a + 2 * k, b + kAlongB * k, with, sa, sb, kb > 0 || k > 0);
+                    products_done<true>(empty + 8 * turn.at);
+                    turn.next();
+                    if (part == 3 || kb == blocks - 1) {
+                        products_done<true>(scales_empty + 8 * scales.at);
+                        scales.next();
                     }
                 }
                 if (ok) products_done<true>(sum_full);
             }
             if (!ok) {
                 products_done<true>(drained);
-                for (int polls = 0; polls < 64 && !barrier_wait(drained, 0, bounds); ++polls) {}
+                for (int polls = 0; polls < kLandings && !barrier_passed(drained, 0); ++polls) {}
             }
         }
     } else if (warp >= 4 && warp < 8) {
         const uint32_t mine = tensor + ((warp & 3) << 21);
         const uint32_t full_there = address_in(scales_full, 0);
-        uint32_t four = 0;
-        bool ok = true;
-        for (int t = first; t < tiles.count() && ok; t += step) {
-            int m, n;
-            tiles.at(t, &m, &n);
-            for (int kb = 0; kb < blocks; kb += 4, ++four) {
-                const uint32_t buffer = four & 1;
-                uint32_t a[4], b[8];
-                scale_words<false>(p.a, int64_t(m) * 256 + rank * 128, kb / 4, a);
-                scale_words<ACROSS>(p.b, int64_t(n) * 256, kb / 4, b);
-                if (four >= 2) {
-                    ok = __all_sync(0xffffffffu, barrier_wait(scales_empty + 8 * buffer, ((four >> 1) - 1) & 1, bounds));
-                    if (!ok) break;
-                    tensor_fence_after();
-                }
-                tensor_store(mine + kScalesA + 4 * buffer, a);
-                tensor_store(mine + kScalesB + 8 * buffer, b);
-                tensor_wait_stores();
-                tensor_fence_before();
-                __syncwarp();
-                if (lane == 0) barrier_arrive_in(full_there + 8 * buffer);
+        // The words of four blocks along k are asked for two such steps before they are needed, in two sets of registers that
+        // take turns (to hand a loaded word on is to wait for it): one step at a time took 350 ns a block.
+        struct Step {
+            int t, kb;
+        } next{first, 0};
+        uint32_t a[2][4], b[2][8], four = 0;
+        const auto load = [&](uint32_t (&a)[4], uint32_t (&b)[8]) {
+            if (next.t < tiles.count()) {
+                int m, n;
+                tiles.at(next.t, &m, &n);
+                scale_words<false>(p.a, int64_t(m) * 256 + rank * 128, next.kb / 4, a);
+                scale_words<ACROSS>(p.b, int64_t(n) * 256, next.kb / 4, b);
+                next.kb += 4;
+                if (next.kb >= blocks) next.kb = 0, next.t += step;
             }
+        };
+        const auto put = [&](const uint32_t (&a)[4], const uint32_t (&b)[8]) -> bool {
+            const uint32_t buffer = four & 1;
+            if (four >= 2) {
+                if (!__all_sync(0xffffffffu, barrier_wait(scales_empty + 8 * buffer, ((four >> 1) - 1) & 1, bounds))) return false;
+                tensor_fence_after();
+            }
+            tensor_store(mine + kScalesA + 4 * buffer, a);
+            tensor_store(mine + kScalesB + 8 * buffer, b);
+            tensor_wait_stores();
+            tensor_fence_before();
+            __syncwarp();
+            if (lane == 0) barrier_arrive_in(full_there + 8 * buffer);
+            ++four;
+            return true;
+        };
+        load(a[0], b[0]);
+        load(a[1], b[1]);
+        const int64_t steps = int64_t((tiles.count() - first + step - 1) / step) * ((blocks + 3) / 4);
+        for (int64_t i = 0; i < steps; i += 2) {
+            if (!put(a[0], b[0])) break;
+            load(a[0], b[0]);
+            if (i + 1 >= steps || !put(a[1], b[1])) break;
+            load(a[1], b[1]);
         }
     } else if (warp >= 8) {
         constexpr int kColumns = 128 / sizeof(T);  // of a stored tile

@@ -30,33 +30,56 @@ __device__ __forceinline__ void barrier_arrive_in(uint32_t cluster_address) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_address) : "memory");
 }
 
-constexpr int kPolls = 1 << 20;  // of a wait; a poll itself may wait for some time
+constexpr int kPolls = 1 << 20;     // of a wait; a poll itself may wait for some time
+constexpr int kLandings = 1 << 14;  // of a wait for what is in flight, once another wait has run out
 
 // What a block shares about waits that ran out: one that does ends all others, and sets the status word.
 struct Bounds {
     volatile int* over;
     uint32_t* status;
 };
-// Waits for the phase `parity`; false when that took too long here or in another thread.
+__device__ __forceinline__ bool barrier_passed(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t"
+        "}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done;
+}
+// Waits for the phase `parity` (a new barrier counts as past the phase before its first, of parity 1); false when that took too
+// long here or in another thread.
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, const Bounds& b) {
+#pragma unroll 1
     for (int i = 0; i < kPolls; ++i) {
-        uint32_t done;
-        asm volatile(
-            "{\n\t"
-            ".reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t"
-            "}"
-            : "=r"(done)
-            : "r"(bar), "r"(parity)
-            : "memory");
-        if (done) return true;
+        if (barrier_passed(bar, parity)) return true;
         if ((i & 63) == 63 && *b.over) return false;
     }
     *b.over = 1;
     if (b.status) atomicOr(b.status, PVQ_STATUS_STAGING_TIMEOUT);
     return false;
 }
+
+// One thread of the warp, all of which call it.  What it does alone has to be under this, not under a comparison of lanes:
+// the products' operands are then known to be the same for all threads that are there (a quarter of the time of a tile).
+__device__ __forceinline__ bool elected() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0u;
+}
+
+// A ring's place and the parity of its turn.
+template <int SIZE>
+struct Turn {
+    uint32_t at = 0, parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++at == SIZE) at = 0, parity ^= 1;
+    }
+};
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;

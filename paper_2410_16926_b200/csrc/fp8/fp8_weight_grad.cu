@@ -1,7 +1,7 @@
 // The gradient of a weight from the 8-bit input that was kept: out[o][i] = sum_t dy[t][o] x[t][i].
 //
 // The scales of x lie along t, inside the sum, so x is made bf16 (a code times a power of two: exact) on its way to the
-// tensor cores: tiles of codes arrive by tiled copies, four warps convert them into the operand's layout, and the product
+// tensor cores: tiles of codes arrive by tiled copies, eight warps convert them into the operand's layout, and the product
 // takes both operands across k, as they lie in memory.  The tensor cores cut off what an addition to a running sum loses
 // instead of rounding it: over 16384 values of t a sum in tensor memory ends 1.9e-5 of itself too small.  So after every
 // 512 values of t the sum is read and added to one in registers (fp32, rounded to nearest), while the products go on in
@@ -11,17 +11,17 @@
 // Otherwise a block makes 128 x 128, and where there are few tiles the blocks of a cluster split t, and add their sums
 // through one another's shared memory in the order of the ranks.
 //
-// Warps of a block: one issues the copies, one the products, four convert, eight hold and store the sums.
+// Warps of a block: one issues the copies, one the products, eight convert, eight hold and store the sums.
 #include "fp8_mma.cuh"
 
 namespace pvq {
 namespace fp8 {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 640;
 constexpr int kDepth = 64;                    // values of t a stage
-constexpr int kStages = 6, kStageBytes = 128 * kDepth * 3;  // 128 columns of dy (bf16), 128 of x (codes)
-constexpr int kConverted = 3, kConvertedBytes = 128 * kDepth * 2;
+constexpr int kStages = 5, kStageBytes = 128 * kDepth * 3;  // 128 columns of dy (bf16), 128 of x (codes)
+constexpr int kConverted = 4, kConvertedBytes = 128 * kDepth * 2;
 constexpr int kRun = 512 / kDepth;            // stages that are added in tensor memory
 constexpr int kStoreBytes = 4096;             // 32 rows of 128 bytes
 constexpr int kAtom = kDepth * 128;           // bytes from 64 bf16 columns to the next 64
@@ -39,10 +39,10 @@ struct Args {
     int split;
 };
 
-// Registers a thread of the four warpgroups of a pair's block: what all are launched with, shared out anew.  A sum of 128
+// Registers a thread of the five warpgroups of a pair's block: what all are launched with, shared out anew.  A sum of 128
 // columns takes 128 of them.
-constexpr int kRegisters = 128, kFew = 48, kSome = 64, kMany = 200;
-static_assert(kFew + kSome + 2 * kMany <= 4 * kRegisters, "a share beyond these would be waited for without end");
+constexpr int kRegisters = 96, kFew = 32, kSome = 56, kMany = 168;
+static_assert(kFew + 2 * kSome + 2 * kMany <= 5 * kRegisters, "a share beyond these would be waited for without end");
 
 template <int REGISTERS>
 __device__ __forceinline__ void more_registers() {
@@ -87,8 +87,9 @@ __device__ __forceinline__ bool convert_row(uint32_t from, uint32_t to, int half
     return byte <= 134u && (most & 0xffffu) != 0x07f0u && (most >> 16) != 0x07f0u;
 }
 // ... any codes and scale, by fp32.
-__device__ __noinline__ void convert_row_any(uint32_t from, uint32_t to, int half, int row, uint32_t byte) {
+__device__ __forceinline__ void convert_row_any(uint32_t from, uint32_t to, int half, int row, uint32_t byte) {
     const float scale = scale_of(byte);
+#pragma unroll 1
     for (int j = 0; j < 8; ++j) {  // eight codes
         uint32_t w[2], v[4];
         asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(from + (((half * 4 + j / 2) ^ (row & 7)) << 4) + j % 2 * 8));
@@ -146,118 +147,117 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     };
 
     if (warp < 4) {
-        if (PAIR) fewer_registers<kFew>();
-        if (warp == 0 && lane == 0) {
-            uint32_t it = 0;
+        fewer_registers<kFew>();
+        if (warp == 0 && elected()) {
+            Turn<kStages> turn;
+            uint32_t issued = 0;
             bool ok = true;
             const uint32_t full_there = PAIR ? address_in(full_dy, 0) : full_dy;
             for (int t = blockIdx.x / team; t < tiles && ok; t += step) {
                 int m, n;
                 tile_at(t, &m, &n);
                 const int row = m * kSide + rank * 128, col = n * kSide + rank * 128;
-                for (int kb = begin; kb < end; ++kb, ++it) {
-                    const uint32_t s = it % kStages, at = base + s * kStageBytes;
-                    if (it >= kStages && !barrier_wait(empty + 8 * s, (it / kStages - 1) & 1, bounds)) {
-                        ok = false;
-                        break;
-                    }
-                    if (rank == 0) barrier_expect(full_dy + 8 * s, kBlocks * 2 * kAtom);
-                    load_tile<PAIR>(at, &maps.dy, row, kb * kDepth, full_there + 8 * s);
-                    load_tile<PAIR>(at + kAtom, &maps.dy, row + 64, kb * kDepth, full_there + 8 * s);
-                    barrier_expect(full_x + 8 * s, kAtom);
-                    load_tile<false>(at + 2 * kAtom, &maps.x, col, kb * kDepth, full_x + 8 * s);
+                for (int kb = begin; kb < end; ++kb) {
+                    const uint32_t at = base + turn.at * kStageBytes;
+                    ok = barrier_wait(empty + 8 * turn.at, turn.parity ^ 1, bounds);
+                    if (!ok) break;
+                    if (rank == 0) barrier_expect(full_dy + 8 * turn.at, kBlocks * 2 * kAtom);
+                    barrier_expect(full_x + 8 * turn.at, kAtom);
+                    load_tile<false>(at + 2 * kAtom, &maps.x, col, kb * kDepth, full_x + 8 * turn.at);
+                    load_tile<PAIR>(at, &maps.dy, row, kb * kDepth, full_there + 8 * turn.at);
+                    load_tile<PAIR>(at + kAtom, &maps.dy, row + 64, kb * kDepth, full_there + 8 * turn.at);
+                    turn.next();
+                    ++issued;
                 }
             }
             if (!ok)  // copies in flight have to land before the block ends
-                for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
-                    for (int polls = 0; polls < 64 && !((rank != 0 || barrier_wait(full_dy + 8 * (i % kStages), (i / kStages) & 1, bounds)) &&
-                                                        barrier_wait(full_x + 8 * (i % kStages), (i / kStages) & 1, bounds));
-                         ++polls) {}
-        } else if (warp == 1 && lane == 0 && rank == 0) {
+                for (uint32_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i) {
+                    const uint32_t s = i % kStages, parity = (i / kStages) & 1;
+                    for (int polls = 0; polls < kLandings && !((rank != 0 || barrier_passed(full_dy + 8 * s, parity)) && barrier_passed(full_x + 8 * s, parity)); ++polls) {}
+                }
+        } else if (warp == 1 && rank == 0 && elected()) {
             constexpr uint32_t product = product_bf16(kSide, kSide, true, true);
-            uint32_t it = 0, run = 0;
+            const uint64_t a0 = operand(base, kAtom), b0 = operand(converted, kAtom);
+            Turn<kStages> turn;
+            Turn<kConverted> ready;
+            Turn<2> sums;
             bool ok = true;
-            for (int t = blockIdx.x / team; t < tiles && ok; t += step)
-                for (int kb = begin; kb < end; ++kb, ++it) {
-                    const uint32_t s = it % kStages, c = it % kConverted, buffer = run & 1;
-                    const int within = (kb - begin) % kRun;
-                    if (within == 0) {
-                        if (run >= 2 && !barrier_wait(sum_empty + 8 * buffer, ((run >> 1) - 1) & 1, bounds)) {
-                            ok = false;
-                            break;
-                        }
-                    }
-                    if (!barrier_wait(full_dy + 8 * s, (it / kStages) & 1, bounds) || !barrier_wait(converted_full + 8 * c, (it / kConverted) & 1, bounds)) {
-                        ok = false;
-                        break;
-                    }
+            for (int t = blockIdx.x / team; t < tiles && ok; t += step) {
+                int within = 0;
+                for (int kb = begin; kb < end; ++kb) {
+                    if (within == 0) ok = barrier_wait(sum_empty + 8 * sums.at, sums.parity ^ 1, bounds);
+                    ok = ok && barrier_wait(full_dy + 8 * turn.at, turn.parity, bounds) && barrier_wait(converted_full + 8 * ready.at, ready.parity, bounds);
+                    if (!ok) break;
                     tensor_fence_after();
-                    const uint32_t a = base + s * kStageBytes, b = converted + c * kConvertedBytes;
+                    const uint64_t a = a0 + turn.at * (kStageBytes >> 4), b = b0 + ready.at * (kConvertedBytes >> 4);
 #pragma unroll
-                    for (int k = 0; k < kDepth / 16; ++k)
-                        multiply_bf16<PAIR>(tensor + buffer * kSide, operand(a + 2048 * k, kAtom), operand(b + 2048 * k, kAtom), product, within > 0 || k > 0);
-                    products_done<PAIR>(empty + 8 * s);
-                    products_done<PAIR>(converted_empty + 8 * c);
-                    if (within == kRun - 1 || kb == end - 1) {
-                        products_done<PAIR>(sum_full + 8 * buffer);
-                        ++run;
+                    for (int k = 0; k < kDepth / 16; ++k) multiply_bf16<PAIR>(tensor + sums.at * kSide, a + 128 * k, b + 128 * k, product, within > 0 || k > 0);
+                    products_done<PAIR>(empty + 8 * turn.at);
+                    products_done<PAIR>(converted_empty + 8 * ready.at);
+                    turn.next();
+                    ready.next();
+                    if (++within == kRun || kb == end - 1) {
+                        products_done<PAIR>(sum_full + 8 * sums.at);
+                        sums.next();
+                        within = 0;
                     }
                 }
+            }
             if (!ok) {
                 products_done<PAIR>(drained);
-                for (int polls = 0; polls < 64 && !barrier_wait(drained, 0, bounds); ++polls) {}
+                for (int polls = 0; polls < kLandings && !barrier_passed(drained, 0); ++polls) {}
             }
         }
-    } else if (warp < 8) {
-        if (PAIR) fewer_registers<kSome>();
+    } else if (warp < 12) {
+        fewer_registers<kSome>();
         // a thread takes 64 codes of one t: a row of the tile, eight neighbouring rows in eight different places
         const int row = lane + 32 * (warp & 1), half = (warp >> 1) & 1;
         const uint32_t full_there = PAIR ? address_in(converted_full, 0) : converted_full;
-        uint32_t it = 0;
+        const int turn = (warp - 4) >> 2;  // four warps take a tile's even stages, four the odd ones
+        uint32_t it0 = 0;
         bool ok = true;
-        for (int t = blockIdx.x / team; t < tiles && ok; t += step) {
+        for (int t = blockIdx.x / team; t < tiles && ok; t += step, it0 += end - begin) {
             int m, n;
             tile_at(t, &m, &n);
             const int block = n * (kSide / kBlock) + rank;
             const uint8_t* scales = p.x.scales + block;
             const auto scale_at = [&](int kb) -> uint32_t {  // (rows behind the end: codes of zero)
-                const int64_t r = int64_t(kb) * kDepth + row;
-                return kb < end && r < p.x.rows && block < p.x.blocks ? __ldg(scales + (r >> p.x.shift) * p.x.ld_scales) : 127u;
+                const uint32_t r = uint32_t(kb) * kDepth + row;
+                return kb < end && r < uint32_t(p.x.rows) && block < p.x.blocks ? __ldg(scales + (r >> p.x.shift) * p.x.ld_scales) : 127u;
             };
-            // (loaded four stages at a time, four ahead: to hand a loaded value on is to wait for it)
-            uint32_t bytes[4], next[4];
+            // (loaded for four stages at a time, those of the next four meanwhile: to hand a loaded value on is to wait for it)
+            uint32_t bytes, next[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) next[i] = scale_at(begin + i);
-            for (int four = begin; four < end && ok; four += 4) {
+            for (int i = 0; i < 4; ++i) next[i] = scale_at(begin + turn + 2 * i);
+            for (int kb0 = begin + turn; kb0 < end && ok; kb0 += 8) {
+                bytes = next[0] | next[1] << 8 | next[2] << 16 | next[3] << 24;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) bytes[i] = next[i];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) next[i] = scale_at(four + 4 + i);
+                for (int i = 0; i < 4; ++i) next[i] = scale_at(kb0 + 8 + 2 * i);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (four + i >= end) break;
-                    const uint32_t s = it % kStages, c = it % kConverted;
+                    if (kb0 + 2 * i >= end) break;
+                    const uint32_t it = it0 + (kb0 + 2 * i - begin), s = it % kStages, c = it % kConverted;
                     ok = barrier_wait(full_x + 8 * s, (it / kStages) & 1, bounds) &&
                          (it < kConverted || barrier_wait(converted_empty + 8 * c, (it / kConverted - 1) & 1, bounds));
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     const uint32_t from = base + s * kStageBytes + 2 * kAtom + row * 128, to = converted + c * kConvertedBytes + half * kAtom + row * 128;
-                    if (!convert_row(from, to, half, row, bytes[i])) convert_row_any(from, to, half, row, bytes[i]);
+                    const uint32_t byte = (bytes >> (8 * i)) & 0xffu;
+                    if (!convert_row(from, to, half, row, byte)) convert_row_any(from, to, half, row, byte);
                     async_fence();
                     __syncwarp();
                     if (lane == 0) {
                         if (PAIR) barrier_arrive_in(full_there + 8 * c);
                         else barrier_arrive(full_there + 8 * c);
                     }
-                    ++it;
                 }
             }
         }
     } else {
-        if (PAIR) more_registers<kMany>();
+        more_registers<kMany>();
         constexpr int kColumns = 128 / sizeof(T);  // of a stored tile
-        const int quarter = warp & 3, half = (warp - 8) >> 2;
-        const uint32_t buffer_at = stores + (warp - 8) * kStoreBytes, empty_there = PAIR ? address_in(sum_empty, 0) : sum_empty;
+        const int quarter = warp & 3, half = (warp - 12) >> 2;
+        const uint32_t buffer_at = stores + (warp - 12) * kStoreBytes, empty_there = PAIR ? address_in(sum_empty, 0) : sum_empty;
         const uint32_t mine = tensor + (quarter << 21) + half * kHeld;
         uint32_t run = 0;
         bool ok = true;
@@ -273,12 +273,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                 if (!ok) break;
                 tensor_fence_after();
 #pragma unroll
-                for (int c = 0; c < kHeld; c += 32) {
-                    float v[32];
+                for (int c = 0; c < kHeld; c += 16) {
+                    float v[16];
                     tensor_load(mine + buffer * kSide + c, v);
                     tensor_wait_loads();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) sum[c + i] += v[i];
+                    for (int i = 0; i < 16; ++i) sum[c + i] += v[i];
                 }
                 tensor_fence_before();
                 __syncwarp();
@@ -343,10 +343,10 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     __syncthreads();
     cluster_barrier();
     if (!PAIR && p.split > 1) {
-        if (warp >= 8) {  // this block's share of the rows, eight columns a thread
+        if (warp >= 12) {  // this block's share of the rows, eight columns a thread
             int m, n;
             tile_at(blockIdx.x / team, &m, &n);
-            const int thread = threadIdx.x - 256, share = 128 / p.split, col = thread % 16 * 8;
+            const int thread = threadIdx.x - 384, share = 128 / p.split, col = thread % 16 * 8;
             const int64_t left = p.x.cols - int64_t(n) * 128 - col;
             for (int r = part * share + thread / 16; r < (part + 1) * share; r += 16) {
                 const int64_t row = int64_t(m) * 128 + r;
@@ -393,7 +393,7 @@ int launch(const Args& p, const void* dy, int64_t ld_dy, int64_t tiles, cudaStre
     if (st == PVQ_OK) st = tile_map(&maps.out, p.out, out, p.outer, p.x.cols, p.ld, 128 / sizeof(T), 32);
     const auto kernel = weight_grad_kernel<PAIR, T>;
     if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), kShared);
-    if (st == PVQ_OK && PAIR) {
+    if (st == PVQ_OK) {
         int registers = 0;
         st = registers_of(reinterpret_cast<const void*>(kernel), &registers);
         if (st == PVQ_OK && registers < kRegisters) st = PVQ_ERR_UNSUPPORTED;
