@@ -9,124 +9,114 @@ namespace pvq {
 namespace fp8 {
 namespace {
 
-constexpr int kThreads = 256;
-
 constexpr float kGelu = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float kCubic = 0.044715f;
 
-// 1 / (1 + e^-w): the exponential and the reciprocal by the special function unit, within 2^-22 and 2^-23 of their
-// values; e^-w may be infinite (the result is zero then).
-__device__ __forceinline__ float sigma(float w) {
-    float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(w * -1.4426950408889634f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+// 1 / (1 + e^-w), from -w / ln 2: the exponential and the reciprocal by the special function unit, within 2^-22 and 2^-23 of
+// their values; e^-w may be infinite (the result is zero then).
+__device__ __forceinline__ float2 sigma(float2 minus_w) {
+    float2 e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(minus_w.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(minus_w.y));
+    e = add2(e, both(1.0f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(e.y));
     return r;
 }
 
+constexpr float kMinusLog2E = -1.4426950408889634f;
+
 template <int ACT>
-__device__ __forceinline__ float activation(float g) {
-    return g * sigma(ACT == PVQ_ACT_SILU ? g : kGelu * g * __fmaf_rn(kCubic * g, g, 1.0f));
+__device__ __forceinline__ float2 activation(float2 g) {
+    if (ACT == PVQ_ACT_SILU) return mul2(g, sigma(mul2(g, both(kMinusLog2E))));
+    const float2 w = mul2(mul2(g, both(kGelu)), fma2(mul2(g, both(kCubic)), g, both(1.0f)));
+    return mul2(g, sigma(mul2(w, both(kMinusLog2E))));
 }
 // The activation and its slope.
 template <int ACT>
-__device__ __forceinline__ float2 activation_slope(float g) {
+__device__ __forceinline__ void activation_slope(float2 g, float2* value, float2* slope) {
     if (ACT == PVQ_ACT_SILU) {
-        const float s = sigma(g), a = g * s;
-        return make_float2(a, __fmaf_rn(a, 1.0f - s, s));
+        const float2 s = sigma(mul2(g, both(kMinusLog2E)));
+        *value = mul2(g, s);
+        *slope = fma2(*value, fma2(s, both(-1.0f), both(1.0f)), s);
+        return;
     }
-    const float square = fminf(g * g, 1e30f);  // (no infinity to be multiplied by s (1 - s) = 0)
-    const float s = sigma(kGelu * g * __fmaf_rn(kCubic, square, 1.0f)), a = g * s;
-    return make_float2(a, __fmaf_rn(a * (1.0f - s), kGelu * __fmaf_rn(3.0f * kCubic, square, 1.0f), s));
+    const float2 square = make_float2(fminf(g.x * g.x, 1e30f), fminf(g.y * g.y, 1e30f));  // (no infinity to be multiplied by s (1 - s) = 0)
+    const float2 s = sigma(mul2(mul2(mul2(g, both(kGelu)), fma2(square, both(kCubic), both(1.0f))), both(kMinusLog2E)));
+    *value = mul2(g, s);
+    const float2 steep = mul2(fma2(square, both(3.0f * kCubic), both(1.0f)), both(kGelu));
+    *slope = fma2(mul2(*value, fma2(s, both(-1.0f), both(1.0f))), steep, s);
 }
 
 template <class T, int ACT, bool KEEP>
-__global__ void __launch_bounds__(kThreads) gated_kernel(GatedArgs a, Division pairs, uint32_t tasks) {
-    const int lane = threadIdx.x & 31, half = lane >> 4;
-    const uint32_t task = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    if (task >= tasks) return;
-    const uint32_t row = divide(task, pairs);
-    const int block = static_cast<int>(task - row * pairs.d) * 2 + half;
-    const int64_t col = int64_t(block) * kBlock + (lane & 15) * 8;
-    const bool first = (lane & 15) == 0 && block < a.h.blocks;
-    float g[8], u[8], h[8];
-    load8(static_cast<const T*>(a.gate) + row * a.ld_gate, col, a.h.cols, g);
-    load8(static_cast<const T*>(a.up) + row * a.ld_up, col, a.h.cols, u);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = activation<ACT>(g[i]) * u[i];
-    uint2 w;
-    uint32_t byte = quantize_block(h, &w);
-    store_codes(a.h.codes + row * a.h.ld_codes, col, a.h.cols, w);
-    if (first) a.h.scales[row * a.h.ld_scales + block] = static_cast<uint8_t>(byte);
+__global__ void __launch_bounds__(kRowThreads) gated_kernel(GatedArgs a, Work work) {
+    const Unit at = unit_at<1>(work, a.h.cols, 0);
+    Values<T> g, u;
+    load_unit(&g, static_cast<const T*>(a.gate) + at.row * a.ld_gate, at, a.h.cols);
+    load_unit(&u, static_cast<const T*>(a.up) + at.row * a.ld_up, at, a.h.cols);
+    Codes c;
+    uint32_t byte;
     if (KEEP) {
-        byte = quantize_block(g, &w);
-        store_codes(a.gate8.codes + row * a.gate8.ld_codes, col, a.h.cols, w);
-        if (first) a.gate8.scales[row * a.gate8.ld_scales + block] = static_cast<uint8_t>(byte);
-        byte = quantize_block(u, &w);
-        store_codes(a.up8.codes + row * a.up8.ld_codes, col, a.h.cols, w);
-        if (first) a.up8.scales[row * a.up8.ld_scales + block] = static_cast<uint8_t>(byte);
+        byte = quantize_block(g, &c);
+        store_unit(a.gate8, at, c, byte);
+        byte = quantize_block(u, &c);
+        store_unit(a.up8, at, c, byte);
     }
+    Values<float> h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h.v[i] = mul2(activation<ACT>(g.pair(i)), u.pair(i));
+    byte = quantize_block(h, &c);
+    store_unit(a.h, at, c, byte);
 }
 
 template <class T, int ACT>
-__global__ void __launch_bounds__(kThreads) gated_backward_kernel(GatedBackwardArgs a, Division pairs, uint32_t tasks) {
-    const int lane = threadIdx.x & 31, half = lane >> 4;
-    const uint32_t task = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    if (task >= tasks) return;
-    const uint32_t row = divide(task, pairs);
-    const int block = static_cast<int>(task - row * pairs.d) * 2 + half;
-    if (block >= a.gate8.blocks) return;
-    const int64_t col = int64_t(block) * kBlock + (lane & 15) * 8, cols = a.gate8.cols;
-    float dh[8], g[8], u[8];
-    load8(static_cast<const T*>(a.dh) + row * a.ld_dh, col, cols, dh);
-    decode8(load_codes(a.gate8.codes + row * a.gate8.ld_codes, col, cols),
-            scale_of(a.gate8.scales[row * a.gate8.ld_scales + block]), g);
-    decode8(load_codes(a.up8.codes + row * a.up8.ld_codes, col, cols), scale_of(a.up8.scales[row * a.up8.ld_scales + block]), u);
+__global__ void __launch_bounds__(kRowThreads) gated_backward_kernel(GatedBackwardArgs a, Work work) {
+    const int64_t cols = a.gate8.cols;
+    const Unit at = unit_at<1>(work, cols, 0);
+    if (!at.there) return;
+    Values<T> dh;
+    Codes gate, up;
+    load_unit(&dh, static_cast<const T*>(a.dh) + at.row * a.ld_dh, at, cols);
+    load_unit(&gate, a.gate8.codes + at.row * a.gate8.ld_codes, at, cols);
+    load_unit(&up, a.up8.codes + at.row * a.up8.ld_codes, at, cols);
+    const float2 gate_scale = both(scale_of(__ldg(a.gate8.scales + at.row * a.gate8.ld_scales + at.block)));
+    const float2 up_scale = both(scale_of(__ldg(a.up8.scales + at.row * a.up8.ld_scales + at.block)));
+    float2 dgate[8], dup[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float2 as = activation_slope<ACT>(g[i]);
-        g[i] = dh[i] * u[i] * as.y;
-        u[i] = dh[i] * as.x;
+        float2 value, slope;
+        activation_slope<ACT>(mul2(gate.pair(i), gate_scale), &value, &slope);
+        dgate[i] = mul2(mul2(dh.pair(i), mul2(up.pair(i), up_scale)), slope);
+        dup[i] = mul2(dh.pair(i), value);
     }
-    store8(static_cast<T*>(a.dgate) + row * a.ld_dgate, col, cols, g);
-    store8(static_cast<T*>(a.dup) + row * a.ld_dup, col, cols, u);
+    store_unit(static_cast<T*>(a.dgate) + at.row * a.ld_dgate, at, cols, dgate);
+    store_unit(static_cast<T*>(a.dup) + at.row * a.ld_dup, at, cols, dup);
 }
 
 template <class T, int ACT>
-void launch_gated(const GatedArgs& a, unsigned grid, const Division& d, uint32_t tasks, cudaStream_t s) {
-    if (a.gate8.codes) gated_kernel<T, ACT, true><<<grid, kThreads, 0, s>>>(a, d, tasks);
-    else gated_kernel<T, ACT, false><<<grid, kThreads, 0, s>>>(a, d, tasks);
+void launch_gated(const GatedArgs& a, cudaStream_t s) {
+    const Work w = work_of(a.h);
+    if (a.gate8.codes) gated_kernel<T, ACT, true><<<grid_of<1>(w), kRowThreads, 0, s>>>(a, w);
+    else gated_kernel<T, ACT, false><<<grid_of<1>(w), kRowThreads, 0, s>>>(a, w);
+}
+template <class T, int ACT>
+void launch_backward(const GatedBackwardArgs& a, cudaStream_t s) {
+    const Work w = work_of(a.gate8);
+    gated_backward_kernel<T, ACT><<<grid_of<1>(w), kRowThreads, 0, s>>>(a, w);
 }
 
 }  // namespace
 
 int gated(const GatedArgs& a, bool bf16, int act, cudaStream_t s) {
-    const int64_t pairs = (a.h.blocks + 1) / 2, tasks = a.h.rows * pairs;
-    const unsigned grid = static_cast<unsigned>((tasks + kThreads / 32 - 1) / (kThreads / 32));
-    const Division d = division_by(pairs);
-    const uint32_t n = static_cast<uint32_t>(tasks);
-    if (act == PVQ_ACT_SILU) {
-        if (bf16) launch_gated<__nv_bfloat16, PVQ_ACT_SILU>(a, grid, d, n, s);
-        else launch_gated<float, PVQ_ACT_SILU>(a, grid, d, n, s);
-    } else {
-        if (bf16) launch_gated<__nv_bfloat16, PVQ_ACT_GELU>(a, grid, d, n, s);
-        else launch_gated<float, PVQ_ACT_GELU>(a, grid, d, n, s);
-    }
+    if (act == PVQ_ACT_SILU) bf16 ? launch_gated<__nv_bfloat16, PVQ_ACT_SILU>(a, s) : launch_gated<float, PVQ_ACT_SILU>(a, s);
+    else bf16 ? launch_gated<__nv_bfloat16, PVQ_ACT_GELU>(a, s) : launch_gated<float, PVQ_ACT_GELU>(a, s);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
 }
 
 int gated_backward(const GatedBackwardArgs& a, bool bf16, int act, cudaStream_t s) {
-    const int64_t pairs = (a.gate8.blocks + 1) / 2, tasks = a.gate8.rows * pairs;
-    const unsigned grid = static_cast<unsigned>((tasks + kThreads / 32 - 1) / (kThreads / 32));
-    const Division d = division_by(pairs);
-    const uint32_t n = static_cast<uint32_t>(tasks);
-    if (act == PVQ_ACT_SILU) {
-        if (bf16) gated_backward_kernel<__nv_bfloat16, PVQ_ACT_SILU><<<grid, kThreads, 0, s>>>(a, d, n);
-        else gated_backward_kernel<float, PVQ_ACT_SILU><<<grid, kThreads, 0, s>>>(a, d, n);
-    } else {
-        if (bf16) gated_backward_kernel<__nv_bfloat16, PVQ_ACT_GELU><<<grid, kThreads, 0, s>>>(a, d, n);
-        else gated_backward_kernel<float, PVQ_ACT_GELU><<<grid, kThreads, 0, s>>>(a, d, n);
-    }
+    if (act == PVQ_ACT_SILU) bf16 ? launch_backward<__nv_bfloat16, PVQ_ACT_SILU>(a, s) : launch_backward<float, PVQ_ACT_SILU>(a, s);
+    else bf16 ? launch_backward<__nv_bfloat16, PVQ_ACT_GELU>(a, s) : launch_backward<float, PVQ_ACT_GELU>(a, s);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
 }

@@ -1,62 +1,64 @@
 // Values to the 8-bit format and back.
-#include <algorithm>
-
 #include "fp8_rows.cuh"
 
 namespace pvq {
 namespace fp8 {
 namespace {
 
-constexpr int kThreads = 256;
-
-// Blocks along rows.  A half warp takes a block; `pairs` blocks of two lie side by side in a row.
-template <class T>
-__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* x, int64_t ld, Matrix q, Division pairs, uint32_t tasks) {
-    const int lane = threadIdx.x & 31, half = lane >> 4;
-    const uint32_t task = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    if (task >= tasks) return;
-    const uint32_t row = divide(task, pairs);
-    const int block = static_cast<int>(task - row * pairs.d) * 2 + half;
-    const int64_t col = int64_t(block) * kBlock + (lane & 15) * 8;
-    float v[8];
-    load8(x + row * ld, col, q.cols, v);
-    uint2 w;
-    const uint32_t byte = quantize_block(v, &w);
-    store_codes(q.codes + row * q.ld_codes, col, q.cols, w);
-    if ((lane & 15) == 0 && block < q.blocks) q.scales[row * q.ld_scales + block] = static_cast<uint8_t>(byte);
+template <class T, int UNITS>
+__global__ void __launch_bounds__(kRowThreads) quantize_rows_kernel(const T* x, int64_t ld, Matrix q, Work work) {
+    Unit at[UNITS];
+    Values<T> v[UNITS];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        at[i] = unit_at<UNITS>(work, q.cols, i);
+        load_unit(&v[i], x + at[i].row * ld, at[i], q.cols);
+    }
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        Codes c;
+        const uint32_t byte = quantize_block(v[i], &c);
+        store_unit(q, at[i], c, byte);
+    }
 }
 
 // Tiles of 128 x 128: a thread block takes one, and holds it in registers between the search and the rounding.
+constexpr int kTileThreads = 256, kTileRows = kTileThreads / 8, kRounds = 128 / kTileRows;
 template <class T>
-__global__ void __launch_bounds__(kThreads) quantize_tiles_kernel(const T* x, int64_t ld, Matrix q) {
+__global__ void __launch_bounds__(kTileThreads) quantize_tiles_kernel(const T* x, int64_t ld, Matrix q, Division across) {
     __shared__ uint32_t found[2];
-    constexpr int kRounds = 128 * 16 / kThreads;
-    const int64_t row0 = int64_t(blockIdx.y) * 128, col = int64_t(blockIdx.x) * 128 + (threadIdx.x & 15) * 8;
+    const uint32_t down = divide(blockIdx.x, across);
+    const int block = static_cast<int>(blockIdx.x - down * across.d), col = block * kBlock + (threadIdx.x & 7) * 8;
+    const int64_t row0 = int64_t(down) * 128 + threadIdx.x / 8;
+    const bool whole = col + 72 <= q.cols;
     if (threadIdx.x < 2) found[threadIdx.x] = 0u;
     __syncthreads();
-    float v[kRounds][8];
+    Values<T> v[kRounds];
     uint32_t m = 0u;
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
-        const int64_t row = row0 + r * (kThreads / 16) + (threadIdx.x >> 4);
-        if (row < q.rows) {
-            load8(x + row * ld, col, q.cols, v[r]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[r][i] = 0.0f;
-        }
+        const int64_t row = row0 + r * kTileRows;
+        if (whole && row < q.rows) v[r].load(x + row * ld, col);
+        else v[r].load_some(x + row * ld, col, row < q.rows ? q.cols : 0);
     }
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) m = max(m, magnitude(v[r]));
-    atomicMax(&found[0], __reduce_max_sync(0xffffffffu, m));
+    for (int r = 0; r < kRounds; ++r) m = max(m, v[r].magnitude());
+    m = __reduce_max_sync(0xffffffffu, m);
+    if ((threadIdx.x & 31) == 0) atomicMax(&found[0], m);
     __syncthreads();
-    const bool finite = found[0] < kFiniteEnd;
     m = found[0];
-    if (!finite) {
+    const bool finite = m < kFiniteEnd;
+    if (!finite) {  // (as in quantize_block)
         m = 0u;
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) m = max(m, finite_magnitude(v[r]));
-        atomicMax(&found[1], __reduce_max_sync(0xffffffffu, m));
+        for (int r = 0; r < kRounds; ++r)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t a = __float_as_uint(v[r].pair(i).x) & 0x7fffffffu, b = __float_as_uint(v[r].pair(i).y) & 0x7fffffffu;
+                m = max(m, max(a < kFiniteEnd ? a : 0u, b < kFiniteEnd ? b : 0u));
+            }
+        m = __reduce_max_sync(0xffffffffu, m);
+        if ((threadIdx.x & 31) == 0) atomicMax(&found[1], m);
         __syncthreads();
         m = found[1];
     }
@@ -64,52 +66,77 @@ __global__ void __launch_bounds__(kThreads) quantize_tiles_kernel(const T* x, in
     const float inverse = inverse_of(byte);
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
-        const int64_t row = row0 + r * (kThreads / 16) + (threadIdx.x >> 4);
-        if (row < q.rows) store_codes(q.codes + row * q.ld_codes, col, q.cols, encode8(v[r], inverse, finite));
+        const int64_t row = row0 + r * kTileRows;
+        Codes c;
+        if (finite) {
+            c = encode(v[r], inverse);
+        } else {
+            Values<float> t;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float2 p = v[r].pair(i);
+                t.v[i] = make_float2(__fmaf_rn(p.x, 0.0f, p.x), __fmaf_rn(p.y, 0.0f, p.y));  // (Inf * 0 is NaN)
+            }
+            c = encode(t, inverse);
+        }
+        if (row >= q.rows) continue;
+        if (whole) c.store(q.codes + row * q.ld_codes, col);
+        else c.store_some(q.codes + row * q.ld_codes, col, q.cols);
     }
-    if (threadIdx.x == 0) q.scales[blockIdx.y * q.ld_scales + blockIdx.x] = static_cast<uint8_t>(byte);
+    if (threadIdx.x == 0) q.scales[down * q.ld_scales + block] = static_cast<uint8_t>(byte);
+}
+
+template <class T, int UNITS>
+__global__ void __launch_bounds__(kRowThreads) dequantize_kernel(Matrix q, T* out, int64_t ld, Work work) {
+    Unit at[UNITS];
+    Codes c[UNITS];
+    uint32_t byte[UNITS];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        at[i] = unit_at<UNITS>(work, q.cols, i);
+        load_unit(&c[i], q.codes + at[i].row * q.ld_codes, at[i], q.cols);
+        byte[i] = __ldg(q.scales + (at[i].row >> q.shift) * q.ld_scales + at[i].block);
+    }
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        if (!at[i].there) continue;
+        const float2 scale = both(scale_of(byte[i]));
+        float2 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = mul2(c[i].pair(k), scale);
+        store_unit(out + at[i].row * ld, at[i], q.cols, v);
+    }
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads) dequantize_kernel(Matrix q, T* out, int64_t ld, Division pairs, uint32_t tasks) {
-    const int lane = threadIdx.x & 31, half = lane >> 4;
-    const uint32_t task = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    if (task >= tasks) return;
-    const uint32_t row = divide(task, pairs);
-    const int block = static_cast<int>(task - row * pairs.d) * 2 + half;
-    if (block >= q.blocks) return;
-    const int64_t col = int64_t(block) * kBlock + (lane & 15) * 8;
-    const float scale = scale_of(q.scales[(row >> q.shift) * q.ld_scales + block]);
-    float v[8];
-    decode8(load_codes(q.codes + row * q.ld_codes, col, q.cols), scale, v);
-    store8(out + row * ld, col, q.cols, v);
+void launch_quantize(const void* x, int64_t ld, const Matrix& q, cudaStream_t s) {
+    const T* from = static_cast<const T*>(x);
+    const Work w = work_of(q);
+    if (q.shift) {
+        const int64_t tiles = (q.rows + 127) / 128 * q.blocks;
+        quantize_tiles_kernel<T><<<static_cast<unsigned>(tiles), kTileThreads, 0, s>>>(from, ld, q, w.blocks);
+    } else {
+        constexpr int kUnits = sizeof(T) == 2 ? 2 : 1;
+        quantize_rows_kernel<T, kUnits><<<grid_of<kUnits>(w), kRowThreads, 0, s>>>(from, ld, q, w);
+    }
+}
+template <class T>
+void launch_dequantize(const Matrix& q, void* out, int64_t ld, cudaStream_t s) {
+    constexpr int kUnits = 2;
+    const Work w = work_of(q);
+    dequantize_kernel<T, kUnits><<<grid_of<kUnits>(w), kRowThreads, 0, s>>>(q, static_cast<T*>(out), ld, w);
 }
 
 }  // namespace
 
 int quantize(const void* x, bool bf16, int64_t ld, const Matrix& q, cudaStream_t s) {
-    if (q.shift) {
-        const dim3 grid(static_cast<unsigned>(q.blocks), static_cast<unsigned>((q.rows + 127) / 128));
-        if (grid.y > 65535u) return PVQ_ERR_UNSUPPORTED;
-        if (bf16) quantize_tiles_kernel<<<grid, kThreads, 0, s>>>(static_cast<const __nv_bfloat16*>(x), ld, q);
-        else quantize_tiles_kernel<<<grid, kThreads, 0, s>>>(static_cast<const float*>(x), ld, q);
-    } else {
-        const int64_t pairs = (q.blocks + 1) / 2, tasks = q.rows * pairs;
-        const unsigned grid = static_cast<unsigned>((tasks + kThreads / 32 - 1) / (kThreads / 32));
-        const Division d = division_by(pairs);
-        if (bf16) quantize_rows_kernel<<<grid, kThreads, 0, s>>>(static_cast<const __nv_bfloat16*>(x), ld, q, d, static_cast<uint32_t>(tasks));
-        else quantize_rows_kernel<<<grid, kThreads, 0, s>>>(static_cast<const float*>(x), ld, q, d, static_cast<uint32_t>(tasks));
-    }
+    bf16 ? launch_quantize<__nv_bfloat16>(x, ld, q, s) : launch_quantize<float>(x, ld, q, s);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
 }
 
 int dequantize(const Matrix& q, void* out, bool bf16, int64_t ld, cudaStream_t s) {
-    const int64_t pairs = (q.blocks + 1) / 2, tasks = q.rows * pairs;
-    const unsigned grid = static_cast<unsigned>((tasks + kThreads / 32 - 1) / (kThreads / 32));
-    const Division d = division_by(pairs);
-    if (bf16) dequantize_kernel<<<grid, kThreads, 0, s>>>(q, static_cast<__nv_bfloat16*>(out), ld, d, static_cast<uint32_t>(tasks));
-    else dequantize_kernel<<<grid, kThreads, 0, s>>>(q, static_cast<float*>(out), ld, d, static_cast<uint32_t>(tasks));
+    bf16 ? launch_dequantize<__nv_bfloat16>(q, out, ld, s) : launch_dequantize<float>(q, out, ld, s);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
 }
