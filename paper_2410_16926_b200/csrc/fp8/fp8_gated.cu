@@ -50,6 +50,8 @@ __device__ __forceinline__ void activation_slope(float2 g, float2* value, float2
 
 template <class T, int ACT, bool KEEP>
 __global__ void __launch_bounds__(kRowThreads) gated_kernel(GatedArgs a, Work work) {
+    launch_dependents();
+    dependency_wait();
     const Unit at = unit_at<1>(work, a.h.cols, 0);
     Values<T> g, u;
     load_unit(&g, static_cast<const T*>(a.gate) + at.row * a.ld_gate, at, a.h.cols);
@@ -71,6 +73,8 @@ __global__ void __launch_bounds__(kRowThreads) gated_kernel(GatedArgs a, Work wo
 
 template <class T, int ACT>
 __global__ void __launch_bounds__(kRowThreads) gated_backward_kernel(GatedBackwardArgs a, Work work) {
+    launch_dependents();
+    dependency_wait();
     const int64_t cols = a.gate8.cols;
     const Unit at = unit_at<1>(work, cols, 0);
     if (!at.there) return;
@@ -94,31 +98,26 @@ __global__ void __launch_bounds__(kRowThreads) gated_backward_kernel(GatedBackwa
 }
 
 template <class T, int ACT>
-void launch_gated(const GatedArgs& a, cudaStream_t s) {
+int launch_gated(const GatedArgs& a, cudaStream_t s) {
     const Work w = work_of(a.h);
-    if (a.gate8.codes) gated_kernel<T, ACT, true><<<grid_of<1>(w), kRowThreads, 0, s>>>(a, w);
-    else gated_kernel<T, ACT, false><<<grid_of<1>(w), kRowThreads, 0, s>>>(a, w);
+    return launch_early(a.gate8.codes ? gated_kernel<T, ACT, true> : gated_kernel<T, ACT, false>, dim3(grid_of<1>(w)), kRowThreads, 0, 0, s, a, w);
 }
 template <class T, int ACT>
-void launch_backward(const GatedBackwardArgs& a, cudaStream_t s) {
+int launch_backward(const GatedBackwardArgs& a, cudaStream_t s) {
     const Work w = work_of(a.gate8);
-    gated_backward_kernel<T, ACT><<<grid_of<1>(w), kRowThreads, 0, s>>>(a, w);
+    return launch_early(gated_backward_kernel<T, ACT>, dim3(grid_of<1>(w)), kRowThreads, 0, 0, s, a, w);
 }
 
 }  // namespace
 
 int gated(const GatedArgs& a, bool bf16, int act, cudaStream_t s) {
-    if (act == PVQ_ACT_SILU) bf16 ? launch_gated<__nv_bfloat16, PVQ_ACT_SILU>(a, s) : launch_gated<float, PVQ_ACT_SILU>(a, s);
-    else bf16 ? launch_gated<__nv_bfloat16, PVQ_ACT_GELU>(a, s) : launch_gated<float, PVQ_ACT_GELU>(a, s);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
+    if (act == PVQ_ACT_SILU) return bf16 ? launch_gated<__nv_bfloat16, PVQ_ACT_SILU>(a, s) : launch_gated<float, PVQ_ACT_SILU>(a, s);
+    return bf16 ? launch_gated<__nv_bfloat16, PVQ_ACT_GELU>(a, s) : launch_gated<float, PVQ_ACT_GELU>(a, s);
 }
 
 int gated_backward(const GatedBackwardArgs& a, bool bf16, int act, cudaStream_t s) {
-    if (act == PVQ_ACT_SILU) bf16 ? launch_backward<__nv_bfloat16, PVQ_ACT_SILU>(a, s) : launch_backward<float, PVQ_ACT_SILU>(a, s);
-    else bf16 ? launch_backward<__nv_bfloat16, PVQ_ACT_GELU>(a, s) : launch_backward<float, PVQ_ACT_GELU>(a, s);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
+    if (act == PVQ_ACT_SILU) return bf16 ? launch_backward<__nv_bfloat16, PVQ_ACT_SILU>(a, s) : launch_backward<float, PVQ_ACT_SILU>(a, s);
+    return bf16 ? launch_backward<__nv_bfloat16, PVQ_ACT_GELU>(a, s) : launch_backward<float, PVQ_ACT_GELU>(a, s);
 }
 
 }  // namespace fp8

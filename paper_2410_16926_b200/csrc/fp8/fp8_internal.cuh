@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <utility>
 
 #include "pvq.h"
 
@@ -76,6 +77,29 @@ __device__ __forceinline__ uint32_t bf16x2_of(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+
+// As the library's other hot kernels, those here may be set up while the kernel before them in the stream still runs: every
+// thread calls dependency_wait() before it touches global memory, and launch_dependents() once what it holds of the SM
+// (tensor memory above all) is its own, so that an early block of the next kernel takes nothing that this one waits for.
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <typename... Params, typename... Args>
+inline int launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t shared, unsigned cluster, cudaStream_t s, Args&&... args) {
+    cudaLaunchConfig_t config = {};
+    config.gridDim = grid;
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = shared;
+    config.stream = s;
+    cudaLaunchAttribute attrs[2];
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = cluster, attrs[1].val.clusterDim.y = 1, attrs[1].val.clusterDim.z = 1;
+    config.attrs = attrs;
+    config.numAttrs = cluster > 0 ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&config, kernel, std::forward<Args>(args)...);
+    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
 }
 
 // launches

@@ -44,37 +44,67 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
     __shared__ int over;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % split;  // in the cluster
-    if (threadIdx.x == 0) {
-        over = 0;
-        for (int i = 0; i < S::kStages; ++i) barrier_init(full + 8 * i, 1), barrier_init(empty + 8 * i, 1);
-        for (int i = 0; i < S::kScaleSets; ++i) barrier_init(scales_full + 8 * i, 4), barrier_init(scales_empty + 8 * i, 1);
-        barrier_init(sum_full, 1);
-        barrier_init_fence();
-        prefetch_map(&maps.a), prefetch_map(&maps.b);
-    }
-    if (warp == 2) tensor_alloc<false>(shared_address(&tensor_base), S::kColumns);
-    tensor_fence_before();
-    __syncthreads();
-    tensor_fence_after();
-    const uint32_t tensor = tensor_base;
-    const Bounds bounds{&over, p.status};
     const int64_t col0 = int64_t(blockIdx.x / split) * 128, row0 = int64_t(blockIdx.y) * ROWS;
     const int blocks = static_cast<int>((p.inner + kBlock - 1) / kBlock);
     const int first = static_cast<int>(int64_t(blocks) * rank / split), last = static_cast<int>(int64_t(blocks) * (rank + 1) / split);  // (split <= blocks)
+    const Bounds bounds{&over, p.status};
+
+    const auto load = [&](int kb, uint32_t stage) {
+        const uint32_t at = base + stage * S::kStageBytes, bar = full + 8 * stage;
+        barrier_expect(bar, S::kStageBytes);
+        if (ACROSS) load_tile<false>(at, &maps.b, static_cast<int>(col0), kb * kBlock, bar);
+        else load_tile<false>(at, &maps.b, kb * kBlock, static_cast<int>(col0), bar);
+        load_tile<false>(at + 128 * kBlock, &maps.a, kb * kBlock, static_cast<int>(row0), bar);
+    };
+    // the first copies and scales are asked for before the block meets
+    uint32_t w[S::kScaleSets][4], x[S::kScaleSets][S::kWordsB];
+    const auto scales_of = [&](int f0) {
+#pragma unroll
+        for (int i = 0; i < S::kScaleSets; ++i) {
+            if (f0 + i > (last - 1) / 4) break;
+            scale_words<ACROSS>(p.b, col0, f0 + i, w[i]);
+            if (p.a.shift && ROWS < 128) {  // (the rows do not begin at a tile of its scales)
+#pragma unroll
+                for (int j = 0; j < S::kWordsB; ++j) x[i][j] = scale_word<false>(p.a, row0 + 32 * j + lane, f0 + i);
+            } else {
+                scale_words<false>(p.a, row0, f0 + i, x[i]);
+            }
+        }
+    };
+    if (warp == 0) {
+        if (elected()) {
+            prefetch_map(&maps.a), prefetch_map(&maps.b);
+            over = 0;
+            for (int i = 0; i < S::kStages; ++i) barrier_init(full + 8 * i, 1), barrier_init(empty + 8 * i, 1);
+            for (int i = 0; i < S::kScaleSets; ++i) barrier_init(scales_full + 8 * i, 4), barrier_init(scales_empty + 8 * i, 1);
+            barrier_init(sum_full, 1);
+            barrier_init_fence();
+            async_fence();
+            dependency_wait();
+            for (int i = 0; i < S::kStages && first + i < last; ++i) load(first + i, i);
+        }
+        __syncwarp();
+    } else if (warp == 2) {
+        tensor_alloc<false>(shared_address(&tensor_base), S::kColumns);
+    }
+    if (warp != 2) dependency_wait();
+    if (warp >= 4) scales_of(first / 4);
+    tensor_fence_before();
+    __syncthreads();
+    tensor_fence_after();
+    launch_dependents();
+    if (warp == 2) dependency_wait();
+    const uint32_t tensor = tensor_base;
 
     if (warp == 0) {
         if (elected()) {
-            Turn<S::kStages> turn;
-            uint32_t issued = 0;
+            Turn<S::kStages> turn;  // the second time round, and so on
+            uint32_t issued = min(S::kStages, last - first);
             bool ok = true;
-            for (int kb = first; kb < last; ++kb) {
-                const uint32_t at = base + turn.at * S::kStageBytes;
-                ok = barrier_wait(empty + 8 * turn.at, turn.parity ^ 1, bounds);
+            for (int kb = first + S::kStages; kb < last; ++kb) {
+                ok = barrier_wait(empty + 8 * turn.at, turn.parity, bounds);
                 if (!ok) break;
-                barrier_expect(full + 8 * turn.at, S::kStageBytes);
-                if (ACROSS) load_tile<false>(at, &maps.b, static_cast<int>(col0), kb * kBlock, full + 8 * turn.at);
-                else load_tile<false>(at, &maps.b, kb * kBlock, static_cast<int>(col0), full + 8 * turn.at);
-                load_tile<false>(at + 128 * kBlock, &maps.a, kb * kBlock, static_cast<int>(row0), full + 8 * turn.at);
+                load(kb, turn.at);
                 turn.next();
                 ++issued;
             }
@@ -116,18 +146,7 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
         bool ok = true;
         // asked for as many steps at once as there are sets of columns: to wait for one before the next is a microsecond each
         for (int f0 = first / 4; f0 <= (last - 1) / 4 && ok; f0 += S::kScaleSets) {
-            uint32_t w[S::kScaleSets][4], x[S::kScaleSets][S::kWordsB];
-#pragma unroll
-            for (int i = 0; i < S::kScaleSets; ++i) {
-                if (f0 + i > (last - 1) / 4) break;
-                scale_words<ACROSS>(p.b, col0, f0 + i, w[i]);
-                if (p.a.shift && ROWS < 128) {  // (the rows do not begin at a tile of its scales)
-#pragma unroll
-                    for (int j = 0; j < S::kWordsB; ++j) x[i][j] = scale_word<false>(p.a, row0 + 32 * j + lane, f0 + i);
-                } else {
-                    scale_words<false>(p.a, row0, f0 + i, x[i]);
-                }
-            }
+            if (f0 > first / 4) scales_of(f0);
 #pragma unroll
             for (int i = 0; i < S::kScaleSets; ++i) {
                 if (f0 + i > (last - 1) / 4) break;
@@ -150,6 +169,7 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
             const uint32_t to = base + ((warp & 3) * 32 + lane) * 4;
 #pragma unroll
             for (int c = 0; c < ROWS; c += 16) {
+                if (row0 + c >= p.rows) break;
                 float v[16];
                 tensor_load(mine + c, v);
                 tensor_wait_loads();
@@ -205,21 +225,11 @@ int launch(const MatmulArgs& p, int split, cudaStream_t s) {
     Maps maps;
     int st = tile_map(&maps.a, p.a.codes, Element::kByte, p.a.rows, p.a.cols, p.a.ld_codes, kBlock, ROWS);
     if (st == PVQ_OK) st = tile_map(&maps.b, p.b.codes, Element::kByte, p.b.rows, p.b.cols, p.b.ld_codes, kBlock, 128);
-    const auto kernel = matmul_few_kernel<ROWS, ACROSS, T>;
+    void (*const kernel)(Maps, MatmulArgs, int) = matmul_few_kernel<ROWS, ACROSS, T>;
     if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), Shape<ROWS>::kShared);
     if (st != PVQ_OK) return st;
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(static_cast<unsigned>((p.outs + 127) / 128 * split), static_cast<unsigned>((p.rows + ROWS - 1) / ROWS));
-    config.blockDim = dim3(kThreads);
-    config.dynamicSmemBytes = Shape<ROWS>::kShared;
-    config.stream = s;
-    cudaLaunchAttribute cluster;
-    cluster.id = cudaLaunchAttributeClusterDimension;
-    cluster.val.clusterDim.x = split, cluster.val.clusterDim.y = 1, cluster.val.clusterDim.z = 1;
-    config.attrs = &cluster;
-    config.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&config, kernel, maps, p, split);
-    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
+    const dim3 grid(static_cast<unsigned>((p.outs + 127) / 128 * split), static_cast<unsigned>((p.rows + ROWS - 1) / ROWS));
+    return launch_early(kernel, grid, kThreads, Shape<ROWS>::kShared, split, s, maps, p, split);
 }
 
 template <int ROWS>

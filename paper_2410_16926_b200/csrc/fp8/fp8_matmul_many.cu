@@ -41,7 +41,7 @@ struct Tiles {
 };
 
 template <bool ACROSS, class T>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_constant__ Maps maps, const __grid_constant__ MatmulArgs p) {
+__global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_constant__ Maps maps, const __grid_constant__ MatmulArgs p) {
     extern __shared__ uint8_t raw[];
     const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
     const uint32_t stores = base + kStages * kStageBytes, bars = stores + 8 * 2 * kStoreBytes;
@@ -65,6 +65,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) matmul_
     __syncthreads();
     cluster_barrier();
     tensor_fence_after();
+    launch_dependents();
+    dependency_wait();
     const uint32_t tensor = tensor_base;
     const Bounds bounds{&over, p.status};
     const Tiles tiles{static_cast<int>((p.rows + 255) / 256), static_cast<int>((p.outs + 255) / 256)};
@@ -260,15 +262,13 @@ int launch(const MatmulArgs& p, cudaStream_t s) {
     int st = tile_map(&maps.a, p.a.codes, Element::kByte, p.a.rows, p.a.cols, p.a.ld_codes, kBlock, 128);
     if (st == PVQ_OK) st = tile_map(&maps.b, p.b.codes, Element::kByte, p.b.rows, p.b.cols, p.b.ld_codes, kBlock, 128);
     if (st == PVQ_OK) st = tile_map(&maps.out, p.out, out, p.rows, p.outs, p.ld, 128 / sizeof(T), 32);
-    const auto kernel = matmul_many_kernel<ACROSS, T>;
+    void (*const kernel)(Maps, MatmulArgs) = matmul_many_kernel<ACROSS, T>;
     if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), kShared);
     if (st != PVQ_OK) return st;
     const int64_t tiles = ((p.rows + 255) / 256) * ((p.outs + 255) / 256);
     if (tiles >= int64_t(1) << 30) return PVQ_ERR_UNSUPPORTED;
     const unsigned pairs = static_cast<unsigned>(tiles < kSms / 2 ? tiles : kSms / 2);
-    kernel<<<2 * pairs, kThreads, kShared, s>>>(maps, p);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
+    return launch_early(kernel, dim3(2 * pairs), kThreads, kShared, 2, s, maps, p);
 }
 
 }  // namespace

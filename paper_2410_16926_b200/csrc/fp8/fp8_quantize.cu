@@ -7,6 +7,8 @@ namespace {
 
 template <class T, int UNITS>
 __global__ void __launch_bounds__(kRowThreads) quantize_rows_kernel(const T* x, int64_t ld, Matrix q, Work work) {
+    launch_dependents();
+    dependency_wait();
     Unit at[UNITS];
     Values<T> v[UNITS];
 #pragma unroll
@@ -32,7 +34,9 @@ __global__ void __launch_bounds__(kTileThreads) quantize_tiles_kernel(const T* x
     const int64_t row0 = int64_t(down) * 128 + threadIdx.x / 8;
     const bool whole = col + 72 <= q.cols;
     if (threadIdx.x < 2) found[threadIdx.x] = 0u;
+    launch_dependents();
     __syncthreads();
+    dependency_wait();
     Values<T> v[kRounds];
     uint32_t m = 0u;
 #pragma unroll
@@ -88,6 +92,8 @@ __global__ void __launch_bounds__(kTileThreads) quantize_tiles_kernel(const T* x
 
 template <class T, int UNITS>
 __global__ void __launch_bounds__(kRowThreads) dequantize_kernel(Matrix q, T* out, int64_t ld, Work work) {
+    launch_dependents();
+    dependency_wait();
     Unit at[UNITS];
     Codes c[UNITS];
     uint32_t byte[UNITS];
@@ -109,36 +115,31 @@ __global__ void __launch_bounds__(kRowThreads) dequantize_kernel(Matrix q, T* ou
 }
 
 template <class T>
-void launch_quantize(const void* x, int64_t ld, const Matrix& q, cudaStream_t s) {
+int launch_quantize(const void* x, int64_t ld, const Matrix& q, cudaStream_t s) {
     const T* from = static_cast<const T*>(x);
     const Work w = work_of(q);
     if (q.shift) {
         const int64_t tiles = (q.rows + 127) / 128 * q.blocks;
-        quantize_tiles_kernel<T><<<static_cast<unsigned>(tiles), kTileThreads, 0, s>>>(from, ld, q, w.blocks);
-    } else {
-        constexpr int kUnits = sizeof(T) == 2 ? 2 : 1;
-        quantize_rows_kernel<T, kUnits><<<grid_of<kUnits>(w), kRowThreads, 0, s>>>(from, ld, q, w);
+        return launch_early(quantize_tiles_kernel<T>, dim3(static_cast<unsigned>(tiles)), kTileThreads, 0, 0, s, from, ld, q, w.blocks);
     }
+    constexpr int kUnits = sizeof(T) == 2 ? 2 : 1;
+    return launch_early(quantize_rows_kernel<T, kUnits>, dim3(grid_of<kUnits>(w)), kRowThreads, 0, 0, s, from, ld, q, w);
 }
 template <class T>
-void launch_dequantize(const Matrix& q, void* out, int64_t ld, cudaStream_t s) {
+int launch_dequantize(const Matrix& q, void* out, int64_t ld, cudaStream_t s) {
     constexpr int kUnits = 2;
     const Work w = work_of(q);
-    dequantize_kernel<T, kUnits><<<grid_of<kUnits>(w), kRowThreads, 0, s>>>(q, static_cast<T*>(out), ld, w);
+    return launch_early(dequantize_kernel<T, kUnits>, dim3(grid_of<kUnits>(w)), kRowThreads, 0, 0, s, q, static_cast<T*>(out), ld, w);
 }
 
 }  // namespace
 
 int quantize(const void* x, bool bf16, int64_t ld, const Matrix& q, cudaStream_t s) {
-    bf16 ? launch_quantize<__nv_bfloat16>(x, ld, q, s) : launch_quantize<float>(x, ld, q, s);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
+    return bf16 ? launch_quantize<__nv_bfloat16>(x, ld, q, s) : launch_quantize<float>(x, ld, q, s);
 }
 
 int dequantize(const Matrix& q, void* out, bool bf16, int64_t ld, cudaStream_t s) {
-    bf16 ? launch_dequantize<__nv_bfloat16>(q, out, ld, s) : launch_dequantize<float>(q, out, ld, s);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
+    return bf16 ? launch_dequantize<__nv_bfloat16>(q, out, ld, s) : launch_dequantize<float>(q, out, ld, s);
 }
 
 }  // namespace fp8

@@ -132,6 +132,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     __syncthreads();
     cluster_barrier();
     tensor_fence_after();
+    launch_dependents();
+    dependency_wait();
     const uint32_t tensor = tensor_base;
     const Bounds bounds{&over, p.status};
     const int down = static_cast<int>((p.outer + kSide - 1) / kSide), across = static_cast<int>((p.x.cols + kSide - 1) / kSide), tiles = down * across;
@@ -391,7 +393,7 @@ int launch(const Args& p, const void* dy, int64_t ld_dy, int64_t tiles, cudaStre
     int st = tile_map(&maps.dy, dy, Element::kBf16, p.x.rows, p.outer, ld_dy, 64, kDepth);
     if (st == PVQ_OK) st = tile_map(&maps.x, p.x.codes, Element::kByte, p.x.rows, p.x.cols, p.x.ld_codes, 128, kDepth);
     if (st == PVQ_OK) st = tile_map(&maps.out, p.out, out, p.outer, p.x.cols, p.ld, 128 / sizeof(T), 32);
-    const auto kernel = weight_grad_kernel<PAIR, T>;
+    void (*const kernel)(Maps, Args) = weight_grad_kernel<PAIR, T>;
     if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), kShared);
     if (st == PVQ_OK) {
         int registers = 0;
@@ -401,18 +403,7 @@ int launch(const Args& p, const void* dy, int64_t ld_dy, int64_t tiles, cudaStre
     if (st != PVQ_OK) return st;
     const int team = PAIR ? 2 : p.split;
     const int64_t teams = p.split > 1 || tiles < kSms / team ? tiles : kSms / team;
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(static_cast<unsigned>(teams * team));
-    config.blockDim = dim3(kThreads);
-    config.dynamicSmemBytes = kShared;
-    config.stream = s;
-    cudaLaunchAttribute cluster;
-    cluster.id = cudaLaunchAttributeClusterDimension;
-    cluster.val.clusterDim.x = team, cluster.val.clusterDim.y = 1, cluster.val.clusterDim.z = 1;
-    config.attrs = &cluster;
-    config.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&config, kernel, maps, p);
-    return e == cudaSuccess ? PVQ_OK : set_cuda_error(e);
+    return launch_early(kernel, dim3(static_cast<unsigned>(teams * team)), kThreads, kShared, team, s, maps, p);
 }
 
 }  // namespace
