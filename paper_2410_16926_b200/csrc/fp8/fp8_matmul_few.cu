@@ -19,7 +19,7 @@ constexpr int kThreads = 256;
 template <int ROWS>
 struct Shape {
     static constexpr int kStageBytes = (128 + ROWS) * kBlock;
-    static constexpr int kStages = ROWS <= 32 ? 5 : (ROWS == 64 ? 4 : 6);  // two blocks an SM up to 64 rows
+    static constexpr int kStages = ROWS <= 32 ? 3 : (ROWS == 64 ? 8 : 6);  // four blocks an SM, then one
     static constexpr int kWordsB = ROWS <= 32 ? 1 : ROWS / 32;             // of scales, a lane
     static constexpr int kScales = ROWS < 32 ? 32 : ROWS;                  // columns before them
     static constexpr int kScaleSets = 4;
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
 #pragma unroll
             for (int i = 0; i < S::kScaleSets; ++i) {
                 if (f0 + i > (last - 1) / 4) break;
-                ok = __all_sync(0xffffffffu, barrier_wait(scales_empty + 8 * turn.at, turn.parity ^ 1, bounds));
+                ok = warp_wait(scales_empty + 8 * turn.at, turn.parity ^ 1, bounds);
                 if (!ok) break;
                 tensor_fence_after();
                 tensor_store(mine + S::kScales + 8 * turn.at, w[i]);
@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
                 turn.next();
             }
         }
-        ok = ok && __all_sync(0xffffffffu, barrier_wait(sum_full, 0, bounds));
+        ok = ok && warp_wait(sum_full, 0, bounds);
         ok = ok && !over;
         if (__all_sync(0xffffffffu, ok)) {  // the part of the sum, in shared memory: [row][128]
             tensor_fence_after();

@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
         const auto put = [&](const uint32_t (&a)[4], const uint32_t (&b)[8]) -> bool {
             const uint32_t buffer = four & 1;
             if (four >= 2) {
-                if (!__all_sync(0xffffffffu, barrier_wait(scales_empty + 8 * buffer, ((four >> 1) - 1) & 1, bounds))) return false;
+                if (!warp_wait(scales_empty + 8 * buffer, ((four >> 1) - 1) & 1, bounds)) return false;
                 tensor_fence_after();
             }
             tensor_store(mine + kScalesA + 4 * buffer, a);
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
         for (int t = first; t < tiles.count(); t += step, ++tile) {
             int m, n;
             tiles.at(t, &m, &n);
-            if (!__all_sync(0xffffffffu, barrier_wait(sum_full + 8 * (tile & 1), (tile >> 1) & 1, bounds))) break;
+            if (!warp_wait(sum_full + 8 * (tile & 1), (tile >> 1) & 1, bounds)) break;
             tensor_fence_after();
             const int64_t row = int64_t(m) * 256 + rank * 128 + quarter * 32;
             // even tiles share their last columns with the next tile, odd ones their first

@@ -37,6 +37,8 @@ struct Args {
     int64_t outer, ld;
     uint32_t* status;
     int split;
+    int tiles;  // of this launch
+    int after;  // without PAIR: tiles are quarters of pairs' tiles from this one on (-1: tiles of their own)
 };
 
 // Registers a thread of the five warpgroups of a pair's block: what all are launched with, shared out anew.  A sum of 128
@@ -136,16 +138,20 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     dependency_wait();
     const uint32_t tensor = tensor_base;
     const Bounds bounds{&over, p.status};
-    const int down = static_cast<int>((p.outer + kSide - 1) / kSide), across = static_cast<int>((p.x.cols + kSide - 1) / kSide), tiles = down * across;
+    const bool quarters = !PAIR && p.after >= 0;
+    const int side = quarters ? 256 : kSide, tiles = p.tiles;
+    const int down = static_cast<int>((p.outer + side - 1) / side), across = static_cast<int>((p.x.cols + side - 1) / side);
     const int team = PAIR ? 2 : p.split, step = gridDim.x / team;
     const int stages = static_cast<int>((p.x.rows + kDepth - 1) / kDepth);
     const int begin = static_cast<int>(int64_t(stages) * part / p.split), end = static_cast<int>(int64_t(stages) * (part + 1) / p.split);
 
     // Tiles of kGroup rows of tiles go down first, so that those of one moment share what they read.
     const auto tile_at = [&](int t, int* m, int* n) {
-        const int group = t / (kGroup * across), first = group * kGroup, rest = t - group * kGroup * across, high = min(kGroup, down - first);
+        const int i = quarters ? p.after + t / 4 : t;
+        const int group = i / (kGroup * across), first = group * kGroup, rest = i - group * kGroup * across, high = min(kGroup, down - first);
         *m = first + rest % high;
         *n = rest / high;
+        if (quarters) *m = 2 * *m + (t & 1), *n = 2 * *n + (t >> 1 & 1);
     };
 
     if (warp < 4) {
@@ -239,9 +245,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                 for (int i = 0; i < 4; ++i) {
                     if (kb0 + 2 * i >= end) break;
                     const uint32_t it = it0 + (kb0 + 2 * i - begin), s = it % kStages, c = it % kConverted;
-                    ok = barrier_wait(full_x + 8 * s, (it / kStages) & 1, bounds) &&
-                         (it < kConverted || barrier_wait(converted_empty + 8 * c, (it / kConverted - 1) & 1, bounds));
-                    ok = __all_sync(0xffffffffu, ok);
+                    ok = warp_wait(full_x + 8 * s, (it / kStages) & 1, bounds) && warp_wait(converted_empty + 8 * c, ((it / kConverted) & 1) ^ 1, bounds);
                     if (!ok) break;
                     const uint32_t from = base + s * kStageBytes + 2 * kAtom + row * 128, to = converted + c * kConvertedBytes + half * kAtom + row * 128;
                     const uint32_t byte = (bytes >> (8 * i)) & 0xffu;
@@ -271,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
             for (int i = 0; i < kHeld; ++i) sum[i] = 0.0f;
             for (int kb = begin; kb < end; kb += kRun, ++run) {
                 const uint32_t buffer = run & 1;
-                ok = __all_sync(0xffffffffu, barrier_wait(sum_full + 8 * buffer, (run >> 1) & 1, bounds));
+                ok = warp_wait(sum_full + 8 * buffer, (run >> 1) & 1, bounds);
                 if (!ok) break;
                 tensor_fence_after();
 #pragma unroll
@@ -387,35 +391,58 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
 }
 
 template <bool PAIR, class T>
-int launch(const Args& p, const void* dy, int64_t ld_dy, int64_t tiles, cudaStream_t s) {
+int launch(const Args& p, const Maps& maps, cudaStream_t s) {
+    void (*const kernel)(Maps, Args) = weight_grad_kernel<PAIR, T>;
+    int st = allow_shared(reinterpret_cast<const void*>(kernel), kShared), registers = 0;
+    if (st == PVQ_OK) st = registers_of(reinterpret_cast<const void*>(kernel), &registers);
+    if (st == PVQ_OK && registers < kRegisters) st = PVQ_ERR_UNSUPPORTED;
+    if (st != PVQ_OK) return st;
+    const int team = PAIR ? 2 : p.split, teams = p.split > 1 || p.tiles < kSms / team ? p.tiles : kSms / team;
+    return launch_early(kernel, dim3(static_cast<unsigned>(teams * team)), kThreads, kShared, team, s, maps, p);
+}
+
+// Parts of t for as many tiles of 128 x 128, so that they fill the GPU and each part is a run at least.
+int parts(int64_t tiles, int64_t stages) {
+    int split = 1;
+    while (split < 8 && tiles * split * 2 <= kSms && stages >= kRun * split * 2) split *= 2;
+    return split;
+}
+
+template <class T>
+int weight_grad_of(Args p, const void* dy, int64_t ld_dy, cudaStream_t s) {
+    const int64_t pairs = ((p.outer + 255) / 256) * ((p.x.cols + 255) / 256), tiles = ((p.outer + 127) / 128) * ((p.x.cols + 127) / 128);
+    const int64_t stages = (p.x.rows + kDepth - 1) / kDepth;
+    if (tiles >= int64_t(1) << 30) return PVQ_ERR_UNSUPPORTED;
     Maps maps;
     const Element out = sizeof(T) == 2 ? Element::kBf16 : Element::kF32;
     int st = tile_map(&maps.dy, dy, Element::kBf16, p.x.rows, p.outer, ld_dy, 64, kDepth);
     if (st == PVQ_OK) st = tile_map(&maps.x, p.x.codes, Element::kByte, p.x.rows, p.x.cols, p.x.ld_codes, 128, kDepth);
     if (st == PVQ_OK) st = tile_map(&maps.out, p.out, out, p.outer, p.x.cols, p.ld, 128 / sizeof(T), 32);
-    void (*const kernel)(Maps, Args) = weight_grad_kernel<PAIR, T>;
-    if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), kShared);
-    if (st == PVQ_OK) {
-        int registers = 0;
-        st = registers_of(reinterpret_cast<const void*>(kernel), &registers);
-        if (st == PVQ_OK && registers < kRegisters) st = PVQ_ERR_UNSUPPORTED;
-    }
     if (st != PVQ_OK) return st;
-    const int team = PAIR ? 2 : p.split;
-    const int64_t teams = p.split > 1 || tiles < kSms / team ? tiles : kSms / team;
-    return launch_early(kernel, dim3(static_cast<unsigned>(teams * team)), kThreads, kShared, team, s, maps, p);
+    p.split = 1, p.after = -1;
+    if (pairs < 48) {
+        p.tiles = static_cast<int>(tiles);
+        p.split = parts(tiles, stages);
+        return launch<false, T>(p, maps, s);
+    }
+    // The last round of tiles, where it is a small one, is shared by all SMs: in quarters, with t in parts.  (14336 x 4096 are
+    // twelve rounds of 74 tiles and 8 tiles.)
+    const int last = static_cast<int>(pairs % (kSms / 2)), split = parts(4 * last, stages);
+    const bool shared = pairs > last && last > 0 && split > 1;
+    p.tiles = static_cast<int>(shared ? pairs - last : pairs);
+    st = launch<true, T>(p, maps, s);
+    if (st != PVQ_OK || !shared) return st;
+    p.after = p.tiles;
+    p.tiles = 4 * last;
+    p.split = split;
+    return launch<false, T>(p, maps, s);
 }
 
 }  // namespace
 
 int weight_grad(const void* dy, int64_t outer, int64_t ld_dy, const Matrix& x, void* out, bool bf16, int64_t ld, uint32_t* status, cudaStream_t s) {
-    Args p{x, out, outer, ld, status, 1};
-    const int64_t pairs = ((outer + 255) / 256) * ((x.cols + 255) / 256), tiles = ((outer + 127) / 128) * ((x.cols + 127) / 128);
-    if (tiles >= int64_t(1) << 30) return PVQ_ERR_UNSUPPORTED;
-    if (pairs >= 48) return bf16 ? launch<true, __nv_bfloat16>(p, dy, ld_dy, pairs, s) : launch<true, float>(p, dy, ld_dy, pairs, s);
-    const int64_t stages = (x.rows + kDepth - 1) / kDepth;
-    while (p.split < 8 && tiles * p.split * 2 <= kSms && stages >= kRun * p.split * 2) p.split *= 2;
-    return bf16 ? launch<false, __nv_bfloat16>(p, dy, ld_dy, tiles, s) : launch<false, float>(p, dy, ld_dy, tiles, s);
+    const Args p{x, out, outer, ld, status, 1, 0, -1};
+    return bf16 ? weight_grad_of<__nv_bfloat16>(p, dy, ld_dy, s) : weight_grad_of<float>(p, dy, ld_dy, s);
 }
 
 }  // namespace fp8

@@ -208,7 +208,8 @@ def check_weight_grad(dy, x, dtype, out=None):
 @pytest.mark.parametrize("rows,inner,outer,tile", [(1, 1, 1, False), (1, 300, 200, False), (7, 130, 7, False), (64, 128, 128, False),
                                                    (65, 256, 264, True), (1000, 513, 257, False), (1001, 1024, 520, True), (2500, 300, 1000, False),
                                                    (4096, 128, 64, False), (129, 2048, 1024, False),
-                                                   (1500, 1500, 2100, False), (700, 2600, 2060, True), (3000, 250, 130, False)])
+                                                   (1500, 1500, 2100, False), (700, 2600, 2060, True), (3000, 250, 130, False),
+                                                   (2049, 2300, 2000, False), (1100, 2500, 2100, False)])
 def test_weight_grad(rows, inner, outer, tile, dtype):
     dy = normal(rows, outer, BF16, rows, pad=16)
     x = random_held(rows, inner, tile, rows + 1, pad=16)
