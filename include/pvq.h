@@ -326,8 +326,7 @@ int pvq_decode_static_table(const uint32_t* d_codes, const uint8_t* d_scale_idx,
  * Every size is at least 1, rows and columns below 2^31, rows * ceil(cols / 128) below 2^31.
  * Other matrices are row-major fp32 or bf16 (PVQ_DTYPE_*), 16-byte aligned, with a leading
  * dimension that is a multiple of 4 (fp32) or 8 (bf16) elements.  Outputs may not overlap
- * inputs or one another.  No call keeps anything, or needs a workspace; all can be captured into
- * graphs.  Results do not depend on launch order: the same inputs give the same bits. */
+ * inputs or one another.  No call keeps anything; all can be captured into graphs.  Results do not depend on launch order: the same inputs give the same bits. */
 typedef struct {
     uint8_t* d_codes;
     uint8_t* d_scales;
@@ -376,9 +375,17 @@ int pvq_fp8_gated_backward(const void* d_dh, int64_t ld_dh, int dtype, const pvq
 /* The gradient of a projection's weight from the 8-bit input that was kept:
  * out[o][i] = sum_t dy[t][o] x[t][i], dy bf16 with x->rows rows and `outer` columns.  Sums are held in
  * fp32 and rounded once to the type of d_out.  The values of x are taken as bf16 (exact unless
- * they leave its range).  d_status as in pvq_fp8_matmul. */
+ * they leave its range).
+ *   d_workspace  pvq_fp8_weight_grad_workspace bytes, 16-byte aligned, free again when the call's
+ *              work is done: large products then read x from there as bf16, converted once and not
+ *              for every tile of the result.  Or NULL: the same sums, somewhat slower.
+ *   d_status   as in pvq_fp8_matmul. */
 int pvq_fp8_weight_grad(const void* d_dy, int64_t outer, int64_t ld_dy, const pvq_fp8_matrix* x, void* d_out, int dtype, int64_t ld_out,
-                        uint32_t* d_status, pvq_stream_t stream);
+                        void* d_workspace, size_t workspace_bytes, uint32_t* d_status, pvq_stream_t stream);
+
+/* Bytes of workspace with which pvq_fp8_weight_grad is faster for an x of rows x inner and `outer` outputs;
+ * 0 where it needs none. */
+size_t pvq_fp8_weight_grad_workspace(int64_t rows, int64_t inner, int64_t outer);
 
 /* ---- bounds-checked build -------------------------------------------------------------- */
 

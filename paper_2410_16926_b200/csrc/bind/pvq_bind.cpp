@@ -42,6 +42,7 @@ struct Entries {
     decltype(&pvq_fp8_gated_backward) fp8_gated_backward;
     decltype(&pvq_fp8_weight_grad) fp8_weight_grad;
     decltype(&pvq_fp8_scale_row_stride) fp8_scale_row_stride;
+    decltype(&pvq_fp8_weight_grad_workspace) fp8_weight_grad_workspace;
 } lib;
 PyObject* raise_error = nullptr;  // raise_error(status, where) raises PvqError
 PyObject *k_get, *k_x, *k_out, *k_codes, *k_scale_idx, *k_row_norm, *k_edges, *k_levels, *k_cols;
@@ -763,9 +764,13 @@ PyObject* bind_fp8_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return nullptr;
     }
     if (!values_out(a[5], &place, static_cast<int>(dtype), dy.cols, x.cols, &out, &refs.r[0]) || !status_word(a[6], &place, &status)) return nullptr;
+    const size_t bytes = lib.fp8_weight_grad_workspace(x.rows, x.cols, dy.cols);
+    at::Tensor workspace;  // (of the current stream: what comes after on it may have the memory once the call's work is done)
+    if (bytes) workspace = at::detail::empty_cuda({static_cast<int64_t>(bytes)}, at::kByte, *place.dev, std::nullopt);
+    void* const w = bytes ? workspace.data_ptr() : nullptr;
     void* s = stream();
     if (failed(unlocked([&] {
-                   return lib.fp8_weight_grad(dy.p, dy.cols, dy.ld, &x, out.p, out.dtype, out.ld, static_cast<uint32_t*>(status), s);
+                   return lib.fp8_weight_grad(dy.p, dy.cols, dy.ld, &x, out.p, out.dtype, out.ld, w, bytes, static_cast<uint32_t*>(status), s);
                }),
                "pvq_fp8_weight_grad"))
         return nullptr;

@@ -98,13 +98,21 @@ extern "C" int pvq_fp8_gated_backward(const void* d_dh, int64_t ld_dh, int dtype
     return fp8::gated_backward(a, dtype == PVQ_DTYPE_BF16, act, static_cast<cudaStream_t>(stream));
 }
 
+extern "C" size_t pvq_fp8_weight_grad_workspace(int64_t rows, int64_t inner, int64_t outer) {
+    return rows < 1 || inner < 1 || outer < 1 ? 0 : fp8::weight_grad_workspace(rows, inner, outer);
+}
+
 extern "C" int pvq_fp8_weight_grad(const void* d_dy, int64_t outer, int64_t ld_dy, const pvq_fp8_matrix* x, void* d_out, int dtype, int64_t ld_out,
-                                   uint32_t* d_status, pvq_stream_t stream) {
+                                   void* d_workspace, size_t workspace_bytes, uint32_t* d_status, pvq_stream_t stream) {
     fp8::Matrix m;
     CHECKED(checked(x, &m));
     if (outer < 1) return PVQ_ERR_INVALID_ARG;
     if (outer >= int64_t(1) << 31) return PVQ_ERR_UNSUPPORTED;
     CHECKED(checked_values(d_dy, PVQ_DTYPE_BF16, outer, ld_dy));
     CHECKED(checked_values(d_out, dtype, m.cols, ld_out));
-    return fp8::weight_grad(d_dy, outer, ld_dy, m, d_out, dtype == PVQ_DTYPE_BF16, ld_out, d_status, static_cast<cudaStream_t>(stream));
+    if (d_workspace) {
+        if (workspace_bytes < fp8::weight_grad_workspace(m.rows, m.cols, outer)) return PVQ_ERR_TABLE_TOO_SMALL;
+        if (!is_aligned(d_workspace, 16)) return PVQ_ERR_ALIGNMENT;
+    }
+    return fp8::weight_grad(d_dy, outer, ld_dy, m, d_out, dtype == PVQ_DTYPE_BF16, ld_out, d_workspace, d_status, static_cast<cudaStream_t>(stream));
 }

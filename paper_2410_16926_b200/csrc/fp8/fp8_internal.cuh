@@ -120,7 +120,9 @@ struct GatedBackwardArgs {
 };
 int gated_backward(const GatedBackwardArgs& a, bool bf16, int act, cudaStream_t s);
 int matmul(const Matrix& a, const Matrix& b, bool transposed, void* out, bool bf16, int64_t ld, uint32_t* status, cudaStream_t s);
-int weight_grad(const void* dy, int64_t outer, int64_t ld_dy, const Matrix& x, void* out, bool bf16, int64_t ld, uint32_t* status, cudaStream_t s);
+size_t weight_grad_workspace(int64_t rows, int64_t inner, int64_t outer);
+int weight_grad(const void* dy, int64_t outer, int64_t ld_dy, const Matrix& x, void* out, bool bf16, int64_t ld, void* workspace, uint32_t* status,
+                cudaStream_t s);
 
 }  // namespace fp8
 }  // namespace pvq

@@ -18,14 +18,19 @@ namespace pvq {
 namespace fp8 {
 namespace {
 
-constexpr int kThreads = 640;
 constexpr int kDepth = 64;                    // values of t a stage
-constexpr int kStages = 5, kStageBytes = 128 * kDepth * 3;  // 128 columns of dy (bf16), 128 of x (codes)
-constexpr int kConverted = 4, kConvertedBytes = 128 * kDepth * 2;
+constexpr int kAtom = kDepth * 128;           // bytes from 64 bf16 columns to the next 64
+// A stage: 128 columns of dy (bf16) and 128 of x, as codes, or READY: as bf16.
+template <bool READY>
+struct Shape {
+    static constexpr int kConverters = READY ? 0 : 8;  // warps
+    static constexpr int kThreads = 32 * (4 + kConverters + 8);
+    static constexpr int kStages = READY ? 6 : 5, kStageBytes = (READY ? 4 : 3) * kAtom;
+    static constexpr int kConverted = READY ? 0 : 4;
+    static constexpr size_t kShared = 1024 + kStages * kStageBytes + kConverted * 2 * kAtom + 8 * 4096 + 256;
+};
 constexpr int kRun = 512 / kDepth;            // stages that are added in tensor memory
 constexpr int kStoreBytes = 4096;             // 32 rows of 128 bytes
-constexpr int kAtom = kDepth * 128;           // bytes from 64 bf16 columns to the next 64
-constexpr size_t kShared = 1024 + kStages * kStageBytes + kConverted * kConvertedBytes + 8 * kStoreBytes + 256;
 constexpr int kGroup = 8;                     // tiles down that are taken together across
 
 struct Maps {
@@ -104,8 +109,11 @@ __device__ __forceinline__ void convert_row_any(uint32_t from, uint32_t to, int 
     }
 }
 
-template <bool PAIR, class T>
-__global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args p) {
+template <bool PAIR, bool READY, class T>
+__global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args p) {
+    using S = Shape<READY>;
+    constexpr int kStages = S::kStages, kStageBytes = S::kStageBytes, kConverted = S::kConverted, kConvertedBytes = 2 * kAtom;
+    constexpr int kFirstHolder = 4 + S::kConverters;  // warp
     constexpr int kSide = PAIR ? 256 : 128;   // of a tile
     constexpr int kHeld = kSide / 2;          // columns of the sum a warp holds
     constexpr uint32_t kBlocks = PAIR ? 2 : 1;
@@ -155,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     };
 
     if (warp < 4) {
-        fewer_registers<kFew>();
+        if constexpr (!READY) fewer_registers<kFew>();
         if (warp == 0 && elected()) {
             Turn<kStages> turn;
             uint32_t issued = 0;
@@ -169,9 +177,14 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                     const uint32_t at = base + turn.at * kStageBytes;
                     ok = barrier_wait(empty + 8 * turn.at, turn.parity ^ 1, bounds);
                     if (!ok) break;
-                    if (rank == 0) barrier_expect(full_dy + 8 * turn.at, kBlocks * 2 * kAtom);
-                    barrier_expect(full_x + 8 * turn.at, kAtom);
-                    load_tile<false>(at + 2 * kAtom, &maps.x, col, kb * kDepth, full_x + 8 * turn.at);
+                    if (rank == 0) barrier_expect(full_dy + 8 * turn.at, kBlocks * (READY ? 4 : 2) * kAtom);
+                    if constexpr (READY) {
+                        load_tile<PAIR>(at + 2 * kAtom, &maps.x, col, kb * kDepth, full_there + 8 * turn.at);
+                        load_tile<PAIR>(at + 3 * kAtom, &maps.x, col + 64, kb * kDepth, full_there + 8 * turn.at);
+                    } else {
+                        barrier_expect(full_x + 8 * turn.at, kAtom);
+                        load_tile<false>(at + 2 * kAtom, &maps.x, col, kb * kDepth, full_x + 8 * turn.at);
+                    }
                     load_tile<PAIR>(at, &maps.dy, row, kb * kDepth, full_there + 8 * turn.at);
                     load_tile<PAIR>(at + kAtom, &maps.dy, row + 64, kb * kDepth, full_there + 8 * turn.at);
                     turn.next();
@@ -181,11 +194,11 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
             if (!ok)  // copies in flight have to land before the block ends
                 for (uint32_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i) {
                     const uint32_t s = i % kStages, parity = (i / kStages) & 1;
-                    for (int polls = 0; polls < kLandings && !((rank != 0 || barrier_passed(full_dy + 8 * s, parity)) && barrier_passed(full_x + 8 * s, parity)); ++polls) {}
+                    for (int polls = 0; polls < kLandings && !((rank != 0 || barrier_passed(full_dy + 8 * s, parity)) && (READY || barrier_passed(full_x + 8 * s, parity))); ++polls) {}
                 }
         } else if (warp == 1 && rank == 0 && elected()) {
             constexpr uint32_t product = product_bf16(kSide, kSide, true, true);
-            const uint64_t a0 = operand(base, kAtom), b0 = operand(converted, kAtom);
+            const uint64_t a0 = operand(base, kAtom), b0 = operand(READY ? base + 2 * kAtom : converted, kAtom);
             Turn<kStages> turn;
             Turn<kConverted> ready;
             Turn<2> sums;
@@ -194,16 +207,19 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                 int within = 0;
                 for (int kb = begin; kb < end; ++kb) {
                     if (within == 0) ok = barrier_wait(sum_empty + 8 * sums.at, sums.parity ^ 1, bounds);
-                    ok = ok && barrier_wait(full_dy + 8 * turn.at, turn.parity, bounds) && barrier_wait(converted_full + 8 * ready.at, ready.parity, bounds);
+                    ok = ok && barrier_wait(full_dy + 8 * turn.at, turn.parity, bounds);
+                    if constexpr (!READY) ok = ok && barrier_wait(converted_full + 8 * ready.at, ready.parity, bounds);
                     if (!ok) break;
                     tensor_fence_after();
-                    const uint64_t a = a0 + turn.at * (kStageBytes >> 4), b = b0 + ready.at * (kConvertedBytes >> 4);
+                    const uint64_t a = a0 + turn.at * (kStageBytes >> 4), b = b0 + (READY ? turn.at * (kStageBytes >> 4) : ready.at * (kConvertedBytes >> 4));
 #pragma unroll
                     for (int k = 0; k < kDepth / 16; ++k) multiply_bf16<PAIR>(tensor + sums.at * kSide, a + 128 * k, b + 128 * k, product, within > 0 || k > 0);
                     products_done<PAIR>(empty + 8 * turn.at);
-                    products_done<PAIR>(converted_empty + 8 * ready.at);
+                    if constexpr (!READY) {
+                        products_done<PAIR>(converted_empty + 8 * ready.at);
+                        ready.next();
+                    }
                     turn.next();
-                    ready.next();
                     if (++within == kRun || kb == end - 1) {
                         products_done<PAIR>(sum_full + 8 * sums.at);
                         sums.next();
@@ -216,7 +232,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                 for (int polls = 0; polls < kLandings && !barrier_passed(drained, 0); ++polls) {}
             }
         }
-    } else if (warp < 12) {
+    } else if (warp < kFirstHolder) {
+        if constexpr (!READY) {
         fewer_registers<kSome>();
         // a thread takes 64 codes of one t: a row of the tile, eight neighbouring rows in eight different places
         const int row = lane + 32 * (warp & 1), half = (warp >> 1) & 1;
@@ -259,12 +276,14 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                 }
             }
         }
+        }
     } else {
-        more_registers<kMany>();
+        if constexpr (!READY) more_registers<kMany>();
         constexpr int kColumns = 128 / sizeof(T);  // of a stored tile
-        const int quarter = warp & 3, half = (warp - 12) >> 2;
-        const uint32_t buffer_at = stores + (warp - 12) * kStoreBytes, empty_there = PAIR ? address_in(sum_empty, 0) : sum_empty;
+        const int quarter = warp & 3, half = (warp - kFirstHolder) >> 2;
+        const uint32_t buffer_at = stores + (warp - kFirstHolder) * kStoreBytes, empty_there = PAIR ? address_in(sum_empty, 0) : sum_empty;
         const uint32_t mine = tensor + (quarter << 21) + half * kHeld;
+        const auto place = [](int j) { return READY ? j : turned(j); };
         uint32_t run = 0;
         bool ok = true;
         for (int t = blockIdx.x / team; t < tiles && ok; t += step) {
@@ -299,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
 #pragma unroll
                 for (int c = 0; c < kHeld / 4; ++c)
                     asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((half * (kHeld / 4) + c) ^ (lane & 7)) << 4)), "f"(sum[4 * c]),
-                                 "f"(sum[4 * c + 2]), "f"(sum[4 * c + 1]), "f"(sum[4 * c + 3])
+                                 "f"(sum[place(4 * c + 1)]), "f"(sum[place(4 * c + 2)]), "f"(sum[4 * c + 3])
                                  : "memory");
                 continue;  // (the only tile)
             }
@@ -310,8 +329,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                 uint32_t w[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
-                    if constexpr (sizeof(T) == 2) w[i] = bf16x2_of(sum[c * kColumns + turned(2 * i)], sum[c * kColumns + turned(2 * i + 1)]);
-                    else w[i] = __float_as_uint(sum[c * kColumns + turned(i)]);
+                    if constexpr (sizeof(T) == 2) w[i] = bf16x2_of(sum[c * kColumns + place(2 * i)], sum[c * kColumns + place(2 * i + 1)]);
+                    else w[i] = __float_as_uint(sum[c * kColumns + place(i)]);
                 }
                 // A tiled store ends at a multiple of 16 bytes behind the last column: where that is not the row's end, and
                 // might be another matrix's, the last tile is stored by values.
@@ -349,10 +368,10 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     __syncthreads();
     cluster_barrier();
     if (!PAIR && p.split > 1) {
-        if (warp >= 12) {  // this block's share of the rows, eight columns a thread
+        if (warp >= kFirstHolder) {  // this block's share of the rows, eight columns a thread
             int m, n;
             tile_at(blockIdx.x / team, &m, &n);
-            const int thread = threadIdx.x - 384, share = 128 / p.split, col = thread % 16 * 8;
+            const int thread = threadIdx.x - 32 * kFirstHolder, share = 128 / p.split, col = thread % 16 * 8;
             const int64_t left = p.x.cols - int64_t(n) * 128 - col;
             for (int r = part * share + thread / 16; r < (part + 1) * share; r += 16) {
                 const int64_t row = int64_t(m) * 128 + r;
@@ -390,15 +409,26 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     }
 }
 
-template <bool PAIR, class T>
+template <bool PAIR, bool READY, class T>
 int launch(const Args& p, const Maps& maps, cudaStream_t s) {
-    void (*const kernel)(Maps, Args) = weight_grad_kernel<PAIR, T>;
+    using S = Shape<READY>;
+    constexpr size_t kShared = S::kShared;
+    constexpr unsigned kThreads = S::kThreads;
+    void (*const kernel)(Maps, Args) = weight_grad_kernel<PAIR, READY, T>;
     int st = allow_shared(reinterpret_cast<const void*>(kernel), kShared), registers = 0;
-    if (st == PVQ_OK) st = registers_of(reinterpret_cast<const void*>(kernel), &registers);
-    if (st == PVQ_OK && registers < kRegisters) st = PVQ_ERR_UNSUPPORTED;
+    if (st == PVQ_OK && !READY) {
+        st = registers_of(reinterpret_cast<const void*>(kernel), &registers);
+        if (st == PVQ_OK && registers < kRegisters) st = PVQ_ERR_UNSUPPORTED;
+    }
     if (st != PVQ_OK) return st;
     const int team = PAIR ? 2 : p.split, teams = p.split > 1 || p.tiles < kSms / team ? p.tiles : kSms / team;
     return launch_early(kernel, dim3(static_cast<unsigned>(teams * team)), kThreads, kShared, team, s, maps, p);
+}
+
+// x as bf16 in the caller's workspace.
+int64_t workspace_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
+bool worth_a_workspace(int64_t rows, int64_t inner, int64_t outer) {
+    return outer >= 2048 && ((outer + 255) / 256) * ((inner + 255) / 256) >= 48 && rows >= 1024;
 }
 
 // Parts of t for as many tiles of 128 x 128, so that they fill the GPU and each part is a run at least.
@@ -409,7 +439,7 @@ int parts(int64_t tiles, int64_t stages) {
 }
 
 template <class T>
-int weight_grad_of(Args p, const void* dy, int64_t ld_dy, cudaStream_t s) {
+int weight_grad_of(Args p, const void* dy, int64_t ld_dy, void* workspace, cudaStream_t s) {
     const int64_t pairs = ((p.outer + 255) / 256) * ((p.x.cols + 255) / 256), tiles = ((p.outer + 127) / 128) * ((p.x.cols + 127) / 128);
     const int64_t stages = (p.x.rows + kDepth - 1) / kDepth;
     if (tiles >= int64_t(1) << 30) return PVQ_ERR_UNSUPPORTED;
@@ -423,26 +453,40 @@ int weight_grad_of(Args p, const void* dy, int64_t ld_dy, cudaStream_t s) {
     if (pairs < 48) {
         p.tiles = static_cast<int>(tiles);
         p.split = parts(tiles, stages);
-        return launch<false, T>(p, maps, s);
+        return launch<false, false, T>(p, maps, s);
     }
     // The last round of tiles, where it is a small one, is shared by all SMs: in quarters, with t in parts.  (14336 x 4096 are
     // twelve rounds of 74 tiles and 8 tiles.)
     const int last = static_cast<int>(pairs % (kSms / 2)), split = parts(4 * last, stages);
     const bool shared = pairs > last && last > 0 && split > 1;
     p.tiles = static_cast<int>(shared ? pairs - last : pairs);
-    st = launch<true, T>(p, maps, s);
+    if (workspace) {
+        const int64_t ld = workspace_ld(p.x.cols);
+        Maps ready = maps;
+        st = dequantize(p.x, workspace, true, ld, s);
+        if (st == PVQ_OK) st = tile_map(&ready.x, workspace, Element::kBf16, p.x.rows, p.x.cols, ld, 64, kDepth);
+        if (st == PVQ_OK) st = launch<true, true, T>(p, ready, s);
+    } else {
+        st = launch<true, false, T>(p, maps, s);
+    }
     if (st != PVQ_OK || !shared) return st;
     p.after = p.tiles;
     p.tiles = 4 * last;
     p.split = split;
-    return launch<false, T>(p, maps, s);
+    return launch<false, false, T>(p, maps, s);
 }
 
 }  // namespace
 
-int weight_grad(const void* dy, int64_t outer, int64_t ld_dy, const Matrix& x, void* out, bool bf16, int64_t ld, uint32_t* status, cudaStream_t s) {
+size_t weight_grad_workspace(int64_t rows, int64_t inner, int64_t outer) {
+    return worth_a_workspace(rows, inner, outer) ? static_cast<size_t>(rows) * workspace_ld(inner) * 2 : 0;
+}
+
+int weight_grad(const void* dy, int64_t outer, int64_t ld_dy, const Matrix& x, void* out, bool bf16, int64_t ld, void* workspace, uint32_t* status,
+                cudaStream_t s) {
     const Args p{x, out, outer, ld, status, 1, 0, -1};
-    return bf16 ? weight_grad_of<__nv_bfloat16>(p, dy, ld_dy, s) : weight_grad_of<float>(p, dy, ld_dy, s);
+    if (!worth_a_workspace(x.rows, x.cols, outer)) workspace = nullptr;
+    return bf16 ? weight_grad_of<__nv_bfloat16>(p, dy, ld_dy, workspace, s) : weight_grad_of<float>(p, dy, ld_dy, workspace, s);
 }
 
 }  // namespace fp8

@@ -93,7 +93,9 @@ def lib():
         L.pvq_fp8_matmul.argtypes = [fp8, fp8, i32, vp, i32, i64, vp, vp]
         L.pvq_fp8_gated.argtypes = [vp, i64, vp, i64, i32, i32, fp8, fp8, fp8, vp]
         L.pvq_fp8_gated_backward.argtypes = [vp, i64, i32, fp8, fp8, i32, vp, i64, vp, i64, vp]
-        L.pvq_fp8_weight_grad.argtypes = [vp, i64, i64, fp8, vp, i32, i64, vp, vp]
+        L.pvq_fp8_weight_grad.argtypes = [vp, i64, i64, fp8, vp, i32, i64, vp, sz, vp, vp]
+        L.pvq_fp8_weight_grad_workspace.argtypes = [i64, i64, i64]
+        L.pvq_fp8_weight_grad_workspace.restype = sz
         L.pvq_debug_status.argtypes = [vp]
         L.pvq_encode_status.argtypes = [vp]
         _lib = L
@@ -105,7 +107,8 @@ EXPORTS = ["pvq_strerror", "pvq_last_cuda_error", "pvq_index_bits", "pvq_max_pul
            "pvq_build_scale_codebook", "pvq_encode", "pvq_decode", "pvq_roundtrip", "pvq_encode_batched",
            "pvq_decode_batched", "pvq_decode_static_table", "pvq_rotate_encode", "pvq_rotate_roundtrip", "pvq_encode_amp",
            "pvq_debug_status", "pvq_encode_status", "pvq_fp8_scale_row_stride", "pvq_fp8_quantize", "pvq_fp8_dequantize",
-           "pvq_fp8_matmul", "pvq_fp8_gated", "pvq_fp8_gated_backward", "pvq_fp8_weight_grad"]
+           "pvq_fp8_matmul", "pvq_fp8_gated", "pvq_fp8_gated_backward", "pvq_fp8_weight_grad",
+           "pvq_fp8_weight_grad_workspace"]
 
 
 def _check(status, where):
@@ -128,7 +131,7 @@ def _load_native():
     loader.exec_module(m)
     names = ("encode", "encode_amp", "decode", "roundtrip", "rotate_encode", "rotate_roundtrip", "encode_batched",
              "decode_batched", "code_words", "scale_row_stride", "fp8_quantize", "fp8_dequantize", "fp8_matmul", "fp8_gated",
-             "fp8_gated_backward", "fp8_weight_grad", "fp8_scale_row_stride")
+             "fp8_gated_backward", "fp8_weight_grad", "fp8_scale_row_stride", "fp8_weight_grad_workspace")
     m.init(_raise, *(C.cast(getattr(L, "pvq_" + n), C.c_void_p).value for n in names))
     _native = m
     return m

@@ -38,7 +38,7 @@ def test_matrices_are_checked(bad, status):
     assert L.pvq_fp8_gated(P, 256, P, 256, 1, 0, good, good, q, None) == status
     assert L.pvq_fp8_gated_backward(P, 256, 1, q, good, 0, P, 256, P, 256, None) == status
     assert L.pvq_fp8_gated_backward(P, 256, 1, good, q, 0, P, 256, P, 256, None) == status
-    assert L.pvq_fp8_weight_grad(P, 64, 64, q, P, 0, ld, None, None) == status
+    assert L.pvq_fp8_weight_grad(P, 64, 64, q, P, 0, ld, None, 0, None, None) == status
     assert L.pvq_fp8_quantize(P, 1, 256, None, None) == INVALID
     assert L.pvq_fp8_matmul(good, None, 0, P, 1, 8, None, None) == INVALID
 
@@ -55,12 +55,12 @@ def test_values_are_checked(p, dtype, ld, status):
     assert L.pvq_fp8_matmul(q, t, 1, p, dtype, ld, None, None) == status
     assert L.pvq_fp8_gated(p, ld, P, 256, dtype, 0, q, None, None, None) == status
     assert L.pvq_fp8_gated_backward(p, ld, dtype, q, q, 0, P, 256, P, 256, None) == status
-    assert L.pvq_fp8_weight_grad(P, 64, 64, q, p, dtype, ld, None, None) == status
+    assert L.pvq_fp8_weight_grad(P, 64, 64, q, p, dtype, ld, None, 0, None, None) == status
     if dtype == 1:
         assert L.pvq_fp8_gated(P, 256, p, ld, dtype, 0, q, None, None, None) == status
         assert L.pvq_fp8_gated_backward(P, 256, dtype, q, q, 0, p, ld, P, 256, None) == status
         assert L.pvq_fp8_gated_backward(P, 256, dtype, q, q, 0, P, 256, p, ld, None) == status
-        assert L.pvq_fp8_weight_grad(p, 256, ld, q, P, dtype, 256, None, None) == status
+        assert L.pvq_fp8_weight_grad(p, 256, ld, q, P, dtype, 256, None, 0, None, None) == status
 
 
 def test_what_does_not_fit_together_is_refused():
@@ -78,8 +78,14 @@ def test_what_does_not_fit_together_is_refused():
         assert L.pvq_fp8_gated(P, 256, P, 256, 1, 0, *args, None) == INVALID
     for args in ((t, t), (q, t), (q, other), (other, q)):
         assert L.pvq_fp8_gated_backward(P, 256, 1, *args, 0, P, 256, P, 256, None) == INVALID
-    assert L.pvq_fp8_weight_grad(P, 0, 64, q, P, 0, 256, None, None) == INVALID
-    assert L.pvq_fp8_weight_grad(P, 1 << 31, 1 << 31, q, P, 0, 256, None, None) == UNSUPPORTED
+    assert L.pvq_fp8_weight_grad(P, 0, 64, q, P, 0, 256, None, 0, None, None) == INVALID
+    big = C.byref(desc(rows=4096, cols=4096, ld_codes=4096, ld_scales=32))
+    need = L.pvq_fp8_weight_grad_workspace(4096, 4096, 4096)
+    assert need == 4096 * 4096 * 2
+    assert L.pvq_fp8_weight_grad(P, 4096, 4096, big, P, 0, 4096, P, need - 1, None, None) == 4
+    assert L.pvq_fp8_weight_grad(P, 4096, 4096, big, P, 0, 4096, P + 8, need, None, None) == ALIGN
+    assert [L.pvq_fp8_weight_grad_workspace(*a) for a in ((0, 4096, 4096), (4096, 0, 4096), (4096, 4096, 0), (1, 1, 1))] == [0, 0, 0, 0]
+    assert L.pvq_fp8_weight_grad(P, 1 << 31, 1 << 31, q, P, 0, 256, None, 0, None, None) == UNSUPPORTED
 
 
 def test_scale_row_stride():

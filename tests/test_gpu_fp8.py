@@ -209,13 +209,29 @@ def check_weight_grad(dy, x, dtype, out=None):
                                                    (65, 256, 264, True), (1000, 513, 257, False), (1001, 1024, 520, True), (2500, 300, 1000, False),
                                                    (4096, 128, 64, False), (129, 2048, 1024, False),
                                                    (1500, 1500, 2100, False), (700, 2600, 2060, True), (3000, 250, 130, False),
-                                                   (2049, 2300, 2000, False), (1100, 2500, 2100, False)])
+                                                   (2049, 2300, 2000, False), (1100, 2500, 2100, False), (1000, 2500, 2100, False)])
 def test_weight_grad(rows, inner, outer, tile, dtype):
     dy = normal(rows, outer, BF16, rows, pad=16)
     x = random_held(rows, inner, tile, rows + 1, pad=16)
     out, check = guarded(outer, inner, dtype, 8)
     check_weight_grad(dy, x, dtype, out)
     check()
+
+
+@pytest.mark.parametrize("rows,inner,outer", [(1100, 2500, 2100), (1500, 1504, 2104)])
+def test_weight_grad_without_a_workspace(rows, inner, outer):
+    """The C call takes NULL: the same bits."""
+    import ctypes as C
+    L = pvq.lib()
+    assert L.pvq_fp8_weight_grad_workspace(rows, inner, outer) > 0
+    dy, x = normal(rows, outer, BF16, 1), random_held(rows, inner, False, 2)
+    want = pvq.fp8_weight_grad(dy, x)
+    out, check = guarded(outer, inner, F32, 4)
+    desc = pvq.Fp8Desc(x.codes.data_ptr(), x.scales.data_ptr(), rows, inner, x.codes.stride(0), x.scales.stride(0), 0)
+    stream = C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert L.pvq_fp8_weight_grad(dy.data_ptr(), outer, dy.stride(0), C.byref(desc), out.data_ptr(), 0, out.stride(0), None, 0, None, stream) == 0
+    check()
+    assert torch.equal(out, want)
 
 
 def test_weight_grad_of_nan():
