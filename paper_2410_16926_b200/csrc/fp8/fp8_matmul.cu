@@ -19,6 +19,8 @@ int matmul(const Matrix& a, const Matrix& b, bool transposed, void* out, bool bf
     const int64_t room = high <= 32 ? 4 * kSms : kSms;
     int split = 1;
     while (split < 8 && tiles * split * 2 <= room && blocks >= 4 * split * 2) split *= 2;
+    if (!bf16)  // (long fp32 sums in parts, as matmul_many's)
+        while (split < 8 && blocks > 64 * split) split *= 2;
     return matmul_few(p, transposed, bf16, split, s);
 }
 

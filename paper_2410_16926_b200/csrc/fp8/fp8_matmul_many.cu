@@ -22,6 +22,11 @@ constexpr int kStoreBytes = 4096;  // 32 rows of 128 bytes
 constexpr int kSecond = 224;                   // first column of odd tiles' results; the first 32 of them are even tiles' last
 constexpr int kScalesA = 480, kScalesB = 488;  // columns, two buffers of 4 and of 8
 constexpr int kGroup = 8;  // tiles down that are taken together across
+// fp32 results of more than kRun blocks along k are summed in parts of about as many: sums in tensor memory are cut off, not
+// rounded, and come out 8e-8 of themselves too small for every 1024 values (14336 values: 1.1e-6).  The parts are added in
+// registers, for which the warpgroups share those of the block out anew.
+constexpr int kRun = 64, kRegisters = 128, kFew = 48, kSome = 64, kMany = 200;
+static_assert(kFew + kSome + 2 * kMany <= 4 * kRegisters, "a share beyond these would be waited for without end");
 constexpr size_t kShared = 1024 + kStages * kStageBytes + 8 * 2 * kStoreBytes + 256;
 
 struct Maps {
@@ -71,7 +76,12 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
     const Bounds bounds{&over, p.status};
     const Tiles tiles{static_cast<int>((p.rows + 255) / 256), static_cast<int>((p.outs + 255) / 256)};
     const int blocks = static_cast<int>((p.inner + kBlock - 1) / kBlock), first = blockIdx.x / 2, step = gridDim.x / 2;
+    constexpr bool kParts = sizeof(T) == 4;
+    const int about = kParts ? (blocks + kRun - 1) / kRun : 1, part_blocks = (blocks + about - 1) / about, parts = (blocks + part_blocks - 1) / part_blocks;
 
+    if (warp < 4) {
+        if constexpr (kParts) fewer_registers<kFew>();
+    }
     if (warp == 0) {
         if (elected()) {
             Turn<kStages> turn;
@@ -108,29 +118,36 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
             Turn<2> sums;           // the two places of the result
             uint32_t shared = 1;    // the parity of the columns that they share
             bool ok = true;
-            for (int t = first; t < tiles.count() && ok; t += step, sums.next(), shared ^= 1) {
-                ok = barrier_wait(sum_empty + 8 * sums.at, sums.parity ^ 1, bounds) && barrier_wait(shared_empty, shared, bounds);
-                if (!ok) break;
-                const uint32_t sum = tensor + kSecond * sums.at;
-                tensor_fence_after();
-                for (int kb = 0; kb < blocks; ++kb) {
+            for (int t = first; t < tiles.count() && ok; t += step) {
+                int left = 0;  // of the part
+                for (int kb = 0; kb < blocks; ++kb, --left) {
                     const uint32_t part = kb & 3;
-                    if (part == 0) ok = barrier_wait(scales_full + 8 * scales.at, scales.parity, bounds);
+                    const bool starts = left == 0;
+                    if (starts) {
+                        ok = barrier_wait(sum_empty + 8 * sums.at, sums.parity ^ 1, bounds) && barrier_wait(shared_empty, shared, bounds);
+                        left = part_blocks;
+                    }
+                    if (part == 0) ok = ok && barrier_wait(scales_full + 8 * scales.at, scales.parity, bounds);
                     ok = ok && barrier_wait(full + 8 * turn.at, turn.parity, bounds);
                     if (!ok) break;
                     tensor_fence_after();
                     const uint64_t a = a0 + turn.at * (kStageBytes >> 4), b = b0 + turn.at * (kStageBytes >> 4);
-                    const uint32_t sa = tensor + kScalesA + 4 * scales.at, sb = tensor + kScalesB + 8 * scales.at, with = with_part(product, part);
+                    const uint32_t sum = tensor + kSecond * sums.at, sa = tensor + kScalesA + 4 * scales.at, sb = tensor + kScalesB + 8 * scales.at,
+                                   with = with_part(product, part);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) multiply_e4m3<true>(sum, a + 2 * k, b + kAlongB * k, with, sa, sb, kb > 0 || k > 0);
+                    for (int k = 0; k < 4; ++k) multiply_e4m3<true>(sum, a + 2 * k, b + kAlongB * k, with, sa, sb, !starts || k > 0);
                     products_done<true>(empty + 8 * turn.at);
                     turn.next();
                     if (part == 3 || kb == blocks - 1) {
                         products_done<true>(scales_empty + 8 * scales.at);
                         scales.next();
                     }
+                    if (left == 1 || kb == blocks - 1) {
+                        products_done<true>(sum_full + 8 * sums.at);
+                        sums.next();
+                        shared ^= 1;
+                    }
                 }
-                if (ok) products_done<true>(sum_full + 8 * sums.at);
             }
             if (!ok) {
                 products_done<true>(drained);
@@ -138,6 +155,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
             }
         }
     } else if (warp >= 4 && warp < 8) {
+        if constexpr (kParts) fewer_registers<kSome>();
         const uint32_t mine = tensor + ((warp & 3) << 21);
         const uint32_t full_there = address_in(scales_full, 0);
         // The words of four blocks along k are asked for two such steps before they are needed, in two sets of registers that
@@ -185,65 +203,104 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
         const int quarter = warp & 3, half = (warp - 8) >> 2;
         constexpr int kChunks = 128 / kColumns;
         const uint32_t buffers = stores + (warp - 8) * 2 * kStoreBytes, empty_there = address_in(sum_empty, 0), shared_there = address_in(shared_empty, 0);
-        uint32_t tile = 0;
-        for (int t = first; t < tiles.count(); t += step, ++tile) {
+        if constexpr (kParts) more_registers<kMany>();
+        // A chunk of 32 words a lane (bf16: 64 columns, fp32: 32) to memory.
+        uint32_t buffer = 0;
+        const auto put = [&](const uint32_t (&w)[32], int64_t row, int64_t col) {
+            // A tiled store ends at a multiple of 16 bytes behind the last column: where that is not the row's end, and
+            // might be another matrix's, the last tile is stored by values.
+            if (col + kColumns > p.outs && p.outs * sizeof(T) % 16 != 0) {
+                if (row + lane < p.rows) {
+                    T* to_row = static_cast<T*>(p.out) + (row + lane) * p.ld + col;
+#pragma unroll
+                    for (int i = 0; i < kColumns; ++i)
+                        if (col + i < p.outs) {
+                            if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(to_row)[i] = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));
+                            else reinterpret_cast<uint32_t*>(to_row)[i] = w[i];
+                        }
+                }
+                return;
+            }
+            const uint32_t to = buffers + buffer * kStoreBytes;
+            buffer ^= 1;
+            if (lane == 0) store_wait_read<1>();
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
+                             "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
+                             : "memory");
+            async_fence();
+            __syncwarp();
+            if (lane == 0) {
+                if (row < p.rows && col < p.outs) store_tile(&maps.out, static_cast<int>(col), static_cast<int>(row), to);
+                store_commit();
+            }
+        };
+        // Parts of tiles: even ones share their last columns with the next, odd ones their first.  Each half begins with what it
+        // may share: the right one goes backwards.
+        uint32_t item = 0;
+        const auto chunk = [&](int i) { return half ? kChunks - 1 - i : i; };
+        bool ok = true;
+        for (int t = first; t < tiles.count() && ok; t += step) {
             int m, n;
             tiles.at(t, &m, &n);
-            if (!warp_wait(sum_full + 8 * (tile & 1), (tile >> 1) & 1, bounds)) break;
-            tensor_fence_after();
-            const int64_t row = int64_t(m) * 256 + rank * 128 + quarter * 32;
-            // even tiles share their last columns with the next tile, odd ones their first
-            const bool backwards = (tile & 1) == 0, shares = half == (backwards ? 1 : 0);
-            const uint32_t mine = tensor + (quarter << 21) + (tile & 1) * kSecond + half * 128;
-#pragma unroll 1
-            for (int i = 0; i < kChunks; ++i) {
-                const int c = backwards ? kChunks - 1 - i : i;
-                const uint32_t to = buffers + (i & 1) * kStoreBytes + lane * 128;
-                const int64_t col = int64_t(n) * 256 + half * 128 + c * kColumns;
-                uint32_t w[32];
-                float v[kColumns];
-#pragma unroll
-                for (int k = 0; k < kColumns; k += 32) tensor_load(mine + c * kColumns + k, reinterpret_cast<float(&)[32]>(v[k]));
-                tensor_wait_loads();
-                if ((i == 0 && shares) || i == kChunks - 1) {
+            const int64_t row = int64_t(m) * 256 + rank * 128 + quarter * 32, col = int64_t(n) * 256 + half * 128;
+            const auto read = [&](int i) {  // has read chunk i of four or two
+                if ((i == 0 && half == ((item & 1) ^ 1)) || i == kChunks - 1) {
                     tensor_fence_before();
                     __syncwarp();
-                    if (lane == 0 && i == 0 && shares) barrier_arrive_in(shared_there);
-                    if (lane == 0 && i == kChunks - 1) barrier_arrive_in(empty_there + 8 * (tile & 1));
+                    if (lane == 0 && i == 0 && half == ((item & 1) ^ 1)) barrier_arrive_in(shared_there);
+                    if (lane == 0 && i == kChunks - 1) barrier_arrive_in(empty_there + 8 * (item & 1));
                 }
+            };
+            if constexpr (kParts) {
+                float sum[128];
 #pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    if constexpr (sizeof(T) == 2) w[k] = bf16x2_of(v[2 * k], v[2 * k + 1]);
-                    else w[k] = __float_as_uint(v[k]);
-                }
-                // A tiled store ends at a multiple of 16 bytes behind the last column: where that is not the row's end, and
-                // might be another matrix's, the last tile is stored by values.
-                if (col + kColumns > p.outs && p.outs * sizeof(T) % 16 != 0) {
-                    if (row + lane < p.rows) {
-                        T* to_row = static_cast<T*>(p.out) + (row + lane) * p.ld + col;
+                for (int k = 0; k < 128; ++k) sum[k] = 0.0f;
+#pragma unroll 1
+                for (int part = 0; part < parts; ++part, ++item) {
+                    ok = warp_wait(sum_full + 8 * (item & 1), (item >> 1) & 1, bounds);
+                    if (!ok) break;
+                    tensor_fence_after();
+                    const uint32_t mine = tensor + (quarter << 21) + (item & 1) * kSecond + half * 128;
 #pragma unroll
-                        for (int i = 0; i < kColumns; ++i)
-                            if (col + i < p.outs) {
-                                if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(to_row)[i] = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));
-                                else reinterpret_cast<uint32_t*>(to_row)[i] = w[i];
-                            }
+                    for (int i = 0; i < 4; ++i) {
+                        float v[32];
+                        tensor_load(mine + chunk(i) * 32, v);
+                        tensor_wait_loads();
+                        read(i);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) sum[i * 32 + k] += v[k];
                     }
-                    if (lane == 0) store_commit();  // (an empty group: the buffers' turns go on)
-                    continue;
                 }
-                if (lane == 0) store_wait_read<1>();
-                __syncwarp();
+                if (!ok) break;
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((j ^ (lane & 7)) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
-                                 "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
-                                 : "memory");
-                async_fence();
-                __syncwarp();
-                if (lane == 0) {
-                    if (row < p.rows && col < p.outs) store_tile(&maps.out, static_cast<int>(col), static_cast<int>(row), to);
-                    store_commit();
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(sum[i * 32 + k]);
+                    put(w, row, col + chunk(i) * 32);
                 }
+            } else {
+                ok = warp_wait(sum_full + 8 * (item & 1), (item >> 1) & 1, bounds);
+                if (!ok) break;
+                tensor_fence_after();
+                const uint32_t mine = tensor + (quarter << 21) + (item & 1) * kSecond + half * 128;
+#pragma unroll 1
+                for (int i = 0; i < kChunks; ++i) {
+                    const int c = chunk(i);
+                    float v[kColumns];
+#pragma unroll
+                    for (int k = 0; k < kColumns; k += 32) tensor_load(mine + c * kColumns + k, reinterpret_cast<float(&)[32]>(v[k]));
+                    tensor_wait_loads();
+                    read(i);
+                    uint32_t w[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) w[k] = bf16x2_of(v[2 * k], v[2 * k + 1]);
+                    put(w, row, col + c * kColumns);
+                }
+                ++item;
             }
         }
         if (lane == 0) store_wait_all();
@@ -263,6 +320,11 @@ int launch(const MatmulArgs& p, cudaStream_t s) {
     if (st == PVQ_OK) st = tile_map(&maps.b, p.b.codes, Element::kByte, p.b.rows, p.b.cols, p.b.ld_codes, kBlock, 128);
     if (st == PVQ_OK) st = tile_map(&maps.out, p.out, out, p.rows, p.outs, p.ld, 128 / sizeof(T), 32);
     void (*const kernel)(Maps, MatmulArgs) = matmul_many_kernel<ACROSS, T>;
+    if (st == PVQ_OK && sizeof(T) == 4) {
+        int registers = 0;
+        st = registers_of(reinterpret_cast<const void*>(kernel), &registers);
+        if (st == PVQ_OK && registers < kRegisters) st = PVQ_ERR_UNSUPPORTED;
+    }
     if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), kShared);
     if (st != PVQ_OK) return st;
     const int64_t tiles = ((p.rows + 255) / 256) * ((p.outs + 255) / 256);

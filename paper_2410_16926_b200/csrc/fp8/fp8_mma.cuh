@@ -245,6 +245,17 @@ __device__ __forceinline__ void products_done(uint32_t bar) {
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// ---- registers: a warpgroup's share, a thread, of those that the block was launched with
+
+template <int REGISTERS>
+__device__ __forceinline__ void more_registers() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGISTERS));
+}
+template <int REGISTERS>
+__device__ __forceinline__ void fewer_registers() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGISTERS));
+}
+
 // ---- scales in tensor memory
 
 // Four blocks' scale bytes along k for one index across it, as the product takes them: block 4 * four + i in byte i.

@@ -51,15 +51,6 @@ struct Args {
 constexpr int kRegisters = 96, kFew = 32, kSome = 56, kMany = 168;
 static_assert(kFew + 2 * kSome + 2 * kMany <= 5 * kRegisters, "a share beyond these would be waited for without end");
 
-template <int REGISTERS>
-__device__ __forceinline__ void more_registers() {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGISTERS));
-}
-template <int REGISTERS>
-__device__ __forceinline__ void fewer_registers() {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGISTERS));
-}
-
 // Column j of four neighbouring ones lies in place turned(j) of the converted operand, and so of the sums: two codes of a word
 // are made two values where they are, bytes 0 and 2, 1 and 3.
 __host__ __device__ constexpr int turned(int j) { return (j & ~3) | (j & 1) << 1 | (j & 2) >> 1; }

@@ -159,6 +159,22 @@ def test_matmul(rows, inner, outer, dtype, transposed):
     check()
 
 
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("rows,inner,outer", [(3, 9000, 200), (1300, 8200, 2100), (2100, 16600, 2400)])
+def test_matmul_of_long_sums(rows, inner, outer, transposed):
+    """fp32 results over more than 8192 values are within 1e-6 of themselves (2-norm): sums that the tensor cores cut off alone
+    would not be (8e-8 of a sum for every 1024 values)."""
+    rng = np.random.default_rng(inner)
+    make = lambda r, c: torch.from_numpy(rng.standard_normal((r, c)).astype(np.float32)).cuda()  # noqa: E731
+    a = pvq.fp8_quantize(make(rows, -(-inner // 8) * 8)[:, :inner])
+    shape = (inner, outer) if transposed else (outer, inner)
+    b = pvq.fp8_quantize(make(shape[0], -(-shape[1] // 8) * 8)[:, :shape[1]], tile=True)
+    va, vb = (pvq.fp8_dequantize(q, dtype=F32).double() for q in (a, b))
+    want = va @ (vb if transposed else vb.t())
+    got = pvq.fp8_matmul(a, b, transposed=transposed, dtype=F32).double()
+    assert float((got - want).norm()) <= 1e-6 * float(want.norm())
+
+
 @pytest.mark.parametrize("tiles", [(False, False), (True, True), (True, False)])
 @pytest.mark.parametrize("rows,inner,outer", [(3, 300, 200), (200, 640, 300), (700, 384, 520), (1300, 700, 2050)])
 def test_matmul_of_other_blocks(rows, inner, outer, tiles):
