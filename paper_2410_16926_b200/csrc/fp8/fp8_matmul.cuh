@@ -11,7 +11,8 @@ struct MatmulArgs {
     int64_t rows, outs, inner, ld;  // a.rows, columns of the result, k
     uint32_t* status;
 };
-// Few rows: 128 columns of the result by up to 128 rows a thread block, k split over `split` blocks of a cluster.
+// Few rows: 128 columns of the result by up to 128 rows a thread block, k split over `split` blocks of a cluster
+// (1, 2, 4 or 8, at most the blocks along k).
 int matmul_few(const MatmulArgs& p, bool transposed, bool bf16, int split, cudaStream_t s);
 // Many rows: 256 x 256 of the result a pair of thread blocks.
 int matmul_many(const MatmulArgs& p, bool transposed, bool bf16, cudaStream_t s);

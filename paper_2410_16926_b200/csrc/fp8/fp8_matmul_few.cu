@@ -33,8 +33,54 @@ struct Maps {
     CUtensorMap a, b;
 };
 
-template <int ROWS, bool ACROSS, class T>
-__global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_constant__ Maps maps, const __grid_constant__ MatmulArgs p, int split) {
+// Adds the parts of this block's share of the columns, 128 / SPLIT, in the order of the ranks, and stores them: four columns a
+// thread, eight reads at a time (one after another they took 250 cycles each).
+template <int SPLIT, class T>
+__device__ __forceinline__ void add_parts(uint32_t base, int rank, const MatmulArgs& p, int64_t row0, int64_t col0, T* out, int most) {
+    constexpr int kAcross = 32 / SPLIT, kStep = kThreads / kAcross, kAtOnce = 8 / SPLIT;
+    const int col = rank * (128 / SPLIT) + threadIdx.x % kAcross * 4;
+    const int rows = static_cast<int>(min(int64_t(most), p.rows - row0));
+    const int64_t left = p.outs - col0 - col;
+    if (left <= 0) return;
+    out += row0 * p.ld + col0 + col;
+    for (int r0 = threadIdx.x / kAcross; r0 < rows; r0 += kStep * kAtOnce) {
+        float4 part[kAtOnce][SPLIT];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+            for (int s = 0; s < SPLIT; ++s)
+                if (r0 + i * kStep < rows) {
+                    const uint32_t at = base + (r0 + i * kStep) * 512 + col * 4;
+                    if (SPLIT == 1)
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                     : "=f"(part[i][s].x), "=f"(part[i][s].y), "=f"(part[i][s].z), "=f"(part[i][s].w)
+                                     : "r"(at));
+                    else
+                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                     : "=f"(part[i][s].x), "=f"(part[i][s].y), "=f"(part[i][s].z), "=f"(part[i][s].w)
+                                     : "r"(address_in(at, s)));
+                }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (r0 + i * kStep >= rows) break;
+            float4 v = part[i][0];
+#pragma unroll
+            for (int s = 1; s < SPLIT; ++s) v.x += part[i][s].x, v.y += part[i][s].y, v.z += part[i][s].z, v.w += part[i][s].w;
+            T* to = out + (r0 + i * kStep) * p.ld;
+            if (left >= 4) {
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(bf16x2_of(v.x, v.y), bf16x2_of(v.z, v.w));
+                else *reinterpret_cast<float4*>(to) = v;
+            } else {
+                to[0] = T(v.x);
+                if (left > 1) to[1] = T(v.y);
+                if (left > 2) to[2] = T(v.z);
+            }
+        }
+    }
+}
+
+template <int ROWS, int SPLIT, bool ACROSS, class T>
+__global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_constant__ Maps maps, const __grid_constant__ MatmulArgs p) {
     using S = Shape<ROWS>;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
@@ -43,10 +89,10 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
     __shared__ uint32_t tensor_base;
     __shared__ int over;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = blockIdx.x % split;  // in the cluster
-    const int64_t col0 = int64_t(blockIdx.x / split) * 128, row0 = int64_t(blockIdx.y) * ROWS;
+    const int rank = blockIdx.x % SPLIT;  // in the cluster
+    const int64_t col0 = int64_t(blockIdx.x / SPLIT) * 128, row0 = int64_t(blockIdx.y) * ROWS;
     const int blocks = static_cast<int>((p.inner + kBlock - 1) / kBlock);
-    const int first = static_cast<int>(int64_t(blocks) * rank / split), last = static_cast<int>(int64_t(blocks) * (rank + 1) / split);  // (split <= blocks)
+    const int first = static_cast<int>(int64_t(blocks) * rank / SPLIT), last = static_cast<int>(int64_t(blocks) * (rank + 1) / SPLIT);  // (SPLIT <= blocks)
     const Bounds bounds{&over, p.status};
 
     const auto load = [&](int kb, uint32_t stage) {
@@ -72,14 +118,15 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
         }
     };
     if (warp == 0) {
+        // a barrier a lane: stages' full and empty, the scales' sets full and empty, the sum
+        constexpr int kBars = 2 * S::kStages + 2 * S::kScaleSets + 1;
+        static_assert(kBars <= 32, "one lane each");
+        if (lane < kBars) barrier_init(full + 8 * lane, lane >= 2 * S::kStages && lane < 2 * S::kStages + S::kScaleSets ? 4 : 1);
+        barrier_init_fence();
+        if (lane == 0) over = 0;
+        __syncwarp();
         if (elected()) {
             prefetch_map(&maps.a), prefetch_map(&maps.b);
-            over = 0;
-            for (int i = 0; i < S::kStages; ++i) barrier_init(full + 8 * i, 1), barrier_init(empty + 8 * i, 1);
-            for (int i = 0; i < S::kScaleSets; ++i) barrier_init(scales_full + 8 * i, 4), barrier_init(scales_empty + 8 * i, 1);
-            barrier_init(sum_full, 1);
-            barrier_init_fence();
-            async_fence();
             dependency_wait();
             for (int i = 0; i < S::kStages && first + i < last; ++i) load(first + i, i);
         }
@@ -180,62 +227,40 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
         tensor_fence_before();
     }
     __syncwarp();
-    cluster_barrier();
-    if (warp >= 4) {
-        // this block's share of the columns: 128 / split, eight a thread
-        const int share = 128 / split, across = share / 8, thread = threadIdx.x - 128;
-        const int col = rank * share + thread % across * 8;
-        T* out = static_cast<T*>(p.out) + row0 * p.ld + col0 + col;
-        const int rows = static_cast<int>(min(int64_t(ROWS), p.rows - row0));
-        const int64_t left = p.outs - col0 - col;
-        for (int r = thread / across; r < rows && left > 0; r += 128 / across) {
-            float v[8] = {};
-            for (int s = 0; s < split; ++s) {
-                const uint32_t from = address_in(base + r * 512 + col * 4, s);
-                float4 lo, hi;
-                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(lo.x), "=f"(lo.y), "=f"(lo.z), "=f"(lo.w) : "r"(from));
-                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(hi.x), "=f"(hi.y), "=f"(hi.z), "=f"(hi.w) : "r"(from + 16));
-                v[0] += lo.x, v[1] += lo.y, v[2] += lo.z, v[3] += lo.w, v[4] += hi.x, v[5] += hi.y, v[6] += hi.z, v[7] += hi.w;
-            }
-            T* to = out + r * p.ld;
-            if (left >= 8) {
-                if constexpr (sizeof(T) == 2) {
-                    *reinterpret_cast<uint4*>(to) = make_uint4(bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3]), bf16x2_of(v[4], v[5]), bf16x2_of(v[6], v[7]));
-                } else {
-                    reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
-                    reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < left) to[i] = T(v[i]);
-            }
-        }
-    }
+    if (SPLIT > 1) cluster_barrier();
+    else __syncthreads();
+    add_parts<SPLIT>(base, rank, p, row0, col0, static_cast<T*>(p.out), ROWS);
     __syncwarp();
-    cluster_barrier();  // the others have read this block's part
+    if (SPLIT > 1) cluster_barrier();  // the others have read this block's part
     if (warp == 2) {
         tensor_fence_after();
         tensor_free<false>(tensor, S::kColumns);
     }
 }
 
-template <int ROWS, bool ACROSS, class T>
-int launch(const MatmulArgs& p, int split, cudaStream_t s) {
+template <int ROWS, int SPLIT, bool ACROSS, class T>
+int launch(const MatmulArgs& p, cudaStream_t s) {
     Maps maps;
     int st = tile_map(&maps.a, p.a.codes, Element::kByte, p.a.rows, p.a.cols, p.a.ld_codes, kBlock, ROWS);
     if (st == PVQ_OK) st = tile_map(&maps.b, p.b.codes, Element::kByte, p.b.rows, p.b.cols, p.b.ld_codes, kBlock, 128);
-    void (*const kernel)(Maps, MatmulArgs, int) = matmul_few_kernel<ROWS, ACROSS, T>;
+    void (*const kernel)(Maps, MatmulArgs) = matmul_few_kernel<ROWS, SPLIT, ACROSS, T>;
     if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), Shape<ROWS>::kShared);
     if (st != PVQ_OK) return st;
-    const dim3 grid(static_cast<unsigned>((p.outs + 127) / 128 * split), static_cast<unsigned>((p.rows + ROWS - 1) / ROWS));
-    return launch_early(kernel, grid, kThreads, Shape<ROWS>::kShared, split, s, maps, p, split);
+    const dim3 grid(static_cast<unsigned>((p.outs + 127) / 128 * SPLIT), static_cast<unsigned>((p.rows + ROWS - 1) / ROWS));
+    return launch_early(kernel, grid, kThreads, Shape<ROWS>::kShared, SPLIT, s, maps, p);
 }
 
+template <int ROWS, int SPLIT>
+int launch_split(const MatmulArgs& p, bool transposed, bool bf16, cudaStream_t s) {
+    if (transposed) return bf16 ? launch<ROWS, SPLIT, true, __nv_bfloat16>(p, s) : launch<ROWS, SPLIT, true, float>(p, s);
+    return bf16 ? launch<ROWS, SPLIT, false, __nv_bfloat16>(p, s) : launch<ROWS, SPLIT, false, float>(p, s);
+}
 template <int ROWS>
 int launch_rows(const MatmulArgs& p, bool transposed, bool bf16, int split, cudaStream_t s) {
-    if (transposed) return bf16 ? launch<ROWS, true, __nv_bfloat16>(p, split, s) : launch<ROWS, true, float>(p, split, s);
-    return bf16 ? launch<ROWS, false, __nv_bfloat16>(p, split, s) : launch<ROWS, false, float>(p, split, s);
+    if (split == 1) return launch_split<ROWS, 1>(p, transposed, bf16, s);
+    if (split == 2) return launch_split<ROWS, 2>(p, transposed, bf16, s);
+    if (split == 4) return launch_split<ROWS, 4>(p, transposed, bf16, s);
+    return launch_split<ROWS, 8>(p, transposed, bf16, s);
 }
 
 }  // namespace
