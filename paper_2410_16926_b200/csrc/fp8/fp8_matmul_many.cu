@@ -56,14 +56,16 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
     __shared__ int over;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
-    if (threadIdx.x == 0) {
-        over = 0;
-        for (int i = 0; i < kStages; ++i) barrier_init(full + 8 * i, 1), barrier_init(empty + 8 * i, 1);
-        for (int i = 0; i < 2; ++i) barrier_init(scales_full + 8 * i, 8), barrier_init(scales_empty + 8 * i, 1);
-        for (int i = 0; i < 2; ++i) barrier_init(sum_full + 8 * i, 1), barrier_init(sum_empty + 8 * i, 16);
-        barrier_init(shared_empty, 8), barrier_init(drained, 1);
+    if (warp == 0) {  // a barrier a lane, in the order of their places
+        constexpr int kBars = 2 * kStages + 10;
+        static_assert(kBars <= 32, "one lane each");
+        const int i = lane - 2 * kStages;  // scales' full and empty, sum's full and empty, two each; shared, drained
+        if (lane < kBars) barrier_init(full + 8 * lane, i == 0 || i == 1 || i == 8 ? 8 : (i == 6 || i == 7 ? 16 : 1));
         barrier_init_fence();
-        prefetch_map(&maps.a), prefetch_map(&maps.b), prefetch_map(&maps.out);
+        if (lane == 0) {
+            over = 0;
+            prefetch_map(&maps.a), prefetch_map(&maps.b), prefetch_map(&maps.out);
+        }
     }
     if (warp == 2) tensor_alloc<true>(shared_address(&tensor_base), 512);
     tensor_fence_before();

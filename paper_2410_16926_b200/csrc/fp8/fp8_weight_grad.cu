@@ -119,14 +119,16 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = PAIR ? cluster_rank() : 0;              // in the pair
     const int part = PAIR ? 0 : static_cast<int>(cluster_rank());  // of t
-    if (threadIdx.x == 0) {
-        over = 0;
-        for (int i = 0; i < kStages; ++i) barrier_init(full_dy + 8 * i, 1), barrier_init(full_x + 8 * i, 1), barrier_init(empty + 8 * i, 1);
-        for (int i = 0; i < kConverted; ++i) barrier_init(converted_full + 8 * i, 4 * kBlocks), barrier_init(converted_empty + 8 * i, 1);
-        for (int i = 0; i < 2; ++i) barrier_init(sum_full + 8 * i, 1), barrier_init(sum_empty + 8 * i, 8 * kBlocks);
-        barrier_init(drained, 1);
+    if (warp == 0) {  // a barrier a lane, in the order of their places
+        constexpr int kBars = 3 * kStages + 2 * kConverted + 5;
+        static_assert(kBars <= 32, "one lane each");
+        const int i = lane - 3 * kStages, j = i - 2 * kConverted;  // converted full and empty; sum's full and empty, two each; drained
+        if (lane < kBars) barrier_init(full_dy + 8 * lane, i >= 0 && i < kConverted ? 4 * kBlocks : (j == 2 || j == 3 ? 8 * kBlocks : 1));
         barrier_init_fence();
-        prefetch_map(&maps.dy), prefetch_map(&maps.x), prefetch_map(&maps.out);
+        if (lane == 0) {
+            over = 0;
+            prefetch_map(&maps.dy), prefetch_map(&maps.x), prefetch_map(&maps.out);
+        }
     }
     if (warp == 2) tensor_alloc<PAIR>(shared_address(&tensor_base), 2 * kSide);
     tensor_fence_before();
