@@ -193,7 +193,7 @@ __device__ __forceinline__ uint32_t quantize_block(const V& v, Codes* codes) {
 
 // ---- blocks of a matrix, one after another, to groups of eight threads: UNITS a thread, a thread block's threads side by side
 
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 128;
 struct Work {
     Division blocks;  // of a row
     uint32_t count;

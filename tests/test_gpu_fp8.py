@@ -199,6 +199,19 @@ def test_matmul_of_nan_and_of_scales_behind_the_end(rows, outer):
     assert np.array_equal(nan, want)
 
 
+@pytest.mark.parametrize("rows,outer", [(2, 256), (300, 512), (1700, 1800)])
+def test_matmul_of_a_scale_of_nan(rows, outer):
+    a = random_held(rows, 500, False, 1)
+    b = random_held(outer, 500, True, 2)
+    a.scales.view(torch.uint8)[1, 2] = 255
+    nan = torch.isnan(pvq.fp8_matmul(a, b, dtype=F32)).cpu().numpy()
+    assert nan[1].all() and not np.delete(nan, 1, axis=0).any()
+    assert torch.isnan(pvq.fp8_dequantize(a)[1, 256:384]).all() and not torch.isnan(pvq.fp8_dequantize(a)[1, :256]).any()
+    dy = normal(rows, outer, BF16, 3)
+    grad = torch.isnan(pvq.fp8_weight_grad(dy, a)).cpu().numpy()
+    assert grad[:, 256:384].all() and not grad[:, :256].any() and not grad[:, 384:].any()
+
+
 @pytest.mark.parametrize("rows", [1, 40, 300, 12300])
 def test_matmul_of_far_apart_scales(rows):
     """Blocks whose scales are at the ends of the range: products that cancel their scales, and ones that vanish."""
