@@ -12,13 +12,14 @@ int matmul(const Matrix& a, const Matrix& b, bool transposed, void* out, bool bf
     const int64_t high = p.rows <= 16 ? 16 : (p.rows <= 32 ? 32 : (p.rows <= 64 ? 64 : 128));
     const int64_t tiles = ((p.outs + 127) / 128) * ((p.rows + high - 1) / high);
     if ((p.rows + high - 1) / high > 65535) return matmul_many(p, transposed, bf16, s);
-    // k is split until the thread blocks fill the GPU, four an SM (their stages leave room for that) up to 32 rows, one from
-    // 64 on, as long as each has four blocks of 128 along it.  One row, 4096 to 14336: 12.5 us with k in four parts (448 thread
-    // blocks of three stages), 13.7 in two, 16.6 in eight; 33 rows, 14336 to 4096: 16.5 us in four (128 thread blocks of eight
-    // stages), 19.7 in two, 34 in eight.
-    const int64_t room = high <= 32 ? 4 * kSms : kSms;
+    // k is split until the thread blocks fill the GPU, two an SM up to 32 rows and one above, as long as each has four blocks of
+    // 128 along it; up to 32 rows not where one an SM is nearly enough, since blocks of their own start sooner than clusters.
+    // One row, 14336 to 4096 (32 tiles): 13.4 us with k in eight parts, 14.6 in four, 28 in one; 4096 to 14336 (112 tiles): 12.9 us
+    // in one, 13.9 in two, 16.4 in four.  33 rows, 14336 to 4096: 16.0 us in four, 19.5 in two, 30 in eight.
+    const int64_t room = high <= 32 ? 2 * kSms : kSms;
     int split = 1;
-    while (split < 8 && tiles * split * 2 <= room && blocks >= 4 * split * 2) split *= 2;
+    if (high > 32 || tiles < 104)
+        while (split < 8 && tiles * split * 2 <= room && blocks >= 4 * split * 2) split *= 2;
     if (!bf16)  // (long fp32 sums in parts, as matmul_many's)
         while (split < 8 && blocks > 64 * split) split *= 2;
     return matmul_few(p, transposed, bf16, split, s);

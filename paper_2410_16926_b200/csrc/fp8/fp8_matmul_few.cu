@@ -19,7 +19,7 @@ constexpr int kThreads = 256;
 template <int ROWS>
 struct Shape {
     static constexpr int kStageBytes = (128 + ROWS) * kBlock;
-    static constexpr int kStages = ROWS <= 32 ? 3 : (ROWS == 64 ? 8 : 6);  // four blocks an SM, then one
+    static constexpr int kStages = ROWS <= 32 ? 5 : (ROWS == 64 ? 8 : 6);  // two blocks an SM up to 32 rows, then one
     static constexpr int kWordsB = ROWS <= 32 ? 1 : ROWS / 32;             // of scales, a lane
     static constexpr int kScales = ROWS < 32 ? 32 : ROWS;                  // columns before them
     static constexpr int kScaleSets = 4;
