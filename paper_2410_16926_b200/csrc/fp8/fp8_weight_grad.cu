@@ -425,9 +425,10 @@ int launch(const Args& p, const Maps& maps, cudaStream_t s) {
 // x as bf16 in the caller's workspace.
 int64_t workspace_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
 // Converting first, or in the kernel, tokens x inputs to outputs: 512 x 4096 to 4096 24.5 and 26.1 us, 1024 x 4096 to 14336 107 and 134,
-// 4096 x 4096 to 1024 34.0 and 37.3; but 256 x 4096 to 4096 19.9 and 19.9, 4096 x 8192 to 512 44.4 and 39.0.
+// 4096 x 4096 to 1024 34.0 and 37.3; 2048 x 4096 to 1024 21.1 and 22.8; but
+// 1001 x 4096 to 1024 14.6 and 13.4 (with the second launch), 4096 x 8192 to 512 44.4 and 39.0.
 bool worth_a_workspace(int64_t rows, int64_t inner, int64_t outer) {
-    return outer >= 1024 && ((outer + 255) / 256) * ((inner + 255) / 256) >= 48 && rows >= 512;
+    return outer >= 1024 && ((outer + 255) / 256) * ((inner + 255) / 256) >= 48 && static_cast<double>(rows) * inner * outer >= 8.0e9;
 }
 
 // Parts of t for as many tiles of 128 x 128, so that they fill the GPU and each part is a run at least.

@@ -238,7 +238,7 @@ def check_weight_grad(dy, x, dtype, out=None):
                                                    (65, 256, 264, True), (1000, 513, 257, False), (1001, 1024, 520, True), (2500, 300, 1000, False),
                                                    (4096, 128, 64, False), (129, 2048, 1024, False),
                                                    (1500, 1500, 2100, False), (700, 2600, 2060, True), (3000, 250, 130, False),
-                                                   (2049, 2300, 2000, False), (1100, 2500, 2100, False), (1000, 2500, 2100, False)])
+                                                   (2049, 2300, 2000, False), (1100, 2500, 2100, False), (1700, 2500, 2100, True)])
 def test_weight_grad(rows, inner, outer, tile, dtype):
     dy = normal(rows, outer, BF16, rows, pad=16)
     x = random_held(rows, inner, tile, rows + 1, pad=16)
@@ -247,7 +247,7 @@ def test_weight_grad(rows, inner, outer, tile, dtype):
     check()
 
 
-@pytest.mark.parametrize("rows,inner,outer", [(1100, 2500, 2100), (1500, 1504, 2104)])
+@pytest.mark.parametrize("rows,inner,outer", [(1700, 2500, 2100), (2800, 1504, 2104)])
 def test_weight_grad_without_a_workspace(rows, inner, outer):
     """The C call takes NULL: the same bits."""
     import ctypes as C
