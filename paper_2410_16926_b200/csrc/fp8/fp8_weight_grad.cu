@@ -455,10 +455,13 @@ int weight_grad_of(Args p, const void* dy, int64_t ld_dy, void* workspace, cudaS
         p.split = parts(tiles, stages);
         return launch<false, false, T>(p, maps, s);
     }
-    // The last round of tiles, where it is a small one, is shared by all SMs: in quarters, with t in parts.  (14336 x 4096 are
-    // twelve rounds of 74 tiles and 8 tiles.)
-    const int last = static_cast<int>(pairs % (kSms / 2)), split = parts(4 * last, stages);
-    const bool shared = pairs > last && last > 0 && split > 1;
+    // The last round of tiles, where it is a small one, is shared by all SMs, in quarters and with t in parts, where a round is
+    // long or one of two: 16384 values of t, 896 tiles (8 in the last round) 1446 us instead of 1500, 80 tiles 171 instead of 192, 4096
+    // values and 80 tiles 50 instead of 54; but 4096 values and 448 tiles (4 in the last) 211 instead of 198: the launch behind
+    // the others, while a few tiles alone run at a higher clock.
+    constexpr int kPairs = kSms / 2;
+    const int last = static_cast<int>(pairs % kPairs), split = parts(4 * last, stages);
+    const bool shared = pairs > last && last > 0 && split > 1 && (stages >= 128 || pairs < 2 * kPairs);
     p.tiles = static_cast<int>(shared ? pairs - last : pairs);
     if (workspace) {
         const int64_t ld = workspace_ld(p.x.cols);
