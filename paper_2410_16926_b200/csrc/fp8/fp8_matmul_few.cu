@@ -6,8 +6,12 @@
 // then every block adds the parts of its share of the columns, in the order of the ranks (no atomics: the same bits every
 // time), reading the others' shared memory.
 //
-// Warps: one issues the copies, one the products, one allocates tensor memory, four bring the scales there (four
-// blocks along k at a time, in four sets of columns) and then read the result.
+// Warps: one issues the copies, one the products, one allocates tensor memory, four bring the scales there (four blocks along k
+// at a time, in four sets of columns) and then read the result.
+//
+// What bounds it: memory, behind a start and an end.  One row, 4096 to 14336: 12.9 us, of which the weight's 58.7 MB take 9.1 at
+// the copy rate; the first tile arrives after 2 to 3 us, the parts are added and stored in the last 1.5.  33 rows, 14336 to 4096:
+// 15.8 us, 64 rows 4096 to 14336 14.4, 128 rows 16.7.
 #include "fp8_matmul.cuh"
 
 namespace pvq {

