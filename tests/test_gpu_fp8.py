@@ -119,6 +119,22 @@ def test_dequantize(rows, cols, pad, dtype, tile):
     assert torch.equal(pvq.fp8_dequantize(q, dtype=dtype), out)
 
 
+def test_new_matrices_are_ordinary_tensors():
+    """Codes and scales that share an allocation: shapes, strides, copies, views, and each outliving the other."""
+    x = normal(130, 250, BF16, 3)
+    q = pvq.fp8_quantize(x)
+    assert q.codes.shape == (130, 250) and q.codes.stride() == (256, 1) and q.scales.shape == (130, 2) and q.scales.stride() == (4, 1)
+    assert q.codes.dtype == torch.float8_e4m3fn and q.scales.dtype == torch.float8_e8m0fnu and q.codes.device == x.device
+    want = ref.values(q)
+    codes, scales = q.codes.clone(), q.scales.clone()
+    assert np.array_equal(ref.to64(codes.float()) * ref.spread(ref.to64(scales.float()), 130, 250, False), want)
+    kept = q.scales
+    del q, codes
+    assert torch.equal(kept.view(torch.uint8), scales.view(torch.uint8)) and not kept.requires_grad
+    out = pvq.fp8_dequantize(pvq.fp8_quantize(x))
+    assert out.shape == (130, 250) and out.stride() == (256, 1) and torch.equal(out.contiguous(), out)
+
+
 def test_dequantize_of_every_code_and_scale():
     codes = torch.arange(256, dtype=torch.int32).to(torch.uint8).repeat(256, 1).cuda()
     scales = torch.arange(256, dtype=torch.int32).to(torch.uint8)[:, None].repeat(1, 4).cuda()[:, :2]
