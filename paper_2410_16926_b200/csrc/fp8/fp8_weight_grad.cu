@@ -113,6 +113,7 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
     constexpr int kSide = PAIR ? 256 : 128;   // of a tile
     constexpr int kHeld = kSide / 2;          // columns of the sum a warp holds
     constexpr uint32_t kBlocks = PAIR ? 2 : 1;
+    static_assert(8 * (kHeld * sizeof(T) / 128 - 1) * kStoreBytes <= kStages * kStageBytes, "the last tile is stored from the stages' place");
     extern __shared__ uint8_t raw[];
     const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
     const uint32_t converted = base + kStages * kStageBytes, stores = converted + kConverted * kConvertedBytes, bars = stores + 8 * kStoreBytes;
@@ -344,17 +345,24 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
                     }
                     continue;
                 }
-                if (lane == 0) store_wait_read<0>();
-                __syncwarp();
+                // behind the last tile the stages are free: a place of its own for each stored tile (one after another through
+                // one place they took 1.6 us)
+                uint32_t at = buffer_at;
+                if (c > 0 && t + step >= tiles) {
+                    at = base + ((warp - kFirstHolder) * (kHeld / kColumns - 1) + c - 1) * kStoreBytes;
+                } else {
+                    if (lane == 0) store_wait_read<0>();
+                    __syncwarp();
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffer_at + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(w[4 * j]),
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(w[4 * j]),
                                  "r"(w[4 * j + 1]), "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
                                  : "memory");
                 async_fence();
                 __syncwarp();
                 if (lane == 0) {
-                    if (row < p.outer && col < p.x.cols) store_tile(&maps.out, static_cast<int>(col), static_cast<int>(row), buffer_at);
+                    if (row < p.outer && col < p.x.cols) store_tile(&maps.out, static_cast<int>(col), static_cast<int>(row), at);
                     store_commit();
                 }
             }
