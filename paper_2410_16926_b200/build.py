@@ -6,7 +6,8 @@ _bind.so, the native part of the Python binding (csrc/bind/pvq_bind.cpp).
 
 --debug builds libpvq_b200_debug.so instead: the bounds-checked variant (-DPVQ_DEBUG, see
 pvq_debug_status in include/pvq.h) of the kernels that keep their tables in shared memory;
-the global-table kernels are left out of it (calls that need them return "unsupported").  The binding is the same.
+the global-table kernels are left out of it (calls that need them return "unsupported"), those of the
+8-bit operators are in it unchanged.  The binding is the same.
 """
 import os
 import subprocess
