@@ -509,3 +509,119 @@ def test_weight_grad_of_every_code_at_the_ends_of_the_scales(rows, inner, outer)
     dy[where, np.arange(outer)] = np.where(np.arange(outer) % 2 == 0, 1.0, -2.0)
     got = ref.to64(pvq.fp8_weight_grad(torch.from_numpy(dy).to(BF16).cuda(), x))
     assert np.array_equal(got, ref.values(x)[where] * np.where(np.arange(outer) % 2 == 0, 1.0, -2.0)[:, None])
+
+
+def test_offsets_beyond_32_bits():
+    """70000 x 32768 values: rows whose offsets pass 2^31, in every operator that takes such a matrix."""
+    rows, cols, outs = 70000, 32768, 136
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn((rows, cols), generator=g, device="cuda", dtype=BF16)
+    some = torch.tensor([0, 1, 65535, 65536, 65537, rows - 2, rows - 1], device="cuda")
+
+    def part(q):  # those rows
+        return pvq.Fp8Matrix(q.codes.view(torch.uint8)[some].view(torch.float8_e4m3fn), q.scales.view(torch.uint8)[some].view(torch.float8_e8m0fnu), False)
+
+    q = pvq.fp8_quantize(x)
+    same(part(q), ref.to64(x[some]), False)
+    v = pvq.fp8_dequantize(q)
+    values = ref.values(part(q))
+    assert np.array_equal(ref.to64(v[some]), values)
+    h, gate8, up8 = pvq.fp8_gated(x, v, checkpoint=True)
+    check_h(part(h), ref.to64(x[some]), ref.to64(v[some]), "silu")
+    same(part(gate8), ref.to64(x[some]), False)
+    same(part(up8), values, False)
+    dgate, dup = pvq.fp8_gated_backward(x, h, gate8, out=(v, torch.empty_like(v)))
+    want = pvq.fp8_gated_backward(x[some], part(h), part(gate8))
+    assert torch.equal(dgate[some], want[0]) and torch.equal(dup[some], want[1])
+    del h, gate8, up8, v, dgate, dup
+    w = random_held(outs, cols, True, 7, scale=0.02)
+    got = pvq.fp8_matmul(q, w, dtype=F32)
+    exact = values @ ref.values(w).T
+    assert np.all(np.abs(ref.to64(got[some]) - exact) <= 1.01 * ref.matmul_slack(values, ref.values(w).T, cols / 32))
+    dy = torch.randn((rows, outs), generator=g, device="cuda", dtype=BF16)
+    grad = pvq.fp8_weight_grad(dy, q)[:, cols - 128:]
+    exponents = q.scales.view(torch.uint8)[:, cols // 128 - 1:].double() - 127
+    exact = dy.double().t() @ (q.codes[:, cols - 128:].float().double() * torch.exp2(exponents))
+    # 70000 / 16 steps in runs of 512: within 1e-6 of the norm, as by the sums' parts
+    assert float((grad.double() - exact).norm()) <= 1e-6 * float(exact.norm())
+
+
+@pytest.mark.parametrize("rows,inner,outer", [(1, 128, 200000), (2, 200000, 130), (100000, 40, 24)])
+def test_matmul_of_long_sides(rows, inner, outer):
+    a, b = random_held(rows, inner, False, 1), random_held(outer, inner, True, 2, scale=0.1)
+    got = pvq.fp8_matmul(a, b, dtype=F32).double()
+    va, vb = (pvq.fp8_dequantize(q, dtype=F32).double() for q in (a, b))
+    want = va @ vb.t()
+    # 1563 blocks of 128 in eight parts: 25000 values, 8e-8 of a sum for every 1024
+    assert float((got - want).norm()) <= 3e-6 * float(want.norm())
+
+
+@pytest.mark.parametrize("rows,inner,outer", [(70000, 130, 70), (300, 20000, 8), (300, 8, 20000)])
+def test_weight_grad_of_long_sides(rows, inner, outer):
+    dy, x = normal(rows, outer, BF16, 1), random_held(rows, inner, False, 2)
+    got = pvq.fp8_weight_grad(dy, x).double()
+    want = dy.double().t() @ pvq.fp8_dequantize(x, dtype=F32).double()
+    assert float((got - want).norm()) <= 1e-6 * float(want.norm())
+
+
+def test_rows_of_a_larger_matrix():
+    """Views of some rows: other base addresses, the same values."""
+    q, w = random_held(400, 500, False, 1), random_held(640, 500, True, 2)
+    whole = pvq.fp8_matmul(q, w)
+    some = pvq.Fp8Matrix(q.codes[37:301], q.scales[37:301], False)
+    assert torch.equal(pvq.fp8_dequantize(some), pvq.fp8_dequantize(q)[37:301])
+    assert torch.allclose(pvq.fp8_matmul(some, w).float(), whole[37:301].float(), rtol=2.0 ** -7, atol=1e-3)
+    lower = pvq.Fp8Matrix(w.codes[128:], w.scales[1:], True)
+    assert torch.allclose(pvq.fp8_matmul(q, lower).float(), whole[:, 128:].float(), rtol=2.0 ** -7, atol=1e-3)
+    with pytest.raises(pvq.PvqError):  # scales that do not begin on a 4-byte boundary
+        pvq.fp8_dequantize(pvq.Fp8Matrix(q.codes[:, 128:], q.scales[:, 1:], False))
+
+
+def test_a_matrix_with_itself():
+    q = random_held(300, 400, False, 1)
+    got = pvq.fp8_matmul(q, q, dtype=F32)
+    v = ref.values(q)
+    assert np.all(np.abs(ref.to64(got) - v @ v.T) <= 2.0 ** -24 * np.abs(v @ v.T) + 1.01 * ref.matmul_slack(v, v.T, 400 / 32))
+    h = pvq.fp8_gated(normal(5, 256, BF16, 1), normal(5, 256, BF16, 1))
+    x = normal(5, 256, BF16, 1)
+    one = pvq.fp8_gated(x, x)
+    assert torch.equal(h.codes.view(torch.uint8), one.codes.view(torch.uint8))
+
+
+def test_two_streams_at_once_and_graphs_with_workspaces():
+    """Calls of every kernel on two streams, and two graphs replayed together, give what they give alone."""
+    def calls(seed):
+        x, dy = normal(2800, 1504, BF16, seed), normal(2800, 2104, BF16, seed + 1)
+        w = pvq.fp8_quantize(normal(2104, 1504, BF16, seed + 2, scale=0.05), tile=True)
+        few = normal(20, 1504, BF16, seed + 3)
+
+        def run():
+            q = pvq.fp8_quantize(x)
+            y = pvq.fp8_matmul(q, w)
+            return [y, pvq.fp8_matmul(pvq.fp8_quantize(few), w), pvq.fp8_matmul(pvq.fp8_quantize(y), w, transposed=True, dtype=F32),
+                    pvq.fp8_weight_grad(dy, q), pvq.fp8_weight_grad(dy[:500], pvq.Fp8Matrix(q.codes[:500], q.scales[:500], False))]
+        return run
+    runs = [calls(10), calls(20)]
+    want = [run() for run in runs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [None, None]
+    for _ in range(3):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                got[i] = runs[i]()
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(a, b) for a, b in zip(got[i], want[i]))
+    graphs, outs = [], []
+    for i in (0, 1):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            outs.append(runs[i]())
+    for _ in range(3):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i]))
