@@ -15,7 +15,7 @@ int matmul(const Matrix& a, const Matrix& b, bool transposed, void* out, bool bf
     // k is split until the thread blocks fill the GPU, two an SM up to 32 rows and one above, as long as each has four blocks of
     // 128 along it; up to 32 rows not where one an SM is nearly enough, since blocks of their own start sooner than clusters.
     // One row, 14336 to 4096 (32 tiles): 13.4 us with k in eight parts, 14.6 in four, 28 in one; 4096 to 14336 (112 tiles): 12.9 us
-    // in one, 13.9 in two, 16.4 in four.  33 rows, 14336 to 4096: 16.0 us in four, 19.5 in two, 30 in eight.
+    // in one, 13.9 in two, 16.4 in four.  33 rows, 14336 to 4096: 14.9 us in four, 19 in two, 30 in eight.
     const int64_t room = high <= 32 ? 2 * kSms : kSms;
     int split = 1;
     if (high > 32 || tiles < 104)

@@ -2,16 +2,17 @@
 //
 // The operands change places: 128 columns of the result (rows of b, the weight) are the product's 128 lanes, ROWS rows of a
 // (16 to 128) its columns, so that a token costs 1/16 of a tile's width and not 1/128 of its height.  k is split over the
-// blocks of a cluster where there are few tiles: each sums its part in tensor memory, puts it into its shared memory, and
-// then every block adds the parts of its share of the columns, in the order of the ranks (no atomics: the same bits every
-// time), reading the others' shared memory.
+// blocks of a cluster where there are few tiles: each sums its part in tensor memory and puts it into the shared memory of the
+// blocks that its columns fall to, each of which adds the parts of its share of the columns in the order of the ranks (no
+// atomics: the same bits every time).
 //
 // Warps: one issues the copies, one the products, one allocates tensor memory, four bring the scales there (four blocks along k
 // at a time, in four sets of columns) and then read the result.
 //
 // What bounds it: memory, behind a start and an end.  One row, 4096 to 14336: 12.9 us, of which the weight's 58.7 MB take 9.1 at
-// the copy rate; the first tile arrives after 2 to 3 us, the parts are added and stored in the last 1.5.  33 rows, 14336 to 4096:
-// 15.8 us, 64 rows 4096 to 14336 14.4, 128 rows 16.7.
+// the copy rate, which it runs at once the first tiles are there (after 2 to 4 us); the parts are added and stored in the last 1.5.
+// 33 rows, 14336 to 4096: 14.9 us (16.0 when each block read the others' shared memory, which needs a second meeting of the
+// cluster), 64 rows 4096 to 14336 14.4, 128 rows 16.7.
 #include "fp8_matmul.cuh"
 
 namespace pvq {
@@ -20,17 +21,23 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <int ROWS>
+template <int ROWS, int SPLIT>
 struct Shape {
     static constexpr int kStageBytes = (128 + ROWS) * kBlock;
-    static constexpr int kStages = ROWS <= 32 ? 5 : (ROWS == 64 ? 8 : 6);  // two blocks an SM up to 32 rows, then one
+    // two blocks an SM up to 32 rows, then one
+    static constexpr int kStages = ROWS == 16 || (ROWS == 32 && SPLIT == 1) ? 5 : (ROWS == 32 ? 4 : (ROWS == 64 ? 8 : (SPLIT == 1 ? 6 : 5)));
+    // The parts of a block's share of the columns: in the stages' place where they are the block's own, otherwise in one of
+    // their own, since the others' arrive while it still loads.
+    static constexpr int kPartsAt = SPLIT == 1 ? 0 : kStages * kStageBytes, kPartsBytes = ROWS * 512;
+    static constexpr int kBarsAt = kStages * kStageBytes + (SPLIT == 1 ? 0 : kPartsBytes);
     static constexpr int kWordsB = ROWS <= 32 ? 1 : ROWS / 32;             // of scales, a lane
     static constexpr int kScales = ROWS < 32 ? 32 : ROWS;                  // columns before them
     static constexpr int kScaleSets = 4;
     static constexpr int kColumns = ROWS == 128 ? 256 : (ROWS == 64 ? 128 : 64);  // of tensor memory, a power of two
-    static constexpr size_t kShared = 1024 + kStages * kStageBytes + 256;
-    static_assert(kStages * kStageBytes >= ROWS * 512, "the result takes the stages' place");
+    static constexpr size_t kShared = 1024 + kBarsAt + 256;
+    static_assert(kStages * kStageBytes >= kPartsBytes, "the result takes the stages' place");
     static_assert(kScales + 8 * kScaleSets <= kColumns, "tensor memory");
+    static_assert(kShared <= 232448 - 64, "shared memory");
 };
 
 struct Maps {
@@ -38,32 +45,25 @@ struct Maps {
 };
 
 // Adds the parts of this block's share of the columns, 128 / SPLIT, in the order of the ranks, and stores them: four columns a
-// thread, eight reads at a time (one after another they took 250 cycles each).
-template <int SPLIT, class T>
-__device__ __forceinline__ void add_parts(uint32_t base, int rank, const MatmulArgs& p, int64_t row0, int64_t col0, T* out, int most) {
-    constexpr int kAcross = 32 / SPLIT, kStep = kThreads / kAcross, kAtOnce = 8 / SPLIT;
-    const int col = rank * (128 / SPLIT) + threadIdx.x % kAcross * 4;
-    const int rows = static_cast<int>(min(int64_t(most), p.rows - row0));
-    const int64_t left = p.outs - col0 - col;
+// thread, eight reads at a time.  parts: [rank][row][column of the share].
+template <int ROWS, int SPLIT, class T>
+__device__ __forceinline__ void add_parts(uint32_t parts, int rank, const MatmulArgs& p, int64_t row0, int64_t col0) {
+    constexpr int kShare = 128 / SPLIT, kAcross = kShare / 4, kStep = kThreads / kAcross, kAtOnce = 8 / SPLIT;
+    const int within = threadIdx.x % kAcross * 4;
+    const int64_t col = col0 + rank * kShare + within, left = p.outs - col;
+    const int rows = static_cast<int>(min(int64_t(ROWS), p.rows - row0));
     if (left <= 0) return;
-    out += row0 * p.ld + col0 + col;
+    T* out = static_cast<T*>(p.out) + row0 * p.ld + col;
     for (int r0 = threadIdx.x / kAcross; r0 < rows; r0 += kStep * kAtOnce) {
         float4 part[kAtOnce][SPLIT];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i)
 #pragma unroll
             for (int s = 0; s < SPLIT; ++s)
-                if (r0 + i * kStep < rows) {
-                    const uint32_t at = base + (r0 + i * kStep) * 512 + col * 4;
-                    if (SPLIT == 1)
-                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                                     : "=f"(part[i][s].x), "=f"(part[i][s].y), "=f"(part[i][s].z), "=f"(part[i][s].w)
-                                     : "r"(at));
-                    else
-                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                                     : "=f"(part[i][s].x), "=f"(part[i][s].y), "=f"(part[i][s].z), "=f"(part[i][s].w)
-                                     : "r"(address_in(at, s)));
-                }
+                if (r0 + i * kStep < rows)
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(part[i][s].x), "=f"(part[i][s].y), "=f"(part[i][s].z), "=f"(part[i][s].w)
+                                 : "r"(parts + ((s * ROWS + r0 + i * kStep) * kShare + within) * 4));
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
             if (r0 + i * kStep >= rows) break;
@@ -85,15 +85,16 @@ __device__ __forceinline__ void add_parts(uint32_t base, int rank, const MatmulA
 
 template <int ROWS, int SPLIT, bool ACROSS, class T>
 __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_constant__ Maps maps, const __grid_constant__ MatmulArgs p) {
-    using S = Shape<ROWS>;
+    using S = Shape<ROWS, SPLIT>;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
-    const uint32_t full = base + S::kStages * S::kStageBytes, empty = full + 8 * S::kStages, scales_full = empty + 8 * S::kStages,
+    const uint32_t parts = base + S::kPartsAt, full = base + S::kBarsAt, empty = full + 8 * S::kStages, scales_full = empty + 8 * S::kStages,
                    scales_empty = scales_full + 8 * S::kScaleSets, sum_full = scales_empty + 8 * S::kScaleSets;
     __shared__ uint32_t tensor_base;
     __shared__ int over;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % SPLIT;  // in the cluster
+    if (SPLIT > 1) cluster_arrive();      // (every block runs before another writes to its shared memory)
     const int64_t col0 = int64_t(blockIdx.x / SPLIT) * 128, row0 = int64_t(blockIdx.y) * ROWS;
     const int blocks = static_cast<int>((p.inner + kBlock - 1) / kBlock);
     const int first = static_cast<int>(int64_t(blocks) * rank / SPLIT), last = static_cast<int>(int64_t(blocks) * (rank + 1) / SPLIT);  // (SPLIT <= blocks)
@@ -170,19 +171,21 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
             const uint64_t w0 = operand(base, ACROSS ? 128 * kBlock : 16), x0 = operand(base + 128 * kBlock);
             Turn<S::kStages> turn;
             Turn<S::kScaleSets> scales;
-            bool ok = true;
+            bool ok = true, there = false;
             for (int kb = first; kb < last; ++kb) {
                 const uint32_t part = kb & 3;
                 if (part == 0 || kb == first) ok = barrier_wait(scales_full + 8 * scales.at, scales.parity, bounds);
-                ok = ok && barrier_wait(full + 8 * turn.at, turn.parity, bounds);
+                ok = ok && (there || barrier_wait(full + 8 * turn.at, turn.parity, bounds));
                 if (!ok) break;
+                const Turn<S::kStages> now = turn;
+                turn.next();
+                there = kb + 1 < last && barrier_over(full + 8 * turn.at, turn.parity);
                 tensor_fence_after();
-                const uint64_t w = w0 + turn.at * (S::kStageBytes >> 4), x = x0 + turn.at * (S::kStageBytes >> 4);
+                const uint64_t w = w0 + now.at * (S::kStageBytes >> 4), x = x0 + now.at * (S::kStageBytes >> 4);
                 const uint32_t sw = tensor + S::kScales + 8 * scales.at, with = with_part(product, part);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) multiply_e4m3<false>(tensor, w + kAlongW * k, x + 2 * k, with, sw, sw + 4, kb > first || k > 0);
-                products_done<false>(empty + 8 * turn.at);
-                turn.next();
+                products_done<false>(empty + 8 * now.at);
                 if (part == 3) {
                     products_done<false>(scales_empty + 8 * scales.at);
                     scales.next();
@@ -215,27 +218,36 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
         }
         ok = ok && warp_wait(sum_full, 0, bounds);
         ok = ok && !over;
-        if (__all_sync(0xffffffffu, ok)) {  // the part of the sum, in shared memory: [row][128]
+        ok = __all_sync(0xffffffffu, ok);
+        if (SPLIT > 1) cluster_wait();
+        if (ok) {  // a lane's column of the part goes to the block whose share it is in
             tensor_fence_after();
-            const uint32_t to = base + ((warp & 3) * 32 + lane) * 4;
+            constexpr int kShare = 128 / SPLIT;
+            const int column = (warp & 3) * 32 + lane;
+            const uint32_t mine_at = parts + (rank * ROWS * kShare + column % kShare) * 4;
+            const uint32_t to = SPLIT > 1 ? address_in(mine_at, column / kShare) : mine_at;
+            const int rows = static_cast<int>(min(int64_t(ROWS), p.rows - row0));
 #pragma unroll
             for (int c = 0; c < ROWS; c += 16) {
-                if (row0 + c >= p.rows) break;
+                if (c >= rows) break;
                 float v[16];
                 tensor_load(mine + c, v);
                 tensor_wait_loads();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + (c + i) * 512), "f"(v[i]) : "memory");
+                for (int i = 0; i < 16; ++i)
+                    if (c + i < rows) {
+                        if (SPLIT > 1) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + (c + i) * kShare * 4), "f"(v[i]) : "memory");
+                        else asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + (c + i) * kShare * 4), "f"(v[i]) : "memory");
+                    }
             }
         }
         tensor_fence_before();
     }
     __syncwarp();
+    if (SPLIT > 1 && warp < 4) cluster_wait();
     if (SPLIT > 1) cluster_barrier();
     else __syncthreads();
-    add_parts<SPLIT>(base, rank, p, row0, col0, static_cast<T*>(p.out), ROWS);
-    __syncwarp();
-    if (SPLIT > 1) cluster_barrier();  // the others have read this block's part
+    add_parts<ROWS, SPLIT, T>(parts, rank, p, row0, col0);
     if (warp == 2) {
         tensor_fence_after();
         tensor_free<false>(tensor, S::kColumns);
@@ -248,10 +260,10 @@ int launch(const MatmulArgs& p, cudaStream_t s) {
     int st = tile_map(&maps.a, p.a.codes, Element::kByte, p.a.rows, p.a.cols, p.a.ld_codes, kBlock, ROWS);
     if (st == PVQ_OK) st = tile_map(&maps.b, p.b.codes, Element::kByte, p.b.rows, p.b.cols, p.b.ld_codes, kBlock, 128);
     void (*const kernel)(Maps, MatmulArgs) = matmul_few_kernel<ROWS, SPLIT, ACROSS, T>;
-    if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), Shape<ROWS>::kShared);
+    if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), Shape<ROWS, SPLIT>::kShared);
     if (st != PVQ_OK) return st;
     const dim3 grid(static_cast<unsigned>((p.outs + 127) / 128 * SPLIT), static_cast<unsigned>((p.rows + ROWS - 1) / ROWS));
-    return launch_early(kernel, grid, kThreads, Shape<ROWS>::kShared, SPLIT, s, maps, p);
+    return launch_early(kernel, grid, kThreads, Shape<ROWS, SPLIT>::kShared, SPLIT, s, maps, p);
 }
 
 template <int ROWS, int SPLIT>

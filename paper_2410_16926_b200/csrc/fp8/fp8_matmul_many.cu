@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
             Turn<2> scales;
             Turn<2> sums;           // the two places of the result
             uint32_t shared = 1;    // the parity of the columns that they share
-            bool ok = true;
+            bool ok = true, there = false;
             for (int t = first; t < tiles.count() && ok; t += step) {
                 int left = 0;  // of the part
                 for (int kb = 0; kb < blocks; ++kb, --left) {
@@ -135,16 +135,18 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
                         left = part_blocks;
                     }
                     if (part == 0) ok = ok && barrier_wait(scales_full + 8 * scales.at, scales.parity, bounds);
-                    ok = ok && barrier_wait(full + 8 * turn.at, turn.parity, bounds);
+                    ok = ok && (there || barrier_wait(full + 8 * turn.at, turn.parity, bounds));
                     if (!ok) break;
+                    const uint32_t now = turn.at;
+                    turn.next();
+                    there = barrier_over(full + 8 * turn.at, turn.parity);
                     tensor_fence_after();
-                    const uint64_t a = a0 + turn.at * (kStageBytes >> 4), b = b0 + turn.at * (kStageBytes >> 4);
+                    const uint64_t a = a0 + now * (kStageBytes >> 4), b = b0 + now * (kStageBytes >> 4);
                     const uint32_t sum = tensor + kSecond * sums.at, sa = tensor + kScalesA + 4 * scales.at, sb = tensor + kScalesB + 8 * scales.at,
                                    with = with_part(product, part);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) multiply_e4m3<true>(sum, a + 2 * k, b + kAlongB * k, with, sa, sb, !starts || k > 0);
-                    products_done<true>(empty + 8 * turn.at);
-                    turn.next();
+                    products_done<true>(empty + 8 * now);
                     if (part == 3 || kb == blocks - 1) {
                         products_done<true>(scales_empty + 8 * scales.at);
                         scales.next();

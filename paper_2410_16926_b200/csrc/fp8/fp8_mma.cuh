@@ -64,6 +64,22 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, cons
     return false;
 }
 
+// Whether the phase is over, without waiting.  (The thread that issues the products asks this of the next stage before it issues
+// this one's: an answer takes 150 to 200 cycles, also where it is yes.  1999 x 4096 by 4096 31.4 us without, 29.7 with.)
+__device__ __forceinline__ bool barrier_over(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t"
+        "}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done;
+}
+
 // The same for a whole warp, which has time: it sleeps between its polls (8 or 12 warps that poll without a pause cost the weight
 // gradient 6%).
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const Bounds& b) {
@@ -105,6 +121,10 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
+
+// Its two halves; the first may be long before the second.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 // ---- copies of tiles
 
