@@ -68,5 +68,34 @@ int registers_of(const void* kernel, int* registers) {
     return PVQ_OK;
 }
 
+int clusters_of(const void* kernel, unsigned threads, size_t shared, unsigned size, int* clusters) {
+    static std::mutex mu;
+    static std::map<std::pair<const void*, int>, int> memo;  // (threads and shared memory are a kernel's own)
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return set_cuda_error(e);
+    std::lock_guard<std::mutex> lock(mu);
+    int& known = memo[{kernel, dev * 16 + static_cast<int>(size)}];
+    if (known == 0) {
+        cudaLaunchConfig_t config = {};
+        config.gridDim = dim3(size);
+        config.blockDim = dim3(threads);
+        config.dynamicSmemBytes = shared;
+        cudaLaunchAttribute cluster;
+        cluster.id = cudaLaunchAttributeClusterDimension;
+        cluster.val.clusterDim.x = size, cluster.val.clusterDim.y = 1, cluster.val.clusterDim.z = 1;
+        config.attrs = &cluster;
+        config.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&known, kernel, &config);
+        if (e != cudaSuccess) {
+            known = 0;
+            return set_cuda_error(e);
+        }
+        if (known < 1) known = 1;
+    }
+    *clusters = known;
+    return PVQ_OK;
+}
+
 }  // namespace fp8
 }  // namespace pvq

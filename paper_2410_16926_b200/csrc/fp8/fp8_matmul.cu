@@ -12,14 +12,21 @@ int matmul(const Matrix& a, const Matrix& b, bool transposed, void* out, bool bf
     const int64_t high = p.rows <= 16 ? 16 : (p.rows <= 32 ? 32 : (p.rows <= 64 ? 64 : 128));
     const int64_t tiles = ((p.outs + 127) / 128) * ((p.rows + high - 1) / high);
     if ((p.rows + high - 1) / high > 65535) return matmul_many(p, transposed, bf16, s);
-    // k is split until the thread blocks fill the GPU, two an SM up to 32 rows and one above, as long as each has four blocks of
-    // 128 along it; up to 32 rows not where one an SM is nearly enough, since blocks of their own start sooner than clusters.
-    // One row, 14336 to 4096 (32 tiles): 13.4 us with k in eight parts, 14.6 in four, 28 in one; 4096 to 14336 (112 tiles): 12.9 us
-    // in one, 13.9 in two, 16.4 in four.  33 rows, 14336 to 4096: 14.9 us in four, 19 in two, 30 in eight.
-    const int64_t room = high <= 32 ? 2 * kSms : kSms;
+    // k is split over clusters as long as they all run at once, with one thread block an SM, or two up to 32 rows (more than that
+    // only for long parts), and each part has four blocks of 128; up to 32 rows not where the tiles alone nearly fill the SMs,
+    // since blocks of their own start sooner than clusters.  One row, 4096 to 4096 (32 tiles): 4.8 us with k in four parts, 5.2
+    // in eight, 8.7 in one; 14336 to 4096: 12.8 us in eight, 13.5 in four; 4096 to 14336 (112 tiles): 12.9 us in one, 13.9 in two.
+    // 33 rows, 14336 to 4096: 14.9 us in four, 19 in two; to 4480 (35 tiles, 33 clusters of four at once): 17.7 in two, 25 in four.
     int split = 1;
     if (high > 32 || tiles < 104)
-        while (split < 8 && tiles * split * 2 <= room && blocks >= 4 * split * 2) split *= 2;
+        for (int next = 2; next <= 8 && blocks >= 4 * next; next *= 2) {
+            int clusters = 0;
+            const int st = matmul_few_clusters(static_cast<int>(high), next, &clusters);
+            if (st != PVQ_OK) return st;
+            const bool second = high <= 32 && (tiles <= 2 * clusters || (tiles * next <= 2 * kSms && blocks >= 12 * next));
+            if (tiles > clusters && !second) break;
+            split = next;
+        }
     if (!bf16)  // (long fp32 sums in parts, as matmul_many's)
         while (split < 8 && blocks > 64 * split) split *= 2;
     return matmul_few(p, transposed, bf16, split, s);

@@ -13,6 +13,8 @@
 // the copy rate, which it runs at once the first tiles are there (after 2 to 4 us); the parts are added and stored in the last 1.5.
 // 33 rows, 14336 to 4096: 14.9 us (16.0 when each block read the others' shared memory, which needs a second meeting of the
 // cluster), 64 rows 4096 to 14336 14.4, 128 rows 16.7.
+#include <atomic>
+
 #include "fp8_matmul.cuh"
 
 namespace pvq {
@@ -279,7 +281,31 @@ int launch_rows(const MatmulArgs& p, bool transposed, bool bf16, int split, cuda
     return launch_split<ROWS, 8>(p, transposed, bf16, s);
 }
 
+template <int ROWS, int SPLIT>
+int clusters(int* n) {
+    static std::atomic<int> known[16];  // of the first devices; every call of few rows asks for it
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return set_cuda_error(e);
+    if (dev < 16 && (*n = known[dev].load(std::memory_order_relaxed)) > 0) return PVQ_OK;
+    const void* kernel = reinterpret_cast<const void*>(matmul_few_kernel<ROWS, SPLIT, false, __nv_bfloat16>);  // (the others take the same)
+    int st = allow_shared(kernel, Shape<ROWS, SPLIT>::kShared);
+    if (st == PVQ_OK) st = clusters_of(kernel, kThreads, Shape<ROWS, SPLIT>::kShared, SPLIT, n);
+    if (st == PVQ_OK && dev < 16) known[dev].store(*n, std::memory_order_relaxed);
+    return st;
+}
+template <int ROWS>
+int clusters_split(int split, int* n) {
+    return split == 2 ? clusters<ROWS, 2>(n) : (split == 4 ? clusters<ROWS, 4>(n) : clusters<ROWS, 8>(n));
+}
+
 }  // namespace
+
+int matmul_few_clusters(int high, int split, int* n) {
+    if (high == 16) return clusters_split<16>(split, n);
+    if (high == 32) return clusters_split<32>(split, n);
+    return high == 64 ? clusters_split<64>(split, n) : clusters_split<128>(split, n);
+}
 
 int matmul_few(const MatmulArgs& p, bool transposed, bool bf16, int split, cudaStream_t s) {
     if (p.rows <= 16) return launch_rows<16>(p, transposed, bf16, split, s);

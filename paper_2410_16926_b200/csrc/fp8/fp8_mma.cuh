@@ -322,6 +322,9 @@ enum class Element { kByte, kBf16, kF32 };
 int tile_map(CUtensorMap* map, const void* p, Element type, int64_t rows, int64_t cols, int64_t ld, int box_x, int box_y);
 // Allows a kernel its shared memory, once a device.
 int allow_shared(const void* kernel, size_t bytes);
+// Clusters of `size` thread blocks that run at once: fewer than the SMs hold blocks, since a cluster's lie in one part of the GPU
+// (of blocks that take an SM each: 74 of 2, 33 of 4, 15 of 8).
+int clusters_of(const void* kernel, unsigned threads, size_t shared, unsigned size, int* clusters);
 // Registers a thread that a kernel is launched with.
 int registers_of(const void* kernel, int* registers);
 

@@ -440,11 +440,20 @@ bool worth_a_workspace(int64_t rows, int64_t inner, int64_t outer) {
     return outer >= 1024 && ((outer + 255) / 256) * ((inner + 255) / 256) >= 48 && static_cast<double>(rows) * inner * outer >= 8.0e9;
 }
 
-// Parts of t for as many tiles of 128 x 128, so that they fill the GPU and each part is a run at least.
-int parts(int64_t tiles, int64_t stages) {
-    int split = 1;
-    while (split < 8 && tiles * split * 2 <= kSms && stages >= kRun * split * 2) split *= 2;
-    return split;
+// Parts of t for as many tiles of 128 x 128: as many as run at once in clusters, with two runs each.  (512 x 512 over 16384 tokens,
+// 16 tiles: 36 us in four parts, 49 in eight, of which 15 clusters run at once, 109 in one.)
+template <class T>
+int parts(int64_t tiles, int64_t stages, int* split) {
+    const void* kernel = reinterpret_cast<const void*>(weight_grad_kernel<false, false, T>);
+    *split = 1;
+    for (int next = 2; next <= 8 && stages >= 2 * kRun * next; next *= 2) {
+        int clusters = 0, st = allow_shared(kernel, Shape<false>::kShared);
+        if (st == PVQ_OK) st = clusters_of(kernel, Shape<false>::kThreads, Shape<false>::kShared, next, &clusters);
+        if (st != PVQ_OK) return st;
+        if (tiles > clusters) break;
+        *split = next;
+    }
+    return PVQ_OK;
 }
 
 template <class T>
@@ -461,15 +470,18 @@ int weight_grad_of(Args p, const void* dy, int64_t ld_dy, void* workspace, cudaS
     p.split = 1, p.after = -1;
     if (pairs < 48) {
         p.tiles = static_cast<int>(tiles);
-        p.split = parts(tiles, stages);
-        return launch<false, false, T>(p, maps, s);
+        st = parts<T>(tiles, stages, &p.split);
+        return st != PVQ_OK ? st : launch<false, false, T>(p, maps, s);
     }
     // The last round of tiles, where it is a small one, is shared by all SMs, in quarters and with t in parts, where a round is
     // long or one of two: 16384 values of t, 896 tiles (8 in the last round) 1446 us instead of 1500, 80 tiles 171 instead of 192, 4096
     // values and 80 tiles 50 instead of 54; but 4096 values and 448 tiles (4 in the last) 211 instead of 198: the launch behind
     // the others, while a few tiles alone run at a higher clock.
     constexpr int kPairs = kSms / 2;
-    const int last = static_cast<int>(pairs % kPairs), split = parts(4 * last, stages);
+    const int last = static_cast<int>(pairs % kPairs);
+    int split = 1;
+    if (last > 0) st = parts<T>(4 * last, stages, &split);
+    if (st != PVQ_OK) return st;
     const bool shared = pairs > last && last > 0 && split > 1 && (stages >= 128 || pairs < 2 * kPairs);
     p.tiles = static_cast<int>(shared ? pairs - last : pairs);
     if (workspace) {
