@@ -232,10 +232,11 @@ def _own(state):
         return pvq.fp8_matmul(pvq.Fp8Matrix(*state["a"]), pvq.Fp8Matrix(*state["b"]), transposed=case["transposed"],
                               dtype=_dtype(case))
     if op == "gated":
-        h, gate, up = pvq.fp8_gated(state["gate"], state["up"], act=case["act"], checkpoint=case["checkpoint"])
-        if case["checkpoint"]:
-            return h.codes, h.scales, gate.codes, gate.scales, up.codes, up.scales
-        return h.codes, h.scales
+        if not case["checkpoint"]:
+            h = pvq.fp8_gated(state["gate"], state["up"], act=case["act"])
+            return h.codes, h.scales
+        h, gate, up = pvq.fp8_gated(state["gate"], state["up"], act=case["act"], checkpoint=True)
+        return h.codes, h.scales, gate.codes, gate.scales, up.codes, up.scales
     if op == "gated_backward":
         return pvq.fp8_gated_backward(state["dh"], pvq.Fp8Matrix(*state["gate"]), pvq.Fp8Matrix(*state["up"]), act=case["act"])
     return pvq.fp8_weight_grad(state["dy"], pvq.Fp8Matrix(*state["x"]), dtype=_dtype(case))
