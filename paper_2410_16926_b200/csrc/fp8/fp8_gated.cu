@@ -53,11 +53,11 @@ __device__ __forceinline__ void activation_slope(float2 g, float2* value, float2
 
 // Thread blocks an SM that the registers are limited for: 9 of 128 threads (bf16, 56 registers) is 296 us for 16384 x 14336 with
 // its checkpoints, 8 and 10 are 302 and 301, no limit (62) 318; in blocks of 256 threads 306 at best, 344 without a limit.
-// Backward 8 is 41.2 us for 1999 x 14336, no limit 42.8, 9 to 12 45.
+// Backward, silu: 8 is 41.2 us for 1999 x 14336, no limit 42.8, 9 to 12 45; gelu: 7 is 82.9 for 4096 x 14336, 8 97.7, 6 90.5, 10 83.3.
 template <class T>
 constexpr int kGatedBlocks = sizeof(T) == 2 ? 9 : 6;
-template <class T>
-constexpr int kBackwardBlocks = sizeof(T) == 2 ? 8 : 6;
+template <class T, int ACT>
+constexpr int kBackwardBlocks = sizeof(T) == 2 ? (ACT == PVQ_ACT_SILU ? 8 : 7) : 6;
 
 template <class T, int ACT, bool KEEP>
 __global__ void __launch_bounds__(kRowThreads, kGatedBlocks<T>) gated_kernel(GatedArgs a, Work work) {
@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(kRowThreads, kGatedBlocks<T>) gated_kernel(Gat
 }
 
 template <class T, int ACT>
-__global__ void __launch_bounds__(kRowThreads, kBackwardBlocks<T>) gated_backward_kernel(GatedBackwardArgs a, Work work) {
+__global__ void __launch_bounds__(kRowThreads, kBackwardBlocks<T, ACT>) gated_backward_kernel(GatedBackwardArgs a, Work work) {
     launch_dependents();
     dependency_wait();
     const int64_t cols = a.gate8.cols;

@@ -135,6 +135,17 @@ def test_new_matrices_are_ordinary_tensors():
     assert out.shape == (130, 250) and out.stride() == (256, 1) and torch.equal(out.contiguous(), out)
 
 
+def test_dequantize_into_rows_on_16_byte_boundaries_alone():
+    q = random_held(40, 4096, False, 1)
+    for ld in (4096, 4100, 4104):
+        whole = torch.full((40, ld + 8), 7.0, device="cuda")
+        for first in (0, 4):
+            out = whole[:, first:first + 4096]
+            pvq.fp8_dequantize(q, dtype=F32, out=out)
+            assert np.array_equal(ref.to64(out), ref.values(q))
+        assert bool((whole[:, 4100:] == 7.0).all())
+
+
 def test_dequantize_of_every_code_and_scale():
     codes = torch.arange(256, dtype=torch.int32).to(torch.uint8).repeat(256, 1).cuda()
     scales = torch.arange(256, dtype=torch.int32).to(torch.uint8)[:, None].repeat(1, 4).cuda()[:, :2]
