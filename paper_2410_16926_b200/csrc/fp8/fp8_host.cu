@@ -28,6 +28,17 @@ int checked_values(const void* p, int dtype, int64_t cols, int64_t ld) {
 
 bool same_shape(const fp8::Matrix& a, const fp8::Matrix& b) { return a.rows == b.rows && a.cols == b.cols; }
 
+// Nothing is thrown across the C boundary: the launchers of the products keep small maps of what they asked the driver, and
+// there may be no memory for them.
+template <class F>
+int without_exceptions(F&& f) {
+    try {
+        return f();
+    } catch (...) {
+        return set_cuda_error(cudaErrorMemoryAllocation);
+    }
+}
+
 #define CHECKED(call)                          \
     do {                                       \
         const int status_ = (call);            \
@@ -63,7 +74,8 @@ extern "C" int pvq_fp8_matmul(const pvq_fp8_matrix* a, const pvq_fp8_matrix* b, 
     if (ma.cols != (transposed ? mb.rows : mb.cols)) return PVQ_ERR_INVALID_ARG;
     CHECKED(checked_values(d_out, dtype, transposed ? mb.cols : mb.rows, ld_out));
     if (transposed && !mb.shift) return PVQ_ERR_UNSUPPORTED;  // the scales would change inside a block of the sum
-    return fp8::matmul(ma, mb, transposed != 0, d_out, dtype == PVQ_DTYPE_BF16, ld_out, d_status, static_cast<cudaStream_t>(stream));
+    return without_exceptions(
+        [&] { return fp8::matmul(ma, mb, transposed != 0, d_out, dtype == PVQ_DTYPE_BF16, ld_out, d_status, static_cast<cudaStream_t>(stream)); });
 }
 
 extern "C" int pvq_fp8_gated(const void* d_gate, int64_t ld_gate, const void* d_up, int64_t ld_up, int dtype, int act, const pvq_fp8_matrix* h,
@@ -114,5 +126,7 @@ extern "C" int pvq_fp8_weight_grad(const void* d_dy, int64_t outer, int64_t ld_d
         if (workspace_bytes < fp8::weight_grad_workspace(m.rows, m.cols, outer)) return PVQ_ERR_TABLE_TOO_SMALL;
         if (!is_aligned(d_workspace, 16)) return PVQ_ERR_ALIGNMENT;
     }
-    return fp8::weight_grad(d_dy, outer, ld_dy, m, d_out, dtype == PVQ_DTYPE_BF16, ld_out, d_workspace, d_status, static_cast<cudaStream_t>(stream));
+    return without_exceptions([&] {
+        return fp8::weight_grad(d_dy, outer, ld_dy, m, d_out, dtype == PVQ_DTYPE_BF16, ld_out, d_workspace, d_status, static_cast<cudaStream_t>(stream));
+    });
 }
