@@ -311,7 +311,7 @@ int pvq_decode_static_table(const uint32_t* d_codes, const uint8_t* d_scale_idx,
 
 /* Operators for what a model does with decoded weights and quantised activations: products of
  * 8-bit matrices, and a backward pass whose activations were kept in 8 bits.  (The paper has no
- * counterpart; it compares with formats of this kind.)
+ * counterpart.)
  *
  * The format: one e4m3 code a value (sign, 4 bits of exponent, 3 of mantissa, largest value 448)
  * and one scale a block, a power of two 2^(byte - 127) kept as its byte (e8m0; 255 is NaN).  A
@@ -326,7 +326,8 @@ int pvq_decode_static_table(const uint32_t* d_codes, const uint8_t* d_scale_idx,
  * Every size is at least 1, rows and columns below 2^31, rows * ceil(cols / 128) below 2^31.
  * Other matrices are row-major fp32 or bf16 (PVQ_DTYPE_*), 16-byte aligned, with a leading
  * dimension that is a multiple of 4 (fp32) or 8 (bf16) elements.  Outputs may not overlap
- * inputs or one another.  No call keeps anything; all can be captured into graphs.  Results do not depend on launch order: the same inputs give the same bits. */
+ * inputs or one another.  No call keeps anything; all can be captured into graphs.  Results do
+ * not depend on launch order: the same inputs give the same bits. */
 typedef struct {
     uint8_t* d_codes;
     uint8_t* d_scales;
