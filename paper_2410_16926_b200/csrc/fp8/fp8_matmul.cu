@@ -7,11 +7,11 @@ namespace fp8 {
 int matmul(const Matrix& a, const Matrix& b, bool transposed, void* out, bool bf16, int64_t ld, uint32_t* status, cudaStream_t s) {
     const MatmulArgs p{a, b, out, a.rows, transposed ? b.cols : b.rows, a.cols, ld, status};
     const int64_t blocks = (p.inner + kBlock - 1) / kBlock;
-    const int64_t pairs = ((p.rows + 255) / 256) * ((p.outs + 255) / 256);
-    if (p.rows > 128 && pairs >= 48) return matmul_many(p, transposed, bf16, s);
     const int64_t high = p.rows <= 16 ? 16 : (p.rows <= 32 ? 32 : (p.rows <= 64 ? 64 : 128));
     const int64_t tiles = ((p.outs + 127) / 128) * ((p.rows + high - 1) / high);
-    if ((p.rows + high - 1) / high > 65535) return matmul_many(p, transposed, bf16, s);
+    // Tiles of 128 x 128 where one round of them does it, else pairs of thread blocks.  512 rows, 4096 to 4736 (148 tiles) 14.0 us
+    // and 16.6 in pairs, 4096 to 5120 (160 tiles) 24.1 and 17.3; 1024 rows, 14336 to 2560 57.1 and 42.8.
+    if (p.rows > 128 && tiles > kSms) return matmul_many(p, transposed, bf16, s);
     // k is split over clusters as long as they all run at once, with one thread block an SM, or two up to 32 rows (more than that
     // only for long parts), and each part has four blocks of 128; up to 32 rows not where the tiles alone nearly fill the SMs,
     // since blocks of their own start sooner than clusters.  One row, 4096 to 4096 (32 tiles): 4.8 us with k in four parts, 5.2

@@ -431,13 +431,18 @@ int launch(const Args& p, const Maps& maps, cudaStream_t s) {
     return launch_early(kernel, dim3(static_cast<unsigned>(teams * team)), kThreads, kShared, team, s, maps, p);
 }
 
+// Tiles of 128 x 128 where one round of them does it, else pairs of thread blocks with 256 x 256.  1024 x 2304 over 4096 tokens (144
+// tiles) 33.0 us and 32.9 in pairs, 1024 x 1152 (72 tiles in two parts) 24.4 and 32.7, 1024 x 2560 (160 tiles) 58.2 and 34.6.
+int64_t small_tiles(int64_t inner, int64_t outer) { return ((outer + 127) / 128) * ((inner + 127) / 128); }
+bool one_round(int64_t inner, int64_t outer) { return small_tiles(inner, outer) <= kSms; }
+
 // x as bf16 in the caller's workspace.
 int64_t workspace_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
 // Converting first, or in the kernel, tokens x inputs to outputs: 512 x 4096 to 4096 24.5 and 26.1 us, 1024 x 4096 to 14336 107 and 134,
-// 4096 x 4096 to 1024 34.0 and 37.3; 2048 x 4096 to 1024 21.1 and 22.8; but
+// 4096 x 4096 to 1024 34.0 and 37.3; 2048 x 4096 to 1024 21.1 and 22.8; 4096 x 1024 to 2560 28.5 and 34.0; but
 // 1001 x 4096 to 1024 14.6 and 13.4 (with the second launch), 4096 x 8192 to 512 44.4 and 39.0.
 bool worth_a_workspace(int64_t rows, int64_t inner, int64_t outer) {
-    return outer >= 1024 && ((outer + 255) / 256) * ((inner + 255) / 256) >= 48 && static_cast<double>(rows) * inner * outer >= 8.0e9;
+    return outer >= 1024 && !one_round(inner, outer) && static_cast<double>(rows) * inner * outer >= 8.0e9;
 }
 
 // Parts of t for as many tiles of 128 x 128: as many as run at once in clusters, with two runs each.  (512 x 512 over 16384 tokens,
@@ -458,7 +463,7 @@ int parts(int64_t tiles, int64_t stages, int* split) {
 
 template <class T>
 int weight_grad_of(Args p, const void* dy, int64_t ld_dy, void* workspace, cudaStream_t s) {
-    const int64_t pairs = ((p.outer + 255) / 256) * ((p.x.cols + 255) / 256), tiles = ((p.outer + 127) / 128) * ((p.x.cols + 127) / 128);
+    const int64_t pairs = ((p.outer + 255) / 256) * ((p.x.cols + 255) / 256), tiles = small_tiles(p.x.cols, p.outer);
     const int64_t stages = (p.x.rows + kDepth - 1) / kDepth;
     if (tiles >= int64_t(1) << 30) return PVQ_ERR_UNSUPPORTED;
     Maps maps;
@@ -468,7 +473,7 @@ int weight_grad_of(Args p, const void* dy, int64_t ld_dy, void* workspace, cudaS
     if (st == PVQ_OK) st = tile_map(&maps.out, p.out, out, p.outer, p.x.cols, p.ld, 128 / sizeof(T), 32);
     if (st != PVQ_OK) return st;
     p.split = 1, p.after = -1;
-    if (pairs < 48) {
+    if (one_round(p.x.cols, p.outer)) {
         p.tiles = static_cast<int>(tiles);
         st = parts<T>(tiles, stages, &p.split);
         return st != PVQ_OK ? st : launch<false, false, T>(p, maps, s);

@@ -176,7 +176,8 @@ def check_matmul(a, b, transposed, dtype, out=None):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,inner,outer", [(1, 1, 1), (1, 128, 128), (2, 130, 7), (1, 4096, 1024), (5, 1000, 333), (8, 512, 4096), (16, 300, 136),
                                               (17, 257, 129), (33, 2048, 512), (64, 640, 200), (65, 127, 640), (128, 1024, 384), (129, 4096, 257),
-                                              (300, 513, 1000), (513, 900, 770), (1024, 256, 2048), (1281, 1400, 2100), (2100, 260, 2600)])
+                                              (300, 513, 1000), (513, 900, 770), (1024, 256, 2048), (1281, 1400, 2100), (2100, 260, 2600),
+                                              (385, 300, 4700), (130, 520, 9480), (1025, 260, 2100)])
 def test_matmul(rows, inner, outer, dtype, transposed):
     a = random_held(rows, inner, False, rows + inner, pad=16)
     shape = (inner, outer) if transposed else (outer, inner)
@@ -265,7 +266,8 @@ def check_weight_grad(dy, x, dtype, out=None):
                                                    (65, 256, 264, True), (1000, 513, 257, False), (1001, 1024, 520, True), (2500, 300, 1000, False),
                                                    (4096, 128, 64, False), (129, 2048, 1024, False),
                                                    (1500, 1500, 2100, False), (700, 2600, 2060, True), (3000, 250, 130, False),
-                                                   (2049, 2300, 2000, False), (1100, 2500, 2100, False), (1700, 2500, 2100, True)])
+                                                   (2049, 2300, 2000, False), (1100, 2500, 2100, False), (1700, 2500, 2100, True),
+                                                   (600, 1300, 1800, False), (2900, 1536, 1800, True), (500, 4736, 500, False)])
 def test_weight_grad(rows, inner, outer, tile, dtype):
     dy = normal(rows, outer, BF16, rows, pad=16)
     x = random_held(rows, inner, tile, rows + 1, pad=16)
