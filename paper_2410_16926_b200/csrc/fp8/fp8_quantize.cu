@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(kTileThreads) quantize_tiles_kernel(const T* x
     const uint32_t down = divide(blockIdx.x, across);
     const int block = static_cast<int>(blockIdx.x - down * across.d), col = block * kBlock + (threadIdx.x & 7) * 8;
     const int64_t row0 = int64_t(down) * 128 + threadIdx.x / 8;
-    const bool whole = col + 72 <= q.cols;
+    const bool whole = col <= q.cols - 72;
     if (threadIdx.x < 2) found[threadIdx.x] = 0u;
     launch_dependents();
     __syncthreads();

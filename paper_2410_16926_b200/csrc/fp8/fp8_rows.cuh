@@ -227,7 +227,7 @@ __device__ __forceinline__ Unit unit_at(const Work& w, int64_t cols, int i) {
     u.row = divide(u.there ? b : 0u, w.blocks);
     u.block = static_cast<int>((u.there ? b : 0u) - u.row * w.blocks.d);
     u.col = u.block * kBlock + (threadIdx.x & 7) * 8;
-    u.whole = u.there && u.col + 72 <= cols;
+    u.whole = u.there && u.col <= cols - 72;  // (64 bits: the last block's col + 72 may be 2^31)
     return u;
 }
 // What is not there is zeros.
