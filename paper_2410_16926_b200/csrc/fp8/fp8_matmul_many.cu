@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
                 const int row = m * 256 + rank * 128, col = n * 256 + rank * 128;
                 for (int kb = 0; kb < blocks; ++kb) {
                     const uint32_t at = base + turn.at * kStageBytes;
-                    ok = barrier_wait(empty + 8 * turn.at, turn.parity ^ 1, bounds);
+                    ok = barrier_wait<true>(empty + 8 * turn.at, turn.parity ^ 1, bounds);
                     if (!ok) break;
                     if (rank == 0) barrier_expect(full + 8 * turn.at, 2 * kStageBytes);  // both blocks' tiles
                     load_tile<true>(at, &maps.a, kb * kBlock, row, full_there + 8 * turn.at);
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
             }
             if (!ok && rank == 0)  // copies in flight have to land before the block ends
                 for (uint32_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
-                    for (int polls = 0; polls < kLandings && !barrier_passed(full + 8 * (i % kStages), (i / kStages) & 1); ++polls) {}
+                    for (int polls = 0; polls < kLandings && !barrier_passed<true>(full + 8 * (i % kStages), (i / kStages) & 1); ++polls) {}
         }
     } else if (warp == 1) {
         if (rank == 0 && elected()) {
@@ -131,15 +131,15 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
                     const uint32_t part = kb & 3;
                     const bool starts = left == 0;
                     if (starts) {
-                        ok = barrier_wait(sum_empty + 8 * sums.at, sums.parity ^ 1, bounds) && barrier_wait(shared_empty, shared, bounds);
+                        ok = barrier_wait<true>(sum_empty + 8 * sums.at, sums.parity ^ 1, bounds) && barrier_wait<true>(shared_empty, shared, bounds);
                         left = part_blocks;
                     }
-                    if (part == 0) ok = ok && barrier_wait(scales_full + 8 * scales.at, scales.parity, bounds);
-                    ok = ok && (there || barrier_wait(full + 8 * turn.at, turn.parity, bounds));
+                    if (part == 0) ok = ok && barrier_wait<true>(scales_full + 8 * scales.at, scales.parity, bounds);
+                    ok = ok && (there || barrier_wait<true>(full + 8 * turn.at, turn.parity, bounds));
                     if (!ok) break;
                     const uint32_t now = turn.at;
                     turn.next();
-                    there = barrier_over(full + 8 * turn.at, turn.parity);
+                    there = barrier_over<true>(full + 8 * turn.at, turn.parity);
                     tensor_fence_after();
                     const uint64_t a = a0 + now * (kStageBytes >> 4), b = b0 + now * (kStageBytes >> 4);
                     const uint32_t sum = tensor + kSecond * sums.at, sa = tensor + kScalesA + 4 * scales.at, sb = tensor + kScalesB + 8 * scales.at,
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
             }
             if (!ok) {
                 products_done<true>(drained);
-                for (int polls = 0; polls < kLandings && !barrier_passed(drained, 0); ++polls) {}
+                for (int polls = 0; polls < kLandings && !barrier_passed<true>(drained, 0); ++polls) {}
             }
         }
     } else if (warp >= 4 && warp < 8) {
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
         const auto put = [&](const uint32_t (&a)[4], const uint32_t (&b)[8]) -> bool {
             const uint32_t buffer = four & 1;
             if (four >= 2) {
-                if (!warp_wait(scales_empty + 8 * buffer, ((four >> 1) - 1) & 1, bounds)) return false;
+                if (!warp_wait<true>(scales_empty + 8 * buffer, ((four >> 1) - 1) & 1, bounds)) return false;
                 tensor_fence_after();
             }
             tensor_store(mine + kScalesA + 4 * buffer, a);
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
                 for (int k = 0; k < 128; ++k) sum[k] = 0.0f;
 #pragma unroll 1
                 for (int part = 0; part < parts; ++part, ++item) {
-                    ok = warp_wait(sum_full + 8 * (item & 1), (item >> 1) & 1, bounds);
+                    ok = warp_wait<true>(sum_full + 8 * (item & 1), (item >> 1) & 1, bounds);
                     if (!ok) break;
                     tensor_fence_after();
                     const uint32_t mine = tensor + (quarter << 21) + (item & 1) * kSecond + half * 128;
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
                     put(w, row, col + chunk(i) * 32);
                 }
             } else {
-                ok = warp_wait(sum_full + 8 * (item & 1), (item >> 1) & 1, bounds);
+                ok = warp_wait<true>(sum_full + 8 * (item & 1), (item >> 1) & 1, bounds);
                 if (!ok) break;
                 tensor_fence_after();
                 const uint32_t mine = tensor + (quarter << 21) + (item & 1) * kSecond + half * 128;

@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
                 const int row = m * kSide + rank * 128, col = n * kSide + rank * 128;
                 for (int kb = begin; kb < end; ++kb) {
                     const uint32_t at = base + turn.at * kStageBytes;
-                    ok = barrier_wait(empty + 8 * turn.at, turn.parity ^ 1, bounds);
+                    ok = barrier_wait<PAIR>(empty + 8 * turn.at, turn.parity ^ 1, bounds);
                     if (!ok) break;
                     if (rank == 0) barrier_expect(full_dy + 8 * turn.at, kBlocks * (READY ? 4 : 2) * kAtom);
                     if constexpr (READY) {
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
             if (!ok)  // copies in flight have to land before the block ends
                 for (uint32_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i) {
                     const uint32_t s = i % kStages, parity = (i / kStages) & 1;
-                    for (int polls = 0; polls < kLandings && !((rank != 0 || barrier_passed(full_dy + 8 * s, parity)) && (READY || barrier_passed(full_x + 8 * s, parity))); ++polls) {}
+                    for (int polls = 0; polls < kLandings && !((rank != 0 || barrier_passed<PAIR>(full_dy + 8 * s, parity)) && (READY || barrier_passed(full_x + 8 * s, parity))); ++polls) {}
                 }
         } else if (warp == 1 && rank == 0 && elected()) {
             constexpr uint32_t product = product_bf16(kSide, kSide, true, true);
@@ -205,9 +205,9 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
             for (int t = blockIdx.x / team; t < tiles && ok; t += step) {
                 int within = 0;
                 for (int kb = begin; kb < end; ++kb) {
-                    if (within == 0) ok = barrier_wait(sum_empty + 8 * sums.at, sums.parity ^ 1, bounds);
-                    ok = ok && barrier_wait(full_dy + 8 * turn.at, turn.parity, bounds);
-                    if constexpr (!READY) ok = ok && barrier_wait(converted_full + 8 * ready.at, ready.parity, bounds);
+                    if (within == 0) ok = barrier_wait<PAIR>(sum_empty + 8 * sums.at, sums.parity ^ 1, bounds);
+                    ok = ok && barrier_wait<PAIR>(full_dy + 8 * turn.at, turn.parity, bounds);
+                    if constexpr (!READY) ok = ok && barrier_wait<PAIR>(converted_full + 8 * ready.at, ready.parity, bounds);
                     if (!ok) break;
                     tensor_fence_after();
                     const uint64_t a = a0 + turn.at * (kStageBytes >> 4), b = b0 + (READY ? turn.at * (kStageBytes >> 4) : ready.at * (kConvertedBytes >> 4));
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
             }
             if (!ok) {
                 products_done<PAIR>(drained);
-                for (int polls = 0; polls < kLandings && !barrier_passed(drained, 0); ++polls) {}
+                for (int polls = 0; polls < kLandings && !barrier_passed<PAIR>(drained, 0); ++polls) {}
             }
         }
     } else if (warp < kFirstHolder) {
@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
                 for (int i = 0; i < 4; ++i) {
                     if (kb0 + 2 * i >= end) break;
                     const uint32_t it = it0 + (kb0 + 2 * i - begin), s = it % kStages, c = it % kConverted;
-                    ok = warp_wait(full_x + 8 * s, (it / kStages) & 1, bounds) && warp_wait(converted_empty + 8 * c, ((it / kConverted) & 1) ^ 1, bounds);
+                    ok = warp_wait(full_x + 8 * s, (it / kStages) & 1, bounds) && warp_wait<PAIR>(converted_empty + 8 * c, ((it / kConverted) & 1) ^ 1, bounds);
                     if (!ok) break;
                     const uint32_t from = base + s * kStageBytes + 2 * kAtom + row * 128, to = converted + c * kConvertedBytes + half * kAtom + row * 128;
                     const uint32_t byte = (bytes >> (8 * i)) & 0xffu;
@@ -269,8 +269,12 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
                     async_fence();
                     __syncwarp();
                     if (lane == 0) {
-                        if (PAIR) barrier_arrive_in(full_there + 8 * c);
-                        else barrier_arrive(full_there + 8 * c);
+                        if (PAIR) {
+                            release_shared();
+                            barrier_arrive_in(full_there + 8 * c);
+                        } else {
+                            barrier_arrive(full_there + 8 * c);
+                        }
                     }
                 }
             }
@@ -293,7 +297,7 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
             for (int i = 0; i < kHeld; ++i) sum[i] = 0.0f;
             for (int kb = begin; kb < end; kb += kRun, ++run) {
                 const uint32_t buffer = run & 1;
-                ok = warp_wait(sum_full + 8 * buffer, (run >> 1) & 1, bounds);
+                ok = warp_wait<PAIR>(sum_full + 8 * buffer, (run >> 1) & 1, bounds);
                 if (!ok) break;
                 tensor_fence_after();
 #pragma unroll
