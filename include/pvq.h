@@ -398,6 +398,11 @@ size_t pvq_fp8_weight_grad_workspace(int64_t rows, int64_t inner, int64_t outer)
 /* Set by the caller: the streamed tables of the kernels for wide codes and the round trip's input tiles
  * are withheld, so that the bounded waits for them run out (sooner than otherwise). */
 #define PVQ_DEBUG_WITHHOLD 0x80000000u
+/* Set by the caller in the status word of pvq_fp8_matmul and pvq_fp8_weight_grad, as PVQ_DEBUG_WITHHOLD
+ * may be there, too: only the copies of every second thread block of a cluster, or the scales (of the
+ * weight gradient: the conversion) are withheld, from a few stages into the call on. */
+#define PVQ_DEBUG_WITHHOLD_SECOND 0x40000000u
+#define PVQ_DEBUG_WITHHOLD_SCALES 0x20000000u
 
 /* The library built with -DPVQ_DEBUG (`python -m paper_2410_16926_b200.build --debug`,
  * libpvq_b200_debug.so; shared-memory kernels only) checks every table read, slot write,

@@ -7,7 +7,7 @@ _bind.so, the native part of the Python binding (csrc/bind/pvq_bind.cpp).
 --debug builds libpvq_b200_debug.so instead: the bounds-checked variant (-DPVQ_DEBUG, see
 pvq_debug_status in include/pvq.h) of the kernels that keep their tables in shared memory;
 the global-table kernels are left out of it (calls that need them return "unsupported"), those of the
-8-bit operators are in it unchanged.  The binding is the same.
+8-bit operators are not checked in it but can be made to wait for copies that never come.  The binding is the same.
 """
 import os
 import subprocess

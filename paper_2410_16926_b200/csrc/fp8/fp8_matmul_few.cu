@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
     extern __shared__ uint8_t raw[];
     const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
     const uint32_t parts = base + S::kPartsAt, full = base + S::kBarsAt, empty = full + 8 * S::kStages, scales_full = empty + 8 * S::kStages,
-                   scales_empty = scales_full + 8 * S::kScaleSets, sum_full = scales_empty + 8 * S::kScaleSets;
-    __shared__ uint32_t tensor_base;
+                   scales_empty = scales_full + 8 * S::kScaleSets, sum_full = scales_empty + 8 * S::kScaleSets, drained = sum_full + 8;
+    __shared__ uint32_t tensor_base, issued_stages;
     __shared__ int over;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % SPLIT;  // in the cluster
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
     const int64_t col0 = int64_t(blockIdx.x / SPLIT) * 128, row0 = int64_t(blockIdx.y) * ROWS;
     const int blocks = static_cast<int>((p.inner + kBlock - 1) / kBlock);
     const int first = static_cast<int>(int64_t(blocks) * rank / SPLIT), last = static_cast<int>(int64_t(blocks) * (rank + 1) / SPLIT);  // (SPLIT <= blocks)
-    const Bounds bounds{&over, p.status};
+    Bounds bounds{&over, p.status};
 
     const auto load = [&](int kb, uint32_t stage) {
         const uint32_t at = base + stage * S::kStageBytes, bar = full + 8 * stage;
@@ -125,8 +125,8 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
         }
     };
     if (warp == 0) {
-        // a barrier a lane: stages' full and empty, the scales' sets full and empty, the sum
-        constexpr int kBars = 2 * S::kStages + 2 * S::kScaleSets + 1;
+        // a barrier a lane: stages' full and empty, the scales' sets full and empty, the sum, drained
+        constexpr int kBars = 2 * S::kStages + 2 * S::kScaleSets + 2;
         static_assert(kBars <= 32, "one lane each");
         if (lane < kBars) barrier_init(full + 8 * lane, lane >= 2 * S::kStages && lane < 2 * S::kStages + S::kScaleSets ? 4 : 1);
         barrier_init_fence();
@@ -149,22 +149,20 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
     launch_dependents();
     if (warp == 2) dependency_wait();
     const uint32_t tensor = tensor_base;
+    const Withheld withheld = withheld_of(bounds, rank);
 
     if (warp == 0) {
         if (elected()) {
             Turn<S::kStages> turn;  // the second time round, and so on
             uint32_t issued = min(S::kStages, last - first);
-            bool ok = true;
             for (int kb = first + S::kStages; kb < last; ++kb) {
-                ok = barrier_wait(empty + 8 * turn.at, turn.parity, bounds);
-                if (!ok) break;
+                if (withheld.copies && issued >= S::kStages + kWithheldFrom) break;
+                if (!barrier_wait(empty + 8 * turn.at, turn.parity, bounds)) break;
                 load(kb, turn.at);
                 turn.next();
                 ++issued;
             }
-            if (!ok)  // copies in flight have to land before the block ends
-                for (uint32_t i = issued > S::kStages ? issued - S::kStages : 0; i < issued; ++i)
-                    for (int polls = 0; polls < kLandings && !barrier_passed(full + 8 * (i % S::kStages), (i / S::kStages) & 1); ++polls) {}
+            issued_stages = issued;
         }
     } else if (warp == 1) {
         if (elected()) {
@@ -193,8 +191,8 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
                     scales.next();
                 }
             }
-            products_done<false>(sum_full);
-            for (int polls = 0; !ok && polls < kLandings && !barrier_passed(sum_full, 0); ++polls) {}
+            products_done<false>(ok ? sum_full : drained);
+            for (int polls = 0; !ok && polls < kLandings && !barrier_passed(drained, 0); ++polls) {}
         }
     } else if (warp >= 4) {
         const uint32_t mine = tensor + ((warp & 3) << 21);
@@ -206,6 +204,7 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
 #pragma unroll
             for (int i = 0; i < S::kScaleSets; ++i) {
                 if (f0 + i > (last - 1) / 4) break;
+                if (withheld.scales && f0 + i >= first / 4 + kWithheldFrom) break;
                 ok = warp_wait(scales_empty + 8 * turn.at, turn.parity ^ 1, bounds);
                 if (!ok) break;
                 tensor_fence_after();
@@ -219,16 +218,15 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
             }
         }
         ok = ok && warp_wait(sum_full, 0, bounds);
-        ok = ok && !over;
-        ok = __all_sync(0xffffffffu, ok);
         if (SPLIT > 1) cluster_wait();
-        if (ok) {  // a lane's column of the part goes to the block whose share it is in
+        // a lane's column of the part goes to the block whose share it is in
+        constexpr int kShare = 128 / SPLIT;
+        const int column = (warp & 3) * 32 + lane;
+        const uint32_t mine_at = parts + (rank * ROWS * kShare + column % kShare) * 4;
+        const uint32_t to = SPLIT > 1 ? address_in(mine_at, column / kShare) : mine_at;
+        const int rows = static_cast<int>(min(int64_t(ROWS), p.rows - row0));
+        if (__builtin_expect(ok, 1)) {
             tensor_fence_after();
-            constexpr int kShare = 128 / SPLIT;
-            const int column = (warp & 3) * 32 + lane;
-            const uint32_t mine_at = parts + (rank * ROWS * kShare + column % kShare) * 4;
-            const uint32_t to = SPLIT > 1 ? address_in(mine_at, column / kShare) : mine_at;
-            const int rows = static_cast<int>(min(int64_t(ROWS), p.rows - row0));
 #pragma unroll
             for (int c = 0; c < ROWS; c += 16) {
                 if (c >= rows) break;
@@ -250,6 +248,7 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
     if (SPLIT > 1) cluster_barrier();
     else __syncthreads();
     add_parts<ROWS, SPLIT, T>(parts, rank, p, row0, col0);
+    if (warp == 0 && __builtin_expect(over, 0)) land<S::kStages>(full, issued_stages);  // copies in flight have to land before the block ends
     if (warp == 2) {
         tensor_fence_after();
         tensor_free<false>(tensor, S::kColumns);

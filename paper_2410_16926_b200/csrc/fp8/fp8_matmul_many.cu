@@ -57,8 +57,8 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
     const uint32_t stores = base + kStages * kStageBytes, bars = stores + 8 * 2 * kStoreBytes;
     const uint32_t full = bars, empty = full + 8 * kStages, scales_full = empty + 8 * kStages, scales_empty = scales_full + 16, sum_full = scales_empty + 16,
                    sum_empty = sum_full + 16, shared_empty = sum_empty + 16, drained = shared_empty + 8;
-    __shared__ uint32_t tensor_base;
-    __shared__ int over;
+    __shared__ uint32_t tensor_base, issued_stages[2];  // (issued: this block's stages, and the other's once a wait has run out)
+    __shared__ int over;  // a wait has run out in either block
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     if (warp == 0) {  // a barrier a lane, in the order of their places
@@ -80,11 +80,21 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
     launch_dependents();
     dependency_wait();
     const uint32_t tensor = tensor_base;
-    const Bounds bounds{&over, p.status};
+    Bounds bounds{&over, p.status, 2};
+    const Withheld withheld = withheld_of(bounds, rank);
     const Tiles tiles{static_cast<int>((p.rows + 255) / 256), static_cast<int>((p.outs + 255) / 256)};
     const int blocks = static_cast<int>((p.inner + kBlock - 1) / kBlock), first = blockIdx.x / 2, step = gridDim.x / 2;
     constexpr bool kParts = sizeof(T) == 4;
     const int about = kParts ? (blocks + kRun - 1) / kRun : 1, part_blocks = (blocks + about - 1) / about, parts = (blocks + part_blocks - 1) / part_blocks;
+
+    const uint32_t full_there = address_in(full, 0);
+    const auto load = [&](uint32_t stage, int row, int col, int kb) {
+        const uint32_t at = base + stage * kStageBytes;
+        if (rank == 0) barrier_expect(full + 8 * stage, 2 * kStageBytes);  // both blocks' tiles
+        load_tile<true>(at, &maps.a, kb * kBlock, row, full_there + 8 * stage);
+        if (ACROSS) load_tile<true>(at + kStageBytes / 2, &maps.b, col, kb * kBlock, full_there + 8 * stage);
+        else load_tile<true>(at + kStageBytes / 2, &maps.b, kb * kBlock, col, full_there + 8 * stage);
+    };
 
     if (warp < 4) {
         if constexpr (kParts) fewer_registers<kFew>();
@@ -94,26 +104,19 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
             Turn<kStages> turn;
             uint32_t issued = 0;
             bool ok = true;
-            const uint32_t full_there = address_in(full, 0);
             for (int t = first; t < tiles.count() && ok; t += step) {
                 int m, n;
                 tiles.at(t, &m, &n);
                 const int row = m * 256 + rank * 128, col = n * 256 + rank * 128;
                 for (int kb = 0; kb < blocks; ++kb) {
-                    const uint32_t at = base + turn.at * kStageBytes;
-                    ok = barrier_wait<true>(empty + 8 * turn.at, turn.parity ^ 1, bounds);
+                    ok = !(withheld.copies && issued >= kStages + kWithheldFrom) && barrier_wait<true>(empty + 8 * turn.at, turn.parity ^ 1, bounds);
                     if (!ok) break;
-                    if (rank == 0) barrier_expect(full + 8 * turn.at, 2 * kStageBytes);  // both blocks' tiles
-                    load_tile<true>(at, &maps.a, kb * kBlock, row, full_there + 8 * turn.at);
-                    if (ACROSS) load_tile<true>(at + kStageBytes / 2, &maps.b, col, kb * kBlock, full_there + 8 * turn.at);
-                    else load_tile<true>(at + kStageBytes / 2, &maps.b, kb * kBlock, col, full_there + 8 * turn.at);
+                    load(turn.at, row, col, kb);
                     turn.next();
                     ++issued;
                 }
             }
-            if (!ok && rank == 0)  // copies in flight have to land before the block ends
-                for (uint32_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
-                    for (int polls = 0; polls < kLandings && !barrier_passed<true>(full + 8 * (i % kStages), (i / kStages) & 1); ++polls) {}
+            issued_stages[rank] = issued;
         }
     } else if (warp == 1) {
         if (rank == 0 && elected()) {
@@ -202,6 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
         load(a[1], b[1]);
         const int64_t steps = int64_t((tiles.count() - first + step - 1) / step) * ((blocks + 3) / 4);
         for (int64_t i = 0; i < steps; i += 2) {
+            if (withheld.scales && i >= kWithheldFrom) break;
             if (!put(a[0], b[0])) break;
             load(a[0], b[0]);
             if (i + 1 >= steps || !put(a[1], b[1])) break;
@@ -250,11 +254,12 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
         // may share: the right one goes backwards.
         uint32_t item = 0;
         const auto chunk = [&](int i) { return half ? kChunks - 1 - i : i; };
-        bool ok = true;
-        for (int t = first; t < tiles.count() && ok; t += step) {
+        int t = first;
+        for (; t < tiles.count(); t += step) {
             int m, n;
             tiles.at(t, &m, &n);
             const int64_t row = int64_t(m) * 256 + rank * 128 + quarter * 32, col = int64_t(n) * 256 + half * 128;
+            bool ok = true;
             const auto read = [&](int i) {  // has read chunk i of four or two
                 if ((i == 0 && half == ((item & 1) ^ 1)) || i == kChunks - 1) {
                     tensor_fence_before();
@@ -318,6 +323,21 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
     tensor_fence_before();
     __syncthreads();
     cluster_barrier();
+    if (__builtin_expect(over, 0)) {
+        // Copies in flight have to land before their block ends, and both blocks' report to the first's barriers.  Stages that one of
+        // them did not ask for any more are filled up, so that each report is complete.
+        if (threadIdx.x == 0) store_in(address_in(shared_address(&issued_stages[rank]), rank ^ 1), issued_stages[rank]);
+        __syncwarp();
+        cluster_barrier();
+        if (threadIdx.x == 0) {
+            const uint32_t all = max(issued_stages[0], issued_stages[1]);
+#pragma unroll 1
+            for (uint32_t i = issued_stages[rank]; i < all; ++i) load(i % kStages, 0, 0, 0);
+            if (rank == 0) land<kStages, true>(full, all);
+        }
+        __syncwarp();
+        cluster_barrier();
+    }
     if (warp == 2) tensor_free<true>(tensor, 512);
 }
 

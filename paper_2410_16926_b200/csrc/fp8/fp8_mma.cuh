@@ -33,14 +33,45 @@ __device__ __forceinline__ void barrier_arrive_in(uint32_t cluster_address) {
 }
 __device__ __forceinline__ void release_shared() { asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory"); }
 
+__device__ __forceinline__ void store_in(uint32_t cluster_address, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_address), "r"(v) : "memory");
+}
+
 constexpr int kPolls = 1 << 20;     // of a wait; a poll itself may wait for some time
 constexpr int kLandings = 1 << 14;  // of a wait for what is in flight, once another wait has run out
 
-// What a block shares about waits that ran out: one that does ends all others, and sets the status word.
+// What a block, or a cluster whose blocks wait for one another, shares about waits that ran out: one that does ends all others, and
+// sets the status word.
 struct Bounds {
     volatile int* over;
     uint32_t* status;
+    uint32_t blocks = 1;  // that are told
+    int polls = kPolls;
 };
+__device__ __forceinline__ void ran_out(volatile int* over, uint32_t* status, uint32_t blocks) {
+    if (blocks == 1) {
+        *over = 1;
+    } else {
+#pragma unroll 1
+        for (uint32_t r = 0; r < blocks; ++r) store_in(address_in(shared_address(const_cast<const int*>(over)), r), 1);
+    }
+    if (status) atomicOr(status, PVQ_STATUS_STAGING_TIMEOUT);
+}
+// The bounds-checked build leaves copies or scales out where the caller's status word says so, and then waits for a short while only.
+struct Withheld {
+    bool copies = false, scales = false;  // from the block's stage `kWithheldFrom` behind the ring's first turn on
+};
+constexpr uint32_t kWithheldFrom = 2;
+__device__ __forceinline__ Withheld withheld_of(Bounds& b, uint32_t rank) {
+    Withheld w;
+#ifdef PVQ_DEBUG
+    const uint32_t bits = b.status ? *const_cast<const volatile uint32_t*>(b.status) : 0u;
+    w.copies = (bits & PVQ_DEBUG_WITHHOLD) != 0u || ((bits & PVQ_DEBUG_WITHHOLD_SECOND) != 0u && (rank & 1u));
+    w.scales = (bits & PVQ_DEBUG_WITHHOLD_SCALES) != 0u;
+    if (bits & (PVQ_DEBUG_WITHHOLD | PVQ_DEBUG_WITHHOLD_SECOND | PVQ_DEBUG_WITHHOLD_SCALES)) b.polls = 1 << 10;
+#endif
+    return w;
+}
 // Whether the phase `parity` is over, after a short wait.  CLUSTER: what another block of the cluster did to shared memory before it
 // arrived (or its copies and products, which do so themselves) is seen from here on.  (Acquiring all memory would empty the L1 cache
 // at each poll, from which the scales are read: a product of 1999 x 4096 by 4096 39.9 us and 34.4 so.)
@@ -75,12 +106,11 @@ __device__ __forceinline__ bool barrier_passed(uint32_t bar, uint32_t parity) {
 template <bool CLUSTER = false>
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, const Bounds& b) {
 #pragma unroll 1
-    for (int i = 0; i < kPolls; ++i) {
+    for (int i = 0; i < b.polls; ++i) {
         if (barrier_passed<CLUSTER>(bar, parity)) return true;
         if ((i & 63) == 63 && *b.over) return false;
     }
-    *b.over = 1;
-    if (b.status) atomicOr(b.status, PVQ_STATUS_STAGING_TIMEOUT);
+    ran_out(b.over, b.status, b.blocks);
     return false;
 }
 
@@ -118,13 +148,13 @@ __device__ __forceinline__ bool barrier_over(uint32_t bar, uint32_t parity) {
 template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const Bounds& b) {
 #pragma unroll 1
-    for (int i = 0; i < kPolls; ++i) {
+    for (int i = 0; i < b.polls; ++i) {
         if (__all_sync(0xffffffffu, barrier_passed<CLUSTER>(bar, parity))) return true;
         if ((i & 63) == 63 && __any_sync(0xffffffffu, *b.over)) return false;
         __nanosleep(40);
     }
-    *b.over = 1;
-    if (b.status && (threadIdx.x & 31) == 0) atomicOr(b.status, PVQ_STATUS_STAGING_TIMEOUT);
+    if ((threadIdx.x & 31) == 0) ran_out(b.over, b.status, b.blocks);
+    __syncwarp();
     return false;
 }
 
@@ -309,6 +339,17 @@ __device__ __forceinline__ void more_registers() {
 template <int REGISTERS>
 __device__ __forceinline__ void fewer_registers() {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGISTERS));
+}
+
+// ---- once a wait has run out
+
+// Waits for the last copies that were asked for, `issued` stages of a ring in all.
+template <int STAGES, bool CLUSTER = false>
+__device__ __forceinline__ void land(uint32_t full, uint32_t issued) {
+#pragma unroll 1
+    for (uint32_t i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i)
+#pragma unroll 1
+        for (int polls = 0; polls < kLandings && !barrier_passed<CLUSTER>(full + 8 * (i % STAGES), (i / STAGES) & 1); ++polls) {}
 }
 
 // ---- scales in tensor memory

@@ -120,8 +120,8 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
     const uint32_t full_dy = bars, full_x = full_dy + 8 * kStages, empty = full_x + 8 * kStages, converted_full = empty + 8 * kStages,
                    converted_empty = converted_full + 8 * kConverted, sum_full = converted_empty + 8 * kConverted, sum_empty = sum_full + 16,
                    drained = sum_empty + 16;
-    __shared__ uint32_t tensor_base;
-    __shared__ int over;
+    __shared__ uint32_t tensor_base, issued_stages[2];  // (issued: this block's stages, and the pair's other's once a wait has run out)
+    __shared__ int over;  // a wait has run out in any block of the cluster
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = PAIR ? cluster_rank() : 0;              // in the pair
     const int part = PAIR ? 0 : static_cast<int>(cluster_rank());  // of t
@@ -144,7 +144,8 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
     launch_dependents();
     dependency_wait();
     const uint32_t tensor = tensor_base;
-    const Bounds bounds{&over, p.status};
+    Bounds bounds{&over, p.status, static_cast<uint32_t>(PAIR ? 2 : p.split)};
+    const Withheld withheld = withheld_of(bounds, PAIR ? rank : part);
     const bool quarters = !PAIR && p.after >= 0;
     const int side = quarters ? 256 : kSide, tiles = p.tiles;
     const int down = static_cast<int>((p.outer + side - 1) / side), across = static_cast<int>((p.x.cols + side - 1) / side);
@@ -161,40 +162,40 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
         if (quarters) *m = 2 * *m + (t & 1), *n = 2 * *n + (t >> 1 & 1);
     };
 
+    const uint32_t dy_there = PAIR ? address_in(full_dy, 0) : full_dy;
+    const auto load = [&](uint32_t stage, int row, int col, int kb) {
+        const uint32_t at = base + stage * kStageBytes, bar = dy_there + 8 * stage;
+        if (rank == 0) barrier_expect(full_dy + 8 * stage, kBlocks * (READY ? 4 : 2) * kAtom);
+        if constexpr (READY) {
+            load_tile<PAIR>(at + 2 * kAtom, &maps.x, col, kb * kDepth, bar);
+            load_tile<PAIR>(at + 3 * kAtom, &maps.x, col + 64, kb * kDepth, bar);
+        } else {
+            barrier_expect(full_x + 8 * stage, kAtom);
+            load_tile<false>(at + 2 * kAtom, &maps.x, col, kb * kDepth, full_x + 8 * stage);
+        }
+        load_tile<PAIR>(at, &maps.dy, row, kb * kDepth, bar);
+        load_tile<PAIR>(at + kAtom, &maps.dy, row + 64, kb * kDepth, bar);
+    };
+
     if (warp < 4) {
         if constexpr (!READY) fewer_registers<kFew>();
         if (warp == 0 && elected()) {
             Turn<kStages> turn;
             uint32_t issued = 0;
             bool ok = true;
-            const uint32_t full_there = PAIR ? address_in(full_dy, 0) : full_dy;
             for (int t = blockIdx.x / team; t < tiles && ok; t += step) {
                 int m, n;
                 tile_at(t, &m, &n);
                 const int row = m * kSide + rank * 128, col = n * kSide + rank * 128;
                 for (int kb = begin; kb < end; ++kb) {
-                    const uint32_t at = base + turn.at * kStageBytes;
-                    ok = barrier_wait<PAIR>(empty + 8 * turn.at, turn.parity ^ 1, bounds);
+                    ok = !(withheld.copies && issued >= kStages + kWithheldFrom) && barrier_wait<PAIR>(empty + 8 * turn.at, turn.parity ^ 1, bounds);
                     if (!ok) break;
-                    if (rank == 0) barrier_expect(full_dy + 8 * turn.at, kBlocks * (READY ? 4 : 2) * kAtom);
-                    if constexpr (READY) {
-                        load_tile<PAIR>(at + 2 * kAtom, &maps.x, col, kb * kDepth, full_there + 8 * turn.at);
-                        load_tile<PAIR>(at + 3 * kAtom, &maps.x, col + 64, kb * kDepth, full_there + 8 * turn.at);
-                    } else {
-                        barrier_expect(full_x + 8 * turn.at, kAtom);
-                        load_tile<false>(at + 2 * kAtom, &maps.x, col, kb * kDepth, full_x + 8 * turn.at);
-                    }
-                    load_tile<PAIR>(at, &maps.dy, row, kb * kDepth, full_there + 8 * turn.at);
-                    load_tile<PAIR>(at + kAtom, &maps.dy, row + 64, kb * kDepth, full_there + 8 * turn.at);
+                    load(turn.at, row, col, kb);
                     turn.next();
                     ++issued;
                 }
             }
-            if (!ok)  // copies in flight have to land before the block ends
-                for (uint32_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i) {
-                    const uint32_t s = i % kStages, parity = (i / kStages) & 1;
-                    for (int polls = 0; polls < kLandings && !((rank != 0 || barrier_passed<PAIR>(full_dy + 8 * s, parity)) && (READY || barrier_passed(full_x + 8 * s, parity))); ++polls) {}
-                }
+            issued_stages[rank] = issued;
         } else if (warp == 1 && rank == 0 && elected()) {
             constexpr uint32_t product = product_bf16(kSide, kSide, true, true);
             const uint64_t a0 = operand(base, kAtom), b0 = operand(READY ? base + 2 * kAtom : converted, kAtom);
@@ -260,6 +261,8 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (kb0 + 2 * i >= end) break;
+                    ok = !(withheld.scales && it0 + (kb0 + 2 * i - begin) >= kStages + kWithheldFrom);
+                    if (!ok) break;
                     const uint32_t it = it0 + (kb0 + 2 * i - begin), s = it % kStages, c = it % kConverted;
                     ok = warp_wait(full_x + 8 * s, (it / kStages) & 1, bounds) && warp_wait<PAIR>(converted_empty + 8 * c, ((it / kConverted) & 1) ^ 1, bounds);
                     if (!ok) break;
@@ -288,10 +291,11 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
         const uint32_t mine = tensor + (quarter << 21) + half * kHeld;
         const auto place = [](int j) { return READY ? j : turned(j); };
         uint32_t run = 0;
-        bool ok = true;
-        for (int t = blockIdx.x / team; t < tiles && ok; t += step) {
+        int t = blockIdx.x / team;
+        for (; t < tiles; t += step) {
             int m, n;
             tile_at(t, &m, &n);
+            bool ok = true;
             float sum[kHeld];
 #pragma unroll
             for (int i = 0; i < kHeld; ++i) sum[i] = 0.0f;
@@ -377,6 +381,27 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
     tensor_fence_before();
     __syncthreads();
     cluster_barrier();
+    if (__builtin_expect(over, 0)) {
+        if (PAIR) {
+            // As in matmul_many_kernel: stages that one block did not ask for any more are filled up, and all copies land before
+            // either block ends.
+            if (threadIdx.x == 0) store_in(address_in(shared_address(&issued_stages[rank]), rank ^ 1), issued_stages[rank]);
+            __syncwarp();
+            cluster_barrier();
+            if (threadIdx.x == 0) {
+                const uint32_t all = max(issued_stages[0], issued_stages[1]);
+#pragma unroll 1
+                for (uint32_t i = issued_stages[rank]; i < all; ++i) load(i % kStages, 0, 0, 0);
+                if (rank == 0) land<kStages, PAIR>(full_dy, all);
+                if (!READY) land<kStages>(full_x, all);
+            }
+        } else if (warp == 0) {
+            land<kStages>(full_dy, issued_stages[0]);
+            if (!READY) land<kStages>(full_x, issued_stages[0]);
+        }
+        __syncwarp();
+        if (PAIR) cluster_barrier();
+    }
     if (!PAIR && p.split > 1) {
         if (warp >= kFirstHolder) {  // this block's share of the rows, eight columns a thread
             int m, n;
