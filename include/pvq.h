@@ -354,7 +354,7 @@ int pvq_fp8_dequantize(const pvq_fp8_matrix* q, void* d_out, int dtype, int64_t 
  * PVQ_ERR_UNSUPPORTED).  a->cols must be b's k.
  *   d_status   optional device word; PVQ_STATUS_STAGING_TIMEOUT is OR-ed into it when a thread
  *              block gave up waiting for its copies (a bounded wait; not expected to happen; its
- *              part of the output is then not valid).  May be NULL. */
+ *              part of the output is then NaN).  May be NULL. */
 int pvq_fp8_matmul(const pvq_fp8_matrix* a, const pvq_fp8_matrix* b, int transposed, void* d_out, int dtype, int64_t ld_out,
                    uint32_t* d_status, pvq_stream_t stream);
 

@@ -240,6 +240,9 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
                         else asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + (c + i) * kShare * 4), "f"(v[i]) : "memory");
                     }
             }
+        } else if (SPLIT > 1) {  // a part that is missing is NaN
+#pragma unroll 1
+            for (int r = 0; r < rows; ++r) store_in(to + r * kShare * 4, 0x7fffffffu);
         }
         tensor_fence_before();
     }
@@ -248,7 +251,13 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
     if (SPLIT > 1) cluster_barrier();
     else __syncthreads();
     add_parts<ROWS, SPLIT, T>(parts, rank, p, row0, col0);
-    if (warp == 0 && __builtin_expect(over, 0)) land<S::kStages>(full, issued_stages);  // copies in flight have to land before the block ends
+    if (__builtin_expect(over, 0)) {
+        if (SPLIT == 1) {
+            __syncthreads();
+            if (32 * warp < ROWS) spoil(static_cast<T*>(p.out), p.ld, row0 + 32 * warp, min(p.rows, row0 + ROWS), col0, p.outs, 128);
+        }
+        if (warp == 0) land<S::kStages>(full, issued_stages);  // copies in flight have to land before the block ends
+    }
     if (warp == 2) {
         tensor_fence_after();
         tensor_free<false>(tensor, S::kColumns);

@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
     const uint32_t full = bars, empty = full + 8 * kStages, scales_full = empty + 8 * kStages, scales_empty = scales_full + 16, sum_full = scales_empty + 16,
                    sum_empty = sum_full + 16, shared_empty = sum_empty + 16, drained = shared_empty + 8;
     __shared__ uint32_t tensor_base, issued_stages[2];  // (issued: this block's stages, and the other's once a wait has run out)
+    __shared__ int lost_from[8];  // a warp's first tile without a result
     __shared__ int over;  // a wait has run out in either block
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -317,6 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
                 ++item;
             }
         }
+        if (lane == 0) lost_from[warp - 8] = t;
         if (lane == 0) store_wait_all();
     }
     __syncwarp();
@@ -335,6 +337,13 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_many_kernel(const __grid_c
             for (uint32_t i = issued_stages[rank]; i < all; ++i) load(i % kStages, 0, 0, 0);
             if (rank == 0) land<kStages, true>(full, all);
         }
+        if (warp >= 8)
+#pragma unroll 1
+            for (int t = lost_from[warp - 8]; t < tiles.count(); t += step) {
+                int m, n;
+                tiles.at(t, &m, &n);
+                spoil(static_cast<T*>(p.out), p.ld, int64_t(m) * 256 + rank * 128 + (warp & 3) * 32, p.rows, int64_t(n) * 256 + (warp - 8) / 4 * 128, p.outs, 128);
+            }
         __syncwarp();
         cluster_barrier();
     }

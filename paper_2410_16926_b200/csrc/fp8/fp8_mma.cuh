@@ -351,6 +351,14 @@ __device__ __forceinline__ void land(uint32_t full, uint32_t issued) {
 #pragma unroll 1
         for (int polls = 0; polls < kLandings && !barrier_passed<CLUSTER>(full + 8 * (i % STAGES), (i / STAGES) & 1); ++polls) {}
 }
+// What was not computed becomes NaN: a warp's 32 rows, a lane's own, of `width` columns.
+template <class T>
+__device__ __forceinline__ void spoil(T* out, int64_t ld, int64_t row, int64_t rows, int64_t col, int64_t cols, int width) {
+    row += threadIdx.x & 31;
+    if (row >= rows) return;
+#pragma unroll 1
+    for (int i = 0; i < width && col + i < cols; ++i) out[row * ld + col + i] = T(__uint_as_float(0x7fffffffu));
+}
 
 // ---- scales in tensor memory
 

@@ -121,7 +121,8 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
                    converted_empty = converted_full + 8 * kConverted, sum_full = converted_empty + 8 * kConverted, sum_empty = sum_full + 16,
                    drained = sum_empty + 16;
     __shared__ uint32_t tensor_base, issued_stages[2];  // (issued: this block's stages, and the pair's other's once a wait has run out)
-    __shared__ int over;  // a wait has run out in any block of the cluster
+    __shared__ int lost_from[8];  // a warp's first tile without a result
+    __shared__ int over;          // a wait has run out in any block of the cluster
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = PAIR ? cluster_rank() : 0;              // in the pair
     const int part = PAIR ? 0 : static_cast<int>(cluster_rank());  // of t
@@ -375,6 +376,7 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
                 }
             }
         }
+        if (lane == 0) lost_from[warp - kFirstHolder] = t;
         if (lane == 0) store_wait_all();
     }
     __syncwarp();
@@ -399,10 +401,19 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
             land<kStages>(full_dy, issued_stages[0]);
             if (!READY) land<kStages>(full_x, issued_stages[0]);
         }
+        if (warp >= kFirstHolder && (PAIR || p.split == 1))
+#pragma unroll 1
+            for (int t = lost_from[warp - kFirstHolder]; t < tiles; t += step) {
+                int m, n;
+                tile_at(t, &m, &n);
+                spoil(static_cast<T*>(p.out), p.ld, int64_t(m) * kSide + rank * 128 + (warp & 3) * 32, p.outer,
+                      int64_t(n) * kSide + (warp - kFirstHolder) / 4 * kHeld, p.x.cols, kHeld);
+            }
         __syncwarp();
         if (PAIR) cluster_barrier();
     }
     if (!PAIR && p.split > 1) {
+        const bool lost = over;
         if (warp >= kFirstHolder) {  // this block's share of the rows, eight columns a thread
             int m, n;
             tile_at(blockIdx.x / team, &m, &n);
@@ -420,6 +431,9 @@ __global__ void __launch_bounds__(Shape<READY>::kThreads, 1) weight_grad_kernel(
                     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(hi.x), "=f"(hi.y), "=f"(hi.z), "=f"(hi.w) : "r"(hi_at));
                     v[0] += lo.x, v[1] += lo.y, v[2] += lo.z, v[3] += lo.w, v[4] += hi.x, v[5] += hi.y, v[6] += hi.z, v[7] += hi.w;
                 }
+                if (lost)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7fffffffu);
                 T* to = static_cast<T*>(p.out) + row * p.ld + int64_t(n) * 128 + col;
                 if (left >= 8) {
                     if constexpr (sizeof(T) == 2) {

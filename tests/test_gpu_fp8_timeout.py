@@ -1,5 +1,5 @@
 """Copies or scales of the 8-bit products and weight gradients that never arrive: every wait is bounded, the call ends, its status word says so,
-nothing outside its output is written, and the same call goes through afterwards.  On the bounds-checked build (in a child
+what was not computed is NaN, nothing else is written, and the same call goes through afterwards.  On the bounds-checked build (in a child
 process), which leaves them out where the status word asks for it, some stages into the call, and then waits for a short while only."""
 import os
 import subprocess
@@ -50,9 +50,11 @@ assert status == 0 and bool(torch.isfinite(want).all())
 for name, bits in (("copies", COPIES), ("second", SECOND), ("scales", SCALES)):
     got, status, took = run(bits)
     bits &= 0xffffffff
+    lost = torch.isnan(got)
+    assert bool((lost | (got == want)).all()), (name, "neither right nor NaN")
     over = status != bits
-    assert status == (bits | pvq.STATUS_STAGING_TIMEOUT if over else bits) and (over or torch.equal(got, want)), (name, hex(status))
-    print("RESULT", name, "over" if over else "through", "%.3f s" % took)
+    assert status == (bits | pvq.STATUS_STAGING_TIMEOUT if over else bits) and over == bool(lost.any()), (name, hex(status))
+    print("RESULT", name, "over" if over else "through", "%.3f of the values lost, %.3f s" % (float(lost.float().mean()), took))
     assert took < 5.0
     again, status, _ = run(0)
     assert status == 0 and torch.equal(again, want), (name, "the next call")
