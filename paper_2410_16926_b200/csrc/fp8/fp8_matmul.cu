@@ -27,7 +27,7 @@ int matmul(const Matrix& a, const Matrix& b, bool transposed, void* out, bool bf
             if (tiles > clusters && !second) break;
             split = next;
         }
-    if (!bf16)  // (long fp32 sums in parts, as matmul_many's)
+    if (!bf16)  // (long fp32 sums in parts, as matmul_many's; eight of them have runs beyond that)
         while (split < 8 && blocks > 64 * split) split *= 2;
     return matmul_few(p, transposed, bf16, split, s);
 }

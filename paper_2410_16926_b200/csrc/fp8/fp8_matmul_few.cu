@@ -22,6 +22,11 @@ namespace fp8 {
 namespace {
 
 constexpr int kThreads = 256;
+// fp32 results: what a block sums in tensor memory, whose sums are cut off and not rounded, is at most about 64 blocks along k, as in
+// matmul_many_kernel.  Where a part of a cluster of eight has more, it goes where it is added in runs of so many sets of scales, of
+// four blocks each.  (200000 values: 2.2e-6 of the result off in eight parts alone, 4.9e-7 so; 128 rows,
+// 128256 to 4096, 175 us and 185.)
+constexpr int kRunSets = 16;
 
 template <int ROWS, int SPLIT>
 struct Shape {
@@ -88,10 +93,11 @@ __device__ __forceinline__ void add_parts(uint32_t parts, int rank, const Matmul
 template <int ROWS, int SPLIT, bool ACROSS, class T>
 __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_constant__ Maps maps, const __grid_constant__ MatmulArgs p) {
     using S = Shape<ROWS, SPLIT>;
+    constexpr bool kRuns = SPLIT == 8 && sizeof(T) == 4;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
     const uint32_t parts = base + S::kPartsAt, full = base + S::kBarsAt, empty = full + 8 * S::kStages, scales_full = empty + 8 * S::kStages,
-                   scales_empty = scales_full + 8 * S::kScaleSets, sum_full = scales_empty + 8 * S::kScaleSets, drained = sum_full + 8;
+                   scales_empty = scales_full + 8 * S::kScaleSets, sum_full = scales_empty + 8 * S::kScaleSets, drained = sum_full + 8, sum_empty = drained + 8;
     __shared__ uint32_t tensor_base, issued_stages;
     __shared__ int over;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -125,10 +131,10 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
         }
     };
     if (warp == 0) {
-        // a barrier a lane: stages' full and empty, the scales' sets full and empty, the sum, drained
-        constexpr int kBars = 2 * S::kStages + 2 * S::kScaleSets + 2;
+        // a barrier a lane: stages' full and empty, the scales' sets full and empty, the sum's full, drained, the sum's empty
+        constexpr int kBars = 2 * S::kStages + 2 * S::kScaleSets + (kRuns ? 3 : 2);
         static_assert(kBars <= 32, "one lane each");
-        if (lane < kBars) barrier_init(full + 8 * lane, lane >= 2 * S::kStages && lane < 2 * S::kStages + S::kScaleSets ? 4 : 1);
+        if (lane < kBars) barrier_init(full + 8 * lane, (lane >= 2 * S::kStages && lane < 2 * S::kStages + S::kScaleSets) || (kRuns && lane == kBars - 1) ? 4 : 1);
         barrier_init_fence();
         if (lane == 0) over = 0;
         __syncwarp();
@@ -171,7 +177,8 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
             const uint64_t w0 = operand(base, ACROSS ? 128 * kBlock : 16), x0 = operand(base + 128 * kBlock);
             Turn<S::kStages> turn;
             Turn<S::kScaleSets> scales;
-            bool ok = true, there = false;
+            bool ok = true, there = false, starts = true;
+            uint32_t run = 0;
             for (int kb = first; kb < last; ++kb) {
                 const uint32_t part = kb & 3;
                 if (part == 0 || kb == first) ok = barrier_wait(scales_full + 8 * scales.at, scales.parity, bounds);
@@ -184,11 +191,19 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
                 const uint64_t w = w0 + now.at * (S::kStageBytes >> 4), x = x0 + now.at * (S::kStageBytes >> 4);
                 const uint32_t sw = tensor + S::kScales + 8 * scales.at, with = with_part(product, part);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) multiply_e4m3<false>(tensor, w + kAlongW * k, x + 2 * k, with, sw, sw + 4, kb > first || k > 0);
+                for (int k = 0; k < 4; ++k) multiply_e4m3<false>(tensor, w + kAlongW * k, x + 2 * k, with, sw, sw + 4, (kRuns ? !starts : kb > first) || k > 0);
+                starts = false;
                 products_done<false>(empty + 8 * now.at);
                 if (part == 3) {
                     products_done<false>(scales_empty + 8 * scales.at);
                     scales.next();
+                }
+                if (kRuns && part == 3 && kb + 1 < last && ((kb + 1) / 4 - first / 4) % kRunSets == 0) {
+                    products_done<false>(sum_full);
+                    ok = barrier_wait(sum_empty, run & 1, bounds);
+                    if (!ok) break;
+                    ++run;
+                    starts = true;
                 }
             }
             products_done<false>(ok ? sum_full : drained);
@@ -196,11 +211,56 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
         }
     } else if (warp >= 4) {
         const uint32_t mine = tensor + ((warp & 3) << 21);
+        constexpr int kShare = 128 / SPLIT;
+        const int column = (warp & 3) * 32 + lane;
+        // A lane's column of the part goes to the block whose share it is in; kRuns: is added to what is there.
+        const auto place = [&]() -> uint32_t {
+            const uint32_t at = parts + (rank * ROWS * kShare + column % kShare) * 4;
+            return SPLIT > 1 ? address_in(at, column / kShare) : at;
+        };
+        const auto put_sum = [&](uint32_t to, int rows, bool add) {
+            tensor_fence_after();
+#pragma unroll
+            for (int c = 0; c < ROWS; c += 16) {
+                if (c >= rows) break;
+                float v[16];
+                tensor_load(mine + c, v);
+                tensor_wait_loads();
+                if (kRuns && add) {
+                    float before[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c + i < rows) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(before[i]) : "r"(to + (c + i) * kShare * 4) : "memory");
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c + i < rows) v[i] += before[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (c + i < rows) {
+                        if (SPLIT > 1) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + (c + i) * kShare * 4), "f"(v[i]) : "memory");
+                        else asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + (c + i) * kShare * 4), "f"(v[i]) : "memory");
+                    }
+            }
+        };
+        uint32_t run = 0;
+        bool met = false;
         Turn<S::kScaleSets> turn;
         bool ok = true;
         // asked for as many steps at once as there are sets of columns: to wait for one before the next is a microsecond each
         for (int f0 = first / 4; f0 <= (last - 1) / 4 && ok; f0 += S::kScaleSets) {
             if (f0 > first / 4) scales_of(f0);
+            if (kRuns && f0 > first / 4 && (f0 - first / 4) % kRunSets == 0) {
+                ok = warp_wait(sum_full, run & 1, bounds);
+                if (!met) cluster_wait();
+                met = true;
+                if (!ok) break;
+                put_sum(place(), static_cast<int>(min(int64_t(ROWS), p.rows - row0)), run > 0);
+                ++run;
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(sum_empty);
+            }
 #pragma unroll
             for (int i = 0; i < S::kScaleSets; ++i) {
                 if (f0 + i > (last - 1) / 4) break;
@@ -217,29 +277,12 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
                 turn.next();
             }
         }
-        ok = ok && warp_wait(sum_full, 0, bounds);
-        if (SPLIT > 1) cluster_wait();
-        // a lane's column of the part goes to the block whose share it is in
-        constexpr int kShare = 128 / SPLIT;
-        const int column = (warp & 3) * 32 + lane;
-        const uint32_t mine_at = parts + (rank * ROWS * kShare + column % kShare) * 4;
-        const uint32_t to = SPLIT > 1 ? address_in(mine_at, column / kShare) : mine_at;
+        ok = ok && warp_wait(sum_full, kRuns ? run & 1 : 0, bounds);
+        if (SPLIT > 1 && !(kRuns && met)) cluster_wait();
+        const uint32_t to = place();
         const int rows = static_cast<int>(min(int64_t(ROWS), p.rows - row0));
         if (__builtin_expect(ok, 1)) {
-            tensor_fence_after();
-#pragma unroll
-            for (int c = 0; c < ROWS; c += 16) {
-                if (c >= rows) break;
-                float v[16];
-                tensor_load(mine + c, v);
-                tensor_wait_loads();
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (c + i < rows) {
-                        if (SPLIT > 1) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + (c + i) * kShare * 4), "f"(v[i]) : "memory");
-                        else asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + (c + i) * kShare * 4), "f"(v[i]) : "memory");
-                    }
-            }
+            put_sum(to, rows, kRuns && run > 0);
         } else if (SPLIT > 1) {  // a part that is missing is NaN
 #pragma unroll 1
             for (int r = 0; r < rows; ++r) store_in(to + r * kShare * 4, 0x7fffffffu);
