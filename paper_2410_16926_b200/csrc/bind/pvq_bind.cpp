@@ -753,7 +753,7 @@ PyObject* bind_fp8_gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// fp8_weight_grad(dy, codes x, scales x, tile x, dtype, out, status)
+// fp8_weight_grad(dy, codes x, scales x, tile x, dtype, out, status, workspace)
 PyObject* bind_fp8_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     Place place;
@@ -762,7 +762,7 @@ PyObject* bind_fp8_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Refs refs;
     long long dtype;
     void* status;
-    if (!want_args(n, 7) || !values(a[0], &place, &dy) || !typed(*dy.t, at::kBFloat16) || !fp8_matrix(a[1], a[2], a[3], &place, &x) ||
+    if (!want_args(n, 8) || !values(a[0], &place, &dy) || !typed(*dy.t, at::kBFloat16) || !fp8_matrix(a[1], a[2], a[3], &place, &x) ||
         !integer(a[4], &dtype))
         return nullptr;
     if (dy.rows != x.rows) {
@@ -770,13 +770,20 @@ PyObject* bind_fp8_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return nullptr;
     }
     if (!values_out(a[5], &place, static_cast<int>(dtype), dy.cols, x.cols, &out, &refs.r[0]) || !status_word(a[6], &place, &status)) return nullptr;
-    const size_t bytes = lib.fp8_weight_grad_workspace(x.rows, x.cols, dy.cols);
+    const int with = PyObject_IsTrue(a[7]);
+    if (with < 0) return nullptr;
+    const size_t bytes = with ? lib.fp8_weight_grad_workspace(x.rows, x.cols, dy.cols) : 0;
     at::Tensor workspace;  // (of the current stream: what comes after on it may have the memory once the call's work is done)
-    if (bytes) workspace = at::detail::empty_cuda({static_cast<int64_t>(bytes)}, at::kByte, *place.dev, std::nullopt);
-    void* const w = bytes ? workspace.data_ptr() : nullptr;
+    if (bytes) {
+        try {
+            workspace = at::detail::empty_cuda({static_cast<int64_t>(bytes)}, at::kByte, *place.dev, std::nullopt);
+        } catch (const c10::OutOfMemoryError&) {  // the same result without it
+        }
+    }
+    void* const w = workspace.defined() ? workspace.data_ptr() : nullptr;
     void* s = stream();
     if (failed(unlocked([&] {
-                   return lib.fp8_weight_grad(dy.p, dy.cols, dy.ld, &x, out.p, out.dtype, out.ld, w, bytes, static_cast<uint32_t*>(status), s);
+                   return lib.fp8_weight_grad(dy.p, dy.cols, dy.ld, &x, out.p, out.dtype, out.ld, w, w ? bytes : 0, static_cast<uint32_t*>(status), s);
                }),
                "pvq_fp8_weight_grad"))
         return nullptr;

@@ -346,6 +346,8 @@ def fp8_gated_backward(dh, gate, up, act="silu", out=(None, None)):
     return (_native or _load_native()).fp8_gated_backward(dh, gate[0], gate[1], up[0], up[1], _activation(act), *out)
 
 
-def fp8_weight_grad(dy, x, dtype=torch.float32, out=None, status=None):
-    """dy [tokens][outputs] bfloat16 transposed, times the values of x [tokens][inputs] -> [outputs][inputs]."""
-    return (_native or _load_native()).fp8_weight_grad(dy, x[0], x[1], x[2], _value_type(dtype), out, status)
+def fp8_weight_grad(dy, x, dtype=torch.float32, out=None, status=None, workspace=True):
+    """dy [tokens][outputs] bfloat16 transposed, times the values of x [tokens][inputs] -> [outputs][inputs].  Large
+    products take 2 bytes a value of x from torch's allocator for the length of the call, where it has them; without
+    (`workspace` false) they give the same bits, somewhat slower."""
+    return (_native or _load_native()).fp8_weight_grad(dy, x[0], x[1], x[2], _value_type(dtype), out, status, workspace)
