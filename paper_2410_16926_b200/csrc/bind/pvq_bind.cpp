@@ -9,6 +9,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -468,10 +469,23 @@ bool at_place(const at::Tensor& t, Place* p) {
     return true;
 }
 
+// These calls record nothing for autograd: what requires a gradient would lose it without a word.
+bool no_gradient(const at::Tensor& t) {
+    if (!t.requires_grad() || !c10::GradMode::is_enabled()) return true;
+    PyErr_SetString(PyExc_ValueError, "a tensor that requires a gradient: nothing is recorded for autograd (detach it, or call under torch.no_grad())");
+    return false;
+}
+// A caller's tensor was written to: autograd has to know where it was saved for a backward pass.
+void written(PyObject* o) {
+    if (o == Py_None) return;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // A matrix with unit steps along its rows; *ld is its leading dimension, for a single row the smallest multiple of `unit`.
 const at::Tensor* matrix(PyObject* o, Place* place, int64_t unit, int64_t* ld) {
     const at::Tensor* t = tensor_of(o);
-    if (!t || !at_place(*t, place)) return nullptr;
+    if (!t || !no_gradient(*t) || !at_place(*t, place)) return nullptr;
     if (t->dim() != 2) {
         PyErr_SetString(PyExc_ValueError, "expected a matrix");
         return nullptr;
@@ -651,6 +665,7 @@ PyObject* bind_fp8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!want_args(n, 3) || !values(a[0], &place, &x) || !fp8_out(a[2], &place, x.rows, x.cols, a[1], &q, &refs.r[0], &refs.r[1])) return nullptr;
     void* s = stream();
     if (failed(unlocked([&] { return lib.fp8_quantize(x.p, x.dtype, x.ld, &q, s); }), "pvq_fp8_quantize")) return nullptr;
+    if (a[2] != Py_None) written(refs.r[0]), written(refs.r[1]);
     return refs.tuple(2);
     END_HANDLE_TH_ERRORS
 }
@@ -668,6 +683,7 @@ PyObject* bind_fp8_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return nullptr;
     void* s = stream();
     if (failed(unlocked([&] { return lib.fp8_dequantize(&q, out.p, out.dtype, out.ld, s); }), "pvq_fp8_dequantize")) return nullptr;
+    written(a[4]);
     return refs.one();
     END_HANDLE_TH_ERRORS
 }
@@ -694,6 +710,7 @@ PyObject* bind_fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* s = stream();
     if (failed(unlocked([&] { return lib.fp8_matmul(&ma, &mb, transposed, out.p, out.dtype, out.ld, static_cast<uint32_t*>(status), s); }), "pvq_fp8_matmul"))
         return nullptr;
+    written(a[8]);
     return refs.one();
     END_HANDLE_TH_ERRORS
 }
@@ -749,6 +766,7 @@ PyObject* bind_fp8_gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
                }),
                "pvq_fp8_gated_backward"))
         return nullptr;
+    written(a[6]), written(a[7]);
     return refs.tuple(2);
     END_HANDLE_TH_ERRORS
 }
@@ -787,6 +805,7 @@ PyObject* bind_fp8_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
                }),
                "pvq_fp8_weight_grad"))
         return nullptr;
+    written(a[5]);
     return refs.one();
     END_HANDLE_TH_ERRORS
 }

@@ -288,6 +288,8 @@ def decode_batched(items, N, K, scale_bits, table, status=None):
 # codes: float8_e4m3fn [rows][cols]; scales: float8_e8m0fnu [rows][ceil(cols / 128)], or, where `tile` is true,
 # [ceil(rows / 128)][ceil(cols / 128)].  Rows of codes start on 16-byte boundaries, rows of scales on 4-byte boundaries
 # (the calls' results do; where the widths are no such multiples, they are views of wider tensors).
+# Nothing is recorded for autograd: a tensor that requires a gradient is refused, unless gradients are off (as they are in the
+# forward and backward of a torch.autograd.Function).  Writing into `out` counts as a change of that tensor.
 Fp8Matrix = collections.namedtuple("Fp8Matrix", "codes scales tile")
 
 ACTIVATIONS = {"silu": 0, "gelu": 1}
