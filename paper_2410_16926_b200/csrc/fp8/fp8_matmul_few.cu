@@ -122,12 +122,7 @@ __global__ void __launch_bounds__(kThreads) matmul_few_kernel(const __grid_const
         for (int i = 0; i < S::kScaleSets; ++i) {
             if (f0 + i > (last - 1) / 4) break;
             scale_words<ACROSS>(p.b, col0, f0 + i, w[i]);
-            if (p.a.shift && ROWS < 128) {  // (the rows do not begin at a tile of its scales)
-#pragma unroll
-                for (int j = 0; j < S::kWordsB; ++j) x[i][j] = scale_word<false>(p.a, row0 + 32 * j + lane, f0 + i);
-            } else {
-                scale_words<false>(p.a, row0, f0 + i, x[i]);
-            }
+            scale_words<false>(p.a, row0, f0 + i, x[i]);  // (row0: a multiple of 128, or 0)
         }
     };
     if (warp == 0) {
