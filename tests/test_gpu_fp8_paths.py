@@ -51,8 +51,8 @@ def guarded(rows, cols, dtype):
 
 
 # rows of a tile, split of k: outputs and k that lead there, with more than 16 blocks of 128 for each part (8 stages at most, 16 blocks of scales)
-SHAPES = {(16, 8): (301, 20011), (16, 4): (5003, 9001), (16, 2): (12001, 4501), (16, 1): (13501, 2301),
-          (32, 8): (301, 20011), (32, 4): (5003, 9001), (32, 2): (12001, 4501), (32, 1): (13501, 2301),
+SHAPES = {(16, 8): (301, 20011), (16, 4): (5003, 9001), (16, 2): (12001, 5201), (16, 1): (13501, 2301),
+          (32, 8): (301, 20011), (32, 4): (5003, 9001), (32, 2): (12001, 5201), (32, 1): (13501, 2301),
           (64, 8): (301, 20011), (64, 4): (2501, 9001), (64, 2): (8003, 4501), (64, 1): (12001, 2301),
           (128, 8): (301, 20011), (128, 4): (2501, 9001), (128, 2): (8003, 4501), (128, 1): (12001, 2301)}
 
