@@ -9,10 +9,10 @@
 // Warps: one issues the copies, one the products, one allocates tensor memory, four bring the scales there (four blocks along k
 // at a time, in four sets of columns) and then read the result.
 //
-// What bounds it: memory, behind a start and an end.  One row, 4096 to 14336: 12.9 us, of which the weight's 58.7 MB take 9.1 at
+// What bounds it: memory, behind a start and an end.  One row, 4096 to 14336: 13.3 us, of which the weight's 58.7 MB take 9.1 at
 // the copy rate, which it runs at once the first tiles are there (after 2 to 4 us); the parts are added and stored in the last 1.5.
-// 33 rows, 14336 to 4096: 14.9 us (16.0 when each block read the others' shared memory, which needs a second meeting of the
-// cluster), 64 rows 4096 to 14336 14.4, 128 rows 16.7.
+// 33 rows, 14336 to 4096: 14.9 to 15.3 us (a microsecond more when each block read the others' shared memory, which needs a second
+// meeting of the cluster), 64 rows 4096 to 14336 14.7, 128 rows 17.7; with the transposed weight 15.7, 16.1 and 18.4.
 #include <atomic>
 
 #include "fp8_matmul.cuh"

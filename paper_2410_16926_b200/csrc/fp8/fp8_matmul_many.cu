@@ -12,7 +12,7 @@
 // columns, which are read first, so that the next tile's products wait for those alone (875 us for 16384 x 4096 by 14336 when
 // they waited for all, 829 so).
 //
-// What bounds it: the power limit.  16384 x 4096 by 14336 takes 800 to 840 us (2.3 to 2.4 PFLOP/s), at 1000 W and 1.15 GHz, with
+// What bounds it: the power limit.  16384 x 4096 by 14336 takes 790 to 840 us (2.3 to 2.4 PFLOP/s), at 1000 W and 1.15 GHz, with
 // the tensor cores at work nine cycles in ten; for a few milliseconds, at a full clock, 690 us.  Multicast copies, which would spare
 // the L2 cache half of its reads, are not used: they must never read another GPU's memory, and a kernel cannot see whose its
 // operands are.
