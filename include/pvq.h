@@ -368,7 +368,7 @@ int pvq_fp8_matmul(const pvq_fp8_matrix* a, const pvq_fp8_matrix* b, int transpo
 
 /* The middle of a gated feed-forward block: h = act(gate) * up, computed in fp32 (the sigmoid in act by the
  * GPU's approximate exponential and reciprocal, within (|w| + 3) 2^-22 of itself, w its argument: gate for
- * silu, sqrt(8/pi) (gate + 0.044715 gate^3) for gelu) and quantised as by
+ * silu, sqrt(8/pi) (gate + 0.044715 gate^3) for gelu; 0 below 2^-126) and quantised as by
  * pvq_fp8_quantize, ready for the next product.  `gate` and `up`, if given, receive the two inputs
  * in the same format, for pvq_fp8_gated_backward; NULL (both) in inference.  All three are in
  * blocks along rows and of the same shape. */

@@ -327,7 +327,8 @@ def fp8_dequantize(q, dtype=torch.bfloat16, out=None):
 
 def fp8_matmul(a, b, transposed=False, dtype=torch.bfloat16, out=None, status=None):
     """a [M][K] times b [N][K] transposed (activations times a weight), or, with `transposed`, a [M][K] times b [K][N] (a
-    gradient times the same weight; b in tiles) -> [M][N].  `status`: optional int32 device tensor of one element."""
+    gradient times the same weight; b in tiles) -> [M][N].  `status`: optional int32 device tensor of one element, into
+    which STATUS_STAGING_TIMEOUT is OR-ed where a bounded wait ran out; what was not computed then is NaN."""
     return (_native or _load_native()).fp8_matmul(a[0], a[1], a[2], b[0], b[1], b[2], transposed, _value_type(dtype), out, status)
 
 
