@@ -50,6 +50,8 @@ def guarded(rows, cols, dtype):
     return out, untouched
 
 
+# (How many clusters run at once differs between GPUs with the SMs that they have in a part: 33 to 37 of four, 15 to 18 of eight.  The numbers
+# of tiles here keep away from those.)
 # rows of a tile, split of k: outputs and k that lead there, with more than 16 blocks of 128 for each part (8 stages at most, 16 blocks of scales)
 SHAPES = {(16, 8): (301, 20011), (16, 4): (5003, 9001), (16, 2): (12001, 5201), (16, 1): (13501, 2301),
           (32, 8): (301, 20011), (32, 4): (5003, 9001), (32, 2): (12001, 5201), (32, 1): (13501, 2301),
@@ -75,7 +77,7 @@ def test_products_of_few_rows(high, split, dtype, transposed):
 
 
 @pytest.mark.parametrize("tiles", [(False, True), (True, True), (True, False)])
-@pytest.mark.parametrize("rows,inner,outer,split", [(300, 20011, 301, 8), (300, 9001, 1501, 2), (300, 2301, 5003, 1), (5000, 9001, 130, 1)])
+@pytest.mark.parametrize("rows,inner,outer,split", [(300, 20011, 301, 8), (300, 9001, 1701, 2), (300, 2301, 5003, 1), (5000, 9001, 130, 1)])
 def test_products_of_few_tiles(rows, inner, outer, split, tiles):
     """More rows than a tile has."""
     a, b = held(rows, inner, tiles[0], 1), held(outer, inner, tiles[1], 2)
