@@ -96,6 +96,9 @@ typedef enum {
 /* bit 2 of the decode status word: the table given to the call was not built for this (N,K)
  * (its header says so); nothing was decoded. */
 #define PVQ_STATUS_TABLE_MISMATCH 4u
+/* bit 3, of the calls on an 8-bit cache: a position without a place in the cache (a page number outside
+ * the pool, a length beyond its table or below the sequence's rows). */
+#define PVQ_STATUS_BAD_PAGE 8u
 
 typedef void* pvq_stream_t; /* a cudaStream_t */
 
@@ -394,6 +397,79 @@ int pvq_fp8_weight_grad(const void* d_dy, int64_t outer, int64_t ld_dy, const pv
 /* Bytes of workspace with which pvq_fp8_weight_grad is faster for an x of rows x inner and `outer` outputs;
  * 0 where it needs none. */
 size_t pvq_fp8_weight_grad_workspace(int64_t rows, int64_t inner, int64_t outer);
+
+/* ---- 8-bit key and value cache -------------------------------------------------------------- */
+
+/* Keys and values that a model keeps, quantised as they are written, read back, and attended to.  (The paper has
+ * no counterpart.)
+ *
+ * The cache: a pool of pages of `page` tokens (16, 32, 64 or 128), each for all `heads` heads, keys and
+ * values apart but laid out alike.  The format is the one above with another block: e4m3 codes, and one
+ * power-of-two scale 2^(byte - 127), from 2^-40 to 2^40, for each page and head.  dim is a multiple of 16, up to 128.
+ *   d_k, d_v                 code of token t of page p, head h, at p * page_step + h * head_step + t * token_step
+ *                            + (0 .. dim - 1); 16-byte aligned, steps (bytes) multiples of 16, none below dim.
+ *   d_k_scales, d_v_scales   scale byte of page p, head h, at p * scale_step + h.
+ * A scale outside the range counts as its end in attention.
+ *
+ * A step: which rows of a call belong to which sequence, and where their tokens lie.
+ *   d_table    [seqs][width], leading dimension ld_table: the numbers of a sequence's pages, in order.
+ *              Position i is token i % page of page table[i / page].  Entries behind a length are not read.  A table
+ *              holds up to 2^30 tokens.
+ *   d_lengths  [seqs] tokens of each sequence, those of this step among them.
+ *   d_starts   [seqs + 1] ascending: rows starts[s] .. starts[s + 1] - 1 are the last tokens of sequence
+ *              s.  Rows in front of the first and behind the last are neither read nor written.  NULL: one row a
+ *              sequence, rows == seqs.
+ * All three are on the device (int32) and only looked at there; what they say is checked there, too: no access
+ * leaves the pool, the table or the rows, whatever they hold, and PVQ_STATUS_BAD_PAGE is OR-ed into *d_status (optional) where a
+ * position has no place.  Calls keep nothing, and can be captured into graphs.  The same inputs give the same bits. */
+typedef struct {
+    uint8_t *d_k, *d_v, *d_k_scales, *d_v_scales;
+    int64_t pages;
+    int heads, page, dim;
+    int64_t page_step, head_step, token_step, scale_step;
+} pvq_fp8_cache;
+
+typedef struct {
+    const int32_t *d_table, *d_lengths, *d_starts;
+    int64_t seqs, rows, width, ld_table;
+} pvq_fp8_step;
+
+/* Quantise the rows' keys and values, [row][head][dim] of fp32 or bf16 (steps in elements, multiples of 4 or 8, 16-byte
+ * aligned), into their sequences' pages.  A page that the step begins gets the smallest scale s of the range with |x| <= 448 s
+ * for the finite values written to it (2^-40 for zeros).  A page that holds tokens of the sequence already keeps its scale, or
+ * takes that one where it is larger: the codes that it holds become those nearest to code * (old scale / new scale).  Codes
+ * are x / s, to nearest even; beyond 448 s (with s = 2^40) +-448; NaN and infinities the code NaN.
+ * Tokens without a place are not written.  Every page is written by one sequence (a page of two tables may be
+ * read by both, but what it holds after a step that writes it through both is not defined). */
+int pvq_fp8_cache_write(const pvq_fp8_cache* cache, const pvq_fp8_step* step, const void* d_k, int64_t k_row, int64_t k_head, const void* d_v,
+                        int64_t v_row, int64_t v_head, int dtype, uint32_t* d_status, pvq_stream_t stream);
+
+/* The values of the rows' tokens: code * scale, as fp32 (exact) or bf16 (exact).  Tokens without a place are zeros.  (With
+ * starts that count whole sequences, all that they hold.) */
+int pvq_fp8_cache_read(const pvq_fp8_cache* cache, const pvq_fp8_step* step, void* d_k, int64_t k_row, int64_t k_head, void* d_v, int64_t v_row,
+                       int64_t v_head, int dtype, uint32_t* d_status, pvq_stream_t stream);
+
+/* Attention of the rows' queries to everything that their sequences hold:
+ *   out[r][h] = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q[r][h] . k_j - lse),  over the positions j that row r sees,
+ * k_j and v_j of head h / (heads / cache->heads).  A row at position i (its sequence's last row: length - 1) sees j < length;
+ * with causal = 1 only j <= i; with window > 0 (and causal = 1) only j > i - window.  A row that sees nothing gets zeros, and -inf in
+ * d_lse.  Pages outside the pool count as keys and values of zero; what lies beyond a table is not seen.
+ *   d_q, d_out  [row][head][dim] bf16, steps in elements (multiples of 8), 16-byte aligned.  heads is a multiple of
+ *               cache->heads, at most 128 times it.
+ *   d_lse       [row][heads] fp32, or NULL: log sum_j exp(scale q . k_j).
+ *   scale       positive.
+ *   d_workspace pvq_fp8_attention_workspace bytes, 16-byte aligned, free again when the call's work is done.
+ *   d_status    as above, and PVQ_STATUS_STAGING_TIMEOUT when a thread block gave up waiting for its copies (its results are
+ *               NaN then).
+ * Scores and sums are held in fp32, over queries taken to 2^-17 of a row's largest value and weights to 2^-8 of
+ * themselves at worst, and the result rounded once.  What keys and values hold that no row of a block of rows sees has no
+ * influence, NaN or not; a NaN among the values that some row of a sequence sees may reach all of its rows in the call. */
+int pvq_fp8_attention(const pvq_fp8_cache* cache, const pvq_fp8_step* step, const void* d_q, int heads, int64_t q_row, int64_t q_head, int causal,
+                      int64_t window, float scale, void* d_out, int64_t out_row, int64_t out_head, float* d_lse, void* d_workspace,
+                      size_t workspace_bytes, uint32_t* d_status, pvq_stream_t stream);
+
+/* Bytes of workspace that a call of these sizes takes; 0 for sizes that are refused. */
+size_t pvq_fp8_attention_workspace(int64_t seqs, int64_t rows, int heads, int kv_heads);
 
 /* ---- bounds-checked build -------------------------------------------------------------- */
 

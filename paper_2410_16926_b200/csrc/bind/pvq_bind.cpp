@@ -44,6 +44,10 @@ struct Entries {
     decltype(&pvq_fp8_weight_grad) fp8_weight_grad;
     decltype(&pvq_fp8_scale_row_stride) fp8_scale_row_stride;
     decltype(&pvq_fp8_weight_grad_workspace) fp8_weight_grad_workspace;
+    decltype(&pvq_fp8_cache_write) fp8_cache_write;
+    decltype(&pvq_fp8_cache_read) fp8_cache_read;
+    decltype(&pvq_fp8_attention) fp8_attention;
+    decltype(&pvq_fp8_attention_workspace) fp8_attention_workspace;
 } lib;
 PyObject* raise_error = nullptr;  // raise_error(status, where) raises PvqError
 PyObject *k_get, *k_x, *k_out, *k_codes, *k_scale_idx, *k_row_norm, *k_edges, *k_levels, *k_cols;
@@ -810,6 +814,216 @@ PyObject* bind_fp8_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the 8-bit key and value cache
+
+const at::Tensor* of_dims(PyObject* o, Place* place, at::ScalarType type, int64_t dims, const char* what) {
+    const at::Tensor* t = tensor_of(o);
+    if (!t || !no_gradient(*t) || !at_place(*t, place) || !typed(*t, type)) return nullptr;
+    if (t->dim() != dims || (t->size(dims - 1) > 1 && t->stride(dims - 1) != 1)) {
+        PyErr_Format(PyExc_ValueError, "expected %s, of %lld dimensions and with unit steps along the last", what, static_cast<long long>(dims));
+        return nullptr;
+    }
+    return t;
+}
+
+// codes and scales of keys and values: four tensors
+bool fp8_cache(PyObject* const* a, Place* place, pvq_fp8_cache* c) {
+    const at::Tensor* t[4];
+    for (int i = 0; i < 4; ++i) {
+        t[i] = i < 2 ? of_dims(a[i], place, at::kFloat8_e4m3fn, 4, "codes [pages][heads][page][dim]")
+                     : of_dims(a[i], place, at::kFloat8_e8m0fnu, 2, "scales [pages][heads]");
+        if (!t[i]) return false;
+    }
+    if (t[0]->sizes() != t[1]->sizes() || t[2]->sizes() != t[3]->sizes() || t[0]->size(0) != t[2]->size(0) || t[0]->size(1) != t[2]->size(1)) {
+        PyErr_SetString(PyExc_ValueError, "the cache's tensors do not fit one another");
+        return false;
+    }
+    const auto step = [](const at::Tensor& x, int64_t d, int64_t least) { return x.size(d) > 1 ? x.stride(d) : least; };  // (of one there is no next)
+    c->dim = static_cast<int>(t[0]->size(3));
+    const int64_t row = (int64_t(c->dim) + 15) / 16 * 16;
+    const int64_t steps[2][4] = {{step(*t[0], 0, row), step(*t[0], 1, row), step(*t[0], 2, row), step(*t[2], 0, t[2]->size(1))},
+                                 {step(*t[1], 0, row), step(*t[1], 1, row), step(*t[1], 2, row), step(*t[3], 0, t[3]->size(1))}};
+    if (std::memcmp(steps[0], steps[1], sizeof steps[0]) != 0) {
+        PyErr_SetString(PyExc_ValueError, "keys and values are laid out differently");
+        return false;
+    }
+    if (t[0]->size(1) > INT32_MAX || t[0]->size(2) > INT32_MAX || t[0]->size(3) > INT32_MAX) {
+        PyErr_SetString(PyExc_ValueError, "the cache is too large");
+        return false;
+    }
+    c->pages = t[0]->size(0), c->heads = static_cast<int>(t[0]->size(1)), c->page = static_cast<int>(t[0]->size(2));
+    c->page_step = steps[0][0], c->head_step = steps[0][1], c->token_step = steps[0][2], c->scale_step = steps[0][3];
+    c->d_k = static_cast<uint8_t*>(t[0]->data_ptr()), c->d_v = static_cast<uint8_t*>(t[1]->data_ptr());
+    c->d_k_scales = static_cast<uint8_t*>(t[2]->data_ptr()), c->d_v_scales = static_cast<uint8_t*>(t[3]->data_ptr());
+    return true;
+}
+
+// table, lengths, starts or None; rows < 0: one a sequence, or not known
+bool fp8_step(PyObject* const* a, Place* place, int64_t rows, pvq_fp8_step* p) {
+    const at::Tensor* table = of_dims(a[0], place, at::kInt, 2, "a table of pages");
+    const at::Tensor* lengths = table ? of_dims(a[1], place, at::kInt, 1, "lengths") : nullptr;
+    if (!lengths) return false;
+    p->seqs = lengths->size(0), p->width = table->size(1), p->ld_table = table->size(0) > 1 ? table->stride(0) : table->size(1);
+    p->d_table = static_cast<const int32_t*>(table->data_ptr()), p->d_lengths = static_cast<const int32_t*>(lengths->data_ptr());
+    p->d_starts = nullptr;
+    p->rows = rows < 0 ? p->seqs : rows;
+    bool fits = table->size(0) == p->seqs;
+    if (a[2] != Py_None) {
+        const at::Tensor* starts = of_dims(a[2], place, at::kInt, 1, "starts");
+        if (!starts) return false;
+        if (rows < 0) {
+            PyErr_SetString(PyExc_ValueError, "expected the number of rows");
+            return false;
+        }
+        p->d_starts = static_cast<const int32_t*>(starts->data_ptr());
+        fits = fits && starts->size(0) == p->seqs + 1;
+    } else {
+        fits = fits && p->rows == p->seqs;
+    }
+    if (fits) return true;
+    PyErr_SetString(PyExc_ValueError, "table, lengths, starts and rows do not fit one another");
+    return false;
+}
+
+struct HeadRows {  // [row][head][dim] of fp32 or bf16
+    const at::Tensor* t;
+    void* p;
+    int dtype;
+    int64_t rows, heads, dim, row, head;
+};
+bool head_rows(PyObject* o, Place* place, HeadRows* x) {
+    x->t = tensor_of(o);
+    if (!x->t) return false;
+    if (x->t->scalar_type() != at::kFloat && x->t->scalar_type() != at::kBFloat16) {
+        PyErr_SetString(PyExc_TypeError, "expected float32 or bfloat16 rows");
+        return false;
+    }
+    x->dtype = x->t->scalar_type() == at::kFloat ? PVQ_DTYPE_F32 : PVQ_DTYPE_BF16;
+    if (!of_dims(o, place, x->t->scalar_type(), 3, "rows [row][head][dim]")) return false;
+    x->rows = x->t->size(0), x->heads = x->t->size(1), x->dim = x->t->size(2);
+    const int64_t least = (x->dim + 7) / 8 * 8;
+    x->row = x->rows > 1 ? x->t->stride(0) : least, x->head = x->heads > 1 ? x->t->stride(1) : least;
+    x->p = x->t->data_ptr();
+    return true;
+}
+bool rows_shaped(const HeadRows& x, int64_t rows, int64_t heads, int64_t dim) {
+    if (x.rows == rows && x.heads == heads && x.dim == dim) return true;
+    PyErr_Format(PyExc_ValueError, "expected rows of %lld x %lld x %lld", static_cast<long long>(rows), static_cast<long long>(heads), static_cast<long long>(dim));
+    return false;
+}
+bool head_rows_out(PyObject* o, Place* place, int dtype, int64_t rows, int64_t heads, int64_t dim, HeadRows* x, PyObject** result) {
+    if (o != Py_None) {
+        if (!head_rows(o, place, x)) return false;
+        if (x->dtype != dtype) {
+            PyErr_SetString(PyExc_TypeError, "the output is of another type");
+            return false;
+        }
+        if (!rows_shaped(*x, rows, heads, dim)) return false;
+        Py_INCREF(o);
+        *result = o;
+        return true;
+    }
+    x->dtype = dtype, x->rows = rows, x->heads = heads, x->dim = dim, x->head = dim, x->row = heads * dim;
+    at::Tensor t = at::detail::empty_cuda({rows, heads, dim}, dtype == PVQ_DTYPE_BF16 ? at::kBFloat16 : at::kFloat, *place->dev, std::nullopt);
+    x->p = t.data_ptr();
+    *result = THPVariable_Wrap(std::move(t));
+    return *result != nullptr;
+}
+
+// fp8_cache_write(k, v, codes k, codes v, scales k, scales v, table, lengths, starts, status)
+PyObject* bind_fp8_cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Place place;
+    HeadRows k, v;
+    pvq_fp8_cache c;
+    pvq_fp8_step p;
+    void* status;
+    if (!want_args(n, 10) || !head_rows(a[0], &place, &k) || !head_rows(a[1], &place, &v) || !fp8_cache(a + 2, &place, &c)) return nullptr;
+    if (k.dtype != v.dtype) {
+        PyErr_SetString(PyExc_TypeError, "keys and values are of different types");
+        return nullptr;
+    }
+    if (!rows_shaped(k, k.rows, c.heads, c.dim) || !rows_shaped(v, k.rows, c.heads, c.dim) || !fp8_step(a + 6, &place, k.rows, &p) ||
+        !status_word(a[9], &place, &status))
+        return nullptr;
+    void* s = stream();
+    if (failed(unlocked([&] { return lib.fp8_cache_write(&c, &p, k.p, k.row, k.head, v.p, v.row, v.head, k.dtype, static_cast<uint32_t*>(status), s); }),
+               "pvq_fp8_cache_write"))
+        return nullptr;
+    for (int i = 2; i < 6; ++i) written(a[i]);
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// fp8_cache_read(codes k, codes v, scales k, scales v, table, lengths, starts, rows or -1, dtype, k or None, v or None, status) -> (k, v)
+PyObject* bind_fp8_cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Place place;
+    HeadRows k, v;
+    pvq_fp8_cache c;
+    pvq_fp8_step p;
+    Refs refs;
+    void* status;
+    long long rows, dtype;
+    if (!want_args(n, 12) || !fp8_cache(a, &place, &c) || !integer(a[7], &rows) || !integer(a[8], &dtype) || !fp8_step(a + 4, &place, rows, &p) ||
+        !status_word(a[11], &place, &status))
+        return nullptr;
+    if (!head_rows_out(a[9], &place, static_cast<int>(dtype), p.rows, c.heads, c.dim, &k, &refs.r[0]) ||
+        !head_rows_out(a[10], &place, static_cast<int>(dtype), p.rows, c.heads, c.dim, &v, &refs.r[1]))
+        return nullptr;
+    void* s = stream();
+    if (failed(unlocked([&] { return lib.fp8_cache_read(&c, &p, k.p, k.row, k.head, v.p, v.row, v.head, static_cast<int>(dtype), static_cast<uint32_t*>(status), s); }),
+               "pvq_fp8_cache_read"))
+        return nullptr;
+    written(a[9]), written(a[10]);
+    return refs.tuple(2);
+    END_HANDLE_TH_ERRORS
+}
+
+// fp8_attention(q, codes k, codes v, scales k, scales v, table, lengths, starts, causal, window, scale, lse, out, status) -> out or (out, lse)
+PyObject* bind_fp8_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Place place;
+    HeadRows q, out;
+    pvq_fp8_cache c;
+    pvq_fp8_step p;
+    Refs refs;
+    void* status;
+    long long window;
+    if (!want_args(n, 14) || !head_rows(a[0], &place, &q) || !typed(*q.t, at::kBFloat16) || !fp8_cache(a + 1, &place, &c) ||
+        !fp8_step(a + 5, &place, q.rows, &p) || !integer(a[9], &window))
+        return nullptr;
+    const int causal = PyObject_IsTrue(a[8]), with_lse = PyObject_IsTrue(a[11]);
+    const double scale = PyFloat_AsDouble(a[10]);
+    if (causal < 0 || with_lse < 0 || PyErr_Occurred()) return nullptr;
+    if (q.dim != c.dim || c.heads < 1 || q.heads % c.heads != 0 || q.heads > INT32_MAX) {
+        PyErr_SetString(PyExc_ValueError, "the queries' heads are not those of the cache");
+        return nullptr;
+    }
+    if (!head_rows_out(a[12], &place, PVQ_DTYPE_BF16, q.rows, q.heads, q.dim, &out, &refs.r[0]) || !status_word(a[13], &place, &status)) return nullptr;
+    float* lse = nullptr;
+    if (with_lse) {
+        at::Tensor t = at::detail::empty_cuda({q.rows, q.heads}, at::kFloat, *place.dev, std::nullopt);
+        lse = static_cast<float*>(t.data_ptr());
+        refs.r[1] = THPVariable_Wrap(std::move(t));
+        if (!refs.r[1]) return nullptr;
+    }
+    const size_t bytes = lib.fp8_attention_workspace(p.seqs, p.rows, static_cast<int>(q.heads), c.heads);
+    at::Tensor workspace;  // (of the current stream: what comes after on it may have the memory once the call's work is done)
+    if (bytes) workspace = at::detail::empty_cuda({static_cast<int64_t>(bytes)}, at::kByte, *place.dev, std::nullopt);
+    void* const w = bytes ? workspace.data_ptr() : nullptr;
+    void* s = stream();
+    if (failed(unlocked([&] {
+                   return lib.fp8_attention(&c, &p, q.p, static_cast<int>(q.heads), q.row, q.head, causal, window, static_cast<float>(scale), out.p, out.row,
+                                            out.head, lse, w, bytes, static_cast<uint32_t*>(status), s);
+               }),
+               "pvq_fp8_attention"))
+        return nullptr;
+    written(a[12]);
+    return with_lse ? refs.tuple(2) : refs.one();
+    END_HANDLE_TH_ERRORS
+}
+
 // init(raise_error, address of every entry of `Entries`, in its order)
 PyObject* bind_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     constexpr Py_ssize_t count = sizeof(Entries) / sizeof(void*);
@@ -843,6 +1057,9 @@ PyMethodDef methods[] = {method<bind_init>("init"),
                          method<bind_fp8_gated>("fp8_gated"),
                          method<bind_fp8_gated_backward>("fp8_gated_backward"),
                          method<bind_fp8_weight_grad>("fp8_weight_grad"),
+                         method<bind_fp8_cache_write>("fp8_cache_write"),
+                         method<bind_fp8_cache_read>("fp8_cache_read"),
+                         method<bind_fp8_attention>("fp8_attention"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods};
 

@@ -1,0 +1,283 @@
+// What the attention kernels over the 8-bit cache share: how the work is cut, the pages' way to shared memory, parts of results.
+//
+// An item is a block of a sequence's query rows (query heads of a cache's head side by side, query for query) over one head of the
+// cache; its units are the tiles of 128 tokens that some row of it sees, one at least.  The units of all items in a row are cut into
+// equal shares, one a thread block, whatever the sequences' lengths; an item that is cut leaves parts (sums that are not yet
+// divided, and what their weights are relative to) in the workspace, which a second kernel adds in the order of the tokens.
+#pragma once
+#include "fp8_cache.cuh"
+
+namespace pvq {
+namespace fp8 {
+
+struct CacheMaps {
+    CUtensorMap k, v;
+};
+
+constexpr int kLeastUnits = 2;   // of a block
+constexpr int kScaleSlots = 8;   // tiles whose scales are on their way
+constexpr float kNone = -INFINITY;
+
+// A part: fp32 sums [rows][128], then what the weights are relative to (as an exponent of 2) and their sum, a row each.
+template <int ROWS>
+__host__ __device__ constexpr size_t part_floats() {
+    return size_t(ROWS) * (128 + 2);
+}
+struct PartHead {  // of a block's second part: the item that is continued by the blocks behind it
+    int parts, row, q0, rows, head;  // parts 0: there is none
+};
+// The workspace: two parts a block (of an item that began before, of one that goes on behind), then their heads.
+template <int ROWS>
+__device__ __forceinline__ PartHead* part_heads(const AttentionArgs& a) {
+    return reinterpret_cast<PartHead*>(a.workspace + 2 * size_t(gridDim.x) * part_floats<ROWS>());
+}
+__device__ __forceinline__ float row_lse(float relative, float all) { return all == 0.0f ? kNone : (relative + log2f(all)) * 0.693147180559945f; }
+
+struct Item {
+    int s, head, block;
+    Sequence q;
+    int q0, rows;        // its rows of the sequence's n * group
+    int tile0, tiles;    // that some row sees
+    int units;
+};
+
+template <int ROWS>
+__device__ __forceinline__ void measure(const AttentionArgs& a, Item& it) {
+    it.q0 = it.block * ROWS;
+    it.rows = min(ROWS, it.q.n * a.group - it.q0);
+    const int i0 = it.q0 / a.group, i1 = (it.q0 + it.rows - 1) / a.group;
+    const int hi = a.causal ? min(it.q.held, it.q.first + i1 + 1) : it.q.held;
+    const int lo = a.window > 0 ? max(0, it.q.first + i0 - a.window + 1) : 0;
+    it.tile0 = lo / kTile;
+    it.tiles = hi > lo ? (hi + kTile - 1) / kTile - it.tile0 : 0;
+    it.units = max(it.tiles, 1);
+}
+template <int ROWS>
+__device__ __forceinline__ int blocks_of(const AttentionArgs& a, const Sequence& q) {
+    return (q.n * a.group + ROWS - 1) / ROWS;
+}
+
+struct PlanShared {
+    long long sums[32], total, left, per_head;
+    int s;
+};
+// A block's share: it begins `skip` units into an item.
+struct Share {
+    int s, head, block, skip;
+    long long begin, left, all;
+    int blocks;  // that have a share
+};
+
+// All threads of the block.
+template <int THREADS, int ROWS>
+__device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& sh) {
+    const int thread = threadIdx.x, lane = thread & 31, warp = thread >> 5, seqs = a.step.seqs;
+    int lanes = 32;  // for a sequence
+    while (lanes > 1 && seqs > THREADS / lanes) lanes >>= 1;
+    const int per = THREADS / lanes;
+    long long units = 0, before = 0, base = 0;
+    const auto chunk = [&](int first) {  // units of a sequence, and of those before it in the chunk; returns those of the chunk
+        const int s = first + thread / lanes;
+        units = 0;
+        if (s < seqs) {
+            Item it;
+            it.q = sequence_of(a.step, s, a.cache.page_shift);
+            if (a.status && blockIdx.x == 0 && it.q.n > 0 && (it.q.first < 0 || it.q.held < it.q.first + it.q.n)) atomicOr(a.status, PVQ_STATUS_BAD_PAGE);
+            const int blocks = blocks_of<ROWS>(a, it.q);
+            for (it.block = thread & (lanes - 1); it.block < blocks; it.block += lanes) {
+                measure<ROWS>(a, it);
+                units += it.units;
+            }
+        }
+        for (int o = lanes >> 1; o > 0; o >>= 1) units += __shfl_xor_sync(0xffffffffu, units, o);
+        units *= a.cache.heads;
+        const bool leads = (thread & (lanes - 1)) == 0;
+        long long sum = leads ? units : 0;
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long other = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += other;
+        }
+        __syncthreads();
+        if (lane == 31) sh.sums[warp] = sum;
+        __syncthreads();
+        before = sum - (leads ? units : 0);
+        long long all = 0;
+        for (int w = 0; w < THREADS / 32; ++w) {
+            if (w < warp) before += sh.sums[w];
+            all += sh.sums[w];
+        }
+        return all;
+    };
+    long long all = 0;
+    for (int first = 0; first < seqs; first += per) all += chunk(first);
+    Share r{};
+    r.all = all;
+    r.blocks = static_cast<int>(min(static_cast<long long>(gridDim.x), max(1ll, all / kLeastUnits)));
+    const int c = blockIdx.x;
+    if (all == 0 || c >= r.blocks) return r;
+    r.begin = all * c / r.blocks;
+    r.left = all * (c + 1) / r.blocks - r.begin;
+    for (int first = 0; first < seqs; first += per) {
+        const long long here = seqs > per ? chunk(first) : all;
+        if ((thread & (lanes - 1)) == 0 && base + before <= r.begin && r.begin < base + before + units) {
+            sh.s = first + thread / lanes;
+            sh.left = r.begin - base - before;
+            sh.per_head = units / a.cache.heads;
+        }
+        base += here;
+        if (base > r.begin) break;
+    }
+    __syncthreads();
+    r.s = sh.s;
+    const long long per_head = sh.per_head;
+    r.head = static_cast<int>(sh.left / per_head);
+    long long rest = sh.left - r.head * per_head;
+    Item it;
+    it.q = sequence_of(a.step, r.s, a.cache.page_shift);
+    const int blocks = blocks_of<ROWS>(a, it.q);
+    for (int b0 = 0; b0 < blocks; b0 += 32) {  // (every warp alike)
+        it.block = b0 + lane;
+        long long sum = 0;
+        if (it.block < blocks) {
+            measure<ROWS>(a, it);
+            sum = it.units;
+        }
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long other = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += other;
+        }
+        const uint32_t behind = __ballot_sync(0xffffffffu, it.block < blocks && sum > rest);
+        if (behind) {
+            const int at = __ffs(behind) - 1;
+            r.block = b0 + at;
+            if (at > 0) rest -= __shfl_sync(0xffffffffu, sum, at - 1);
+            break;
+        }
+        rest -= __shfl_sync(0xffffffffu, sum, 31);
+    }
+    r.skip = static_cast<int>(rest);
+    return r;
+}
+
+// Goes through a block's share, item by item.  Every role of the block does so by itself.
+template <int ROWS>
+struct Walk {
+    const AttentionArgs& a;
+    Item it;
+    long long at, left, all;
+    int blocks, skip, take;
+
+    __device__ __forceinline__ Walk(const AttentionArgs& args, const Share& sh) : a(args), at(sh.begin), left(sh.left), all(sh.all), blocks(sh.blocks), skip(sh.skip), take(0) {
+        if (left <= 0) return;
+        it.s = sh.s, it.head = sh.head, it.block = sh.block;
+        it.q = sequence_of(a.step, it.s, a.cache.page_shift);
+        measure<ROWS>(a, it);
+        take = static_cast<int>(min(left, static_cast<long long>(it.units - skip)));
+    }
+    __device__ __forceinline__ bool there() const { return left > 0; }
+    __device__ __forceinline__ int begin() const { return it.tile0 + skip; }  // tiles of this share
+    __device__ __forceinline__ int count() const { return min(take, it.tiles); }
+    __device__ __forceinline__ bool first() const { return skip == 0; }
+    __device__ __forceinline__ bool last() const { return skip + take == it.units; }
+    // Blocks that the item is shared by, from its first one on (called where first()).
+    __device__ __forceinline__ int parts() const {
+        return static_cast<int>(((at + it.units) * blocks - 1) / all - blockIdx.x) + 1;
+    }
+    __device__ __forceinline__ void next() {
+        at += take, left -= take;
+        if (left <= 0) return;
+        skip = 0;
+        if (++it.block == blocks_of<ROWS>(a, it.q)) {
+            it.block = 0;
+            if (++it.head == a.cache.heads) {
+                it.head = 0;
+                do {
+                    it.q = sequence_of(a.step, ++it.s, a.cache.page_shift);
+                } while (it.q.n == 0 && it.s + 1 < a.step.seqs);
+            }
+        }
+        measure<ROWS>(a, it);
+        take = static_cast<int>(min(left, static_cast<long long>(it.units)));
+    }
+};
+
+// Where a row's result goes: its query's row and head.
+struct RowPlace {
+    int row, head;
+};
+__device__ __forceinline__ RowPlace place_of(const AttentionArgs& a, const Sequence& q, int head, int packed) {
+    const int i = packed / a.group;
+    return {q.row + i, head * a.group + packed - i * a.group};
+}
+
+// The pages of a run of tiles, 32 at a time, a lane each: their numbers are asked for two turns ahead, their scales one.
+struct Pages {
+    const AttentionArgs& a;
+    const int* table;
+    int head, entry, end, id, id1, id2;
+    uint32_t scales, scales1;
+
+    __device__ __forceinline__ int ask(int e) const {
+        if (e >= end) return -1;
+        const int i = __ldg(table + e);
+        if (i >= 0 && i < a.cache.pages) return i;
+        if (a.status) atomicOr(a.status, PVQ_STATUS_BAD_PAGE);
+        return -1;
+    }
+    __device__ __forceinline__ uint32_t ask_scales(int i) const {  // (a page that is not there: zeros)
+        if (i < 0) return 127u | 127u << 8;
+        const int64_t at = i * a.cache.scale_step + head;
+        const int k = __ldg(a.cache.k_scales + at), v = __ldg(a.cache.v_scales + at);
+        return static_cast<uint32_t>(min(max(k, kLeastScale), kMostScale)) | static_cast<uint32_t>(min(max(v, kLeastScale), kMostScale)) << 8;
+    }
+    __device__ __forceinline__ Pages(const AttentionArgs& args, const Item& it, int first_entry) : a(args) {
+        table = a.step.table + it.s * a.step.ld;
+        head = it.head;
+        end = (it.q.held + (1 << a.cache.page_shift) - 1) >> a.cache.page_shift;
+        entry = first_entry + (threadIdx.x & 31);
+        id = ask(entry), id1 = ask(entry + 32), id2 = ask(entry + 64);
+        scales = ask_scales(id), scales1 = ask_scales(id1);
+    }
+    __device__ __forceinline__ void next() {
+        entry += 32;
+        id = id1, id1 = id2, id2 = ask(entry + 64);
+        scales = scales1, scales1 = ask_scales(id1);
+    }
+};
+
+// One page of a head to shared memory.
+__device__ __forceinline__ void load_page(uint32_t to, const CUtensorMap* map, int head, int page, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to), "l"(map), "r"(0),
+                 "r"(0), "r"(head), "r"(page), "r"(bar)
+                 : "memory");
+}
+
+__device__ __forceinline__ float exp2_of(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// e4m3 operands without scales, sums in fp32.
+__host__ __device__ constexpr uint32_t product_codes(int m, int n, bool a_across, bool b_across) {
+    return 1u << 4 | uint32_t(a_across) << 15 | uint32_t(b_across) << 16 | uint32_t(n / 8) << 17 | uint32_t(m / 16) << 24;
+}
+__device__ __forceinline__ void multiply_codes(uint32_t d, uint64_t a, uint64_t b, uint32_t product, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(product), "r"(static_cast<uint32_t>(add))
+                 : "memory");
+}
+
+// A row's values times 2^-e, |values| at most 448, as two codes each: the nearest one, and the nearest one to what it leaves.
+// Together they are a bf16 value but for 2^-17 of the row's largest.
+__device__ __forceinline__ void two_codes(float x, float y, uint32_t& hi, uint32_t& lo) {
+    hi = codes_of(x, y);
+    const float2 h = values_of(hi);
+    lo = codes_of(x - h.x, y - h.y);
+}
+
+int cache_maps(const Cache& c, CacheMaps* maps);
+int attention_few(const AttentionArgs& a, int rows, int blocks, cudaStream_t s);  // 16 or 32 rows an item
+
+}  // namespace fp8
+}  // namespace pvq

@@ -1,0 +1,378 @@
+// Attention of few query rows over the 8-bit cache: bound by reading the cache.
+//
+// For each tile of 128 tokens the tokens are the products' 128 lanes and the query rows their columns: S^T = K Q^T, then, with
+// a thread a token, the weights w = 2^(s - m) and P^T, and O^T = V^T P^T with the dims as lanes, added to sums in registers.  Both
+// products take the cache's codes as they lie in memory, the keys along k and the values across it.  What they are multiplied
+// by is split into two codes each (queries to 2^-17 of the row's largest, weights to 2^-8 of themselves).
+//
+// A page's scales are powers of two: that of the keys multiplies a token's scores, that of the values is added to their exponents, so that
+// the weights are relative to the largest of w * scale, whatever the pages' scales are; their sum takes it out again.
+//
+// Warps: one issues the copies, one the products, four hold the tokens (then the dims).
+#include "fp8_attention.cuh"
+
+namespace pvq {
+namespace fp8 {
+namespace {
+
+constexpr int kThreads = 192;
+constexpr int kHalf = kTile * 128;       // bytes of a tile's keys or values, rows of 128 bytes
+constexpr float kShift = 8.0f;           // weights are up to 2^8: their smallest code is 2^-9
+
+template <int ROWS>
+struct Few {
+    static constexpr int kHalves = ROWS == 16 ? 6 : 5;
+    static constexpr int kQueries = kHalves * kHalf, kQueryBytes = ROWS * 128;  // two codes each
+    static constexpr int kWeights = kQueries + 2 * kQueryBytes, kWeightBytes = ROWS * kTile;
+    static constexpr int kBars = kWeights + 2 * kWeightBytes;
+    static constexpr size_t kShared = 1024 + kBars + 256;
+    static constexpr int kColumns = ROWS == 16 ? 64 : 128;  // of tensor memory: scores twice, sums
+    static_assert(2 * (kShared + 4096) <= 231424, "two blocks an SM");
+};
+
+// Operand across k whose 16 columns of one k lie together: eight k's are 128 bytes, the next 16 columns are `further`.
+__device__ __forceinline__ uint64_t operand_plain(uint32_t at, uint32_t further) {
+    return static_cast<uint64_t>((at & 0x3ffffu) >> 4) | static_cast<uint64_t>(128u >> 4) << 16 | static_cast<uint64_t>(further >> 4) << 32 | uint64_t(1) << 46;
+}
+
+__device__ __forceinline__ float warp_max(float x) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ void tokens_meet() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+template <int ROWS>
+__global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid_constant__ CacheMaps maps, const __grid_constant__ AttentionArgs p) {
+    using S = Few<ROWS>;
+    constexpr int kHalves = S::kHalves;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
+    const uint32_t full = base + S::kBars, empty = full + 8 * kHalves, scales_full = empty + 8 * kHalves, scores_full = scales_full + 8 * kScaleSlots,
+                   weights_full = scores_full + 16, sums_full = weights_full + 8, queries_full = sums_full + 8, drained = queries_full + 8;
+    __shared__ uint32_t tensor_base, issued_halves;
+    __shared__ int over;
+    __shared__ PlanShared plan;
+    __shared__ uint32_t page_scales[kScaleSlots][8];  // of 16 tokens each: keys', values'
+    __shared__ __align__(16) float factor[ROWS], tops[2][4][ROWS];
+    __shared__ int from[ROWS], to[ROWS];  // positions that a row sees
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp == 0) {  // a barrier a lane
+        constexpr int kAll = 2 * kHalves + kScaleSlots + 6;
+        static_assert(kAll <= 32, "one lane each");
+        const int i = lane - (2 * kHalves + kScaleSlots);  // scores twice, weights, sums, queries, drained
+        if (lane < kAll) barrier_init(full + 8 * lane, i == 2 || i == 4 ? 4 : 1);
+        barrier_init_fence();
+        if (lane == 0) {
+            over = 0;
+            issued_halves = 0;
+            prefetch_map(&maps.k), prefetch_map(&maps.v);
+        }
+    } else if (warp == 1) {
+        tensor_alloc<false>(shared_address(&tensor_base), S::kColumns);
+    }
+    tensor_fence_before();
+    __syncthreads();
+    tensor_fence_after();
+    launch_dependents();
+    dependency_wait();
+    const uint32_t tensor = tensor_base, sums = tensor + 2 * ROWS;
+    Bounds bounds{&over, p.status};
+    const Withheld withheld = withheld_of(bounds, blockIdx.x);
+    const Share share = find_share<kThreads, ROWS>(p, plan);
+    Walk<ROWS> walk(p, share);
+
+    if (warp == 0) {
+        const int pages = kTile >> p.cache.page_shift, page_bytes = 128 << p.cache.page_shift;  // of a tile
+        Turn<kHalves> turn;
+        uint32_t issued = 0, tile = 0;
+        bool ok = true;
+        for (; walk.there() && ok; walk.next()) {
+            if (walk.count() == 0) continue;
+            Pages list(p, walk.it, walk.begin() * pages);
+            int within = 0;
+            for (int t = 0; t < walk.count() && ok; ++t, ++tile) {
+                if (within == 32) list.next(), within = 0;
+                const uint32_t slot = tile % kScaleSlots;
+                const uint32_t word = __shfl_sync(0xffffffffu, list.scales, within + ((lane & 7) * pages >> 3));
+                const int page = __shfl_sync(0xffffffffu, list.id, within + (lane & (pages - 1)));
+                within += pages;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    ok = !(withheld.copies && issued >= kHalves + kWithheldFrom) && warp_wait(empty + 8 * turn.at, turn.parity ^ 1, bounds);
+                    if (!ok) break;
+                    const uint32_t bar = full + 8 * turn.at;
+                    if (half == 0) {
+                        if (lane < 8) page_scales[slot][lane] = word;
+                        __syncwarp();
+                        if (lane == 0) barrier_arrive(scales_full + 8 * slot);
+                    }
+                    if (lane == 0) barrier_expect(bar, kHalf);
+                    __syncwarp();
+                    if (lane < pages) load_page(base + turn.at * kHalf + lane * page_bytes, half ? &maps.v : &maps.k, walk.it.head, page, bar);
+                    __syncwarp();
+                    turn.next();
+                    ++issued;
+                }
+            }
+        }
+        if (lane == 0) issued_halves = issued;
+    } else if (warp == 1) {
+        if (elected()) {
+            constexpr uint32_t scores = product_codes(128, ROWS, false, false), results = product_codes(128, ROWS, true, true);
+            const uint64_t tiles0 = operand(base), queries0 = operand(base + S::kQueries), weights0 = operand_plain(base + S::kWeights, kTile * 16);
+            const int steps = (p.cache.dim + 31) / 32;
+            uint32_t tile = 0, items = 0;
+            bool ok = true;
+            const auto half_at = [&](uint32_t h) { return tiles0 + (h % kHalves) * (kHalf >> 4); };
+            const auto arrived = [&](uint32_t h) { return barrier_wait(full + 8 * (h % kHalves), (h / kHalves) & 1, bounds); };
+            const auto score = [&](uint32_t t) {
+                ok = arrived(2 * t);
+                if (!ok) return;
+                tensor_fence_after();
+                const uint64_t k = half_at(2 * t);
+                const uint32_t d = tensor + (t & 1) * ROWS;
+                for (int i = 0; i < steps; ++i) {
+                    multiply_codes(d, k + 2 * i, queries0 + 2 * i, scores, i > 0);
+                    multiply_codes(d, k + 2 * i, queries0 + (S::kQueryBytes >> 4) + 2 * i, scores, true);
+                }
+                products_done<false>(empty + 8 * (2 * t % kHalves));
+                products_done<false>(scores_full + 8 * (t & 1));
+            };
+            for (; walk.there() && ok; walk.next(), ++items) {
+                const int count = walk.count();
+                ok = barrier_wait(queries_full, items & 1, bounds);
+                if (!ok) break;
+                tensor_fence_after();
+                if (count > 0) score(tile);
+                for (int t = 0; t < count && ok; ++t, ++tile) {
+                    if (t + 1 < count) score(tile + 1);
+                    ok = ok && barrier_wait(weights_full, tile & 1, bounds) && arrived(2 * tile + 1);
+                    if (!ok) break;
+                    tensor_fence_after();
+                    const uint64_t v = half_at(2 * tile + 1);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        multiply_codes(sums, v + 256 * i, weights0 + 32 * i, results, i > 0);
+                        multiply_codes(sums, v + 256 * i, weights0 + (S::kWeightBytes >> 4) + 32 * i, results, true);
+                    }
+                    products_done<false>(empty + 8 * ((2 * tile + 1) % kHalves));
+                    products_done<false>(sums_full);
+                }
+            }
+            if (!ok) {
+                products_done<false>(drained);
+                for (int polls = 0; polls < kLandings && !barrier_passed(drained, 0); ++polls) {}
+            }
+        }
+    } else {
+        const int quarter = warp & 3, thread = quarter * 32 + lane;  // token, then dim
+        const uint32_t mine = quarter << 21;
+        PartHead* head = part_heads<ROWS>(p) + blockIdx.x;
+        if (thread == 0 && gridDim.x > 1) head->parts = 0;
+        uint32_t tile = 0;
+        bool ok = true;
+        for (; walk.there(); walk.next()) {
+            const Item& it = walk.it;
+            const int count = walk.count();
+            {  // queries: 128 / ROWS threads a row
+                constexpr int kAcross = 128 / ROWS, kEach = 128 / kAcross;  // dims of a thread
+                const int r = thread / kAcross, col = thread % kAcross * kEach;
+                float x[kEach];
+                uint32_t most = 0u;
+                const RowPlace place = place_of(p, it.q, it.head, it.q0 + min(r, it.rows - 1));
+                const __nv_bfloat16* q = p.q + place.row * p.q_row + place.head * p.q_head + col;
+#pragma unroll
+                for (int j = 0; j < kEach / 8; ++j) {
+                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                    if (col + 8 * j < p.cache.dim) w = __ldg(reinterpret_cast<const uint4*>(q + 8 * j));
+                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[8 * j + 2 * i] = __uint_as_float(u[i] << 16), x[8 * j + 2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+                }
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+#pragma unroll
+                for (int o = 1; o < kAcross; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+                const uint32_t byte = most < kFiniteEnd ? scale_byte(most) : 127u;
+                const float inverse = inverse_of(byte);
+                const uint32_t at = base + S::kQueries + r * 128;
+#pragma unroll
+                for (int j = 0; j < kEach / 16; ++j) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t h0, l0, h1, l1;
+                        const float* y = x + 16 * j + 4 * i;
+                        two_codes(y[0] * inverse, y[1] * inverse, h0, l0);
+                        two_codes(y[2] * inverse, y[3] * inverse, h1, l1);
+                        hi[i] = h0 | h1 << 16, lo[i] = l0 | l1 << 16;
+                    }
+                    const uint32_t chunk = at + (((col / 16 + j) ^ (r & 7)) << 4);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk + S::kQueryBytes), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3])
+                                 : "memory");
+                }
+                if (thread % kAcross == 0) {
+                    const int position = it.q.first + (it.q0 + r) / p.group;
+                    factor[r] = most < kFiniteEnd ? scale_of(byte) * p.scale : __uint_as_float(0x7fffffffu);
+                    to[r] = r < it.rows ? (p.causal ? min(it.q.held, position + 1) : it.q.held) : 0;
+                    from[r] = p.window > 0 ? max(0, position - p.window + 1) : 0;
+                }
+                async_fence();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(queries_full);
+            }
+            tokens_meet();
+            // positions that every row sees, and that any does (a later query sees from later on, and farther)
+            const int all_from = from[it.rows - 1], all_to = to[0], any_from = from[0], any_to = to[it.rows - 1];
+            float top[ROWS], weight[ROWS], sum[ROWS];
+#pragma unroll
+            for (int n = 0; n < ROWS; ++n) top[n] = kNone, weight[n] = 0.0f, sum[n] = 0.0f;
+            const auto add_sums = [&](uint32_t t) {
+                ok = ok && warp_wait(sums_full, t & 1, bounds);
+                tensor_fence_after();
+#pragma unroll
+                for (int c = 0; c < ROWS; c += 16) {
+                    float v[16];
+                    tensor_load(sums + mine + c, v);
+                    tensor_wait_loads();
+#pragma unroll
+                    for (int n = 0; n < 16; ++n) sum[c + n] += v[n];
+                }
+            };
+            for (int t = 0; t < count; ++t, ++tile) {
+                const int tile_at = (walk.begin() + t) * kTile, position = tile_at + thread;
+                const uint32_t slot = tile % kScaleSlots;
+                ok = ok && warp_wait(scales_full + 8 * slot, (tile / kScaleSlots) & 1, bounds) &&
+                     warp_wait(scores_full + 8 * (tile & 1), (tile >> 1) & 1, bounds);
+                tensor_fence_after();
+                float s[ROWS];
+                tensor_load(tensor + mine + (tile & 1) * ROWS, s);
+                const uint32_t word = page_scales[slot][thread >> 4];
+                const float key = __uint_as_float((word & 0xffu) << 23), value = static_cast<float>(static_cast<int>(word >> 8) - 127);
+                tensor_wait_loads();
+#pragma unroll
+                for (int n = 0; n < ROWS; ++n) s[n] = fmaf(s[n] * factor[n], key, value);
+                if (tile_at < all_from || tile_at + kTile > all_to) {
+#pragma unroll
+                    for (int n = 0; n < ROWS; ++n)
+                        if (position < from[n] || position >= to[n]) s[n] = kNone;
+                }
+                float (&high)[4][ROWS] = tops[tile & 1];
+#pragma unroll
+                for (int n = 0; n < ROWS; n += 4) {
+                    const float4 h = make_float4(warp_max(s[n]), warp_max(s[n + 1]), warp_max(s[n + 2]), warp_max(s[n + 3]));
+                    if (lane == 0) *reinterpret_cast<float4*>(&high[quarter][n]) = h;
+                }
+                tokens_meet();
+                if (t > 0) add_sums(tile - 1);
+                const float out_of = __uint_as_float((254u - (word >> 8)) << 23);  // 1 / the values' scale
+                uint32_t hi[ROWS / 4], lo[ROWS / 4];
+#pragma unroll
+                for (int n = 0; n < ROWS; n += 4) {
+                    const float4 a = *reinterpret_cast<const float4*>(&high[0][n]), b = *reinterpret_cast<const float4*>(&high[1][n]),
+                                 c = *reinterpret_cast<const float4*>(&high[2][n]), d = *reinterpret_cast<const float4*>(&high[3][n]);
+                    const float h[4] = {fmaxf(fmaxf(a.x, b.x), fmaxf(c.x, d.x)), fmaxf(fmaxf(a.y, b.y), fmaxf(c.y, d.y)),
+                                        fmaxf(fmaxf(a.z, b.z), fmaxf(c.z, d.z)), fmaxf(fmaxf(a.w, b.w), fmaxf(c.w, d.w))};
+                    if (h[0] > top[n] || h[1] > top[n + 1] || h[2] > top[n + 2] || h[3] > top[n + 3]) {  // (the same for all threads)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float next = fmaxf(top[n + i], h[i]), less = next == kNone ? 1.0f : exp2_of(top[n + i] - next);
+                            sum[n + i] *= less, weight[n + i] *= less;
+                            top[n + i] = next;
+                        }
+                    }
+                    float w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        w[i] = exp2_of(s[n + i] - (top[n + i] == kNone ? 0.0f : top[n + i] - kShift));
+                        weight[n + i] = fmaf(w[i], out_of, weight[n + i]);
+                    }
+                    uint32_t h0, l0, h1, l1;
+                    two_codes(w[0], w[1], h0, l0);
+                    two_codes(w[2], w[3], h1, l1);
+                    hi[n / 4] = h0 | h1 << 16, lo[n / 4] = l0 | l1 << 16;
+                }
+#pragma unroll
+                for (int n = 0; n < ROWS; n += 16) {
+                    const uint32_t at = base + S::kWeights + n * kTile + thread * 16;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(hi[n / 4]), "r"(hi[n / 4 + 1]), "r"(hi[n / 4 + 2]), "r"(hi[n / 4 + 3])
+                                 : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + S::kWeightBytes), "r"(lo[n / 4]), "r"(lo[n / 4 + 1]), "r"(lo[n / 4 + 2]),
+                                 "r"(lo[n / 4 + 3])
+                                 : "memory");
+                }
+                // What no row sees may be anything, NaN too, which a weight of zero would not take out.
+                if (tile_at < any_from || tile_at + kTile > any_to) {
+                    const uint32_t h = 2 * tile + 1, row = base + (h % kHalves) * kHalf + thread * 128;
+                    ok = ok && warp_wait(full + 8 * (h % kHalves), (h / kHalves) & 1, bounds);
+                    if (position < any_from || position >= any_to) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(row + 16 * j), "r"(0u) : "memory");
+                    }
+                }
+                async_fence();
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(weights_full);
+            }
+            if (count > 0) add_sums(tile - 1);
+            tensor_fence_before();
+            // the weights' sums over all tokens, in a fixed order
+#pragma unroll
+            for (int n = 0; n < ROWS; ++n) {
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) weight[n] += __shfl_xor_sync(0xffffffffu, weight[n], o);
+            }
+            tokens_meet();  // (the last tile's largest are read)
+            if (lane == 0) {
+#pragma unroll
+                for (int n = 0; n < ROWS; ++n) tops[0][quarter][n] = weight[n];
+            }
+            tokens_meet();
+            const bool lost = over != 0, whole = walk.first() && walk.last();
+            if (!whole && walk.first() && thread == 0) *head = {walk.parts(), it.q.row, it.q0, it.rows, it.head};
+            float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<ROWS>();
+#pragma unroll
+            for (int n = 0; n < ROWS; ++n) {
+                if (n >= it.rows) break;
+                float all = (tops[0][0][n] + tops[0][1][n]) + (tops[0][2][n] + tops[0][3][n]), v = sum[n], relative = top[n] - kShift;
+                if (lost) all = v = relative = __uint_as_float(0x7fffffffu);
+                if (whole) {
+                    const RowPlace place = place_of(p, it.q, it.head, it.q0 + n);
+                    if (thread < p.cache.dim) p.out[place.row * p.out_row + place.head * p.out_head + thread] = __float2bfloat16(all == 0.0f ? 0.0f : v / all);
+                    if (p.lse && thread == 0) p.lse[int64_t(place.row) * p.heads + place.head] = row_lse(relative, all);
+                } else {
+                    part[n * 128 + thread] = v;
+                    if (thread == 0) part[ROWS * 128 + n] = relative, part[ROWS * 129 + n] = all;
+                }
+            }
+            tokens_meet();  // (what the block knows of this item is read)
+        }
+    }
+    __syncwarp();
+    tensor_fence_before();
+    __syncthreads();
+    if (__builtin_expect(over, 0) && warp == 0) land<kHalves>(full, issued_halves);  // copies in flight have to land before the block ends
+    if (warp == 1) {
+        tensor_fence_after();
+        tensor_free<false>(tensor, S::kColumns);
+    }
+}
+
+template <int ROWS>
+int launch(const AttentionArgs& a, int blocks, cudaStream_t s) {
+    CacheMaps maps;
+    int st = cache_maps(a.cache, &maps);
+    if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(attention_few_kernel<ROWS>), Few<ROWS>::kShared);
+    if (st != PVQ_OK) return st;
+    return launch_early(attention_few_kernel<ROWS>, dim3(static_cast<unsigned>(blocks)), kThreads, Few<ROWS>::kShared, 0, s, maps, a);
+}
+
+}  // namespace
+
+int attention_few(const AttentionArgs& a, int rows, int blocks, cudaStream_t s) { return rows == 16 ? launch<16>(a, blocks, s) : launch<32>(a, blocks, s); }
+
+}  // namespace fp8
+}  // namespace pvq

@@ -5,7 +5,7 @@
 #include <mutex>
 #include <utility>
 
-#include "fp8_mma.cuh"
+#include "fp8_attention.cuh"
 
 namespace pvq {
 namespace fp8 {
@@ -33,6 +33,22 @@ int tile_map(CUtensorMap* map, const void* p, Element type, int64_t rows, int64_
     const CUresult r = encode(map, t, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? PVQ_OK : set_cuda_error(cudaErrorInvalidValue);
+}
+
+// Boxes are a page of a head, rows of 128 bytes: what a row is short of that is filled with zeros.
+int cache_maps(const Cache& c, CacheMaps* maps) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return set_cuda_error(cudaErrorInitializationError);
+    const cuuint32_t page = 1u << c.page_shift;
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(c.dim), page, static_cast<cuuint64_t>(c.heads), static_cast<cuuint64_t>(c.pages)},
+                     strides[3] = {static_cast<cuuint64_t>(c.token_step), static_cast<cuuint64_t>(c.head_step), static_cast<cuuint64_t>(c.page_step)};
+    const cuuint32_t box[4] = {128, page, 1, 1}, steps[4] = {1, 1, 1, 1};
+    for (int i = 0; i < 2; ++i) {
+        const CUresult r = encode(i ? &maps->v : &maps->k, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, i ? c.v : c.k, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r != CUDA_SUCCESS) return set_cuda_error(cudaErrorInvalidValue);
+    }
+    return PVQ_OK;
 }
 
 int allow_shared(const void* kernel, size_t bytes) {

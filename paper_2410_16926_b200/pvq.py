@@ -11,6 +11,7 @@ import collections
 import ctypes as C
 import importlib.machinery
 import importlib.util
+import math
 import os
 
 import torch
@@ -26,6 +27,7 @@ DTYPE_BF16 = 1
 STATUS_INVALID_CODE = 1
 STATUS_STAGING_TIMEOUT = 2
 STATUS_TABLE_MISMATCH = 4
+STATUS_BAD_PAGE = 8
 
 _lib = None
 _native = None
@@ -52,6 +54,19 @@ class Fp8Desc(C.Structure):
     """Mirror of pvq_fp8_matrix."""
     _fields_ = [("d_codes", C.c_void_p), ("d_scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
                 ("ld_codes", C.c_int64), ("ld_scales", C.c_int64), ("tile", C.c_int)]
+
+
+class Fp8CacheDesc(C.Structure):
+    """Mirror of pvq_fp8_cache."""
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scales", C.c_void_p), ("d_v_scales", C.c_void_p), ("pages", C.c_int64),
+                ("heads", C.c_int), ("page", C.c_int), ("dim", C.c_int), ("page_step", C.c_int64), ("head_step", C.c_int64),
+                ("token_step", C.c_int64), ("scale_step", C.c_int64)]
+
+
+class Fp8StepDesc(C.Structure):
+    """Mirror of pvq_fp8_step."""
+    _fields_ = [("d_table", C.c_void_p), ("d_lengths", C.c_void_p), ("d_starts", C.c_void_p), ("seqs", C.c_int64), ("rows", C.c_int64),
+                ("width", C.c_int64), ("ld_table", C.c_int64)]
 
 
 def lib():
@@ -96,6 +111,12 @@ def lib():
         L.pvq_fp8_weight_grad.argtypes = [vp, i64, i64, fp8, vp, i32, i64, vp, sz, vp, vp]
         L.pvq_fp8_weight_grad_workspace.argtypes = [i64, i64, i64]
         L.pvq_fp8_weight_grad_workspace.restype = sz
+        cache, step = C.POINTER(Fp8CacheDesc), C.POINTER(Fp8StepDesc)
+        L.pvq_fp8_cache_write.argtypes = [cache, step, vp, i64, i64, vp, i64, i64, i32, vp, vp]
+        L.pvq_fp8_cache_read.argtypes = [cache, step, vp, i64, i64, vp, i64, i64, i32, vp, vp]
+        L.pvq_fp8_attention.argtypes = [cache, step, vp, i32, i64, i64, i32, i64, C.c_float, vp, i64, i64, vp, vp, sz, vp, vp]
+        L.pvq_fp8_attention_workspace.argtypes = [i64, i64, i32, i32]
+        L.pvq_fp8_attention_workspace.restype = sz
         L.pvq_debug_status.argtypes = [vp]
         L.pvq_encode_status.argtypes = [vp]
         _lib = L
@@ -108,7 +129,8 @@ EXPORTS = ["pvq_strerror", "pvq_last_cuda_error", "pvq_index_bits", "pvq_max_pul
            "pvq_decode_batched", "pvq_decode_static_table", "pvq_rotate_encode", "pvq_rotate_roundtrip", "pvq_encode_amp",
            "pvq_debug_status", "pvq_encode_status", "pvq_fp8_scale_row_stride", "pvq_fp8_quantize", "pvq_fp8_dequantize",
            "pvq_fp8_matmul", "pvq_fp8_gated", "pvq_fp8_gated_backward", "pvq_fp8_weight_grad",
-           "pvq_fp8_weight_grad_workspace"]
+           "pvq_fp8_weight_grad_workspace", "pvq_fp8_cache_write", "pvq_fp8_cache_read", "pvq_fp8_attention",
+           "pvq_fp8_attention_workspace"]
 
 
 def _check(status, where):
@@ -131,7 +153,8 @@ def _load_native():
     loader.exec_module(m)
     names = ("encode", "encode_amp", "decode", "roundtrip", "rotate_encode", "rotate_roundtrip", "encode_batched",
              "decode_batched", "code_words", "scale_row_stride", "fp8_quantize", "fp8_dequantize", "fp8_matmul", "fp8_gated",
-             "fp8_gated_backward", "fp8_weight_grad", "fp8_scale_row_stride", "fp8_weight_grad_workspace")
+             "fp8_gated_backward", "fp8_weight_grad", "fp8_scale_row_stride", "fp8_weight_grad_workspace", "fp8_cache_write",
+             "fp8_cache_read", "fp8_attention", "fp8_attention_workspace")
     m.init(_raise, *(C.cast(getattr(L, "pvq_" + n), C.c_void_p).value for n in names))
     _native = m
     return m
@@ -354,3 +377,41 @@ def fp8_weight_grad(dy, x, dtype=torch.float32, out=None, status=None, workspace
     products take 2 bytes a value of x from torch's allocator for the length of the call, where it has them; without
     (`workspace` false) they give the same bits, somewhat slower."""
     return (_native or _load_native()).fp8_weight_grad(dy, x[0], x[1], x[2], _value_type(dtype), out, status, workspace)
+
+
+# ---- key and value cache in 8 bits, with a scale for each page and head ----------------
+
+# k, v: float8_e4m3fn [pages][heads][page][dim], page 16, 32, 64 or 128, dim a multiple of 16 up to 128; k_scales, v_scales:
+# float8_e8m0fnu [pages][heads].  Views of other orders will do, as long as a token's dims lie together, and keys and values alike.
+# A step's calls share `table` int32 [seqs][pages of the longest], `lengths` int32 [seqs] (with the step's tokens) and `starts` int32
+# [seqs + 1]: rows starts[s] to starts[s + 1] are the last tokens of sequence s; None: one row a sequence.  They stay on the GPU.
+Fp8Cache = collections.namedtuple("Fp8Cache", "k v k_scales v_scales")
+
+
+def alloc_fp8_cache(pages, heads, page, dim, device="cuda"):
+    """An Fp8Cache of uninitialised pages."""
+    k, v = (torch.empty((pages, heads, page, dim), dtype=torch.float8_e4m3fn, device=device) for _ in range(2))
+    k_scales, v_scales = (torch.empty((pages, heads), dtype=torch.float8_e8m0fnu, device=device) for _ in range(2))
+    return Fp8Cache(k, v, k_scales, v_scales)
+
+
+def fp8_cache_write(k, v, cache, table, lengths, starts=None, status=None):
+    """Quantises k, v [rows][heads][dim] (float32 / bfloat16) into the pages of their sequences, at positions lengths[s] - n to
+    lengths[s].  A page that held tokens before keeps its scale or gets a larger one, to which they are rounded again.  `status`:
+    optional int32 device tensor of one element, into which STATUS_BAD_PAGE is OR-ed where a token has no place."""
+    (_native or _load_native()).fp8_cache_write(k, v, *cache, table, lengths, starts, status)
+
+
+def fp8_cache_read(cache, table, lengths, starts=None, rows=None, dtype=torch.bfloat16, out=(None, None), status=None):
+    """(k, v) [rows][heads][dim]: the values of the rows' tokens (whole sequences, with starts the sums of the lengths).  `rows`:
+    how many, where there are starts; those of no sequence are left as they were."""
+    return (_native or _load_native()).fp8_cache_read(*cache, table, lengths, starts, -1 if rows is None else rows, _value_type(dtype), *out, status)
+
+
+def fp8_attention(q, cache, table, lengths, starts=None, causal=True, window=0, scale=None, lse=False, out=None, status=None):
+    """Attention of q [rows][query heads][dim] bfloat16 to what the sequences hold -> bfloat16 of the same shape.  A row at position i
+    sees positions j < lengths[s], j <= i with `causal`, j > i - window with `window`; what sees nothing is zeros.  scale:
+    1 / sqrt(dim) if not given.  With `lse` also float32 [rows][query heads], the logarithm of the sum of exp(scale q k).  Rows of no
+    sequence are left as they were.  `status` as above, and STATUS_STAGING_TIMEOUT as for fp8_matmul."""
+    return (_native or _load_native()).fp8_attention(q, *cache, table, lengths, starts, causal, window,
+                                                     1 / math.sqrt(q.shape[-1]) if scale is None else scale, lse, out, status)
