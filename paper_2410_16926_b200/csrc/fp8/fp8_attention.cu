@@ -61,11 +61,12 @@ struct Form {
 };
 Form form_of(int64_t seqs, int64_t rows, int heads, int kv_heads) {
     const int64_t each = (rows * (heads / kv_heads) + seqs - 1) / (seqs > 0 ? seqs : 1);  // of a sequence and head
+    if (each > 64) return {256, kSms};
     return {each <= 16 ? 16 : 32, 2 * kSms};
 }
 
 size_t bytes_of(const Form& f) {
-    const size_t floats = f.rows == 16 ? part_floats<16>() : part_floats<32>();
+    const size_t floats = f.rows == 16 ? part_floats<16>() : (f.rows == 32 ? part_floats<32>() : part_floats<256>());
     return f.blocks > 1 ? f.blocks * (2 * floats * sizeof(float) + sizeof(PartHead)) : 0;
 }
 
@@ -80,8 +81,8 @@ size_t attention_workspace(int64_t seqs, int64_t rows, int heads, int kv_heads) 
 
 int attention(const AttentionArgs& a, cudaStream_t s) {
     const Form f = form_of(a.step.seqs, a.step.rows, a.heads, a.cache.heads);
-    int st = attention_few(a, f.rows, f.blocks, s);
-    if (st == PVQ_OK && f.blocks > 1) st = f.rows == 16 ? join<16>(a, f.blocks, s) : join<32>(a, f.blocks, s);
+    int st = f.rows == 256 ? attention_many(a, f.blocks, s) : attention_few(a, f.rows, f.blocks, s);
+    if (st == PVQ_OK && f.blocks > 1) st = f.rows == 16 ? join<16>(a, f.blocks, s) : (f.rows == 32 ? join<32>(a, f.blocks, s) : join<256>(a, f.blocks, s));
     return st;
 }
 

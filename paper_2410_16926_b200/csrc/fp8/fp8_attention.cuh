@@ -37,7 +37,8 @@ struct Item {
     int s, head, block;
     Sequence q;
     int q0, rows;        // its rows of the sequence's n * group
-    int tile0, tiles;    // that some row sees
+    int lo, hi;          // positions that some row sees
+    int tile0, tiles;    // of those
     int units;
 };
 
@@ -46,10 +47,10 @@ __device__ __forceinline__ void measure(const AttentionArgs& a, Item& it) {
     it.q0 = it.block * ROWS;
     it.rows = min(ROWS, it.q.n * a.group - it.q0);
     const int i0 = it.q0 / a.group, i1 = (it.q0 + it.rows - 1) / a.group;
-    const int hi = a.causal ? min(it.q.held, it.q.first + i1 + 1) : it.q.held;
-    const int lo = a.window > 0 ? max(0, it.q.first + i0 - a.window + 1) : 0;
-    it.tile0 = lo / kTile;
-    it.tiles = hi > lo ? (hi + kTile - 1) / kTile - it.tile0 : 0;
+    it.hi = a.causal ? min(it.q.held, it.q.first + i1 + 1) : it.q.held;
+    it.lo = a.window > 0 ? max(0, it.q.first + i0 - a.window + 1) : 0;
+    it.tile0 = it.lo / kTile;
+    it.tiles = it.hi > it.lo ? (it.hi + kTile - 1) / kTile - it.tile0 : 0;
     it.units = max(it.tiles, 1);
 }
 template <int ROWS>
@@ -278,6 +279,7 @@ __device__ __forceinline__ void two_codes(float x, float y, uint32_t& hi, uint32
 
 int cache_maps(const Cache& c, CacheMaps* maps);
 int attention_few(const AttentionArgs& a, int rows, int blocks, cudaStream_t s);  // 16 or 32 rows an item
+int attention_many(const AttentionArgs& a, int blocks, cudaStream_t s);           // 256
 
 }  // namespace fp8
 }  // namespace pvq

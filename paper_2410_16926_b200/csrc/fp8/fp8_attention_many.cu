@@ -1,0 +1,425 @@
+// Attention of many query rows over the 8-bit cache: bound by the tensor cores and the exponentials.
+//
+// A block takes 256 query rows, as two tiles of 128 that take turns: while the tensor cores multiply for one, four warps compute the
+// weights of the other, a thread a row.  S = Q K^T from the codes of K as they lie, Q split into two codes (2^-17 of the row's largest),
+// which costs what a product of 16-bit operands would, and K needs no conversion.  The weights go back into tensor memory as fp16, over
+// the scores, and O += P V takes V as fp16, which four warps make of its codes (exact) for both tiles.
+//
+// As in the kernel for few rows, exponents of the pages' scales of V are added to the scores, so that weights are relative to the largest of
+// w * scale; 16 tokens, of one page, share both scales, which are applied to their largest score and inside the exponent, at no cost
+// a score.  Sums of V in tensor memory are rescaled only when a row's largest has grown by 2^8 since: fp16 has the room.
+//
+// Warps: eight for the weights, four convert V, one issues the copies, one the products.
+#include "fp8_attention.cuh"
+
+namespace pvq {
+namespace fp8 {
+namespace {
+
+constexpr int kThreads = 512, kRows = 256;
+constexpr int kBytes = kTile * 128;     // a tile's codes, rows of 128 bytes
+constexpr int kKeys = 3, kCodes = 2, kValues = 2;  // stages
+constexpr int kQueryAt = 0, kKeyAt = 4 * kBytes, kCodeAt = kKeyAt + kKeys * kBytes, kValueAt = kCodeAt + kCodes * kBytes,
+              kBarAt = kValueAt + kValues * 2 * kBytes;
+constexpr size_t kShared = 1024 + kBarAt + 256;
+constexpr float kRoom = 8.0f;           // exponent by which a row's largest may be behind
+
+constexpr int kRegisters = 128, kMany = 192, kFew = 64;
+static_assert(2 * kMany + 2 * kFew <= 4 * kRegisters, "a share beyond these would be waited for without end");
+static_assert(kShared + 2048 <= 232448, "shared memory");
+
+// D += A B with A in tensor memory, both fp16.
+__device__ __forceinline__ void multiply_f16(uint32_t d, uint32_t a, uint64_t b, uint32_t product, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b),
+                 "r"(product), "r"(static_cast<uint32_t>(add))
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t f16x2_of(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// 32 of a lane's words to as many columns.
+__device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&w)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,"
+        "%29,%30,%31,%32};" ::"r"(at),
+        "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(w[8]), "r"(w[9]), "r"(w[10]), "r"(w[11]), "r"(w[12]),
+        "r"(w[13]), "r"(w[14]), "r"(w[15]), "r"(w[16]), "r"(w[17]), "r"(w[18]), "r"(w[19]), "r"(w[20]), "r"(w[21]), "r"(w[22]), "r"(w[23]), "r"(w[24]),
+        "r"(w[25]), "r"(w[26]), "r"(w[27]), "r"(w[28]), "r"(w[29]), "r"(w[30]), "r"(w[31])
+        : "memory");
+}
+
+__global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __grid_constant__ CacheMaps maps, const __grid_constant__ AttentionArgs p) {
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
+    const uint32_t keys_full = base + kBarAt, keys_empty = keys_full + 8 * kKeys, codes_full = keys_empty + 8 * kKeys, codes_empty = codes_full + 8 * kCodes,
+                   values_full = codes_empty + 8 * kCodes, values_empty = values_full + 8 * kValues, scores_full = values_empty + 8 * kValues,
+                   weights_full = scores_full + 16, sums_full = weights_full + 16, queries_full = sums_full + 16, scales_full = queries_full + 16,
+                   drained = scales_full + 8 * kScaleSlots;
+    __shared__ uint32_t tensor_base, issued[2];
+    __shared__ int over;
+    __shared__ PlanShared plan;
+    __shared__ __align__(16) uint32_t page_scales[kScaleSlots][8];  // of 16 tokens each: keys', values'
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp == 0) {  // a barrier a lane
+        constexpr int kCodesEmpty = 2 * kKeys + kCodes, kValuesFull = kCodesEmpty + kCodes, kScores = kValuesFull + 2 * kValues, kAll = kScores + 8 + kScaleSlots + 1;
+        static_assert(kAll <= 32, "one lane each");
+        const bool by_warps = (lane >= kCodesEmpty && lane < kValuesFull + kValues) || lane == kScores + 2 || lane == kScores + 3 || lane == kScores + 6 ||
+                              lane == kScores + 7;  // codes empty, values full, weights, queries
+        if (lane < kAll) barrier_init(keys_full + 8 * lane, by_warps ? 4 : 1);
+        barrier_init_fence();
+        if (lane == 0) {
+            over = 0;
+            issued[0] = issued[1] = 0;
+            prefetch_map(&maps.k), prefetch_map(&maps.v);
+        }
+    } else if (warp == 13) {
+        tensor_alloc<false>(shared_address(&tensor_base), 512);
+    }
+    tensor_fence_before();
+    __syncthreads();
+    tensor_fence_after();
+    launch_dependents();
+    dependency_wait();
+    const uint32_t tensor = tensor_base;
+    Bounds bounds{&over, p.status};
+    const Withheld withheld = withheld_of(bounds, blockIdx.x);
+    const Share share = find_share<kThreads, kRows>(p, plan);
+    Walk<kRows> walk(p, share);
+
+    if (warp < 8) {
+        more_registers<kMany>();
+        const int which = warp >> 2, row = (warp & 3) * 32 + lane;  // tile of rows, row in it
+        const uint32_t mine = (warp & 3) << 21, scores = tensor + mine + which * 128, sums = tensor + mine + 256 + which * 128;
+        PartHead* head = part_heads<kRows>(p) + blockIdx.x;
+        if (threadIdx.x == 0 && gridDim.x > 1) head->parts = 0;
+        uint32_t tile = 0, scored = 0, items = 0;  // tiles and items of this block, and of this tile of rows
+        bool ok = true;
+        for (; walk.there(); walk.next()) {
+            const Item& it = walk.it;
+            const int count = walk.count();
+            if (it.rows <= 128 * which) {  // no rows here
+                tile += count;
+                continue;
+            }
+            const int packed = min(which * 128 + row, it.rows - 1);
+            const RowPlace place = place_of(p, it.q, it.head, it.q0 + packed);
+            const int position = it.q.first + place.row - it.q.row;
+            const int to = p.causal ? min(it.q.held, position + 1) : it.q.held, from = p.window > 0 ? max(0, position - p.window + 1) : 0;
+            float factor;
+            bool finite;
+            {
+                const uint4* q = reinterpret_cast<const uint4*>(p.q + place.row * p.q_row + place.head * p.q_head);
+                uint32_t x[64];  // two values a word
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                    if (8 * j < p.cache.dim) w = __ldg(q + j);
+                    x[4 * j] = w.x, x[4 * j + 1] = w.y, x[4 * j + 2] = w.z, x[4 * j + 3] = w.w;
+                }
+                uint32_t most = 0u;
+#pragma unroll
+                for (int j = 0; j < 64; ++j) most = max(most, max((x[j] << 16) & 0x7fffffffu, x[j] & 0x7fff0000u));
+                finite = most < kFiniteEnd;
+                const uint32_t byte = finite ? scale_byte(most) : 127u;
+                const float inverse = inverse_of(byte);
+                factor = scale_of(byte) * p.scale;
+                const uint32_t at = base + kQueryAt + which * 2 * kBytes + row * 128;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t h0, l0, h1, l1;
+                        const uint32_t a = x[8 * j + 2 * i], b = x[8 * j + 2 * i + 1];
+                        two_codes(__uint_as_float(a << 16) * inverse, __uint_as_float(a & 0xffff0000u) * inverse, h0, l0);
+                        two_codes(__uint_as_float(b << 16) * inverse, __uint_as_float(b & 0xffff0000u) * inverse, h1, l1);
+                        hi[i] = h0 | h1 << 16, lo[i] = l0 | l1 << 16;
+                    }
+                    const uint32_t chunk = at + ((j ^ (row & 7)) << 4);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk + kBytes), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                }
+                async_fence();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(queries_full + 8 * which);
+            }
+            float top = kNone, weight = 0.0f;
+            for (int t = 0; t < count; ++t, ++tile, ++scored) {
+                const uint32_t slot = tile % kScaleSlots;
+                const int tile_at = (walk.begin() + t) * kTile;
+                ok = ok && warp_wait(scales_full + 8 * slot, (tile / kScaleSlots) & 1, bounds) && warp_wait(scores_full + 8 * which, scored & 1, bounds);
+                tensor_fence_after();
+                float s[128];
+#pragma unroll
+                for (int c = 0; c < 128; c += 32) tensor_load(scores + c, reinterpret_cast<float(&)[32]>(s[c]));
+                uint32_t words[8];
+                {
+                    const uint4 a = *reinterpret_cast<const uint4*>(&page_scales[slot][0]), b = *reinterpret_cast<const uint4*>(&page_scales[slot][4]);
+                    words[0] = a.x, words[1] = a.y, words[2] = a.z, words[3] = a.w, words[4] = b.x, words[5] = b.y, words[6] = b.z, words[7] = b.w;
+                }
+                tensor_wait_loads();
+                if (__any_sync(0xffffffffu, tile_at < from || tile_at + kTile > to)) {
+                    const int end = to - tile_at, begin = from - tile_at;
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i >= end || i < begin) s[i] = kNone;
+                }
+                const auto key_of = [&](int c) { return fmaxf(factor * __uint_as_float((words[c] & 0xffu) << 23), 0x1p-120f); };  // (never 0: times -inf)
+                const auto value_of = [&](int c) { return static_cast<float>(static_cast<int>(words[c] >> 8) - 127); };
+                float high = kNone;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    float most = s[16 * c];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[16 * c + i]);
+                    high = fmaxf(high, fmaf(most, key_of(c), value_of(c)));
+                }
+                if (t == 0) {
+                    top = high;
+                } else if (__any_sync(0xffffffffu, high > top + kRoom)) {
+                    const float next = fmaxf(top, high), less = next == kNone ? 1.0f : exp2_of(top - next);
+                    weight *= less;
+                    top = next;
+#pragma unroll
+                    for (int c = 0; c < 128; c += 32) {
+                        float v[32];
+                        uint32_t w[32];
+                        tensor_load(sums + c, v);
+                        tensor_wait_loads();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i] * less);
+                        tensor_store(sums + c, w);
+                    }
+                }
+                const float against = top == kNone ? 0.0f : top;
+#pragma unroll
+                for (int c0 = 0; c0 < 8; c0 += 4) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int c = c0; c < c0 + 4; ++c) {
+                        const float key = key_of(c), value = value_of(c) - against;
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            const float a = exp2_of(fmaf(s[16 * c + i], key, value)), b = exp2_of(fmaf(s[16 * c + i + 1], key, value));
+                            sum += a + b;
+                            w[(c - c0) * 8 + i / 2] = f16x2_of(a, b);
+                        }
+                        weight = fmaf(sum, __uint_as_float((254u - (words[c] >> 8)) << 23), weight);
+                    }
+                    tensor_store(scores + c0 * 8, w);
+                }
+                tensor_wait_stores();
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(weights_full + 8 * which);
+            }
+            if (count > 0) {
+                ok = ok && warp_wait(sums_full + 8 * which, items & 1, bounds);
+                ++items;
+                tensor_fence_after();
+            }
+            const bool there = which * 128 + row < it.rows, whole = walk.first() && walk.last();
+            if (!ok || over) weight = top = __uint_as_float(0x7fffffffu);
+            if (!finite) weight = __uint_as_float(0x7fffffffu);
+            if (!whole && walk.first() && row == 0 && which == 0) *head = {walk.parts(), it.q.row, it.q0, it.rows, it.head};
+            float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<kRows>();
+            const float one = weight == 0.0f ? 0.0f : 1.0f / weight;
+            __nv_bfloat16* out = p.out + place.row * p.out_row + place.head * p.out_head;
+#pragma unroll
+            for (int c = 0; c < 128; c += 32) {
+                float v[32];
+                if (count > 0) {
+                    tensor_load(sums + c, v);
+                    tensor_wait_loads();
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+                }
+                if (!there) continue;
+                if (whole) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8)
+                        if (c + i < p.cache.dim)
+                            *reinterpret_cast<uint4*>(out + c + i) = make_uint4(bf16x2_of(v[i] * one, v[i + 1] * one), bf16x2_of(v[i + 2] * one, v[i + 3] * one),
+                                                                                bf16x2_of(v[i + 4] * one, v[i + 5] * one), bf16x2_of(v[i + 6] * one, v[i + 7] * one));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4)
+                        *reinterpret_cast<float4*>(part + (which * 128 + row) * 128 + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                }
+            }
+            if (there && whole && p.lse) p.lse[int64_t(place.row) * p.heads + place.head] = row_lse(top, weight);
+            if (there && !whole) part[kRows * 128 + which * 128 + row] = top, part[kRows * 129 + which * 128 + row] = weight;
+            tensor_fence_before();  // (the sums are read before the next item's queries are there)
+        }
+    } else if (warp < 12) {
+        fewer_registers<kFew>();
+        const int token = (warp & 3) * 32 + lane;
+        const int chunks = (p.cache.dim + 15) / 16;  // of 16 codes
+        uint32_t tile = 0;
+        bool ok = true;
+        for (; walk.there() && ok; walk.next())
+            for (int t = 0; t < walk.count(); ++t, ++tile) {
+                const uint32_t from = tile % kCodes, to = tile % kValues;
+                ok = warp_wait(codes_full + 8 * from, (tile / kCodes) & 1, bounds) && warp_wait(values_empty + 8 * to, ((tile / kValues) & 1) ^ 1, bounds);
+                if (!ok) break;
+                // What no row sees may be anything, NaN too, which a weight of zero would not take out.
+                const int position = (walk.begin() + t) * kTile + token;
+                const bool seen = position >= walk.it.lo && position < walk.it.hi;
+                const uint32_t codes = base + kCodeAt + from * kBytes + token * 128, values = base + kValueAt + to * 2 * kBytes + token * 128;
+#pragma unroll 1
+                for (int j = 0; j < chunks; ++j) {
+                    uint32_t w[4], v[8];
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                                 : "r"(codes + ((j ^ (token & 7)) << 4)));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v[2 * i]) : "h"(static_cast<uint16_t>(w[i])));
+                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v[2 * i + 1]) : "h"(static_cast<uint16_t>(w[i] >> 16)));
+                    }
+                    if (!seen) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = 0u;
+                    }
+                    const uint32_t at = values + (j >> 2) * kBytes;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((2 * (j & 3) + i) ^ (token & 7)) << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]),
+                                     "r"(v[4 * i + 2]), "r"(v[4 * i + 3])
+                                     : "memory");
+                }
+                async_fence();
+                __syncwarp();
+                if (lane == 0) {
+                    barrier_arrive(codes_empty + 8 * from);
+                    barrier_arrive(values_full + 8 * to);
+                }
+            }
+    } else {
+        fewer_registers<kFew>();
+        if (warp == 12) {
+            const int pages = kTile >> p.cache.page_shift, page_bytes = 128 << p.cache.page_shift;  // of a tile
+            uint32_t tile = 0, loaded[2] = {0, 0};
+            bool ok = true;
+            for (; walk.there() && ok; walk.next()) {
+                if (walk.count() == 0) continue;
+                Pages list(p, walk.it, walk.begin() * pages);
+                int within = 0;
+                for (int t = 0; t < walk.count() && ok; ++t, ++tile) {
+                    if (within == 32) list.next(), within = 0;
+                    const uint32_t slot = tile % kScaleSlots;
+                    const uint32_t word = __shfl_sync(0xffffffffu, list.scales, within + ((lane & 7) * pages >> 3));
+                    const int page = __shfl_sync(0xffffffffu, list.id, within + (lane & (pages - 1)));
+                    within += pages;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t stages = half ? kCodes : kKeys, at = tile % stages, parity = ((tile / stages) & 1) ^ 1;
+                        const uint32_t bar = (half ? codes_full : keys_full) + 8 * at;
+                        ok = !(withheld.copies && tile >= kKeys + kWithheldFrom) && warp_wait((half ? codes_empty : keys_empty) + 8 * at, parity, bounds);
+                        if (!ok) break;
+                        if (half == 0) {
+                            if (lane < 8) page_scales[slot][lane] = word;
+                            __syncwarp();
+                            if (lane == 0) barrier_arrive(scales_full + 8 * slot);
+                        }
+                        if (lane == 0) barrier_expect(bar, kBytes);
+                        __syncwarp();
+                        if (lane < pages) load_page(base + (half ? kCodeAt : kKeyAt) + at * kBytes + lane * page_bytes, half ? &maps.v : &maps.k, walk.it.head, page, bar);
+                        __syncwarp();
+                        ++loaded[half];
+                    }
+                }
+            }
+            if (lane == 0) issued[0] = loaded[0], issued[1] = loaded[1];
+        } else if (warp == 13 && elected()) {
+            constexpr uint32_t to_scores = product_codes(128, 128, false, false);
+            const uint32_t to_sums = product_codes(128, p.cache.dim, false, true);  // (fp16 has the code of e4m3)
+            const uint64_t queries0 = operand(base + kQueryAt), keys0 = operand(base + kKeyAt), values0 = operand(base + kValueAt, kBytes);
+            const int steps = (p.cache.dim + 31) / 32;
+            uint32_t tile = 0, scored[2] = {0, 0}, items[2] = {0, 0};
+            bool ok = true;
+            const auto score = [&](int which, uint32_t t) {
+                const uint64_t k = keys0 + (t % kKeys) * (kBytes >> 4), q = queries0 + which * (2 * kBytes >> 4);
+                const uint32_t d = tensor + which * 128;
+                for (int i = 0; i < steps; ++i) {
+                    multiply_codes(d, q + 2 * i, k + 2 * i, to_scores, i > 0);
+                    multiply_codes(d, q + (kBytes >> 4) + 2 * i, k + 2 * i, to_scores, true);
+                }
+                products_done<false>(scores_full + 8 * which);
+            };
+            const auto add = [&](int which, uint32_t t, bool first) {
+                const uint64_t v = values0 + (t % kValues) * (2 * kBytes >> 4);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) multiply_f16(tensor + 256 + which * 128, tensor + which * 128 + 8 * i, v + 128 * i, to_sums, !first || i > 0);
+            };
+            for (; walk.there() && ok; walk.next()) {
+                const int count = walk.count();
+                const bool two = walk.it.rows > 128;
+                ok = barrier_wait(queries_full, items[0]++ & 1, bounds) && (!two || barrier_wait(queries_full + 8, items[1]++ & 1, bounds));
+                if (!ok) break;
+                if (count == 0) continue;
+                ok = barrier_wait(keys_full + 8 * (tile % kKeys), (tile / kKeys) & 1, bounds);
+                if (!ok) break;
+                tensor_fence_after();
+                score(0, tile);
+                if (two) score(1, tile);
+                products_done<false>(keys_empty + 8 * (tile % kKeys));
+                for (int t = 0; t < count; ++t, ++tile) {
+                    const bool more = t + 1 < count;
+                    ok = barrier_wait(values_full + 8 * (tile % kValues), (tile / kValues) & 1, bounds) && barrier_wait(weights_full, scored[0]++ & 1, bounds) &&
+                         (!more || barrier_wait(keys_full + 8 * ((tile + 1) % kKeys), ((tile + 1) / kKeys) & 1, bounds));
+                    if (!ok) break;
+                    tensor_fence_after();
+                    add(0, tile, t == 0);
+                    if (more) score(0, tile + 1);
+                    else products_done<false>(sums_full);
+                    if (two) {
+                        ok = barrier_wait(weights_full + 8, scored[1]++ & 1, bounds);
+                        if (!ok) break;
+                        tensor_fence_after();
+                        add(1, tile, t == 0);
+                    }
+                    products_done<false>(values_empty + 8 * (tile % kValues));
+                    if (two && more) score(1, tile + 1);
+                    if (two && !more) products_done<false>(sums_full + 8);
+                    if (more) products_done<false>(keys_empty + 8 * ((tile + 1) % kKeys));
+                }
+            }
+            if (!ok) {
+                products_done<false>(drained);
+                for (int polls = 0; polls < kLandings && !barrier_passed(drained, 0); ++polls) {}
+            }
+        }
+    }
+    __syncwarp();
+    tensor_fence_before();
+    __syncthreads();
+    if (__builtin_expect(over, 0) && warp == 12) {  // copies in flight have to land before the block ends
+        land<kKeys>(keys_full, issued[0]);
+        land<kCodes>(codes_full, issued[1]);
+    }
+    if (warp == 13) {
+        tensor_fence_after();
+        tensor_free<false>(tensor, 512);
+    }
+}
+
+}  // namespace
+
+int attention_many(const AttentionArgs& a, int blocks, cudaStream_t s) {
+    CacheMaps maps;
+    int st = cache_maps(a.cache, &maps);
+    if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(attention_many_kernel), kShared);
+    int registers = 0;
+    if (st == PVQ_OK) st = registers_of(reinterpret_cast<const void*>(attention_many_kernel), &registers);
+    if (st != PVQ_OK) return st;
+    if (registers < kRegisters) return PVQ_ERR_UNSUPPORTED;  // (a build that gives it fewer: the warps' shares would be waited for without end)
+    return launch_early(attention_many_kernel, dim3(static_cast<unsigned>(blocks)), kThreads, kShared, 0, s, maps, a);
+}
+
+}  // namespace fp8
+}  // namespace pvq
