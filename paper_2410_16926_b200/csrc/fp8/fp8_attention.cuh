@@ -38,8 +38,9 @@ struct Item {
     Sequence q;
     int q0, rows;        // its rows of the sequence's n * group
     int lo, hi;          // positions that some row sees
-    int tile0, tiles;    // of those
-    int units;
+    __device__ __forceinline__ int tile0() const { return lo / kTile; }  // of those
+    __device__ __forceinline__ int tiles() const { return hi > lo ? (hi + kTile - 1) / kTile - tile0() : 0; }
+    __device__ __forceinline__ int units() const { return max(tiles(), 1); }
 };
 
 template <int ROWS>
@@ -49,24 +50,22 @@ __device__ __forceinline__ void measure(const AttentionArgs& a, Item& it) {
     const int i0 = it.q0 / a.group, i1 = (it.q0 + it.rows - 1) / a.group;
     it.hi = a.causal ? min(it.q.held, it.q.first + i1 + 1) : it.q.held;
     it.lo = a.window > 0 ? max(0, it.q.first + i0 - a.window + 1) : 0;
-    it.tile0 = it.lo / kTile;
-    it.tiles = it.hi > it.lo ? (it.hi + kTile - 1) / kTile - it.tile0 : 0;
-    it.units = max(it.tiles, 1);
 }
 template <int ROWS>
 __device__ __forceinline__ int blocks_of(const AttentionArgs& a, const Sequence& q) {
     return (q.n * a.group + ROWS - 1) / ROWS;
 }
 
-struct PlanShared {
-    long long sums[32], total, left, per_head;
-    int s;
-};
 // A block's share: it begins `skip` units into an item.
 struct Share {
     int s, head, block, skip;
     long long begin, left, all;
     int blocks;  // that have a share
+};
+struct PlanShared {
+    long long sums[32], left, per_head;
+    int s;
+    Share share;
 };
 
 // All threads of the block.
@@ -87,7 +86,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
             const int blocks = blocks_of<ROWS>(a, it.q);
             for (it.block = thread & (lanes - 1); it.block < blocks; it.block += lanes) {
                 measure<ROWS>(a, it);
-                units += it.units;
+                units += it.units();
             }
         }
         for (int o = lanes >> 1; o > 0; o >>= 1) units += __shfl_xor_sync(0xffffffffu, units, o);
@@ -141,7 +140,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
         long long sum = 0;
         if (it.block < blocks) {
             measure<ROWS>(a, it);
-            sum = it.units;
+            sum = it.units();
         }
         for (int o = 1; o < 32; o <<= 1) {
             const long long other = __shfl_up_sync(0xffffffffu, sum, o);
@@ -157,35 +156,36 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
         rest -= __shfl_sync(0xffffffffu, sum, 31);
     }
     r.skip = static_cast<int>(rest);
+    if (thread == 0) sh.share = r;
+    __syncthreads();
     return r;
 }
 
-// Goes through a block's share, item by item.  Every role of the block does so by itself.
+// Goes through a block's share, item by item.  Every role of the block does so by itself.  (A share of 2^31 tiles would take an hour.)
 template <int ROWS>
 struct Walk {
     const AttentionArgs& a;
     Item it;
-    long long at, left, all;
-    int blocks, skip, take;
+    int left, skip, take;
 
-    __device__ __forceinline__ Walk(const AttentionArgs& args, const Share& sh) : a(args), at(sh.begin), left(sh.left), all(sh.all), blocks(sh.blocks), skip(sh.skip), take(0) {
+    __device__ __forceinline__ Walk(const AttentionArgs& args, const Share& sh) : a(args), left(static_cast<int>(sh.left)), skip(sh.skip), take(0) {
         if (left <= 0) return;
         it.s = sh.s, it.head = sh.head, it.block = sh.block;
         it.q = sequence_of(a.step, it.s, a.cache.page_shift);
         measure<ROWS>(a, it);
-        take = static_cast<int>(min(left, static_cast<long long>(it.units - skip)));
+        take = min(left, it.units() - skip);
     }
     __device__ __forceinline__ bool there() const { return left > 0; }
-    __device__ __forceinline__ int begin() const { return it.tile0 + skip; }  // tiles of this share
-    __device__ __forceinline__ int count() const { return min(take, it.tiles); }
+    __device__ __forceinline__ int begin() const { return it.tile0() + skip; }  // tiles of this share
+    __device__ __forceinline__ int count() const { return min(take, it.tiles()); }
     __device__ __forceinline__ bool first() const { return skip == 0; }
-    __device__ __forceinline__ bool last() const { return skip + take == it.units; }
+    __device__ __forceinline__ bool last() const { return skip + take == it.units(); }
     // Blocks that the item is shared by, from its first one on (called where first()).
-    __device__ __forceinline__ int parts() const {
-        return static_cast<int>(((at + it.units) * blocks - 1) / all - blockIdx.x) + 1;
+    __device__ __forceinline__ int parts(const PlanShared& plan) const {
+        return static_cast<int>(((plan.share.begin + plan.share.left - left + it.units()) * plan.share.blocks - 1) / plan.share.all - blockIdx.x) + 1;
     }
     __device__ __forceinline__ void next() {
-        at += take, left -= take;
+        left -= take;
         if (left <= 0) return;
         skip = 0;
         if (++it.block == blocks_of<ROWS>(a, it.q)) {
@@ -198,7 +198,7 @@ struct Walk {
             }
         }
         measure<ROWS>(a, it);
-        take = static_cast<int>(min(left, static_cast<long long>(it.units)));
+        take = min(left, it.units());
     }
 };
 

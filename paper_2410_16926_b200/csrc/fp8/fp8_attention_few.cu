@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
             }
             tokens_meet();
             const bool lost = over != 0, whole = walk.first() && walk.last();
-            if (!whole && walk.first() && thread == 0) *head = {walk.parts(), it.q.row, it.q0, it.rows, it.head};
+            if (!whole && walk.first() && thread == 0) *head = {walk.parts(plan), it.q.row, it.q0, it.rows, it.head};
             float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<ROWS>();
 #pragma unroll
             for (int n = 0; n < ROWS; ++n) {

@@ -24,7 +24,7 @@ constexpr int kQueryAt = 0, kKeyAt = 4 * kBytes, kCodeAt = kKeyAt + kKeys * kByt
 constexpr size_t kShared = 1024 + kBarAt + 256;
 constexpr float kRoom = 8.0f;           // exponent by which a row's largest may be behind
 
-constexpr int kRegisters = 128, kMany = 192, kFew = 64;
+constexpr int kRegisters = 128, kMany = 168, kFew = 88;
 static_assert(2 * kMany + 2 * kFew <= 4 * kRegisters, "a share beyond these would be waited for without end");
 static_assert(kShared + 2048 <= 232448, "shared memory");
 
@@ -48,6 +48,52 @@ __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&w)[32
         "r"(w[13]), "r"(w[14]), "r"(w[15]), "r"(w[16]), "r"(w[17]), "r"(w[18]), "r"(w[19]), "r"(w[20]), "r"(w[21]), "r"(w[22]), "r"(w[23]), "r"(w[24]),
         "r"(w[25]), "r"(w[26]), "r"(w[27]), "r"(w[28]), "r"(w[29]), "r"(w[30]), "r"(w[31])
         : "memory");
+}
+
+__device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&w)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(w[8]), "r"(w[9]), "r"(w[10]), "r"(w[11]), "r"(w[12]), "r"(w[13]), "r"(w[14]), "r"(w[15])
+                 : "memory");
+}
+// Waits for the loads, of which v's values are not to be looked at before.
+__device__ __forceinline__ void tensor_wait(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]),
+                   "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
+                   "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29])
+                 :
+                 : "memory");
+    asm volatile("" : "+f"(v[30]), "+f"(v[31]));
+}
+// Two values at a time.
+__device__ __forceinline__ float2 two_fma(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 two_add(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// The largest of 16.
+__device__ __forceinline__ float most_of(const float* v) {
+    const float a = max3(v[0], v[1], v[2]), b = max3(v[3], v[4], v[5]), c = max3(v[6], v[7], v[8]), d = max3(v[9], v[10], v[11]), e = max3(v[12], v[13], v[14]);
+    return max3(max3(a, b, c), max3(d, e, v[15]), a);
+}
+__device__ __forceinline__ void hide(float (&v)[32], int begin, int end) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        if (i < begin || i >= end) v[i] = kNone;
 }
 
 __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __grid_constant__ CacheMaps maps, const __grid_constant__ AttentionArgs p) {
@@ -151,30 +197,26 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 const int tile_at = (walk.begin() + t) * kTile;
                 ok = ok && warp_wait(scales_full + 8 * slot, (tile / kScaleSlots) & 1, bounds) && warp_wait(scores_full + 8 * which, scored & 1, bounds);
                 tensor_fence_after();
-                float s[128];
-#pragma unroll
-                for (int c = 0; c < 128; c += 32) tensor_load(scores + c, reinterpret_cast<float(&)[32]>(s[c]));
+                const bool cut = __any_sync(0xffffffffu, tile_at < from || tile_at + kTile > to);
+                const int end = to - tile_at, begin = from - tile_at;
+                float s[2][32];
+                tensor_load(scores, s[0]);
                 uint32_t words[8];
                 {
                     const uint4 a = *reinterpret_cast<const uint4*>(&page_scales[slot][0]), b = *reinterpret_cast<const uint4*>(&page_scales[slot][4]);
                     words[0] = a.x, words[1] = a.y, words[2] = a.z, words[3] = a.w, words[4] = b.x, words[5] = b.y, words[6] = b.z, words[7] = b.w;
                 }
-                tensor_wait_loads();
-                if (__any_sync(0xffffffffu, tile_at < from || tile_at + kTile > to)) {
-                    const int end = to - tile_at, begin = from - tile_at;
-#pragma unroll
-                    for (int i = 0; i < 128; ++i)
-                        if (i >= end || i < begin) s[i] = kNone;
-                }
                 const auto key_of = [&](int c) { return fmaxf(factor * __uint_as_float((words[c] & 0xffu) << 23), 0x1p-120f); };  // (never 0: times -inf)
                 const auto value_of = [&](int c) { return static_cast<float>(static_cast<int>(words[c] >> 8) - 127); };
                 float high = kNone;
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    float most = s[16 * c];
+                for (int c = 0; c < 4; ++c) {
+                    float (&v)[32] = s[c & 1];
+                    tensor_wait(v);
+                    tensor_load(scores + (c < 3 ? 32 * (c + 1) : 0), s[(c + 1) & 1]);
+                    if (cut) hide(v, begin - 32 * c, end - 32 * c);
 #pragma unroll
-                    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[16 * c + i]);
-                    high = fmaxf(high, fmaf(most, key_of(c), value_of(c)));
+                    for (int i = 0; i < 2; ++i) high = fmaxf(high, fmaf(most_of(&v[16 * i]), key_of(2 * c + i), value_of(2 * c + i)));
                 }
                 if (t == 0) {
                     top = high;
@@ -182,12 +224,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                     const float next = fmaxf(top, high), less = next == kNone ? 1.0f : exp2_of(top - next);
                     weight *= less;
                     top = next;
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < 128; c += 32) {
                         float v[32];
                         uint32_t w[32];
                         tensor_load(sums + c, v);
-                        tensor_wait_loads();
+                        tensor_wait(v);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i] * less);
                         tensor_store(sums + c, w);
@@ -195,21 +237,26 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 }
                 const float against = top == kNone ? 0.0f : top;
 #pragma unroll
-                for (int c0 = 0; c0 < 8; c0 += 4) {
-                    uint32_t w[32];
+                for (int c = 0; c < 4; ++c) {
+                    float (&v)[32] = s[c & 1];
+                    tensor_wait(v);
+                    if (c < 3) tensor_load(scores + 32 * (c + 1), s[(c + 1) & 1]);
+                    if (cut) hide(v, begin - 32 * c, end - 32 * c);
+                    uint32_t w[16];
 #pragma unroll
-                    for (int c = c0; c < c0 + 4; ++c) {
-                        const float key = key_of(c), value = value_of(c) - against;
-                        float sum = 0.0f;
+                    for (int h = 0; h < 2; ++h) {
+                        const float2 key = make_float2(key_of(2 * c + h), key_of(2 * c + h)), value = make_float2(value_of(2 * c + h) - against, value_of(2 * c + h) - against);
+                        float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {
-                            const float a = exp2_of(fmaf(s[16 * c + i], key, value)), b = exp2_of(fmaf(s[16 * c + i + 1], key, value));
-                            sum += a + b;
-                            w[(c - c0) * 8 + i / 2] = f16x2_of(a, b);
+                            const float2 x = two_fma(make_float2(v[16 * h + i], v[16 * h + i + 1]), key, value);
+                            const float2 e = make_float2(exp2_of(x.x), exp2_of(x.y));
+                            sum = two_add(sum, e);
+                            w[8 * h + i / 2] = f16x2_of(e.x, e.y);
                         }
-                        weight = fmaf(sum, __uint_as_float((254u - (words[c] >> 8)) << 23), weight);
+                        weight = fmaf(sum.x + sum.y, __uint_as_float((254u - (words[2 * c + h] >> 8)) << 23), weight);
                     }
-                    tensor_store(scores + c0 * 8, w);
+                    tensor_store(scores + 16 * c, w);  // (where scores are that have been read)
                 }
                 tensor_wait_stores();
                 tensor_fence_before();
@@ -224,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             const bool there = which * 128 + row < it.rows, whole = walk.first() && walk.last();
             if (!ok || over) weight = top = __uint_as_float(0x7fffffffu);
             if (!finite) weight = __uint_as_float(0x7fffffffu);
-            if (!whole && walk.first() && row == 0 && which == 0) *head = {walk.parts(), it.q.row, it.q0, it.rows, it.head};
+            if (!whole && walk.first() && row == 0 && which == 0) *head = {walk.parts(plan), it.q.row, it.q0, it.rows, it.head};
             float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<kRows>();
             const float one = weight == 0.0f ? 0.0f : 1.0f / weight;
             __nv_bfloat16* out = p.out + place.row * p.out_row + place.head * p.out_head;
@@ -270,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 const int position = (walk.begin() + t) * kTile + token;
                 const bool seen = position >= walk.it.lo && position < walk.it.hi;
                 const uint32_t codes = base + kCodeAt + from * kBytes + token * 128, values = base + kValueAt + to * 2 * kBytes + token * 128;
-#pragma unroll 1
+#pragma unroll 2
                 for (int j = 0; j < chunks; ++j) {
                     uint32_t w[4], v[8];
                     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
