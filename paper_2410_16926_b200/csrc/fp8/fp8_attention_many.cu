@@ -1,7 +1,8 @@
 // Attention of many query rows over the 8-bit cache: bound by the tensor cores and the exponentials.
 //
-// A block takes 256 query rows, as two tiles of 128 that take turns: while the tensor cores multiply for one, four warps compute the
-// weights of the other, a thread a row.  S = Q K^T from the codes of K as they lie, Q split into two codes (2^-17 of the row's largest),
+// A block takes 256 query rows, as two tiles of 128 with four warps each, a thread a row, which compute weights while the tensor cores
+// multiply: for each tile of rows there are scores of 64 tokens in two places of tensor memory, so that those of the next 64 are there when the
+// weights of these are done.  S = Q K^T from the codes of K as they lie, Q split into two codes (2^-17 of the row's largest),
 // which costs what a product of 16-bit operands would, and K needs no conversion.  The weights go back into tensor memory as fp16, over
 // the scores, and O += P V takes V as fp16, which four warps make of its codes (exact) for both tiles.
 //
@@ -21,7 +22,7 @@ constexpr int kBytes = kTile * 128;     // a tile's codes, rows of 128 bytes
 constexpr int kKeys = 3, kCodes = 2, kValues = 2;  // stages
 constexpr int kQueryAt = 0, kKeyAt = 4 * kBytes, kCodeAt = kKeyAt + kKeys * kBytes, kValueAt = kCodeAt + kCodes * kBytes,
               kBarAt = kValueAt + kValues * 2 * kBytes;
-constexpr size_t kShared = 1024 + kBarAt + 256;
+constexpr size_t kShared = 1024 + kBarAt + 512;
 constexpr float kRoom = 8.0f;           // exponent by which a row's largest may be behind
 
 constexpr int kRegisters = 128, kMany = 168, kFew = 88;
@@ -50,11 +51,6 @@ __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&w)[32
         : "memory");
 }
 
-__device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&w)[16]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(w[8]), "r"(w[9]), "r"(w[10]), "r"(w[11]), "r"(w[12]), "r"(w[13]), "r"(w[14]), "r"(w[15])
-                 : "memory");
-}
 // Waits for the loads, of which v's values are not to be looked at before.
 __device__ __forceinline__ void tensor_wait(float (&v)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -101,19 +97,19 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
     const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
     const uint32_t keys_full = base + kBarAt, keys_empty = keys_full + 8 * kKeys, codes_full = keys_empty + 8 * kKeys, codes_empty = codes_full + 8 * kCodes,
                    values_full = codes_empty + 8 * kCodes, values_empty = values_full + 8 * kValues, scores_full = values_empty + 8 * kValues,
-                   weights_full = scores_full + 16, sums_full = weights_full + 16, queries_full = sums_full + 16, scales_full = queries_full + 16,
-                   drained = scales_full + 8 * kScaleSlots;
+                   weights_full = scores_full + 32, queries_full = weights_full + 32, scales_full = queries_full + 16,
+                   drained = scales_full + 8 * kScaleSlots;  // (scores and weights: [tile of rows][half of the tokens])
     __shared__ uint32_t tensor_base, issued[2];
     __shared__ int over;
     __shared__ PlanShared plan;
     __shared__ __align__(16) uint32_t page_scales[kScaleSlots][8];  // of 16 tokens each: keys', values'
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (warp == 0) {  // a barrier a lane
-        constexpr int kCodesEmpty = 2 * kKeys + kCodes, kValuesFull = kCodesEmpty + kCodes, kScores = kValuesFull + 2 * kValues, kAll = kScores + 8 + kScaleSlots + 1;
-        static_assert(kAll <= 32, "one lane each");
-        const bool by_warps = (lane >= kCodesEmpty && lane < kValuesFull + kValues) || lane == kScores + 2 || lane == kScores + 3 || lane == kScores + 6 ||
-                              lane == kScores + 7;  // codes empty, values full, weights, queries
-        if (lane < kAll) barrier_init(keys_full + 8 * lane, by_warps ? 4 : 1);
+    if (warp == 0) {
+        constexpr int kCodesEmpty = 2 * kKeys + kCodes, kValuesFull = kCodesEmpty + kCodes, kScores = kValuesFull + 2 * kValues, kAll = kScores + 10 + kScaleSlots + 1;
+        const auto by_warps = [](int i) {  // codes empty, values full, weights, queries
+            return (i >= kCodesEmpty && i < kValuesFull + kValues) || (i >= kScores + 4 && i < kScores + 10);
+        };
+        for (int i = lane; i < kAll; i += 32) barrier_init(keys_full + 8 * i, by_warps(i) ? 4 : 1);
         barrier_init_fence();
         if (lane == 0) {
             over = 0;
@@ -140,7 +136,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
         const uint32_t mine = (warp & 3) << 21, scores = tensor + mine + which * 128, sums = tensor + mine + 256 + which * 128;
         PartHead* head = part_heads<kRows>(p) + blockIdx.x;
         if (threadIdx.x == 0 && gridDim.x > 1) head->parts = 0;
-        uint32_t tile = 0, scored = 0, items = 0;  // tiles and items of this block, and of this tile of rows
+        const uint32_t scores_bar = scores_full + 16 * which, weights_bar = weights_full + 16 * which;
+        uint32_t tile = 0, phase = 0;  // tiles of this block; phases of each half's scores
         bool ok = true;
         for (; walk.there(); walk.next()) {
             const Item& it = walk.it;
@@ -192,80 +189,83 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 if (lane == 0) barrier_arrive(queries_full + 8 * which);
             }
             float top = kNone, weight = 0.0f;
-            for (int t = 0; t < count; ++t, ++tile, ++scored) {
+            bool next_there = false;
+            for (int t = 0; t < count; ++t, ++tile, ++phase) {
                 const uint32_t slot = tile % kScaleSlots;
-                const int tile_at = (walk.begin() + t) * kTile;
-                ok = ok && warp_wait(scales_full + 8 * slot, (tile / kScaleSlots) & 1, bounds) && warp_wait(scores_full + 8 * which, scored & 1, bounds);
-                tensor_fence_after();
-                const bool cut = __any_sync(0xffffffffu, tile_at < from || tile_at + kTile > to);
-                const int end = to - tile_at, begin = from - tile_at;
-                float s[2][32];
-                tensor_load(scores, s[0]);
-                uint32_t words[8];
-                {
-                    const uint4 a = *reinterpret_cast<const uint4*>(&page_scales[slot][0]), b = *reinterpret_cast<const uint4*>(&page_scales[slot][4]);
-                    words[0] = a.x, words[1] = a.y, words[2] = a.z, words[3] = a.w, words[4] = b.x, words[5] = b.y, words[6] = b.z, words[7] = b.w;
-                }
-                const auto key_of = [&](int c) { return fmaxf(factor * __uint_as_float((words[c] & 0xffu) << 23), 0x1p-120f); };  // (never 0: times -inf)
-                const auto value_of = [&](int c) { return static_cast<float>(static_cast<int>(words[c] >> 8) - 127); };
-                float high = kNone;
+                ok = ok && warp_wait(scales_full + 8 * slot, (tile / kScaleSlots) & 1, bounds);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    float (&v)[32] = s[c & 1];
-                    tensor_wait(v);
-                    tensor_load(scores + (c < 3 ? 32 * (c + 1) : 0), s[(c + 1) & 1]);
-                    if (cut) hide(v, begin - 32 * c, end - 32 * c);
+                for (int half = 0; half < 2; ++half) {
+                    const int tile_at = (walk.begin() + t) * kTile + 64 * half;
+                    ok = ok && (next_there || warp_wait(scores_bar + 8 * half, phase & 1, bounds));
+                    tensor_fence_after();
+                    float s[2][32];
+                    tensor_load(scores + 64 * half, s[0]);
+                    tensor_load(scores + 64 * half + 32, s[1]);
+                    const uint4 four = *reinterpret_cast<const uint4*>(&page_scales[slot][4 * half]);
+                    const uint32_t words[4] = {four.x, four.y, four.z, four.w};
+                    float key[4], value[4];  // (a key's never 0: it is multiplied by -inf)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) high = fmaxf(high, fmaf(most_of(&v[16 * i]), key_of(2 * c + i), value_of(2 * c + i)));
-                }
-                if (t == 0) {
-                    top = high;
-                } else if (__any_sync(0xffffffffu, high > top + kRoom)) {
-                    const float next = fmaxf(top, high), less = next == kNone ? 1.0f : exp2_of(top - next);
-                    weight *= less;
-                    top = next;
-#pragma unroll 1
-                    for (int c = 0; c < 128; c += 32) {
-                        float v[32];
-                        uint32_t w[32];
-                        tensor_load(sums + c, v);
-                        tensor_wait(v);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i] * less);
-                        tensor_store(sums + c, w);
+                    for (int c = 0; c < 4; ++c) {
+                        key[c] = fmaxf(factor * __uint_as_float((words[c] & 0xffu) << 23), 0x1p-120f);
+                        value[c] = static_cast<float>(static_cast<int>(words[c] >> 8) - 127);
                     }
-                }
-                const float against = top == kNone ? 0.0f : top;
+                    tensor_wait(s[0]);
+                    tensor_wait(s[1]);
+                    if (__any_sync(0xffffffffu, tile_at < from || tile_at + 64 > to)) {
+                        hide(s[0], from - tile_at, to - tile_at);
+                        hide(s[1], from - tile_at - 32, to - tile_at - 32);
+                    }
+                    float high = kNone;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    float (&v)[32] = s[c & 1];
-                    tensor_wait(v);
-                    if (c < 3) tensor_load(scores + 32 * (c + 1), s[(c + 1) & 1]);
-                    if (cut) hide(v, begin - 32 * c, end - 32 * c);
-                    uint32_t w[16];
+                    for (int c = 0; c < 4; ++c) high = fmaxf(high, fmaf(most_of(&s[c >> 1][16 * (c & 1)]), key[c], value[c]));
+                    if (t == 0 && half == 0) {
+                        top = high;
+                    } else if (__any_sync(0xffffffffu, high > top + kRoom)) {
+                        // (the products with the weights before are done when the scores behind them are)
+                        ok = ok && warp_wait(scores_bar + 8 * (half ^ 1), half ? (phase + 1) & 1 : phase & 1, bounds);
+                        tensor_fence_after();
+                        const float next = fmaxf(top, high), less = next == kNone ? 1.0f : exp2_of(top - next);
+                        weight *= less;
+                        top = next;
+#pragma unroll 1
+                        for (int c = 0; c < 128; c += 32) {
+                            float v[32];
+                            uint32_t w[32];
+                            tensor_load(sums + c, v);
+                            tensor_wait(v);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float2 key = make_float2(key_of(2 * c + h), key_of(2 * c + h)), value = make_float2(value_of(2 * c + h) - against, value_of(2 * c + h) - against);
+                            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i] * less);
+                            tensor_store(sums + c, w);
+                        }
+                    }
+                    // (asked before there is something to do: an answer takes 150 to 200 cycles, also where it is yes)
+                    next_there = (half == 0 || t + 1 < count) && barrier_over(scores_bar + 8 * (half ^ 1), half ? (phase + 1) & 1 : phase & 1);
+                    const float against = top == kNone ? 0.0f : top;
+                    uint32_t w[32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float (&v)[32] = s[c >> 1];
+                        const float2 k = make_float2(key[c], key[c]), r = make_float2(value[c] - against, value[c] - against);
                         float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {
-                            const float2 x = two_fma(make_float2(v[16 * h + i], v[16 * h + i + 1]), key, value);
+                            const float2 x = two_fma(make_float2(v[16 * (c & 1) + i], v[16 * (c & 1) + i + 1]), k, r);
                             const float2 e = make_float2(exp2_of(x.x), exp2_of(x.y));
                             sum = two_add(sum, e);
-                            w[8 * h + i / 2] = f16x2_of(e.x, e.y);
+                            w[8 * c + i / 2] = f16x2_of(e.x, e.y);
                         }
-                        weight = fmaf(sum.x + sum.y, __uint_as_float((254u - (words[2 * c + h] >> 8)) << 23), weight);
+                        weight = fmaf(sum.x + sum.y, __uint_as_float((254u - (words[c] >> 8)) << 23), weight);
                     }
-                    tensor_store(scores + 16 * c, w);  // (where scores are that have been read)
+                    tensor_store(scores + 64 * half, w);  // (over the scores that have been read)
+                    tensor_wait_stores();
+                    tensor_fence_before();
+                    next_there = __all_sync(0xffffffffu, next_there);
+                    if (lane == 0) barrier_arrive(weights_bar + 8 * half);
                 }
-                tensor_wait_stores();
-                tensor_fence_before();
-                __syncwarp();
-                if (lane == 0) barrier_arrive(weights_full + 8 * which);
             }
-            if (count > 0) {
-                ok = ok && warp_wait(sums_full + 8 * which, items & 1, bounds);
-                ++items;
+            if (count > 0) {  // the last phases: the products with the last weights
+                ok = ok && warp_wait(scores_bar, phase & 1, bounds) && warp_wait(scores_bar + 8, phase & 1, bounds);
+                ++phase;
                 tensor_fence_after();
             }
             const bool there = which * 128 + row < it.rows, whole = walk.first() && walk.last();
@@ -383,56 +383,57 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             }
             if (lane == 0) issued[0] = loaded[0], issued[1] = loaded[1];
         } else if (warp == 13 && elected()) {
-            constexpr uint32_t to_scores = product_codes(128, 128, false, false);
+            constexpr uint32_t to_scores = product_codes(128, 64, false, false);
             const uint32_t to_sums = product_codes(128, p.cache.dim, false, true);  // (fp16 has the code of e4m3)
             const uint64_t queries0 = operand(base + kQueryAt), keys0 = operand(base + kKeyAt), values0 = operand(base + kValueAt, kBytes);
             const int steps = (p.cache.dim + 31) / 32;
-            uint32_t tile = 0, scored[2] = {0, 0}, items[2] = {0, 0};
+            uint32_t tile = 0, weighted[2] = {0, 0}, items[2] = {0, 0};
             bool ok = true;
-            const auto score = [&](int which, uint32_t t) {
-                const uint64_t k = keys0 + (t % kKeys) * (kBytes >> 4), q = queries0 + which * (2 * kBytes >> 4);
-                const uint32_t d = tensor + which * 128;
+            const auto score = [&](int which, int half, uint32_t t) {
+                const uint64_t k = keys0 + (t % kKeys) * (kBytes >> 4) + half * (kBytes >> 5), q = queries0 + which * (2 * kBytes >> 4);
+                const uint32_t d = tensor + which * 128 + half * 64;
                 for (int i = 0; i < steps; ++i) {
                     multiply_codes(d, q + 2 * i, k + 2 * i, to_scores, i > 0);
                     multiply_codes(d, q + (kBytes >> 4) + 2 * i, k + 2 * i, to_scores, true);
                 }
-                products_done<false>(scores_full + 8 * which);
             };
-            const auto add = [&](int which, uint32_t t, bool first) {
-                const uint64_t v = values0 + (t % kValues) * (2 * kBytes >> 4);
+            const auto add = [&](int which, int half, uint32_t t, bool first) {
+                const uint64_t v = values0 + (t % kValues) * (2 * kBytes >> 4) + half * (kBytes >> 5);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) multiply_f16(tensor + 256 + which * 128, tensor + which * 128 + 8 * i, v + 128 * i, to_sums, !first || i > 0);
+                for (int i = 0; i < 4; ++i)
+                    multiply_f16(tensor + 256 + which * 128, tensor + which * 128 + half * 64 + 8 * i, v + 128 * i, to_sums, !first || i > 0);
             };
             for (; walk.there() && ok; walk.next()) {
-                const int count = walk.count();
-                const bool two = walk.it.rows > 128;
-                ok = barrier_wait(queries_full, items[0]++ & 1, bounds) && (!two || barrier_wait(queries_full + 8, items[1]++ & 1, bounds));
+                const int count = walk.count(), tiles = walk.it.rows > 128 ? 2 : 1;  // of rows
+                for (int q = 0; q < tiles && ok; ++q) ok = barrier_wait(queries_full + 8 * q, items[q]++ & 1, bounds);
                 if (!ok) break;
                 if (count == 0) continue;
                 ok = barrier_wait(keys_full + 8 * (tile % kKeys), (tile / kKeys) & 1, bounds);
                 if (!ok) break;
                 tensor_fence_after();
-                score(0, tile);
-                if (two) score(1, tile);
-                products_done<false>(keys_empty + 8 * (tile % kKeys));
-                for (int t = 0; t < count; ++t, ++tile) {
-                    const bool more = t + 1 < count;
-                    ok = barrier_wait(values_full + 8 * (tile % kValues), (tile / kValues) & 1, bounds) && barrier_wait(weights_full, scored[0]++ & 1, bounds) &&
-                         (!more || barrier_wait(keys_full + 8 * ((tile + 1) % kKeys), ((tile + 1) / kKeys) & 1, bounds));
-                    if (!ok) break;
-                    tensor_fence_after();
-                    add(0, tile, t == 0);
-                    if (more) score(0, tile + 1);
-                    else products_done<false>(sums_full);
-                    if (two) {
-                        ok = barrier_wait(weights_full + 8, scored[1]++ & 1, bounds);
-                        if (!ok) break;
-                        tensor_fence_after();
-                        add(1, tile, t == 0);
+                for (int half = 0; half < 2; ++half)
+                    for (int q = 0; q < tiles; ++q) {
+                        score(q, half, tile);
+                        products_done<false>(scores_full + 16 * q + 8 * half);
                     }
+                products_done<false>(keys_empty + 8 * (tile % kKeys));
+                for (int t = 0; t < count && ok; ++t, ++tile) {
+                    const bool more = t + 1 < count;
+                    ok = barrier_wait(values_full + 8 * (tile % kValues), (tile / kValues) & 1, bounds) &&
+                         (!more || barrier_wait(keys_full + 8 * ((tile + 1) % kKeys), ((tile + 1) / kKeys) & 1, bounds));
+                    for (int half = 0; half < 2 && ok; ++half) {
+                        for (int q = 0; q < tiles; ++q) {
+                            ok = barrier_wait(weights_full + 16 * q + 8 * half, weighted[q] & 1, bounds);
+                            if (!ok) break;
+                            tensor_fence_after();
+                            add(q, half, tile, t == 0 && half == 0);
+                            if (more) score(q, half, tile + 1);  // (over these weights, behind the products with them)
+                            products_done<false>(scores_full + 16 * q + 8 * half);
+                        }
+                    }
+                    if (!ok) break;
+                    for (int q = 0; q < tiles; ++q) ++weighted[q];
                     products_done<false>(values_empty + 8 * (tile % kValues));
-                    if (two && more) score(1, tile + 1);
-                    if (two && !more) products_done<false>(sums_full + 8);
                     if (more) products_done<false>(keys_empty + 8 * ((tile + 1) % kKeys));
                 }
             }
