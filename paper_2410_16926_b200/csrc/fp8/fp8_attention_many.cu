@@ -10,7 +10,7 @@
 // w * scale; 16 tokens, of one page, share both scales, which are applied to their largest score and inside the exponent, at no cost
 // a score.  Sums of V in tensor memory are rescaled only when a row's largest has grown by 2^8 since: fp16 has the room.
 //
-// Warps: eight for the weights, four convert V, one issues the copies, one the products.
+// Warps: eight for the weights, four convert V, one issues the copies, one for each tile of rows the products.
 #include "fp8_attention.cuh"
 
 namespace pvq {
@@ -98,18 +98,19 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
     const uint32_t keys_full = base + kBarAt, keys_empty = keys_full + 8 * kKeys, codes_full = keys_empty + 8 * kKeys, codes_empty = codes_full + 8 * kCodes,
                    values_full = codes_empty + 8 * kCodes, values_empty = values_full + 8 * kValues, scores_full = values_empty + 8 * kValues,
                    weights_full = scores_full + 32, queries_full = weights_full + 32, scales_full = queries_full + 16,
-                   drained = scales_full + 8 * kScaleSlots;  // (scores and weights: [tile of rows][half of the tokens])
+                   drained = scales_full + 8 * kScaleSlots;  // (scores, weights: [tile of rows][half of the tokens]; drained: [tile of rows])
     __shared__ uint32_t tensor_base, issued[2];
     __shared__ int over;
     __shared__ PlanShared plan;
     __shared__ __align__(16) uint32_t page_scales[kScaleSlots][8];  // of 16 tokens each: keys', values'
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (warp == 0) {
-        constexpr int kCodesEmpty = 2 * kKeys + kCodes, kValuesFull = kCodesEmpty + kCodes, kScores = kValuesFull + 2 * kValues, kAll = kScores + 10 + kScaleSlots + 1;
-        const auto by_warps = [](int i) {  // codes empty, values full, weights, queries
-            return (i >= kCodesEmpty && i < kValuesFull + kValues) || (i >= kScores + 4 && i < kScores + 10);
-        };
-        for (int i = lane; i < kAll; i += 32) barrier_init(keys_full + 8 * i, by_warps(i) ? 4 : 1);
+        constexpr int kCodesEmpty = 2 * kKeys + kCodes, kValuesFull = kCodesEmpty + kCodes, kScores = kValuesFull + 2 * kValues, kAll = kScores + 10 + kScaleSlots + 2;
+        for (int i = lane; i < kAll; i += 32) {
+            const bool by_warps = (i >= kCodesEmpty && i < kValuesFull + kValues) || (i >= kScores + 4 && i < kScores + 10);  // codes empty, values full, weights, queries
+            const bool by_both = (i >= kKeys && i < 2 * kKeys) || (i >= kValuesFull + kValues && i < kScores);  // keys empty, values empty
+            barrier_init(keys_full + 8 * i, by_warps ? 4 : (by_both ? 2 : 1));
+        }
         barrier_init_fence();
         if (lane == 0) {
             over = 0;
@@ -189,10 +190,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 if (lane == 0) barrier_arrive(queries_full + 8 * which);
             }
             float top = kNone, weight = 0.0f;
-            bool next_there = false;
+            bool next_there = false, scales_there = false;
             for (int t = 0; t < count; ++t, ++tile, ++phase) {
                 const uint32_t slot = tile % kScaleSlots;
-                ok = ok && warp_wait(scales_full + 8 * slot, (tile / kScaleSlots) & 1, bounds);
+                ok = ok && (scales_there || warp_wait(scales_full + 8 * slot, (tile / kScaleSlots) & 1, bounds));
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const int tile_at = (walk.begin() + t) * kTile + 64 * half;
@@ -240,6 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                     }
                     // (asked before there is something to do: an answer takes 150 to 200 cycles, also where it is yes)
                     next_there = (half == 0 || t + 1 < count) && barrier_over(scores_bar + 8 * (half ^ 1), half ? (phase + 1) & 1 : phase & 1);
+                    if (half == 1) scales_there = t + 1 < count && barrier_over(scales_full + 8 * ((tile + 1) % kScaleSlots), ((tile + 1) / kScaleSlots) & 1);
                     const float against = top == kNone ? 0.0f : top;
                     uint32_t w[32];
 #pragma unroll
@@ -260,6 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                     tensor_wait_stores();
                     tensor_fence_before();
                     next_there = __all_sync(0xffffffffu, next_there);
+                    if (half == 1) scales_there = __all_sync(0xffffffffu, scales_there);
                     if (lane == 0) barrier_arrive(weights_bar + 8 * half);
                 }
             }
@@ -382,64 +385,82 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 }
             }
             if (lane == 0) issued[0] = loaded[0], issued[1] = loaded[1];
-        } else if (warp == 13 && elected()) {
+        } else if (warp < 15 && elected()) {  // a tile of rows each: neither waits for what the other waits for
+            const int which = warp - 13;
             constexpr uint32_t to_scores = product_codes(128, 64, false, false);
             const uint32_t to_sums = product_codes(128, p.cache.dim, false, true);  // (fp16 has the code of e4m3)
-            const uint64_t queries0 = operand(base + kQueryAt), keys0 = operand(base + kKeyAt), values0 = operand(base + kValueAt, kBytes);
+            const uint64_t queries0 = operand(base + kQueryAt + which * 2 * kBytes), keys0 = operand(base + kKeyAt), values0 = operand(base + kValueAt, kBytes);
+            const uint32_t scores0 = tensor + which * 128, sums = tensor + 256 + which * 128, scores_bar = scores_full + 16 * which,
+                           weights_bar = weights_full + 16 * which;
             const int steps = (p.cache.dim + 31) / 32;
-            uint32_t tile = 0, weighted[2] = {0, 0}, items[2] = {0, 0};
+            uint32_t tile = 0, weighted = 0, items = 0;
             bool ok = true;
-            const auto score = [&](int which, int half, uint32_t t) {
-                const uint64_t k = keys0 + (t % kKeys) * (kBytes >> 4) + half * (kBytes >> 5), q = queries0 + which * (2 * kBytes >> 4);
-                const uint32_t d = tensor + which * 128 + half * 64;
+            const auto score = [&](int half, uint32_t t) {
+                const uint64_t k = keys0 + (t % kKeys) * (kBytes >> 4) + half * (kBytes >> 5);
+                const uint32_t d = scores0 + half * 64;
                 for (int i = 0; i < steps; ++i) {
-                    multiply_codes(d, q + 2 * i, k + 2 * i, to_scores, i > 0);
-                    multiply_codes(d, q + (kBytes >> 4) + 2 * i, k + 2 * i, to_scores, true);
+                    multiply_codes(d, queries0 + 2 * i, k + 2 * i, to_scores, i > 0);
+                    multiply_codes(d, queries0 + (kBytes >> 4) + 2 * i, k + 2 * i, to_scores, true);
                 }
             };
-            const auto add = [&](int which, int half, uint32_t t, bool first) {
+            const auto add = [&](int half, uint32_t t, bool first) {
                 const uint64_t v = values0 + (t % kValues) * (2 * kBytes >> 4) + half * (kBytes >> 5);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    multiply_f16(tensor + 256 + which * 128, tensor + which * 128 + half * 64 + 8 * i, v + 128 * i, to_sums, !first || i > 0);
+                for (int i = 0; i < 4; ++i) multiply_f16(sums, scores0 + half * 64 + 8 * i, v + 128 * i, to_sums, !first || i > 0);
             };
+            const auto keys_there = [&](uint32_t t) { return barrier_over(keys_full + 8 * (t % kKeys), (t / kKeys) & 1); };
+            const auto keys_wait = [&](uint32_t t) { return barrier_wait(keys_full + 8 * (t % kKeys), (t / kKeys) & 1, bounds); };
+            const auto values_there = [&](uint32_t t) { return barrier_over(values_full + 8 * (t % kValues), (t / kValues) & 1); };
+            const auto values_wait = [&](uint32_t t) { return barrier_wait(values_full + 8 * (t % kValues), (t / kValues) & 1, bounds); };
             for (; walk.there() && ok; walk.next()) {
-                const int count = walk.count(), tiles = walk.it.rows > 128 ? 2 : 1;  // of rows
-                for (int q = 0; q < tiles && ok; ++q) ok = barrier_wait(queries_full + 8 * q, items[q]++ & 1, bounds);
+                const int count = walk.count();
+                if (walk.it.rows <= 128 * which) {  // no rows here: the other's tiles pass
+                    for (int t = 0; t < count && ok; ++t, ++tile) {
+                        ok = keys_wait(tile) && values_wait(tile);
+                        if (!ok) break;
+                        barrier_arrive(keys_empty + 8 * (tile % kKeys));
+                        barrier_arrive(values_empty + 8 * (tile % kValues));
+                    }
+                    continue;
+                }
+                ok = barrier_wait(queries_full + 8 * which, items++ & 1, bounds);
                 if (!ok) break;
                 if (count == 0) continue;
-                ok = barrier_wait(keys_full + 8 * (tile % kKeys), (tile / kKeys) & 1, bounds);
+                ok = keys_wait(tile);
                 if (!ok) break;
                 tensor_fence_after();
-                for (int half = 0; half < 2; ++half)
-                    for (int q = 0; q < tiles; ++q) {
-                        score(q, half, tile);
-                        products_done<false>(scores_full + 16 * q + 8 * half);
-                    }
+                for (int half = 0; half < 2; ++half) {
+                    score(half, tile);
+                    products_done<false>(scores_bar + 8 * half);
+                }
                 products_done<false>(keys_empty + 8 * (tile % kKeys));
-                for (int t = 0; t < count && ok; ++t, ++tile) {
+                // (what the next step waits for is asked before this one's products: an answer takes 150 to 200 cycles, also where it is yes)
+                bool values = false, keys = false, weights = false;
+                for (int t = 0; t < count; ++t, ++tile, ++weighted) {
                     const bool more = t + 1 < count;
-                    ok = barrier_wait(values_full + 8 * (tile % kValues), (tile / kValues) & 1, bounds) &&
-                         (!more || barrier_wait(keys_full + 8 * ((tile + 1) % kKeys), ((tile + 1) / kKeys) & 1, bounds));
-                    for (int half = 0; half < 2 && ok; ++half) {
-                        for (int q = 0; q < tiles; ++q) {
-                            ok = barrier_wait(weights_full + 16 * q + 8 * half, weighted[q] & 1, bounds);
-                            if (!ok) break;
-                            tensor_fence_after();
-                            add(q, half, tile, t == 0 && half == 0);
-                            if (more) score(q, half, tile + 1);  // (over these weights, behind the products with them)
-                            products_done<false>(scores_full + 16 * q + 8 * half);
+                    ok = (values || values_wait(tile)) && (!more || keys || keys_wait(tile + 1));
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        ok = ok && (weights || barrier_wait(weights_bar + 8 * half, weighted & 1, bounds));
+                        if (!ok) break;
+                        tensor_fence_after();
+                        add(half, tile, t == 0 && half == 0);
+                        weights = (half == 0 || more) && barrier_over(weights_bar + 8 * (half ^ 1), (weighted + half) & 1);
+                        if (half == 1) {
+                            values = more && values_there(tile + 1);
+                            keys = t + 2 < count && keys_there(tile + 2);
                         }
+                        if (more) score(half, tile + 1);  // (over these weights, behind the products with them)
+                        products_done<false>(scores_bar + 8 * half);
                     }
                     if (!ok) break;
-                    for (int q = 0; q < tiles; ++q) ++weighted[q];
                     products_done<false>(values_empty + 8 * (tile % kValues));
                     if (more) products_done<false>(keys_empty + 8 * ((tile + 1) % kKeys));
                 }
             }
             if (!ok) {
-                products_done<false>(drained);
-                for (int polls = 0; polls < kLandings && !barrier_passed(drained, 0); ++polls) {}
+                products_done<false>(drained + 8 * which);
+                for (int polls = 0; polls < kLandings && !barrier_passed(drained + 8 * which, 0); ++polls) {}
             }
         }
     }
