@@ -41,7 +41,7 @@ __device__ __forceinline__ uint32_t f16x2_of(float lo, float hi) {
     return r;
 }
 // 32 of a lane's words to as many columns.
-__device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&w)[32]) {
+__device__ __forceinline__ void tensor_store32(uint32_t at, const uint32_t (&w)[32]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,"
         "%29,%30,%31,%32};" ::"r"(at),
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
     __shared__ uint32_t tensor_base, issued[2];
     __shared__ int over;
     __shared__ PlanShared plan;
-    __shared__ __align__(16) uint32_t page_scales[kScaleSlots][8];  // of 16 tokens each: keys', values'
+    __shared__ __align__(16) float page_scales[kScaleSlots][3][8];  // of 16 tokens each: keys', values' exponent, 1 / values'
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (warp == 0) {
         constexpr int kCodesEmpty = 2 * kKeys + kCodes, kValuesFull = kCodesEmpty + kCodes, kScores = kValuesFull + 2 * kValues, kAll = kScores + 10 + kScaleSlots + 2;
@@ -189,36 +189,33 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 __syncwarp();
                 if (lane == 0) barrier_arrive(queries_full + 8 * which);
             }
+            // what every row of the warp sees
+            const int all_to = __reduce_min_sync(0xffffffffu, to), all_from = __reduce_max_sync(0xffffffffu, from);
             float top = kNone, weight = 0.0f;
-            bool next_there = false, scales_there = false;
+            float s[2][32];
+            if (count > 0) {
+                ok = ok && warp_wait(scales_full + 8 * (tile % kScaleSlots), (tile / kScaleSlots) & 1, bounds) && warp_wait(scores_bar, phase & 1, bounds);
+                tensor_fence_after();
+                tensor_load(scores, s[0]);
+                tensor_load(scores + 32, s[1]);
+            }
             for (int t = 0; t < count; ++t, ++tile, ++phase) {
                 const uint32_t slot = tile % kScaleSlots;
-                ok = ok && (scales_there || warp_wait(scales_full + 8 * slot, (tile / kScaleSlots) & 1, bounds));
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const int tile_at = (walk.begin() + t) * kTile + 64 * half;
-                    ok = ok && (next_there || warp_wait(scores_bar + 8 * half, phase & 1, bounds));
-                    tensor_fence_after();
-                    float s[2][32];
-                    tensor_load(scores + 64 * half, s[0]);
-                    tensor_load(scores + 64 * half + 32, s[1]);
-                    const uint4 four = *reinterpret_cast<const uint4*>(&page_scales[slot][4 * half]);
-                    const uint32_t words[4] = {four.x, four.y, four.z, four.w};
-                    float key[4], value[4];  // (a key's never 0: it is multiplied by -inf)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        key[c] = fmaxf(factor * __uint_as_float((words[c] & 0xffu) << 23), 0x1p-120f);
-                        value[c] = static_cast<float>(static_cast<int>(words[c] >> 8) - 127);
-                    }
+                    const int first = (walk.begin() + t) * kTile + 64 * half;
+                    const float4 keys = *reinterpret_cast<const float4*>(&page_scales[slot][0][4 * half]), value = *reinterpret_cast<const float4*>(&page_scales[slot][1][4 * half]),
+                                 out_of = *reinterpret_cast<const float4*>(&page_scales[slot][2][4 * half]);
+                    const float key[4] = {fmaxf(factor * keys.x, 0x1p-120f), fmaxf(factor * keys.y, 0x1p-120f), fmaxf(factor * keys.z, 0x1p-120f),
+                                          fmaxf(factor * keys.w, 0x1p-120f)};  // (never 0: times -inf)
                     tensor_wait(s[0]);
                     tensor_wait(s[1]);
-                    if (__any_sync(0xffffffffu, tile_at < from || tile_at + 64 > to)) {
-                        hide(s[0], from - tile_at, to - tile_at);
-                        hide(s[1], from - tile_at - 32, to - tile_at - 32);
+                    if (first < all_from || first + 64 > all_to) {
+                        hide(s[0], from - first, to - first);
+                        hide(s[1], from - first - 32, to - first - 32);
                     }
-                    float high = kNone;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) high = fmaxf(high, fmaf(most_of(&s[c >> 1][16 * (c & 1)]), key[c], value[c]));
+                    const float high = fmaxf(max3(fmaf(most_of(&s[0][0]), key[0], value.x), fmaf(most_of(&s[0][16]), key[1], value.y), fmaf(most_of(&s[1][0]), key[2], value.z)),
+                                             fmaf(most_of(&s[1][16]), key[3], value.w));
                     if (t == 0 && half == 0) {
                         top = high;
                     } else if (__any_sync(0xffffffffu, high > top + kRoom)) {
@@ -229,26 +226,30 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                         weight *= less;
                         top = next;
 #pragma unroll 1
-                        for (int c = 0; c < 128; c += 32) {
-                            float v[32];
-                            uint32_t w[32];
+                        for (int c = 0; c < 128; c += 16) {
+                            float v[16];
+                            uint32_t w[16];
                             tensor_load(sums + c, v);
-                            tensor_wait(v);
+                            tensor_wait_loads();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i] * less);
+                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[i] * less);
                             tensor_store(sums + c, w);
                         }
                     }
-                    // (asked before there is something to do: an answer takes 150 to 200 cycles, also where it is yes)
-                    next_there = (half == 0 || t + 1 < count) && barrier_over(scores_bar + 8 * (half ^ 1), half ? (phase + 1) & 1 : phase & 1);
-                    if (half == 1) scales_there = t + 1 < count && barrier_over(scales_full + 8 * ((tile + 1) % kScaleSlots), ((tile + 1) / kScaleSlots) & 1);
                     const float against = top == kNone ? 0.0f : top;
+                    const float rest[4] = {value.x - against, value.y - against, value.z - against, value.w - against}, back[4] = {out_of.x, out_of.y, out_of.z, out_of.w};
+                    const bool more = half == 0 || t + 1 < count;
                     uint32_t w[32];
+                    bool there = false;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const float (&v)[32] = s[c >> 1];
-                        const float2 k = make_float2(key[c], key[c]), r = make_float2(value[c] - against, value[c] - against);
+                        const float2 k = make_float2(key[c], key[c]), r = make_float2(rest[c], rest[c]);
                         float2 sum = make_float2(0.0f, 0.0f);
+                        // (asked before there is nothing else to do: an answer takes 150 to 200 cycles, also where it is yes)
+                        if (c == 2 && more)
+                            there = barrier_over(scores_bar + 8 * (half ^ 1), (phase + half) & 1) &&
+                                    (half == 0 || barrier_over(scales_full + 8 * ((tile + 1) % kScaleSlots), ((tile + 1) / kScaleSlots) & 1));
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {
                             const float2 x = two_fma(make_float2(v[16 * (c & 1) + i], v[16 * (c & 1) + i + 1]), k, r);
@@ -256,14 +257,26 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                             sum = two_add(sum, e);
                             w[8 * c + i / 2] = f16x2_of(e.x, e.y);
                         }
-                        weight = fmaf(sum.x + sum.y, __uint_as_float((254u - (words[c] >> 8)) << 23), weight);
+                        weight = fmaf(sum.x + sum.y, back[c], weight);
                     }
-                    tensor_store(scores + 64 * half, w);  // (over the scores that have been read)
+                    tensor_store32(scores + 64 * half, w);  // (over the scores that have been read)
+                    const bool early = __all_sync(0xffffffffu, there);
+                    if (early) {  // the next scores, while the weights are on their way
+                        tensor_fence_after();
+                        tensor_load(scores + 64 * (half ^ 1), s[0]);
+                        tensor_load(scores + 64 * (half ^ 1) + 32, s[1]);
+                    }
                     tensor_wait_stores();
                     tensor_fence_before();
-                    next_there = __all_sync(0xffffffffu, next_there);
-                    if (half == 1) scales_there = __all_sync(0xffffffffu, scales_there);
+                    __syncwarp();
                     if (lane == 0) barrier_arrive(weights_bar + 8 * half);
+                    if (more && !early) {
+                        ok = ok && (half == 0 || warp_wait(scales_full + 8 * ((tile + 1) % kScaleSlots), ((tile + 1) / kScaleSlots) & 1, bounds)) &&
+                             warp_wait(scores_bar + 8 * (half ^ 1), (phase + half) & 1, bounds);
+                        tensor_fence_after();
+                        tensor_load(scores + 64 * (half ^ 1), s[0]);
+                        tensor_load(scores + 64 * (half ^ 1) + 32, s[1]);
+                    }
                 }
             }
             if (count > 0) {  // the last phases: the products with the last weights
@@ -372,7 +385,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                         ok = !(withheld.copies && tile >= kKeys + kWithheldFrom) && warp_wait((half ? codes_empty : keys_empty) + 8 * at, parity, bounds);
                         if (!ok) break;
                         if (half == 0) {
-                            if (lane < 8) page_scales[slot][lane] = word;
+                            if (lane < 8) {
+                                page_scales[slot][0][lane] = __uint_as_float((word & 0xffu) << 23);
+                                page_scales[slot][1][lane] = static_cast<float>(static_cast<int>(word >> 8) - 127);
+                                page_scales[slot][2][lane] = __uint_as_float((254u - (word >> 8)) << 23);
+                            }
                             __syncwarp();
                             if (lane == 0) barrier_arrive(scales_full + 8 * slot);
                         }

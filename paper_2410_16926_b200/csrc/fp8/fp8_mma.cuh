@@ -261,7 +261,7 @@ __device__ __forceinline__ void tensor_load(uint32_t at, float (&v)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
-// A lane's words of 1, 2, 4 or 8 columns.
+// A lane's words of 1, 2, 4, 8 or 16 columns.
 __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&w)[1]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(at), "r"(w[0]) : "memory");
 }
@@ -274,6 +274,12 @@ __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&w)[4]
 __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&w)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
                  "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+
+__device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t (&w)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(w[8]), "r"(w[9]), "r"(w[10]), "r"(w[11]), "r"(w[12]), "r"(w[13]), "r"(w[14]), "r"(w[15])
                  : "memory");
 }
 
