@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(32 * kJoinRows) attention_join_kernel(const __
             all = fmaf(w, f, all);
         }
     }
-    const int packed = head.q0 + n, query = packed / p.group;
+    const int packed = head.q0 + n, query = divide(packed, p.by_group);
     const int64_t row = head.row + query;
     const int q_head = head.head * p.group + packed - query * p.group;
     const float one = all == 0.0f ? 0.0f : 1.0f / all;
@@ -60,15 +60,12 @@ struct Form {
     int rows, blocks;
 };
 Form form_of(int64_t seqs, int64_t rows, int heads, int kv_heads) {
-    const int64_t each = (rows * (heads / kv_heads) + seqs - 1) / (seqs > 0 ? seqs : 1);  // of a sequence and head
+    const int64_t each = (rows * (heads / kv_heads) + seqs - 1) / seqs;  // of a sequence and head
     if (each > 64) return {256, kSms};
-    return {each <= 16 ? 16 : 32, 2 * kSms};
+    return {each <= 4 ? 4 : (each <= 8 ? 8 : (each <= 16 ? 16 : 32)), 2 * kSms};
 }
 
-size_t bytes_of(const Form& f) {
-    const size_t floats = f.rows == 16 ? part_floats<16>() : (f.rows == 32 ? part_floats<32>() : part_floats<256>());
-    return f.blocks > 1 ? f.blocks * (2 * floats * sizeof(float) + sizeof(PartHead)) : 0;
-}
+size_t bytes_of(const Form& f) { return f.blocks * (2 * size_t(f.rows) * (128 + 2) * sizeof(float) + sizeof(PartHead)); }
 
 template <int ROWS>
 int join(const AttentionArgs& a, int blocks, cudaStream_t s) {
@@ -79,11 +76,23 @@ int join(const AttentionArgs& a, int blocks, cudaStream_t s) {
 
 size_t attention_workspace(int64_t seqs, int64_t rows, int heads, int kv_heads) { return bytes_of(form_of(seqs, rows, heads, kv_heads)); }
 
-int attention(const AttentionArgs& a, cudaStream_t s) {
-    const Form f = form_of(a.step.seqs, a.step.rows, a.heads, a.cache.heads);
+int attention(const AttentionArgs& call, cudaStream_t s) {
+    AttentionArgs a = call;
+    const int64_t seqs = a.step.seqs, rows = a.step.rows;
+    const Form f = form_of(seqs, rows, a.heads, a.cache.heads);
+    // (items of all sequences, each of at most as many tiles as a table holds)
+    const int64_t items = rows * a.group / f.rows + seqs, tiles = ((int64_t(a.step.width) << a.cache.page_shift) + kTile - 1) / kTile;
+    if (items * a.cache.heads >= int64_t(1) << 31 || items * a.cache.heads * tiles >= int64_t(1) << 31) return PVQ_ERR_UNSUPPORTED;
+    a.by_group = division_by(a.group);
+    const int threads = 128;  // (the least of a kernel's: a sequence's lanes for all of them, where there are few)
+    a.plan_lanes = 1;
+    while (a.plan_lanes < 32 && seqs * a.plan_lanes * 2 <= threads && rows * a.group > f.rows * seqs * a.plan_lanes) a.plan_lanes *= 2;
     int st = f.rows == 256 ? attention_many(a, f.blocks, s) : attention_few(a, f.rows, f.blocks, s);
-    if (st == PVQ_OK && f.blocks > 1) st = f.rows == 16 ? join<16>(a, f.blocks, s) : (f.rows == 32 ? join<32>(a, f.blocks, s) : join<256>(a, f.blocks, s));
-    return st;
+    if (st != PVQ_OK) return st;
+    if (f.rows == 4) return join<4>(a, f.blocks, s);
+    if (f.rows == 8) return join<8>(a, f.blocks, s);
+    if (f.rows == 16) return join<16>(a, f.blocks, s);
+    return f.rows == 32 ? join<32>(a, f.blocks, s) : join<256>(a, f.blocks, s);
 }
 
 }  // namespace fp8

@@ -47,7 +47,7 @@ template <int ROWS>
 __device__ __forceinline__ void measure(const AttentionArgs& a, Item& it) {
     it.q0 = it.block * ROWS;
     it.rows = min(ROWS, it.q.n * a.group - it.q0);
-    const int i0 = it.q0 / a.group, i1 = (it.q0 + it.rows - 1) / a.group;
+    const int i0 = divide(it.q0, a.by_group), i1 = divide(it.q0 + it.rows - 1, a.by_group);
     it.hi = a.causal ? min(it.q.held, it.q.first + i1 + 1) : it.q.held;
     it.lo = a.window > 0 ? max(0, it.q.first + i0 - a.window + 1) : 0;
 }
@@ -56,26 +56,31 @@ __device__ __forceinline__ int blocks_of(const AttentionArgs& a, const Sequence&
     return (q.n * a.group + ROWS - 1) / ROWS;
 }
 
-// A block's share: it begins `skip` units into an item.
+// A block's share: it begins `skip` units into an item.  (All units are fewer than 2^31: the host sees to that.)
 struct Share {
     int s, head, block, skip;
-    long long begin, left, all;
-    int blocks;  // that have a share
+    int begin, left;
+    int all, blocks;  // units, and blocks that have a share
 };
+// Where block c's share of `all` begins: shares differ by one at most, larger ones first.
+__device__ __forceinline__ int share_begin(uint32_t all, uint32_t blocks, uint32_t c) { return all / blocks * c + min(c, all % blocks); }
+// The block whose share unit u is in.
+__device__ __forceinline__ int share_of(uint32_t all, uint32_t blocks, uint32_t u) {
+    const uint32_t each = all / blocks, larger = all % blocks, edge = larger * (each + 1);
+    return u < edge ? u / (each + 1) : larger + (u - edge) / each;
+}
 struct PlanShared {
-    long long sums[32], left, per_head;
-    int s;
+    int sums[32], left, per_head, s;
     Share share;
 };
 
-// All threads of the block.
+// All threads of the block; `keeper` is the one that will ask Walk::parts.
 template <int THREADS, int ROWS>
-__device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& sh) {
+__device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& sh, int keeper) {
     const int thread = threadIdx.x, lane = thread & 31, warp = thread >> 5, seqs = a.step.seqs;
-    int lanes = 32;  // for a sequence
-    while (lanes > 1 && seqs > THREADS / lanes) lanes >>= 1;
-    const int per = THREADS / lanes;
-    long long units = 0, before = 0, base = 0;
+    const int lanes = a.plan_lanes, per = THREADS / lanes;  // for a sequence; sequences at a time
+    const bool leads = (thread & (lanes - 1)) == 0;
+    int units = 0, before = 0;
     const auto chunk = [&](int first) {  // units of a sequence, and of those before it in the chunk; returns those of the chunk
         const int s = first + thread / lanes;
         units = 0;
@@ -91,59 +96,64 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
         }
         for (int o = lanes >> 1; o > 0; o >>= 1) units += __shfl_xor_sync(0xffffffffu, units, o);
         units *= a.cache.heads;
-        const bool leads = (thread & (lanes - 1)) == 0;
-        long long sum = leads ? units : 0;
+        int sum = leads ? units : 0;
+#pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long other = __shfl_up_sync(0xffffffffu, sum, o);
+            const int other = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += other;
         }
-        __syncthreads();
+        if (first > 0) __syncthreads();
         if (lane == 31) sh.sums[warp] = sum;
         __syncthreads();
         before = sum - (leads ? units : 0);
-        long long all = 0;
+        int all = 0;
+#pragma unroll
         for (int w = 0; w < THREADS / 32; ++w) {
-            if (w < warp) before += sh.sums[w];
-            all += sh.sums[w];
+            const int here = sh.sums[w];
+            before += w < warp ? here : 0;
+            all += here;
         }
         return all;
     };
-    long long all = 0;
-    for (int first = 0; first < seqs; first += per) all += chunk(first);
     Share r{};
-    r.all = all;
-    r.blocks = static_cast<int>(min(static_cast<long long>(gridDim.x), max(1ll, all / kLeastUnits)));
+    for (int first = 0; first < seqs; first += per) r.all += chunk(first);
+    r.blocks = min(static_cast<int>(gridDim.x), max(1, r.all / kLeastUnits));
     const int c = blockIdx.x;
-    if (all == 0 || c >= r.blocks) return r;
-    r.begin = all * c / r.blocks;
-    r.left = all * (c + 1) / r.blocks - r.begin;
-    for (int first = 0; first < seqs; first += per) {
-        const long long here = seqs > per ? chunk(first) : all;
-        if ((thread & (lanes - 1)) == 0 && base + before <= r.begin && r.begin < base + before + units) {
+    if (r.all == 0 || c >= r.blocks) return r;
+    r.begin = share_begin(r.all, r.blocks, c);
+    r.left = share_begin(r.all, r.blocks, c + 1) - r.begin;
+    int base = 0;
+    if (seqs > per) __syncthreads();
+    for (int first = 0; first < seqs && base <= r.begin; first += per) {
+        const int here = seqs > per ? chunk(first) : r.all;
+        if (leads && base + before <= r.begin && r.begin - base - before < units) {
             sh.s = first + thread / lanes;
             sh.left = r.begin - base - before;
             sh.per_head = units / a.cache.heads;
         }
         base += here;
-        if (base > r.begin) break;
     }
     __syncthreads();
     r.s = sh.s;
-    const long long per_head = sh.per_head;
-    r.head = static_cast<int>(sh.left / per_head);
-    long long rest = sh.left - r.head * per_head;
+    int rest = sh.left;
+    const int per_head = sh.per_head;
+    if (rest >= per_head) {
+        r.head = static_cast<uint32_t>(rest) / static_cast<uint32_t>(per_head);
+        rest -= r.head * per_head;
+    }
     Item it;
     it.q = sequence_of(a.step, r.s, a.cache.page_shift);
     const int blocks = blocks_of<ROWS>(a, it.q);
-    for (int b0 = 0; b0 < blocks; b0 += 32) {  // (every warp alike)
+    for (int b0 = 0; b0 < blocks && blocks > 1; b0 += 32) {  // (every warp alike)
         it.block = b0 + lane;
-        long long sum = 0;
+        int sum = 0;
         if (it.block < blocks) {
             measure<ROWS>(a, it);
             sum = it.units();
         }
+#pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long other = __shfl_up_sync(0xffffffffu, sum, o);
+            const int other = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += other;
         }
         const uint32_t behind = __ballot_sync(0xffffffffu, it.block < blocks && sum > rest);
@@ -155,20 +165,19 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
         }
         rest -= __shfl_sync(0xffffffffu, sum, 31);
     }
-    r.skip = static_cast<int>(rest);
-    if (thread == 0) sh.share = r;
-    __syncthreads();
+    r.skip = rest;
+    if (thread == keeper) sh.share = r;
     return r;
 }
 
-// Goes through a block's share, item by item.  Every role of the block does so by itself.  (A share of 2^31 tiles would take an hour.)
+// Goes through a block's share, item by item.  Every role of the block does so by itself.
 template <int ROWS>
 struct Walk {
     const AttentionArgs& a;
     Item it;
     int left, skip, take;
 
-    __device__ __forceinline__ Walk(const AttentionArgs& args, const Share& sh) : a(args), left(static_cast<int>(sh.left)), skip(sh.skip), take(0) {
+    __device__ __forceinline__ Walk(const AttentionArgs& args, const Share& sh) : a(args), left(sh.left), skip(sh.skip), take(0) {
         if (left <= 0) return;
         it.s = sh.s, it.head = sh.head, it.block = sh.block;
         it.q = sequence_of(a.step, it.s, a.cache.page_shift);
@@ -182,7 +191,7 @@ struct Walk {
     __device__ __forceinline__ bool last() const { return skip + take == it.units(); }
     // Blocks that the item is shared by, from its first one on (called where first()).
     __device__ __forceinline__ int parts(const PlanShared& plan) const {
-        return static_cast<int>(((plan.share.begin + plan.share.left - left + it.units()) * plan.share.blocks - 1) / plan.share.all - blockIdx.x) + 1;
+        return share_of(plan.share.all, plan.share.blocks, plan.share.begin + plan.share.left - left + it.units() - 1) - blockIdx.x + 1;
     }
     __device__ __forceinline__ void next() {
         left -= take;
@@ -207,25 +216,26 @@ struct RowPlace {
     int row, head;
 };
 __device__ __forceinline__ RowPlace place_of(const AttentionArgs& a, const Sequence& q, int head, int packed) {
-    const int i = packed / a.group;
+    const int i = divide(packed, a.by_group);
     return {q.row + i, head * a.group + packed - i * a.group};
 }
 
-// The pages of a run of tiles, 32 at a time, a lane each: their numbers are asked for two turns ahead, their scales one.
+// The pages of a run of tiles, 32 at a time, a lane each: their numbers are asked for two turns ahead, their scales one (of the first
+// turn by first_scales, behind the first copies).
 struct Pages {
     const AttentionArgs& a;
     const int* table;
     int head, entry, end, id, id1, id2;
     uint32_t scales, scales1;
 
-    __device__ __forceinline__ int ask(int e) const {
+    __device__ __forceinline__ int ask(int e) const { return e < end ? __ldg(table + e) : -1; }
+    __device__ __forceinline__ int known(int i, int e) const {  // -1: a page that is not there, zeros
         if (e >= end) return -1;
-        const int i = __ldg(table + e);
         if (i >= 0 && i < a.cache.pages) return i;
         if (a.status) atomicOr(a.status, PVQ_STATUS_BAD_PAGE);
         return -1;
     }
-    __device__ __forceinline__ uint32_t ask_scales(int i) const {  // (a page that is not there: zeros)
+    __device__ __forceinline__ uint32_t ask_scales(int i) const {
         if (i < 0) return 127u | 127u << 8;
         const int64_t at = i * a.cache.scale_step + head;
         const int k = __ldg(a.cache.k_scales + at), v = __ldg(a.cache.v_scales + at);
@@ -237,11 +247,16 @@ struct Pages {
         end = (it.q.held + (1 << a.cache.page_shift) - 1) >> a.cache.page_shift;
         entry = first_entry + (threadIdx.x & 31);
         id = ask(entry), id1 = ask(entry + 32), id2 = ask(entry + 64);
-        scales = ask_scales(id), scales1 = ask_scales(id1);
+        id = known(id, entry);
+    }
+    __device__ __forceinline__ void first_scales() {
+        scales = ask_scales(id);
+        id1 = known(id1, entry + 32);
+        scales1 = ask_scales(id1);
     }
     __device__ __forceinline__ void next() {
         entry += 32;
-        id = id1, id1 = id2, id2 = ask(entry + 64);
+        id = id1, id1 = known(id2, entry + 32), id2 = ask(entry + 64);
         scales = scales1, scales1 = ask_scales(id1);
     }
 };
@@ -278,7 +293,7 @@ __device__ __forceinline__ void two_codes(float x, float y, uint32_t& hi, uint32
 }
 
 int cache_maps(const Cache& c, CacheMaps* maps);
-int attention_few(const AttentionArgs& a, int rows, int blocks, cudaStream_t s);  // 16 or 32 rows an item
+int attention_few(const AttentionArgs& a, int rows, int blocks, cudaStream_t s);  // 4, 8, 16 or 32 rows an item
 int attention_many(const AttentionArgs& a, int blocks, cudaStream_t s);           // 256
 
 }  // namespace fp8

@@ -19,14 +19,16 @@ constexpr int kThreads = 192;
 constexpr int kHalf = kTile * 128;       // bytes of a tile's keys or values, rows of 128 bytes
 constexpr float kShift = 8.0f;           // weights are up to 2^8: their smallest code is 2^-9
 
+// ROWS query rows of an item: a product has 16 or 32 columns, of which 4, 8 or all are used.
 template <int ROWS>
 struct Few {
-    static constexpr int kHalves = ROWS == 16 ? 6 : 5;
-    static constexpr int kQueries = kHalves * kHalf, kQueryBytes = ROWS * 128;  // two codes each
-    static constexpr int kWeights = kQueries + 2 * kQueryBytes, kWeightBytes = ROWS * kTile;
+    static constexpr int kWide = ROWS <= 16 ? 16 : 32;  // columns of a product
+    static constexpr int kHalves = kWide == 16 ? 6 : 5;
+    static constexpr int kQueries = kHalves * kHalf, kQueryBytes = kWide * 128;  // two codes each
+    static constexpr int kWeights = kQueries + 2 * kQueryBytes, kWeightBytes = kWide * kTile;
     static constexpr int kBars = kWeights + 2 * kWeightBytes;
     static constexpr size_t kShared = 1024 + kBars + 256;
-    static constexpr int kColumns = ROWS == 16 ? 64 : 128;  // of tensor memory: scores twice, sums
+    static constexpr int kColumns = kWide == 16 ? 64 : 128;  // of tensor memory: scores twice, sums
     static_assert(2 * (kShared + 4096) <= 231424, "two blocks an SM");
 };
 
@@ -42,10 +44,30 @@ __device__ __forceinline__ float warp_max(float x) {
 }
 __device__ __forceinline__ void tokens_meet() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
+// A lane's values of 4, 8, 16 or 32 columns.
+template <int N>
+__device__ __forceinline__ void load_columns(uint32_t at, float (&v)[N]) {
+    if constexpr (N == 4) {
+        uint32_t r[4];
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
+    } else if constexpr (N == 8) {
+        uint32_t r[8];
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                     : "r"(at));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+    } else {
+        tensor_load(at, v);
+    }
+}
+
 template <int ROWS>
 __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid_constant__ CacheMaps maps, const __grid_constant__ AttentionArgs p) {
     using S = Few<ROWS>;
-    constexpr int kHalves = S::kHalves;
+    constexpr int kHalves = S::kHalves, kWide = S::kWide;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
     const uint32_t full = base + S::kBars, empty = full + 8 * kHalves, scales_full = empty + 8 * kHalves, scores_full = scales_full + 8 * kScaleSlots,
@@ -53,7 +75,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
     __shared__ uint32_t tensor_base, issued_halves;
     __shared__ int over;
     __shared__ PlanShared plan;
-    __shared__ uint32_t page_scales[kScaleSlots][8];  // of 16 tokens each: keys', values'
+    __shared__ float page_scales[kScaleSlots][3][8];  // of 16 tokens each: keys', values' exponent, 1 / values'
     __shared__ __align__(16) float factor[ROWS], tops[2][4][ROWS];
     __shared__ int from[ROWS], to[ROWS];  // positions that a row sees
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -76,10 +98,10 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
     tensor_fence_after();
     launch_dependents();
     dependency_wait();
-    const uint32_t tensor = tensor_base, sums = tensor + 2 * ROWS;
+    const uint32_t tensor = tensor_base, sums = tensor + 2 * kWide;
     Bounds bounds{&over, p.status};
     const Withheld withheld = withheld_of(bounds, blockIdx.x);
-    const Share share = find_share<kThreads, ROWS>(p, plan);
+    const Share share = find_share<kThreads, ROWS>(p, plan, 128);
     Walk<ROWS> walk(p, share);
 
     if (warp == 0) {
@@ -94,19 +116,13 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
             for (int t = 0; t < walk.count() && ok; ++t, ++tile) {
                 if (within == 32) list.next(), within = 0;
                 const uint32_t slot = tile % kScaleSlots;
-                const uint32_t word = __shfl_sync(0xffffffffu, list.scales, within + ((lane & 7) * pages >> 3));
                 const int page = __shfl_sync(0xffffffffu, list.id, within + (lane & (pages - 1)));
-                within += pages;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    ok = !(withheld.copies && issued >= kHalves + kWithheldFrom) && warp_wait(empty + 8 * turn.at, turn.parity ^ 1, bounds);
+                    ok = !(withheld.copies && issued >= kHalves + kWithheldFrom) &&
+                         (issued < kHalves || warp_wait(empty + 8 * turn.at, turn.parity ^ 1, bounds));
                     if (!ok) break;
                     const uint32_t bar = full + 8 * turn.at;
-                    if (half == 0) {
-                        if (lane < 8) page_scales[slot][lane] = word;
-                        __syncwarp();
-                        if (lane == 0) barrier_arrive(scales_full + 8 * slot);
-                    }
                     if (lane == 0) barrier_expect(bar, kHalf);
                     __syncwarp();
                     if (lane < pages) load_page(base + turn.at * kHalf + lane * page_bytes, half ? &maps.v : &maps.k, walk.it.head, page, bar);
@@ -114,12 +130,23 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                     turn.next();
                     ++issued;
                 }
+                if (t == 0) list.first_scales();
+                const uint32_t word = __shfl_sync(0xffffffffu, list.scales, within + ((lane & 7) * pages >> 3));
+                within += pages;
+                if (!ok) break;
+                if (lane < 8) {
+                    page_scales[slot][0][lane] = __uint_as_float((word & 0xffu) << 23);
+                    page_scales[slot][1][lane] = static_cast<float>(static_cast<int>(word >> 8) - 127);
+                    page_scales[slot][2][lane] = __uint_as_float((254u - (word >> 8)) << 23);
+                }
+                __syncwarp();
+                if (lane == 0) barrier_arrive(scales_full + 8 * slot);
             }
         }
         if (lane == 0) issued_halves = issued;
     } else if (warp == 1) {
         if (elected()) {
-            constexpr uint32_t scores = product_codes(128, ROWS, false, false), results = product_codes(128, ROWS, true, true);
+            constexpr uint32_t scores = product_codes(128, kWide, false, false), results = product_codes(128, kWide, true, true);
             const uint64_t tiles0 = operand(base), queries0 = operand(base + S::kQueries), weights0 = operand_plain(base + S::kWeights, kTile * 16);
             const int steps = (p.cache.dim + 31) / 32;
             uint32_t tile = 0, items = 0;
@@ -131,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                 if (!ok) return;
                 tensor_fence_after();
                 const uint64_t k = half_at(2 * t);
-                const uint32_t d = tensor + (t & 1) * ROWS;
+                const uint32_t d = tensor + (t & 1) * kWide;
                 for (int i = 0; i < steps; ++i) {
                     multiply_codes(d, k + 2 * i, queries0 + 2 * i, scores, i > 0);
                     multiply_codes(d, k + 2 * i, queries0 + (S::kQueryBytes >> 4) + 2 * i, scores, true);
@@ -170,54 +197,61 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
         const uint32_t mine = quarter << 21;
         PartHead* head = part_heads<ROWS>(p) + blockIdx.x;
         if (thread == 0 && gridDim.x > 1) head->parts = 0;
+        if (ROWS < S::kWide) {  // columns that are not used: zeros
+            for (int i = thread; i < (2 * S::kQueryBytes + 2 * S::kWeightBytes) / 16; i += 128)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + S::kQueries + 16 * i), "r"(0u) : "memory");
+            tokens_meet();
+        }
         uint32_t tile = 0;
         bool ok = true;
         for (; walk.there(); walk.next()) {
             const Item& it = walk.it;
             const int count = walk.count();
-            {  // queries: 128 / ROWS threads a row
-                constexpr int kAcross = 128 / ROWS, kEach = 128 / kAcross;  // dims of a thread
+            {  // queries, 8 threads a row (4 of 32 rows); rows that are not used were zeros from the start
+                constexpr int kAcross = ROWS <= 16 ? 8 : 4, kEach = 128 / kAcross;  // dims of a thread
                 const int r = thread / kAcross, col = thread % kAcross * kEach;
-                float x[kEach];
-                uint32_t most = 0u;
-                const RowPlace place = place_of(p, it.q, it.head, it.q0 + min(r, it.rows - 1));
-                const __nv_bfloat16* q = p.q + place.row * p.q_row + place.head * p.q_head + col;
+                if (r < ROWS) {  // (whole warps)
+                    float x[kEach];
+                    uint32_t most = 0u;
+                    const RowPlace place = place_of(p, it.q, it.head, it.q0 + min(r, it.rows - 1));
+                    const __nv_bfloat16* q = p.q + place.row * p.q_row + place.head * p.q_head + col;
 #pragma unroll
-                for (int j = 0; j < kEach / 8; ++j) {
-                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                    if (col + 8 * j < p.cache.dim) w = __ldg(reinterpret_cast<const uint4*>(q + 8 * j));
-                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+                    for (int j = 0; j < kEach / 8; ++j) {
+                        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                        if (col + 8 * j < p.cache.dim) w = __ldg(reinterpret_cast<const uint4*>(q + 8 * j));
+                        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[8 * j + 2 * i] = __uint_as_float(u[i] << 16), x[8 * j + 2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-                }
-#pragma unroll
-                for (int j = 0; j < kEach; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
-#pragma unroll
-                for (int o = 1; o < kAcross; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-                const uint32_t byte = most < kFiniteEnd ? scale_byte(most) : 127u;
-                const float inverse = inverse_of(byte);
-                const uint32_t at = base + S::kQueries + r * 128;
-#pragma unroll
-                for (int j = 0; j < kEach / 16; ++j) {
-                    uint32_t hi[4], lo[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t h0, l0, h1, l1;
-                        const float* y = x + 16 * j + 4 * i;
-                        two_codes(y[0] * inverse, y[1] * inverse, h0, l0);
-                        two_codes(y[2] * inverse, y[3] * inverse, h1, l1);
-                        hi[i] = h0 | h1 << 16, lo[i] = l0 | l1 << 16;
+                        for (int i = 0; i < 4; ++i) x[8 * j + 2 * i] = __uint_as_float(u[i] << 16), x[8 * j + 2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
                     }
-                    const uint32_t chunk = at + (((col / 16 + j) ^ (r & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk + S::kQueryBytes), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3])
-                                 : "memory");
-                }
-                if (thread % kAcross == 0) {
-                    const int position = it.q.first + (it.q0 + r) / p.group;
-                    factor[r] = most < kFiniteEnd ? scale_of(byte) * p.scale : __uint_as_float(0x7fffffffu);
-                    to[r] = r < it.rows ? (p.causal ? min(it.q.held, position + 1) : it.q.held) : 0;
-                    from[r] = p.window > 0 ? max(0, position - p.window + 1) : 0;
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+#pragma unroll
+                    for (int o = 1; o < kAcross; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+                    const uint32_t byte = most < kFiniteEnd ? scale_byte(most) : 127u;
+                    const float inverse = inverse_of(byte);
+                    const uint32_t at = base + S::kQueries + r * 128;
+#pragma unroll
+                    for (int j = 0; j < kEach / 16; ++j) {
+                        uint32_t hi[4], lo[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t h0, l0, h1, l1;
+                            const float* y = x + 16 * j + 4 * i;
+                            two_codes(y[0] * inverse, y[1] * inverse, h0, l0);
+                            two_codes(y[2] * inverse, y[3] * inverse, h1, l1);
+                            hi[i] = h0 | h1 << 16, lo[i] = l0 | l1 << 16;
+                        }
+                        const uint32_t chunk = at + (((col / 16 + j) ^ (r & 7)) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk + S::kQueryBytes), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3])
+                                     : "memory");
+                    }
+                    if (thread % kAcross == 0) {
+                        const int position = it.q.first + divide(it.q0 + r, p.by_group);
+                        factor[r] = most < kFiniteEnd ? scale_of(byte) * p.scale : __uint_as_float(0x7fffffffu);
+                        to[r] = r < it.rows ? (p.causal ? min(it.q.held, position + 1) : it.q.held) : 0;
+                        from[r] = p.window > 0 ? max(0, position - p.window + 1) : 0;
+                    }
                 }
                 async_fence();
                 __syncwarp();
@@ -234,11 +268,12 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                 tensor_fence_after();
 #pragma unroll
                 for (int c = 0; c < ROWS; c += 16) {
-                    float v[16];
-                    tensor_load(sums + mine + c, v);
+                    constexpr int kHere = ROWS < 16 ? ROWS : 16;
+                    float v[kHere];
+                    load_columns(sums + mine + c, v);
                     tensor_wait_loads();
 #pragma unroll
-                    for (int n = 0; n < 16; ++n) sum[c + n] += v[n];
+                    for (int n = 0; n < kHere; ++n) sum[c + n] += v[n];
                 }
             };
             for (int t = 0; t < count; ++t, ++tile) {
@@ -248,9 +283,8 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                      warp_wait(scores_full + 8 * (tile & 1), (tile >> 1) & 1, bounds);
                 tensor_fence_after();
                 float s[ROWS];
-                tensor_load(tensor + mine + (tile & 1) * ROWS, s);
-                const uint32_t word = page_scales[slot][thread >> 4];
-                const float key = __uint_as_float((word & 0xffu) << 23), value = static_cast<float>(static_cast<int>(word >> 8) - 127);
+                load_columns(tensor + mine + (tile & 1) * kWide, s);
+                const float key = page_scales[slot][0][thread >> 4], value = page_scales[slot][1][thread >> 4], out_of = page_scales[slot][2][thread >> 4];
                 tensor_wait_loads();
 #pragma unroll
                 for (int n = 0; n < ROWS; ++n) s[n] = fmaf(s[n] * factor[n], key, value);
@@ -267,7 +301,6 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                 }
                 tokens_meet();
                 if (t > 0) add_sums(tile - 1);
-                const float out_of = __uint_as_float((254u - (word >> 8)) << 23);  // 1 / the values' scale
                 uint32_t hi[ROWS / 4], lo[ROWS / 4];
 #pragma unroll
                 for (int n = 0; n < ROWS; n += 4) {
@@ -294,14 +327,21 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                     two_codes(w[2], w[3], h1, l1);
                     hi[n / 4] = h0 | h1 << 16, lo[n / 4] = l0 | l1 << 16;
                 }
+                const uint32_t place = base + S::kWeights + thread * 16;
+                if constexpr (ROWS == 4) {
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(place), "r"(hi[0]) : "memory");
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(place + S::kWeightBytes), "r"(lo[0]) : "memory");
+                } else if constexpr (ROWS == 8) {
+                    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(place), "r"(hi[0]), "r"(hi[1]) : "memory");
+                    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(place + S::kWeightBytes), "r"(lo[0]), "r"(lo[1]) : "memory");
+                } else {
 #pragma unroll
-                for (int n = 0; n < ROWS; n += 16) {
-                    const uint32_t at = base + S::kWeights + n * kTile + thread * 16;
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(hi[n / 4]), "r"(hi[n / 4 + 1]), "r"(hi[n / 4 + 2]), "r"(hi[n / 4 + 3])
-                                 : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + S::kWeightBytes), "r"(lo[n / 4]), "r"(lo[n / 4 + 1]), "r"(lo[n / 4 + 2]),
-                                 "r"(lo[n / 4 + 3])
-                                 : "memory");
+                    for (int n = 0; n < ROWS / 4; n += 4) {
+                        const uint32_t at = place + n * 4 * kTile;
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(hi[n]), "r"(hi[n + 1]), "r"(hi[n + 2]), "r"(hi[n + 3]) : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + S::kWeightBytes), "r"(lo[n]), "r"(lo[n + 1]), "r"(lo[n + 2]), "r"(lo[n + 3])
+                                     : "memory");
+                    }
                 }
                 // What no row sees may be anything, NaN too, which a weight of zero would not take out.
                 if (tile_at < any_from || tile_at + kTile > any_to) {
@@ -372,7 +412,11 @@ int launch(const AttentionArgs& a, int blocks, cudaStream_t s) {
 
 }  // namespace
 
-int attention_few(const AttentionArgs& a, int rows, int blocks, cudaStream_t s) { return rows == 16 ? launch<16>(a, blocks, s) : launch<32>(a, blocks, s); }
+int attention_few(const AttentionArgs& a, int rows, int blocks, cudaStream_t s) {
+    if (rows == 4) return launch<4>(a, blocks, s);
+    if (rows == 8) return launch<8>(a, blocks, s);
+    return rows == 16 ? launch<16>(a, blocks, s) : launch<32>(a, blocks, s);
+}
 
 }  // namespace fp8
 }  // namespace pvq

@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
     const uint32_t tensor = tensor_base;
     Bounds bounds{&over, p.status};
     const Withheld withheld = withheld_of(bounds, blockIdx.x);
-    const Share share = find_share<kThreads, kRows>(p, plan);
+    const Share share = find_share<kThreads, kRows>(p, plan, 0);
     Walk<kRows> walk(p, share);
 
     if (warp < 8) {
@@ -375,30 +375,31 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 for (int t = 0; t < walk.count() && ok; ++t, ++tile) {
                     if (within == 32) list.next(), within = 0;
                     const uint32_t slot = tile % kScaleSlots;
-                    const uint32_t word = __shfl_sync(0xffffffffu, list.scales, within + ((lane & 7) * pages >> 3));
                     const int page = __shfl_sync(0xffffffffu, list.id, within + (lane & (pages - 1)));
-                    within += pages;
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const uint32_t stages = half ? kCodes : kKeys, at = tile % stages, parity = ((tile / stages) & 1) ^ 1;
                         const uint32_t bar = (half ? codes_full : keys_full) + 8 * at;
-                        ok = !(withheld.copies && tile >= kKeys + kWithheldFrom) && warp_wait((half ? codes_empty : keys_empty) + 8 * at, parity, bounds);
+                        ok = !(withheld.copies && tile >= kKeys + kWithheldFrom) &&
+                             (tile < stages || warp_wait((half ? codes_empty : keys_empty) + 8 * at, parity, bounds));
                         if (!ok) break;
-                        if (half == 0) {
-                            if (lane < 8) {
-                                page_scales[slot][0][lane] = __uint_as_float((word & 0xffu) << 23);
-                                page_scales[slot][1][lane] = static_cast<float>(static_cast<int>(word >> 8) - 127);
-                                page_scales[slot][2][lane] = __uint_as_float((254u - (word >> 8)) << 23);
-                            }
-                            __syncwarp();
-                            if (lane == 0) barrier_arrive(scales_full + 8 * slot);
-                        }
                         if (lane == 0) barrier_expect(bar, kBytes);
                         __syncwarp();
                         if (lane < pages) load_page(base + (half ? kCodeAt : kKeyAt) + at * kBytes + lane * page_bytes, half ? &maps.v : &maps.k, walk.it.head, page, bar);
                         __syncwarp();
                         ++loaded[half];
                     }
+                    if (t == 0) list.first_scales();
+                    const uint32_t word = __shfl_sync(0xffffffffu, list.scales, within + ((lane & 7) * pages >> 3));
+                    within += pages;
+                    if (!ok) break;
+                    if (lane < 8) {
+                        page_scales[slot][0][lane] = __uint_as_float((word & 0xffu) << 23);
+                        page_scales[slot][1][lane] = static_cast<float>(static_cast<int>(word >> 8) - 127);
+                        page_scales[slot][2][lane] = __uint_as_float((254u - (word >> 8)) << 23);
+                    }
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive(scales_full + 8 * slot);
                 }
             }
             if (lane == 0) issued[0] = loaded[0], issued[1] = loaded[1];

@@ -65,6 +65,8 @@ struct AttentionArgs {
     float* lse;  // [row][head], or null
     int64_t q_row, q_head, out_row, out_head;
     int heads, group;  // of queries; of them a head of the cache
+    Division by_group;
+    int plan_lanes;    // that add up a sequence's work: a power of two up to 32
     int causal, window;
     float scale;  // of the scores, times log2 e
     uint32_t* status;
