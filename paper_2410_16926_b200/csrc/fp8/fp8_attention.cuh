@@ -71,6 +71,7 @@ __device__ __forceinline__ int share_of(uint32_t all, uint32_t blocks, uint32_t 
 }
 struct PlanShared {
     int sums[32], left, per_head, s;
+    Sequence q;  // of the sequence that the share begins in
     Share share;
 };
 
@@ -81,6 +82,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
     const int lanes = a.plan_lanes, per = THREADS / lanes;  // for a sequence; sequences at a time
     const bool leads = (thread & (lanes - 1)) == 0;
     int units = 0, before = 0;
+    Sequence q{};
     const auto chunk = [&](int first) {  // units of a sequence, and of those before it in the chunk; returns those of the chunk
         const int s = first + thread / lanes;
         units = 0;
@@ -88,6 +90,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
             Item it;
             it.q = sequence_of(a.step, s, a.cache.page_shift);
             if (a.status && blockIdx.x == 0 && it.q.n > 0 && (it.q.first < 0 || it.q.held < it.q.first + it.q.n)) atomicOr(a.status, PVQ_STATUS_BAD_PAGE);
+            q = it.q;
             const int blocks = blocks_of<ROWS>(a, it.q);
             for (it.block = thread & (lanes - 1); it.block < blocks; it.block += lanes) {
                 measure<ROWS>(a, it);
@@ -130,6 +133,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
             sh.s = first + thread / lanes;
             sh.left = r.begin - base - before;
             sh.per_head = units / a.cache.heads;
+            sh.q = q;
         }
         base += here;
     }
@@ -142,7 +146,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
         rest -= r.head * per_head;
     }
     Item it;
-    it.q = sequence_of(a.step, r.s, a.cache.page_shift);
+    it.q = sh.q;
     const int blocks = blocks_of<ROWS>(a, it.q);
     for (int b0 = 0; b0 < blocks && blocks > 1; b0 += 32) {  // (every warp alike)
         it.block = b0 + lane;
@@ -177,10 +181,10 @@ struct Walk {
     Item it;
     int left, skip, take;
 
-    __device__ __forceinline__ Walk(const AttentionArgs& args, const Share& sh) : a(args), left(sh.left), skip(sh.skip), take(0) {
+    __device__ __forceinline__ Walk(const AttentionArgs& args, const Share& sh, const PlanShared& plan) : a(args), left(sh.left), skip(sh.skip), take(0) {
         if (left <= 0) return;
         it.s = sh.s, it.head = sh.head, it.block = sh.block;
-        it.q = sequence_of(a.step, it.s, a.cache.page_shift);
+        it.q = plan.q;
         measure<ROWS>(a, it);
         take = min(left, it.units() - skip);
     }

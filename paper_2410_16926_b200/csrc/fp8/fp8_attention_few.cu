@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
     Bounds bounds{&over, p.status};
     const Withheld withheld = withheld_of(bounds, blockIdx.x);
     const Share share = find_share<kThreads, ROWS>(p, plan, 128);
-    Walk<ROWS> walk(p, share);
+    Walk<ROWS> walk(p, share, plan);
 
     if (warp == 0) {
         const int pages = kTile >> p.cache.page_shift, page_bytes = 128 << p.cache.page_shift;  // of a tile

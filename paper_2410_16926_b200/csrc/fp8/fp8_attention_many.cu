@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
     Bounds bounds{&over, p.status};
     const Withheld withheld = withheld_of(bounds, blockIdx.x);
     const Share share = find_share<kThreads, kRows>(p, plan, 0);
-    Walk<kRows> walk(p, share);
+    Walk<kRows> walk(p, share, plan);
 
     if (warp < 8) {
         more_registers<kMany>();
@@ -147,48 +147,46 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 tile += count;
                 continue;
             }
-            const int packed = min(which * 128 + row, it.rows - 1);
-            const RowPlace place = place_of(p, it.q, it.head, it.q0 + packed);
+            const RowPlace place = place_of(p, it.q, it.head, it.q0 + min(which * 128 + row, it.rows - 1));
             const int position = it.q.first + place.row - it.q.row;
             const int to = p.causal ? min(it.q.held, position + 1) : it.q.held, from = p.window > 0 ? max(0, position - p.window + 1) : 0;
-            float factor;
-            bool finite;
-            {
-                const uint4* q = reinterpret_cast<const uint4*>(p.q + place.row * p.q_row + place.head * p.q_head);
-                uint32_t x[64];  // two values a word
+            uint32_t byte = 127u;
+            // The warp's 32 rows of queries: 16 lanes a row, eight dims each.
+#pragma unroll 1
+            for (int i0 = 0; i0 < 16; i0 += 8) {
+                uint4 w[8];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                    if (8 * j < p.cache.dim) w = __ldg(q + j);
-                    x[4 * j] = w.x, x[4 * j + 1] = w.y, x[4 * j + 2] = w.z, x[4 * j + 3] = w.w;
+                for (int i = 0; i < 8; ++i) {
+                    const int r = 2 * (i0 + i) + (lane >> 4);
+                    const int64_t at = __shfl_sync(0xffffffffu, place.row * p.q_row + place.head * p.q_head, r);
+                    w[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (8 * (lane & 15) < p.cache.dim) w[i] = __ldg(reinterpret_cast<const uint4*>(p.q + at) + (lane & 15));
                 }
-                uint32_t most = 0u;
 #pragma unroll
-                for (int j = 0; j < 64; ++j) most = max(most, max((x[j] << 16) & 0x7fffffffu, x[j] & 0x7fff0000u));
-                finite = most < kFiniteEnd;
-                const uint32_t byte = finite ? scale_byte(most) : 127u;
-                const float inverse = inverse_of(byte);
-                factor = scale_of(byte) * p.scale;
-                const uint32_t at = base + kQueryAt + which * 2 * kBytes + row * 128;
+                for (int i = 0; i < 8; ++i) {
+                    const int r = (warp & 3) * 32 + 2 * (i0 + i) + (lane >> 4);
+                    const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                    uint32_t most = 0u, hi[4], lo[4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    uint32_t hi[4], lo[4];
+                    for (int j = 0; j < 4; ++j) most = max(most, max((u[j] << 16) & 0x7fffffffu, u[j] & 0x7fff0000u));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t h0, l0, h1, l1;
-                        const uint32_t a = x[8 * j + 2 * i], b = x[8 * j + 2 * i + 1];
-                        two_codes(__uint_as_float(a << 16) * inverse, __uint_as_float(a & 0xffff0000u) * inverse, h0, l0);
-                        two_codes(__uint_as_float(b << 16) * inverse, __uint_as_float(b & 0xffff0000u) * inverse, h1, l1);
-                        hi[i] = h0 | h1 << 16, lo[i] = l0 | l1 << 16;
-                    }
-                    const uint32_t chunk = at + ((j ^ (row & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk + kBytes), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                    for (int o = 1; o < 16; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+                    const uint32_t its = most < kFiniteEnd ? scale_byte(most) : 255u;
+                    const uint32_t own = __shfl_sync(0xffffffffu, its, (lane & 1) * 16);
+                    if ((lane >> 1) == i0 + i) byte = own;
+                    const float inverse = inverse_of(its == 255u ? 127u : its);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) two_codes(__uint_as_float(u[j] << 16) * inverse, __uint_as_float(u[j] & 0xffff0000u) * inverse, hi[j], lo[j]);
+                    const uint32_t at = base + kQueryAt + which * 2 * kBytes + r * 128 + ((((lane & 15) >> 1) ^ (r & 7)) << 4) + (lane & 1) * 8;
+                    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(hi[0] | hi[1] << 16), "r"(hi[2] | hi[3] << 16) : "memory");
+                    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + kBytes), "r"(lo[0] | lo[1] << 16), "r"(lo[2] | lo[3] << 16) : "memory");
                 }
-                async_fence();
-                __syncwarp();
-                if (lane == 0) barrier_arrive(queries_full + 8 * which);
             }
+            async_fence();
+            __syncwarp();
+            if (lane == 0) barrier_arrive(queries_full + 8 * which);
+            const bool finite = byte != 255u;
+            const float factor = finite ? scale_of(byte) * p.scale : p.scale;
             // what every row of the warp sees
             const int all_to = __reduce_min_sync(0xffffffffu, to), all_from = __reduce_max_sync(0xffffffffu, from);
             float top = kNone, weight = 0.0f;
@@ -284,38 +282,67 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 ++phase;
                 tensor_fence_after();
             }
-            const bool there = which * 128 + row < it.rows, whole = walk.first() && walk.last();
+            const bool whole = walk.first() && walk.last();
+            const int rows = it.rows - which * 128 - (warp & 3) * 32;  // of the warp, those that there are
             if (!ok || over) weight = top = __uint_as_float(0x7fffffffu);
             if (!finite) weight = __uint_as_float(0x7fffffffu);
-            if (!whole && walk.first() && row == 0 && which == 0) *head = {walk.parts(plan), it.q.row, it.q0, it.rows, it.head};
+            if (!whole && walk.first() && threadIdx.x == 0) *head = {walk.parts(plan), it.q.row, it.q0, it.rows, it.head};
             float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<kRows>();
-            const float one = weight == 0.0f ? 0.0f : 1.0f / weight;
-            __nv_bfloat16* out = p.out + place.row * p.out_row + place.head * p.out_head;
+            const float one = whole ? (weight == 0.0f ? 0.0f : 1.0f / weight) : 1.0f;
+            // The rows' results go through the place of their queries, from where 16 lanes store 256 bytes of a row: all of it in bf16, or, of a part,
+            // 64 columns of fp32 at a time.
+            const uint32_t stage = base + kQueryAt + which * 2 * kBytes + (warp & 3) * 32 * 256;
+#pragma unroll 1
+            for (int turn = 0; turn < (whole ? 1 : 2); ++turn) {
+                __syncwarp();
+#pragma unroll 1
+                for (int c = 0; c < (whole ? 4 : 2); ++c) {
+                    float v[32];
+                    if (count > 0) {
+                        tensor_load(sums + 64 * turn + 32 * c, v);
+                        tensor_wait(v);
+                    } else {
 #pragma unroll
-            for (int c = 0; c < 128; c += 32) {
-                float v[32];
-                if (count > 0) {
-                    tensor_load(sums + c, v);
-                    tensor_wait_loads();
-                } else {
+                        for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+                    }
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+                    for (int i = 0; i < 4; ++i) {  // 16 bytes a store, in places turned by the row
+                        if (whole) {
+                            const uint32_t at = stage + lane * 256 + (((4 * c + i) ^ (lane & 15)) << 4);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(bf16x2_of(v[8 * i] * one, v[8 * i + 1] * one)),
+                                         "r"(bf16x2_of(v[8 * i + 2] * one, v[8 * i + 3] * one)), "r"(bf16x2_of(v[8 * i + 4] * one, v[8 * i + 5] * one)),
+                                         "r"(bf16x2_of(v[8 * i + 6] * one, v[8 * i + 7] * one))
+                                         : "memory");
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const uint32_t at = stage + lane * 256 + (((8 * c + 2 * i + j) ^ (lane & 15)) << 4);
+                                asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v[8 * i + 4 * j]), "f"(v[8 * i + 4 * j + 1]),
+                                             "f"(v[8 * i + 4 * j + 2]), "f"(v[8 * i + 4 * j + 3])
+                                             : "memory");
+                            }
+                        }
+                    }
                 }
-                if (!there) continue;
-                if (whole) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 8)
-                        if (c + i < p.cache.dim)
-                            *reinterpret_cast<uint4*>(out + c + i) = make_uint4(bf16x2_of(v[i] * one, v[i + 1] * one), bf16x2_of(v[i + 2] * one, v[i + 3] * one),
-                                                                                bf16x2_of(v[i + 4] * one, v[i + 5] * one), bf16x2_of(v[i + 6] * one, v[i + 7] * one));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4)
-                        *reinterpret_cast<float4*>(part + (which * 128 + row) * 128 + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                __syncwarp();
+#pragma unroll 4
+                for (int i = 0; i < 16; ++i) {
+                    const int r = 2 * i + (lane >> 4);
+                    const int64_t at = __shfl_sync(0xffffffffu, place.row * p.out_row + place.head * p.out_head, r);
+                    uint4 w;
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                                 : "r"(stage + r * 256 + (((lane & 15) ^ (r & 15)) << 4)));
+                    if (r >= rows) continue;
+                    if (!whole) *reinterpret_cast<uint4*>(part + (which * 128 + (warp & 3) * 32 + r) * 128 + 64 * turn + 4 * (lane & 15)) = w;
+                    else if (8 * (lane & 15) < p.cache.dim) *reinterpret_cast<uint4*>(p.out + at + 8 * (lane & 15)) = w;
                 }
             }
-            if (there && whole && p.lse) p.lse[int64_t(place.row) * p.heads + place.head] = row_lse(top, weight);
-            if (there && !whole) part[kRows * 128 + which * 128 + row] = top, part[kRows * 129 + which * 128 + row] = weight;
+            if (lane < rows) {
+                if (!whole) part[kRows * 128 + which * 128 + row] = top, part[kRows * 129 + which * 128 + row] = weight;
+                else if (p.lse) p.lse[int64_t(place.row) * p.heads + place.head] = row_lse(top, weight);
+            }
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + which) : "memory");  // (the next item's queries come to the same place)
             tensor_fence_before();  // (the sums are read before the next item's queries are there)
         }
     } else if (warp < 12) {
