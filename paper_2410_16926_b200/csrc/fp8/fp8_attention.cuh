@@ -62,9 +62,7 @@ struct Share {
     int begin, left;
     int all, blocks;  // units, and blocks that have a share
 };
-// Where block c's share of `all` begins: shares differ by one at most, larger ones first.
-__device__ __forceinline__ int share_begin(uint32_t all, uint32_t blocks, uint32_t c) { return all / blocks * c + min(c, all % blocks); }
-// The block whose share unit u is in.
+// The block whose share unit u is in: shares differ by one at most, larger ones first.
 __device__ __forceinline__ int share_of(uint32_t all, uint32_t blocks, uint32_t u) {
     const uint32_t each = all / blocks, larger = all % blocks, edge = larger * (each + 1);
     return u < edge ? u / (each + 1) : larger + (u - edge) / each;
@@ -81,7 +79,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
     const int thread = threadIdx.x, lane = thread & 31, warp = thread >> 5, seqs = a.step.seqs;
     const int lanes = a.plan_lanes, per = THREADS / lanes;  // for a sequence; sequences at a time
     const bool leads = (thread & (lanes - 1)) == 0;
-    int units = 0, before = 0;
+    int units = 0, of_head = 0, before = 0;
     Sequence q{};
     const auto chunk = [&](int first) {  // units of a sequence, and of those before it in the chunk; returns those of the chunk
         const int s = first + thread / lanes;
@@ -98,6 +96,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
             }
         }
         for (int o = lanes >> 1; o > 0; o >>= 1) units += __shfl_xor_sync(0xffffffffu, units, o);
+        of_head = units;
         units *= a.cache.heads;
         int sum = leads ? units : 0;
 #pragma unroll
@@ -123,8 +122,9 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
     r.blocks = min(static_cast<int>(gridDim.x), max(1, r.all / kLeastUnits));
     const int c = blockIdx.x;
     if (r.all == 0 || c >= r.blocks) return r;
-    r.begin = share_begin(r.all, r.blocks, c);
-    r.left = share_begin(r.all, r.blocks, c + 1) - r.begin;
+    const int each = static_cast<uint32_t>(r.all) / static_cast<uint32_t>(r.blocks), larger = r.all - each * r.blocks;
+    r.begin = each * c + min(c, larger);
+    r.left = each + (c < larger ? 1 : 0);
     int base = 0;
     if (seqs > per) __syncthreads();
     for (int first = 0; first < seqs && base <= r.begin; first += per) {
@@ -132,7 +132,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
         if (leads && base + before <= r.begin && r.begin - base - before < units) {
             sh.s = first + thread / lanes;
             sh.left = r.begin - base - before;
-            sh.per_head = units / a.cache.heads;
+            sh.per_head = of_head;
             sh.q = q;
         }
         base += here;
