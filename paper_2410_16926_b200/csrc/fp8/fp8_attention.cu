@@ -40,7 +40,8 @@ __global__ void __launch_bounds__(32 * kJoinRows) attention_join_kernel(const __
 #pragma unroll 4
         for (int i = 0; i < here; ++i) {
             const float f = __shfl_sync(0xffffffffu, less, i), w = __shfl_sync(0xffffffffu, weights, i);
-            const float4 v = *reinterpret_cast<const float4*>(part(i0 + i) + n * 128 + lane * 4);
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // (behind the dims there may be anything)
+            if (lane * 4 < p.cache.dim) v = *reinterpret_cast<const float4*>(part(i0 + i) + n * 128 + lane * 4);
             sum.x = fmaf(v.x, f, sum.x), sum.y = fmaf(v.y, f, sum.y), sum.z = fmaf(v.z, f, sum.z), sum.w = fmaf(v.w, f, sum.w);
             all = fmaf(w, f, all);
         }
@@ -61,7 +62,7 @@ struct Form {
 };
 Form form_of(int64_t seqs, int64_t rows, int heads, int kv_heads) {
     const int64_t each = (rows * (heads / kv_heads) + seqs - 1) / seqs;  // of a sequence and head
-    if (each > 64) return {256, kSms};
+    if (each > 32) return {256, kSms};
     return {each <= 4 ? 4 : (each <= 8 ? 8 : (each <= 16 ? 16 : 32)), 2 * kSms};
 }
 

@@ -293,10 +293,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             // 64 columns of fp32 at a time.
             const uint32_t stage = base + kQueryAt + which * 2 * kBytes + (warp & 3) * 32 * 256;
 #pragma unroll 1
-            for (int turn = 0; turn < (whole ? 1 : 2); ++turn) {
+            for (int turn = 0; turn < (whole || p.cache.dim <= 64 ? 1 : 2); ++turn) {
                 __syncwarp();
 #pragma unroll 1
-                for (int c = 0; c < (whole ? 4 : 2); ++c) {
+                for (int c = 0; c < (whole ? (p.cache.dim + 31) / 32 : 2); ++c) {
                     float v[32];
                     if (count > 0) {
                         tensor_load(sums + 64 * turn + 32 * c, v);
