@@ -76,7 +76,9 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
     __shared__ int over;
     __shared__ PlanShared plan;
     __shared__ float page_scales[kScaleSlots][3][8];  // of 16 tokens each: keys', values' exponent, 1 / values'
-    __shared__ __align__(16) float factor[ROWS], tops[2][4][ROWS];
+    __shared__ __align__(16) float factor[ROWS], highs[2][4][ROWS];  // rows' factors; their largest scores, of each warp
+    __shared__ __align__(16) float tops[2][ROWS], ends[4][ROWS], ones[ROWS];  // ... of all tiles so far; their weights' sums, and 1 over them
+    __shared__ int64_t places[ROWS];      // of their results
     __shared__ int from[ROWS], to[ROWS];  // positions that a row sees
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (warp == 0) {  // a barrier a lane
@@ -251,6 +253,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                         factor[r] = most < kFiniteEnd ? scale_of(byte) * p.scale : __uint_as_float(0x7fffffffu);
                         to[r] = r < it.rows ? (p.causal ? min(it.q.held, position + 1) : it.q.held) : 0;
                         from[r] = p.window > 0 ? max(0, position - p.window + 1) : 0;
+                        tops[tile & 1][r] = kNone;
                     }
                 }
                 async_fence();
@@ -260,9 +263,9 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
             tokens_meet();
             // positions that every row sees, and that any does (a later query sees from later on, and farther)
             const int all_from = from[it.rows - 1], all_to = to[0], any_from = from[0], any_to = to[it.rows - 1];
-            float top[ROWS], weight[ROWS], sum[ROWS];
+            float weight[ROWS], sum[ROWS];
 #pragma unroll
-            for (int n = 0; n < ROWS; ++n) top[n] = kNone, weight[n] = 0.0f, sum[n] = 0.0f;
+            for (int n = 0; n < ROWS; ++n) weight[n] = 0.0f, sum[n] = 0.0f;
             const auto add_sums = [&](uint32_t t) {
                 ok = ok && warp_wait(sums_full, t & 1, bounds);
                 tensor_fence_after();
@@ -293,7 +296,9 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                     for (int n = 0; n < ROWS; ++n)
                         if (position < from[n] || position >= to[n]) s[n] = kNone;
                 }
-                float (&high)[4][ROWS] = tops[tile & 1];
+                float (&high)[4][ROWS] = highs[tile & 1];
+                const float (&top)[ROWS] = tops[tile & 1];
+                float (&next_top)[ROWS] = tops[(tile & 1) ^ 1];
 #pragma unroll
                 for (int n = 0; n < ROWS; n += 4) {
                     const float4 h = make_float4(warp_max(s[n]), warp_max(s[n + 1]), warp_max(s[n + 2]), warp_max(s[n + 3]));
@@ -308,18 +313,22 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                                  c = *reinterpret_cast<const float4*>(&high[2][n]), d = *reinterpret_cast<const float4*>(&high[3][n]);
                     const float h[4] = {fmaxf(fmaxf(a.x, b.x), fmaxf(c.x, d.x)), fmaxf(fmaxf(a.y, b.y), fmaxf(c.y, d.y)),
                                         fmaxf(fmaxf(a.z, b.z), fmaxf(c.z, d.z)), fmaxf(fmaxf(a.w, b.w), fmaxf(c.w, d.w))};
-                    if (h[0] > top[n] || h[1] > top[n + 1] || h[2] > top[n + 2] || h[3] > top[n + 3]) {  // (the same for all threads)
+                    const float4 before = *reinterpret_cast<const float4*>(&top[n]);
+                    const float old[4] = {before.x, before.y, before.z, before.w};
+                    float now[4], w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) now[i] = fmaxf(old[i], h[i]);
+                    if (thread == 0) *reinterpret_cast<float4*>(&next_top[n]) = make_float4(now[0], now[1], now[2], now[3]);
+                    if (now[0] > old[0] || now[1] > old[1] || now[2] > old[2] || now[3] > old[3]) {  // (the same for all threads)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float next = fmaxf(top[n + i], h[i]), less = next == kNone ? 1.0f : exp2_of(top[n + i] - next);
+                            const float less = now[i] == kNone ? 1.0f : exp2_of(old[i] - now[i]);
                             sum[n + i] *= less, weight[n + i] *= less;
-                            top[n + i] = next;
                         }
                     }
-                    float w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        w[i] = exp2_of(s[n + i] - (top[n + i] == kNone ? 0.0f : top[n + i] - kShift));
+                        w[i] = exp2_of(s[n + i] - (now[i] == kNone ? 0.0f : now[i] - kShift));
                         weight[n + i] = fmaf(w[i], out_of, weight[n + i]);
                     }
                     uint32_t h0, l0, h1, l1;
@@ -359,34 +368,49 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
             }
             if (count > 0) add_sums(tile - 1);
             tensor_fence_before();
-            // the weights' sums over all tokens, in a fixed order
+            // The weights' sums over the warp's tokens, in a fixed order: of halves of the columns by halves of the lanes, until lane n has column n.
 #pragma unroll
-            for (int n = 0; n < ROWS; ++n) {
+            for (int o = 16; o > 0; o >>= 1) {
+                if (o >= ROWS) {
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) weight[n] += __shfl_xor_sync(0xffffffffu, weight[n], o);
-            }
-            tokens_meet();  // (the last tile's largest are read)
-            if (lane == 0) {
-#pragma unroll
-                for (int n = 0; n < ROWS; ++n) tops[0][quarter][n] = weight[n];
-            }
-            tokens_meet();
-            const bool lost = over != 0, whole = walk.first() && walk.last();
-            if (!whole && walk.first() && thread == 0) *head = {walk.parts(plan), it.q.row, it.q0, it.rows, it.head};
-            float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<ROWS>();
-#pragma unroll
-            for (int n = 0; n < ROWS; ++n) {
-                if (n >= it.rows) break;
-                float all = (tops[0][0][n] + tops[0][1][n]) + (tops[0][2][n] + tops[0][3][n]), v = sum[n], relative = top[n] - kShift;
-                if (lost) all = v = relative = __uint_as_float(0x7fffffffu);
-                if (whole) {
-                    const RowPlace place = place_of(p, it.q, it.head, it.q0 + n);
-                    if (thread < p.cache.dim) p.out[place.row * p.out_row + place.head * p.out_head + thread] = __float2bfloat16(all == 0.0f ? 0.0f : v / all);
-                    if (p.lse && thread == 0) p.lse[int64_t(place.row) * p.heads + place.head] = row_lse(relative, all);
+                    for (int n = 0; n < ROWS; ++n) weight[n] += __shfl_xor_sync(0xffffffffu, weight[n], o);
                 } else {
-                    part[n * 128 + thread] = v;
-                    if (thread == 0) part[ROWS * 128 + n] = relative, part[ROWS * 129 + n] = all;
+#pragma unroll
+                    for (int n = 0; n < o; ++n) {
+                        const bool upper = (lane & o) != 0;
+                        const float keep = upper ? weight[n + o] : weight[n], send = upper ? weight[n] : weight[n + o];
+                        weight[n] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+                    }
                 }
+            }
+            if (lane < ROWS) ends[quarter][lane] = weight[0];
+            tokens_meet();
+            const bool whole = walk.first() && walk.last();
+            float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<ROWS>();
+            if (thread < it.rows) {
+                float all = (ends[0][thread] + ends[1][thread]) + (ends[2][thread] + ends[3][thread]), relative = tops[tile & 1][thread] - kShift;
+                if (over) all = relative = __uint_as_float(0x7fffffffu);
+                if (whole) {
+                    const RowPlace place = place_of(p, it.q, it.head, it.q0 + thread);
+                    places[thread] = place.row * p.out_row + place.head * p.out_head;
+                    ones[thread] = all == 0.0f ? 0.0f : 1.0f / all;
+                    if (p.lse) p.lse[int64_t(place.row) * p.heads + place.head] = row_lse(relative, all);
+                } else {
+                    part[ROWS * 128 + thread] = relative, part[ROWS * 129 + thread] = all;
+                }
+            }
+            if (!whole && walk.first() && thread == 0) *head = {walk.parts(plan), it.q.row, it.q0, it.rows, it.head};
+            if (whole) {
+                tokens_meet();
+                if (thread < p.cache.dim) {
+#pragma unroll
+                    for (int n = 0; n < ROWS; ++n)
+                        if (n < it.rows) p.out[places[n] + thread] = __float2bfloat16(sum[n] * ones[n]);
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < ROWS; ++n)
+                    if (n < it.rows) part[n * 128 + thread] = sum[n];
             }
             tokens_meet();  // (what the block knows of this item is read)
         }
