@@ -265,6 +265,41 @@ struct Pages {
     }
 };
 
+// Waits as those of fp8_mma.cuh, whose polls are asked to take up to 20 us each: what a poll costs, others of the SM's quarter lack (a tile of
+// 256 rows 2.23 us, so 2.16).
+__device__ __forceinline__ bool passed_slowly(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t"
+        "}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done;
+}
+__device__ __forceinline__ bool thread_waits(uint32_t bar, uint32_t parity, const Bounds& b) {
+#pragma unroll 1
+    for (int i = 0; i < b.polls >> 6; ++i) {
+        if (passed_slowly(bar, parity)) return true;
+        if (*b.over) return false;
+    }
+    ran_out(b.over, b.status, b.blocks);
+    return false;
+}
+__device__ __forceinline__ bool warp_waits(uint32_t bar, uint32_t parity, const Bounds& b) {
+#pragma unroll 1
+    for (int i = 0; i < b.polls >> 6; ++i) {
+        if (__all_sync(0xffffffffu, passed_slowly(bar, parity))) return true;
+        if (__any_sync(0xffffffffu, *b.over)) return false;
+    }
+    if ((threadIdx.x & 31) == 0) ran_out(b.over, b.status, b.blocks);
+    __syncwarp();
+    return false;
+}
+
 // One page of a head to shared memory.
 __device__ __forceinline__ void load_page(uint32_t to, const CUtensorMap* map, int head, int page, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to), "l"(map), "r"(0),

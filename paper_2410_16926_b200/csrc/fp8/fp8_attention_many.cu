@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             float top = kNone, weight = 0.0f;
             float s[2][32];
             if (count > 0) {
-                ok = ok && warp_wait(scales_full + 8 * (tile % kScaleSlots), (tile / kScaleSlots) & 1, bounds) && warp_wait(scores_bar, phase & 1, bounds);
+                ok = ok && warp_waits(scales_full + 8 * (tile % kScaleSlots), (tile / kScaleSlots) & 1, bounds) && warp_waits(scores_bar, phase & 1, bounds);
                 tensor_fence_after();
                 tensor_load(scores, s[0]);
                 tensor_load(scores + 32, s[1]);
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                         top = high;
                     } else if (__any_sync(0xffffffffu, high > top + kRoom)) {
                         // (the products with the weights before are done when the scores behind them are)
-                        ok = ok && warp_wait(scores_bar + 8 * (half ^ 1), half ? (phase + 1) & 1 : phase & 1, bounds);
+                        ok = ok && warp_waits(scores_bar + 8 * (half ^ 1), half ? (phase + 1) & 1 : phase & 1, bounds);
                         tensor_fence_after();
                         const float next = fmaxf(top, high), less = next == kNone ? 1.0f : exp2_of(top - next);
                         weight *= less;
@@ -269,8 +269,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                     __syncwarp();
                     if (lane == 0) barrier_arrive(weights_bar + 8 * half);
                     if (more && !early) {
-                        ok = ok && (half == 0 || warp_wait(scales_full + 8 * ((tile + 1) % kScaleSlots), ((tile + 1) / kScaleSlots) & 1, bounds)) &&
-                             warp_wait(scores_bar + 8 * (half ^ 1), (phase + half) & 1, bounds);
+                        ok = ok && (half == 0 || warp_waits(scales_full + 8 * ((tile + 1) % kScaleSlots), ((tile + 1) / kScaleSlots) & 1, bounds)) &&
+                             warp_waits(scores_bar + 8 * (half ^ 1), (phase + half) & 1, bounds);
                         tensor_fence_after();
                         tensor_load(scores + 64 * (half ^ 1), s[0]);
                         tensor_load(scores + 64 * (half ^ 1) + 32, s[1]);
@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 }
             }
             if (count > 0) {  // the last phases: the products with the last weights
-                ok = ok && warp_wait(scores_bar, phase & 1, bounds) && warp_wait(scores_bar + 8, phase & 1, bounds);
+                ok = ok && warp_waits(scores_bar, phase & 1, bounds) && warp_waits(scores_bar + 8, phase & 1, bounds);
                 ++phase;
                 tensor_fence_after();
             }
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
         for (; walk.there() && ok; walk.next())
             for (int t = 0; t < walk.count(); ++t, ++tile) {
                 const uint32_t from = tile % kCodes, to = tile % kValues;
-                ok = warp_wait(codes_full + 8 * from, (tile / kCodes) & 1, bounds) && warp_wait(values_empty + 8 * to, ((tile / kValues) & 1) ^ 1, bounds);
+                ok = warp_waits(codes_full + 8 * from, (tile / kCodes) & 1, bounds) && warp_waits(values_empty + 8 * to, ((tile / kValues) & 1) ^ 1, bounds);
                 if (!ok) break;
                 // What no row sees may be anything, NaN too, which a weight of zero would not take out.
                 const int position = (walk.begin() + t) * kTile + token;
@@ -408,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                         const uint32_t stages = half ? kCodes : kKeys, at = tile % stages, parity = ((tile / stages) & 1) ^ 1;
                         const uint32_t bar = (half ? codes_full : keys_full) + 8 * at;
                         ok = !(withheld.copies && tile >= kKeys + kWithheldFrom) &&
-                             (tile < stages || warp_wait((half ? codes_empty : keys_empty) + 8 * at, parity, bounds));
+                             (tile < stages || warp_waits((half ? codes_empty : keys_empty) + 8 * at, parity, bounds));
                         if (!ok) break;
                         if (lane == 0) barrier_expect(bar, kBytes);
                         __syncwarp();
@@ -454,9 +454,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                 for (int i = 0; i < 4; ++i) multiply_f16(sums, scores0 + half * 64 + 8 * i, v + 128 * i, to_sums, !first || i > 0);
             };
             const auto keys_there = [&](uint32_t t) { return barrier_over(keys_full + 8 * (t % kKeys), (t / kKeys) & 1); };
-            const auto keys_wait = [&](uint32_t t) { return barrier_wait(keys_full + 8 * (t % kKeys), (t / kKeys) & 1, bounds); };
+            const auto keys_wait = [&](uint32_t t) { return thread_waits(keys_full + 8 * (t % kKeys), (t / kKeys) & 1, bounds); };
             const auto values_there = [&](uint32_t t) { return barrier_over(values_full + 8 * (t % kValues), (t / kValues) & 1); };
-            const auto values_wait = [&](uint32_t t) { return barrier_wait(values_full + 8 * (t % kValues), (t / kValues) & 1, bounds); };
+            const auto values_wait = [&](uint32_t t) { return thread_waits(values_full + 8 * (t % kValues), (t / kValues) & 1, bounds); };
             for (; walk.there() && ok; walk.next()) {
                 const int count = walk.count();
                 if (walk.it.rows <= 128 * which) {  // no rows here: the other's tiles pass
@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                     }
                     continue;
                 }
-                ok = barrier_wait(queries_full + 8 * which, items++ & 1, bounds);
+                ok = thread_waits(queries_full + 8 * which, items++ & 1, bounds);
                 if (!ok) break;
                 if (count == 0) continue;
                 ok = keys_wait(tile);
@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                     ok = (values || values_wait(tile)) && (!more || keys || keys_wait(tile + 1));
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        ok = ok && (weights || barrier_wait(weights_bar + 8 * half, weighted & 1, bounds));
+                        ok = ok && (weights || thread_waits(weights_bar + 8 * half, weighted & 1, bounds));
                         if (!ok) break;
                         tensor_fence_after();
                         add(half, tile, t == 0 && half == 0);
