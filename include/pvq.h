@@ -459,7 +459,8 @@ int pvq_fp8_cache_read(const pvq_fp8_cache* cache, const pvq_fp8_step* step, voi
  *   d_lse       [row][heads] fp32, or NULL: log sum_j exp(scale q . k_j).
  *   scale       positive.
  * Calls whose rows, heads and table would make 2^31 tiles of work or more are refused (PVQ_ERR_UNSUPPORTED).
- *   d_workspace pvq_fp8_attention_workspace bytes, 16-byte aligned, free again when the call's work is done.
+ *   d_workspace pvq_fp8_attention_workspace bytes, 16-byte aligned, free again when the call's work is done.  NULL where
+ *               that is 0.
  *   d_status    as above, and PVQ_STATUS_STAGING_TIMEOUT when a thread block gave up waiting for its copies (its results are
  *               NaN then).
  * Scores and sums are held in fp32, over queries taken to 2^-17 of a row's largest value and weights to 2^-8 of
@@ -469,8 +470,8 @@ int pvq_fp8_attention(const pvq_fp8_cache* cache, const pvq_fp8_step* step, cons
                       int64_t window, float scale, void* d_out, int64_t out_row, int64_t out_head, float* d_lse, void* d_workspace,
                       size_t workspace_bytes, uint32_t* d_status, pvq_stream_t stream);
 
-/* Bytes of workspace that a call of these sizes takes; 0 for sizes that are refused. */
-size_t pvq_fp8_attention_workspace(int64_t seqs, int64_t rows, int heads, int kv_heads);
+/* Bytes of workspace that a call of these sizes takes (short ones take none); 0 for what is refused. */
+size_t pvq_fp8_attention_workspace(const pvq_fp8_cache* cache, const pvq_fp8_step* step, int heads);
 
 /* ---- bounds-checked build -------------------------------------------------------------- */
 

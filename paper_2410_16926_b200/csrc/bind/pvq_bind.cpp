@@ -1008,7 +1008,7 @@ PyObject* bind_fp8_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         refs.r[1] = THPVariable_Wrap(std::move(t));
         if (!refs.r[1]) return nullptr;
     }
-    const size_t bytes = lib.fp8_attention_workspace(p.seqs, p.rows, static_cast<int>(q.heads), c.heads);
+    const size_t bytes = lib.fp8_attention_workspace(&c, &p, static_cast<int>(q.heads));
     at::Tensor workspace;  // (of the current stream: what comes after on it may have the memory once the call's work is done)
     if (bytes) workspace = at::detail::empty_cuda({static_cast<int64_t>(bytes)}, at::kByte, *place.dev, std::nullopt);
     void* const w = bytes ? workspace.data_ptr() : nullptr;

@@ -6,6 +6,10 @@ namespace fp8 {
 namespace {
 
 constexpr int kJoinRows = 4;  // of a block, one a warp
+// Clusters of single tokens' items: their blocks that run at once, two an SM (a cluster's lie in one part of the GPU: 33 of four and 15 of eight with
+// one an SM), and the tiles of a block up to which they are taken.
+constexpr int kAtOnce[] = {2 * kSms, 2 * kSms, 66 * 4, 30 * 8};  // of 1, 2, 4, 8
+constexpr int kClusterTiles = 16;
 
 // Block c of a group adds the item that block c of the attention was the first, but not the last, to work on.
 template <int ROWS>
@@ -58,17 +62,28 @@ __global__ void __launch_bounds__(32 * kJoinRows) attention_join_kernel(const __
     }
 }
 
-// Rows of an item, and thread blocks, for a call of this size.
+// Rows of an item, thread blocks, and how many of them make a cluster that shares an item (0: all share all work).
 struct Form {
-    int rows, blocks;
+    int rows, blocks, split;
 };
-Form form_of(int64_t seqs, int64_t rows, int heads, int kv_heads) {
-    const int64_t each = (rows * (heads / kv_heads) + seqs - 1) / seqs;  // of a sequence and head
-    if (each > 32) return {256, kSms};
-    return {each <= 4 ? 4 : (each <= 8 ? 8 : (each <= 16 ? 16 : 32)), 2 * kSms};
+Form form_of(const Cache& c, const Step& p, int heads) {
+    const int group = heads / c.heads;
+    const int64_t each = (int64_t(p.rows) * group + p.seqs - 1) / p.seqs;  // rows of a sequence and head
+    if (each > 32) return {256, kSms, 0};
+    Form f{each <= 4 ? 4 : (each <= 8 ? 8 : (each <= 16 ? 16 : 32)), 2 * kSms, 0};
+    // Single tokens of few sequences whose tables are short: an item for a cluster, whose blocks find their work without a scan and join it without
+    // a second kernel.  8 heads, in us, so and with shares: one sequence of 100 tokens 4.6 and 10.3, of 1000 6.0 and 9.5, of 16000 17.2 and 21.8; 37 of 2000
+    // (one block an item) 28.8 and 31.4, of a quarter of that and up 21.3 and 25.5; 4 of 8000 20.0 and 18.3.
+    const int64_t items = int64_t(p.seqs) * c.heads, tiles = ((int64_t(p.width) << c.page_shift) + kTile - 1) / kTile;
+    if (!p.starts && f.rows <= 16 && items <= kAtOnce[0]) {
+        int log = 0;
+        while (log < 3 && (1 << log) < tiles && items << (log + 1) <= kAtOnce[log + 1]) ++log;
+        if (tiles <= int64_t(kClusterTiles) << log) f.split = 1 << log, f.blocks = static_cast<int>(items) << log;
+    }
+    return f;
 }
 
-size_t bytes_of(const Form& f) { return f.blocks * (2 * size_t(f.rows) * (128 + 2) * sizeof(float) + sizeof(PartHead)); }
+size_t bytes_of(const Form& f) { return f.split ? 0 : f.blocks * (2 * size_t(f.rows) * (128 + 2) * sizeof(float) + sizeof(PartHead)); }
 
 template <int ROWS>
 int join(const AttentionArgs& a, int blocks, cudaStream_t s) {
@@ -77,12 +92,13 @@ int join(const AttentionArgs& a, int blocks, cudaStream_t s) {
 
 }  // namespace
 
-size_t attention_workspace(int64_t seqs, int64_t rows, int heads, int kv_heads) { return bytes_of(form_of(seqs, rows, heads, kv_heads)); }
+size_t attention_workspace(const Cache& c, const Step& p, int heads) { return bytes_of(form_of(c, p, heads)); }
 
 int attention(const AttentionArgs& call, cudaStream_t s) {
     AttentionArgs a = call;
     const int64_t seqs = a.step.seqs, rows = a.step.rows;
-    const Form f = form_of(seqs, rows, a.heads, a.cache.heads);
+    const Form f = form_of(a.cache, a.step, a.heads);
+    a.split = f.split;
     // (items of all sequences, each of at most as many tiles as a table holds)
     const int64_t items = rows * a.group / f.rows + seqs, tiles = ((int64_t(a.step.width) << a.cache.page_shift) + kTile - 1) / kTile;
     if (items * a.cache.heads >= int64_t(1) << 31 || items * a.cache.heads * tiles >= int64_t(1) << 31) return PVQ_ERR_UNSUPPORTED;
@@ -91,7 +107,7 @@ int attention(const AttentionArgs& call, cudaStream_t s) {
     a.plan_lanes = 1;
     while (a.plan_lanes < 32 && seqs * a.plan_lanes * 2 <= threads && rows * a.group > f.rows * seqs * a.plan_lanes) a.plan_lanes *= 2;
     int st = f.rows == 256 ? attention_many(a, f.blocks, s) : attention_few(a, f.rows, f.blocks, s);
-    if (st != PVQ_OK) return st;
+    if (st != PVQ_OK || f.split) return st;
     if (f.rows == 4) return join<4>(a, f.blocks, s);
     if (f.rows == 8) return join<8>(a, f.blocks, s);
     if (f.rows == 16) return join<16>(a, f.blocks, s);

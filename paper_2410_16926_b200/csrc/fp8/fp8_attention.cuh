@@ -180,6 +180,20 @@ struct Walk {
     const AttentionArgs& a;
     Item it;
     int left, skip, take;
+    bool over = false;  // (of an item of a cluster's, which may leave a block no units)
+
+    // Of one item, the units that are this block's of the cluster's `split`.
+    __device__ __forceinline__ Walk(const AttentionArgs& args, int item, int rank, int split) : a(args), left(-1) {
+        const uint32_t blocks = (a.group + ROWS - 1) / ROWS, each = a.cache.heads * blocks;  // (one row a sequence)
+        it.s = item / each;
+        const uint32_t rest = item - it.s * each;
+        it.head = rest / blocks, it.block = rest - it.head * blocks;
+        it.q = sequence_of(a.step, it.s, a.cache.page_shift);
+        measure<ROWS>(a, it);
+        const int units = it.units();
+        skip = units * rank / split;
+        take = units * (rank + 1) / split - skip;
+    }
 
     __device__ __forceinline__ Walk(const AttentionArgs& args, const Share& sh, const PlanShared& plan) : a(args), left(sh.left), skip(sh.skip), take(0) {
         if (left <= 0) return;
@@ -188,7 +202,7 @@ struct Walk {
         measure<ROWS>(a, it);
         take = min(left, it.units() - skip);
     }
-    __device__ __forceinline__ bool there() const { return left > 0; }
+    __device__ __forceinline__ bool there() const { return left > 0 || (left < 0 && !over); }
     __device__ __forceinline__ int begin() const { return it.tile0() + skip; }  // tiles of this share
     __device__ __forceinline__ int count() const { return min(take, it.tiles()); }
     __device__ __forceinline__ bool first() const { return skip == 0; }
@@ -198,6 +212,8 @@ struct Walk {
         return share_of(plan.share.all, plan.share.blocks, plan.share.begin + plan.share.left - left + it.units() - 1) - blockIdx.x + 1;
     }
     __device__ __forceinline__ void next() {
+        over = true;
+        if (left < 0) return;
         left -= take;
         if (left <= 0) return;
         skip = 0;

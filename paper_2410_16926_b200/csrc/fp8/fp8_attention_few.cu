@@ -64,7 +64,8 @@ __device__ __forceinline__ void load_columns(uint32_t at, float (&v)[N]) {
     }
 }
 
-template <int ROWS>
+// CLUSTER: an item for each cluster (of a.split blocks; one block alone is one too) instead of a share of all items' work for each block.
+template <int ROWS, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid_constant__ CacheMaps maps, const __grid_constant__ AttentionArgs p) {
     using S = Few<ROWS>;
     constexpr int kHalves = S::kHalves, kWide = S::kWide;
@@ -103,8 +104,15 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
     const uint32_t tensor = tensor_base, sums = tensor + 2 * kWide;
     Bounds bounds{&over, p.status};
     const Withheld withheld = withheld_of(bounds, blockIdx.x);
-    const Share share = find_share<kThreads, ROWS>(p, plan, 128);
-    Walk<ROWS> walk(p, share, plan);
+    const int rank = CLUSTER && p.split > 1 ? static_cast<int>(cluster_rank()) : 0;
+    Walk<ROWS> walk = [&] {
+        if constexpr (CLUSTER) return Walk<ROWS>(p, blockIdx.x / p.split, rank, p.split);
+        else return Walk<ROWS>(p, find_share<kThreads, ROWS>(p, plan, 128), plan);
+    }();
+    if (CLUSTER && p.status && threadIdx.x == 0 && rank == 0) {
+        const Sequence& q = walk.it.q;
+        if (q.first < 0 || q.held < q.first + q.n) atomicOr(p.status, PVQ_STATUS_BAD_PAGE);
+    }
 
     if (warp == 0) {
         const int pages = kTile >> p.cache.page_shift, page_bytes = 128 << p.cache.page_shift;  // of a tile
@@ -198,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
         const int quarter = warp & 3, thread = quarter * 32 + lane;  // token, then dim
         const uint32_t mine = quarter << 21;
         PartHead* head = part_heads<ROWS>(p) + blockIdx.x;
-        if (thread == 0 && gridDim.x > 1) head->parts = 0;
+        if (!CLUSTER && thread == 0) head->parts = 0;
         if (ROWS < S::kWide) {  // columns that are not used: zeros
             for (int i = thread; i < (2 * S::kQueryBytes + 2 * S::kWeightBytes) / 16; i += 128)
                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + S::kQueries + 16 * i), "r"(0u) : "memory");
@@ -385,6 +393,52 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
             }
             if (lane < ROWS) ends[quarter][lane] = weight[0];
             tokens_meet();
+            if (CLUSTER && p.split > 1) {
+                // The parts of the cluster's blocks, in the stages' place, which is free once all are here: those of a share of the dims go to the
+                // block that adds them up, in the order of the ranks: [rank][row][dim of the share], then [rank][largest, weights][row].
+                const int split = p.split, share = 128 / split;
+                const uint32_t stats = base + ROWS * 512;
+                float all = 0.0f, relative = kNone;
+                if (thread < ROWS) {
+                    all = (ends[0][thread] + ends[1][thread]) + (ends[2][thread] + ends[3][thread]), relative = tops[tile & 1][thread] - kShift;
+                    if (over) all = relative = __uint_as_float(0x7fffffffu);
+                }
+                cluster_barrier();
+#pragma unroll
+                for (int n = 0; n < ROWS; ++n)
+                    if (n < it.rows) store_in(address_in(base + ((rank * ROWS + n) * share + thread % share) * 4, thread / share), __float_as_uint(sum[n]));
+                if (thread < it.rows)
+                    for (int r = 0; r < split; ++r) {
+                        store_in(address_in(stats + (rank * 2 * ROWS + thread) * 4, r), __float_as_uint(relative));
+                        store_in(address_in(stats + (rank * 2 * ROWS + ROWS + thread) * 4, r), __float_as_uint(all));
+                    }
+                cluster_barrier();
+                for (int i = thread; i < it.rows * share; i += 128) {
+                    const int n = i / share, d = i - n * share;
+                    float m[8], top = kNone;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        m[r] = kNone;
+                        if (r < split) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(m[r]) : "r"(stats + (r * 2 * ROWS + n) * 4));
+                        top = m[r] != m[r] ? m[r] : (top != top ? top : fmaxf(top, m[r]));
+                    }
+                    float v = 0.0f, weights = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        if (r < split) {
+                            const float less = exp2_of(m[r] - (top == kNone ? 0.0f : top));
+                            float x, w;
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(base + ((r * ROWS + n) * share + d) * 4));
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(w) : "r"(stats + (r * 2 * ROWS + ROWS + n) * 4));
+                            v = fmaf(x, less, v), weights = fmaf(w, less, weights);
+                        }
+                    const RowPlace place = place_of(p, it.q, it.head, it.q0 + n);
+                    const int dim = rank * share + d;
+                    if (dim < p.cache.dim) p.out[place.row * p.out_row + place.head * p.out_head + dim] = __float2bfloat16(weights == 0.0f ? 0.0f : v / weights);
+                    if (p.lse && dim == 0) p.lse[int64_t(place.row) * p.heads + place.head] = row_lse(top, weights);
+                }
+                continue;
+            }
             const bool whole = walk.first() && walk.last();
             float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<ROWS>();
             if (thread < it.rows) {
@@ -416,6 +470,10 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
         }
     }
     __syncwarp();
+    if (CLUSTER && p.split > 1 && warp < 2) {  // (the others have met twice)
+        cluster_barrier();
+        cluster_barrier();
+    }
     tensor_fence_before();
     __syncthreads();
     if (__builtin_expect(over, 0) && warp == 0) land<kHalves>(full, issued_halves);  // copies in flight have to land before the block ends
@@ -425,21 +483,22 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
     }
 }
 
-template <int ROWS>
+template <int ROWS, bool CLUSTER>
 int launch(const AttentionArgs& a, int blocks, cudaStream_t s) {
     CacheMaps maps;
     int st = cache_maps(a.cache, &maps);
-    if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(attention_few_kernel<ROWS>), Few<ROWS>::kShared);
+    void (*const kernel)(CacheMaps, AttentionArgs) = attention_few_kernel<ROWS, CLUSTER>;
+    if (st == PVQ_OK) st = allow_shared(reinterpret_cast<const void*>(kernel), Few<ROWS>::kShared);
     if (st != PVQ_OK) return st;
-    return launch_early(attention_few_kernel<ROWS>, dim3(static_cast<unsigned>(blocks)), kThreads, Few<ROWS>::kShared, 0, s, maps, a);
+    return launch_early(kernel, dim3(static_cast<unsigned>(blocks)), kThreads, Few<ROWS>::kShared, CLUSTER && a.split > 1 ? a.split : 0, s, maps, a);
 }
-
 }  // namespace
 
 int attention_few(const AttentionArgs& a, int rows, int blocks, cudaStream_t s) {
-    if (rows == 4) return launch<4>(a, blocks, s);
-    if (rows == 8) return launch<8>(a, blocks, s);
-    return rows == 16 ? launch<16>(a, blocks, s) : launch<32>(a, blocks, s);
+    if (rows == 4) return a.split ? launch<4, true>(a, blocks, s) : launch<4, false>(a, blocks, s);
+    if (rows == 8) return a.split ? launch<8, true>(a, blocks, s) : launch<8, false>(a, blocks, s);
+    if (rows == 16) return a.split ? launch<16, true>(a, blocks, s) : launch<16, false>(a, blocks, s);
+    return launch<32, false>(a, blocks, s);
 }
 
 }  // namespace fp8

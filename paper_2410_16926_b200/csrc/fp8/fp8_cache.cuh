@@ -67,12 +67,13 @@ struct AttentionArgs {
     int heads, group;  // of queries; of them a head of the cache
     Division by_group;
     int plan_lanes;    // that add up a sequence's work: a power of two up to 32
+    int split;         // of few rows: blocks of a cluster that an item is shared by; 0: shares of all items' work
     int causal, window;
     float scale;  // of the scores, times log2 e
     uint32_t* status;
     float* workspace;
 };
-size_t attention_workspace(int64_t seqs, int64_t rows, int heads, int kv_heads);
+size_t attention_workspace(const Cache& c, const Step& p, int heads);
 int attention(const AttentionArgs& a, cudaStream_t s);
 
 }  // namespace fp8

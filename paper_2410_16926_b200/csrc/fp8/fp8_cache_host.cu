@@ -76,10 +76,11 @@ extern "C" int pvq_fp8_cache_read(const pvq_fp8_cache* cache, const pvq_fp8_step
     return fp8::cache_read(c, p, {d_k, d_v, k_row, k_head, v_row, v_head}, dtype == PVQ_DTYPE_BF16, d_status, static_cast<cudaStream_t>(stream));
 }
 
-extern "C" size_t pvq_fp8_attention_workspace(int64_t seqs, int64_t rows, int heads, int kv_heads) {
-    if (seqs < 1 || rows < 1 || kv_heads < 1 || heads < 1 || heads % kv_heads != 0 || heads / kv_heads > 128) return 0;
-    if (seqs >= 1 << 24 || rows >= 1 << 28 || rows * heads >= int64_t(1) << 31) return 0;
-    return fp8::attention_workspace(seqs, rows, heads, kv_heads);
+extern "C" size_t pvq_fp8_attention_workspace(const pvq_fp8_cache* cache, const pvq_fp8_step* step, int heads) {
+    fp8::Cache c;
+    fp8::Step p;
+    if (checked(cache, &c) != PVQ_OK || heads < 1 || heads % c.heads != 0 || heads / c.heads > 128 || checked(step, c, heads, &p) != PVQ_OK) return 0;
+    return fp8::attention_workspace(c, p, heads);
 }
 
 extern "C" int pvq_fp8_attention(const pvq_fp8_cache* cache, const pvq_fp8_step* step, const void* d_q, int heads, int64_t q_row, int64_t q_head, int causal,
@@ -94,7 +95,7 @@ extern "C" int pvq_fp8_attention(const pvq_fp8_cache* cache, const pvq_fp8_step*
     CHECKED(checked_rows(d_q, PVQ_DTYPE_BF16, a.cache.dim, q_row, q_head));
     CHECKED(checked_rows(d_out, PVQ_DTYPE_BF16, a.cache.dim, out_row, out_head));
     if (d_lse && !is_aligned(d_lse, 4)) return PVQ_ERR_ALIGNMENT;
-    const size_t needed = fp8::attention_workspace(a.step.seqs, a.step.rows, heads, a.cache.heads);
+    const size_t needed = fp8::attention_workspace(a.cache, a.step, heads);
     if (needed > 0 && !d_workspace) return PVQ_ERR_INVALID_ARG;
     if (workspace_bytes < needed) return PVQ_ERR_TABLE_TOO_SMALL;
     if (d_workspace && !is_aligned(d_workspace, 16)) return PVQ_ERR_ALIGNMENT;

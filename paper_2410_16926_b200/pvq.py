@@ -115,7 +115,7 @@ def lib():
         L.pvq_fp8_cache_write.argtypes = [cache, step, vp, i64, i64, vp, i64, i64, i32, vp, vp]
         L.pvq_fp8_cache_read.argtypes = [cache, step, vp, i64, i64, vp, i64, i64, i32, vp, vp]
         L.pvq_fp8_attention.argtypes = [cache, step, vp, i32, i64, i64, i32, i64, C.c_float, vp, i64, i64, vp, vp, sz, vp, vp]
-        L.pvq_fp8_attention_workspace.argtypes = [i64, i64, i32, i32]
+        L.pvq_fp8_attention_workspace.argtypes = [cache, step, i32]
         L.pvq_fp8_attention_workspace.restype = sz
         L.pvq_debug_status.argtypes = [vp]
         L.pvq_encode_status.argtypes = [vp]

@@ -90,26 +90,30 @@ def attention(q, codes, exponents, table, lengths, starts, page, causal=True, wi
             continue
         total = min(length, table.shape[1] * page)
         k, v = (sequence(c, e, table[s], total, page) for c, e in zip(codes, exponents))
+        position = np.arange(length - (b - a), length)[:, None]
+        token = np.arange(total)[None, :]
+        seen = np.ones((b - a, total), dtype=bool)
+        if causal:
+            seen &= token <= position
+        if window:
+            seen &= token > position - window
+        some = seen.any(axis=1)
+        count = seen.sum(axis=1)
+        steps = (count / 32 + 64) * 2.0 ** -23
         for h in range(heads):
-            kh, vh = k[h // group], v[h // group]
-            for r in range(a, b):
-                i = length - (b - r)
-                to = min(total, i + 1) if causal else total
-                at = max(0, i - window + 1) if window else 0
-                if to <= at:
-                    out[r, h], lse[r, h] = 0.0, -np.inf
-                    continue
-                kk, vv, qq = kh[at:to], vh[at:to], q[r, h]
-                w = scale * (kk @ qq)
-                m = w.max()
-                p = np.exp(w - m)
-                lse[r, h] = m + np.log(p.sum())
-                p /= p.sum()
-                out[r, h] = p @ vv
-                off = scale * (2.0 ** -17 * np.abs(qq).max() * np.abs(kk).sum(axis=1) + (dim + 32) * 2.0 ** -23 * (np.abs(kk) @ np.abs(qq)))
-                off = off.max() + (np.abs(w).max() + 64) * 2.0 ** -22
-                steps = ((to - at) / 32 + 64) * 2.0 ** -23
-                size = p @ np.abs(vv)
-                slack[r, h] = 2.0 ** -8 * np.abs(out[r, h]) + (2.0 ** -8 + 2 * off + 2 * steps) * size + 2.0 ** -17 * np.abs(vv).max() + 2.0 ** -130
-                slack_lse[r, h] = off + steps + 2.0 ** -22 * abs(lse[r, h]) + 2.0 ** -21
+            kh, vh, qh = k[h // group], v[h // group], q[a:b, h]
+            with np.errstate(invalid="ignore"):
+                w = np.where(seen, scale * (qh @ kh.T), -np.inf)
+            m = np.where(some, w.max(axis=1, initial=-np.inf), 0.0)
+            p = np.exp(w - m[:, None])
+            sums = p.sum(axis=1)
+            with np.errstate(divide="ignore"):
+                lse[a:b, h] = np.where(some, m + np.log(sums), -np.inf)
+            p = p / np.where(some, sums, 1.0)[:, None]
+            out[a:b, h] = p @ vh
+            off = scale * (2.0 ** -17 * np.abs(qh).max(axis=1)[:, None] * np.abs(kh).sum(axis=1)[None, :] + (dim + 32) * 2.0 ** -23 * (np.abs(qh) @ np.abs(kh).T))
+            off = np.where(seen, off, 0.0).max(axis=1, initial=0.0) + (np.where(seen, np.abs(w), 0.0).max(axis=1, initial=0.0) + 64) * 2.0 ** -22
+            largest = np.where(seen, np.abs(vh).max(axis=1, initial=0.0)[None, :], 0.0).max(axis=1, initial=0.0)
+            slack[a:b, h] = 2.0 ** -8 * np.abs(out[a:b, h]) + (2.0 ** -8 + 2 * off + 2 * steps)[:, None] * (p @ np.abs(vh)) + (2.0 ** -17 * largest + 2.0 ** -130)[:, None]
+            slack_lse[a:b, h] = off + steps + 2.0 ** -22 * np.abs(np.where(some, lse[a:b, h], 0.0)) + 2.0 ** -21
     return out, lse, slack, slack_lse

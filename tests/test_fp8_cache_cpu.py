@@ -86,10 +86,17 @@ def test_other_arguments_are_checked():
     for scale in (0.0, -1.0, float("nan"), float("inf")):
         assert attention(scale=scale) == INVALID
     assert attention(lse=P + 2) == ALIGN and attention(workspace=P + 8) == ALIGN and attention(workspace=None) == INVALID
-    need = L.pvq_fp8_attention_workspace(3, 10, 4, 2)
+    need = L.pvq_fp8_attention_workspace(cache(), step(), 4)
     assert need > 0 and attention(size=need - 1) == SMALL
-    bad = ((0, 1, 4, 2), (1, 0, 4, 2), (1, 1, 0, 2), (1, 1, 4, 0), (1, 1, 5, 2), (1, 1, 258, 2), (1 << 24, 1 << 24, 4, 2), (1, 1 << 28, 4, 2), (1, 1 << 27, 32, 8))
-    assert [L.pvq_fp8_attention_workspace(*a) for a in bad] == [0] * len(bad)
+    for heads in (0, 5, 258, -4):
+        assert L.pvq_fp8_attention_workspace(cache(), step(), heads) == 0
+    assert [L.pvq_fp8_attention_workspace(cache(**bad), step(), 4) for bad, _ in BAD_CACHES] == [0] * len(BAD_CACHES)
+    assert [L.pvq_fp8_attention_workspace(cache(), step(**bad), 4) for bad, _ in BAD_STEPS] == [0] * len(BAD_STEPS)
+    # single tokens of few short sequences need none; longer tables, more sequences and more rows do
+    one = dict(starts=None, seqs=2, rows=2)
+    assert L.pvq_fp8_attention_workspace(cache(), step(**one), 4) == 0
+    for more in (dict(width=4000, ld=4000), dict(seqs=200, rows=200), dict(starts=P)):
+        assert L.pvq_fp8_attention_workspace(cache(), step(**{**one, **more}), 4) > 0
 
 
 def test_the_binding_refuses_what_is_not_on_the_gpu_or_of_another_type():

@@ -42,7 +42,7 @@ def kernels(call):
 
 @pytest.mark.parametrize("heads,kv,n,rows", [(2, 2, 1, 4), (8, 2, 1, 4), (4, 1, 2, 8), (16, 4, 3, 16), (13, 1, 1, 16), (32, 2, 2, 32), (32, 1, 1, 32), (8, 2, 9, 256),
                                              (33, 1, 1, 256), (128, 1, 1, 256), (4, 4, 40, 256), (10, 2, 70, 256)])
-@pytest.mark.parametrize("lengths", [[300, 41, 130], [7000, 129, 500]])
+@pytest.mark.parametrize("lengths", [[300, 41, 130], [5000, 129, 0], [40000, 129, 500]])
 def test_attention(heads, kv, n, rows, lengths):
     dim, page = 128, 32
     lengths = [max(n, length) for length in lengths]
@@ -52,9 +52,27 @@ def test_attention(heads, kv, n, rows, lengths):
     starts = None if n == 1 else [n * i for i in range(len(lengths) + 1)]
     q = queries(rng, n * len(lengths), heads, dim)
     device = ints(table), ints(lengths), None if starts is None else ints(starts)
-    name = "attention_many_kernel" if rows == 256 else "attention_few_kernel"
-    assert set(kernels(lambda: pvq.fp8_attention(q, cache, *device))) == {(name, None if rows == 256 else str(rows)), ("attention_join_kernel", str(rows))}
+    expected = {("attention_many_kernel", None) if rows == 256 else ("attention_few_kernel", str(rows))}
+    if n > 1 or rows > 16 or lengths[0] > 16 * 8 * 128:  # (otherwise an item for a cluster)
+        expected.add(("attention_join_kernel", str(rows)))
+    assert set(kernels(lambda: pvq.fp8_attention(q, cache, *device))) == expected
     check(q, cache, table, lengths, starts, page)
+
+
+@pytest.mark.parametrize("group,seqs,kv,length", [(4, 1, 1, 100), (1, 1, 1, 200), (7, 1, 2, 500), (16, 1, 3, 900), (4, 1, 30, 2000), (2, 1, 31, 2000), (8, 33, 2, 1000),
+                                                   (5, 67, 1, 1000), (16, 148, 1, 300), (3, 148, 2, 700), (4, 148, 2, 1), (1, 1, 296, 300)])
+def test_single_tokens_in_clusters(group, seqs, kv, length):
+    """Clusters of one, two, four and eight blocks, some of which may have no tile; sequences of every length."""
+    rng = np.random.default_rng(seqs + kv + group)
+    dim, page = 64, 32
+    lengths = [length] + [int(x) for x in rng.integers(0, length, seqs - 1)]
+    table, pool = tables(rng, lengths, page)
+    cache = filled(rng, table, lengths, pool, kv, page, dim)
+    q = queries(rng, seqs, group * kv, dim)
+    device = ints(table), ints(lengths)
+    assert [name for name, _ in kernels(lambda: pvq.fp8_attention(q, cache, *device))] == ["attention_few_kernel"]
+    check(q, cache, table, lengths, None, page)
+    check(q, cache, table, lengths, None, page, window=130)
 
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
@@ -64,6 +82,7 @@ def test_every_dim_and_page(dim, page):
     lengths = [page * 3 + 1, 259, 128]
     table, pool = tables(rng, lengths, page)
     cache = filled(rng, table, lengths, pool, 2, page, dim)
+    check(queries(rng, 3, 6, dim), cache, table, lengths, None, page)
     for heads, n in ((6, 1), (10, 6), (4, 30)):
         check(queries(rng, 3 * n, heads, dim), cache, table, lengths, [0, n, 2 * n, 3 * n], page)
         check(queries(rng, 3 * n, heads, dim), cache, table, lengths, [0, n, 2 * n, 3 * n], page, window=100)
@@ -75,6 +94,7 @@ def test_every_group_of_heads(group):
     lengths, page, dim = [290, 77], 64, 64
     table, pool = tables(rng, lengths, page)
     cache = filled(rng, table, lengths, pool, 2, page, dim)
+    check(queries(rng, 2, 2 * group, dim), cache, table, lengths, None, page)
     for starts in ([0, 1, 2], [0, 5, 8], [0, 77, 130]):
         check(queries(rng, starts[-1], 2 * group, dim), cache, table, lengths, starts, page)
 

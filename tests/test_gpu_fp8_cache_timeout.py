@@ -25,7 +25,7 @@ table = torch.arange(pages, dtype=torch.int32, device="cuda").view(seqs, -1)
 lengths = torch.full((seqs,), length, dtype=torch.int32, device="cuda")
 every = torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * length
 pvq.fp8_cache_write(rand(seqs * length, kv, dim), rand(seqs * length, kv, dim), cache, table, lengths, every)
-q, starts = rand(seqs * n, heads, dim), torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * n
+q, starts = rand(seqs * n, heads, dim), torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * n if n > 1 else None
 def run(bits):
     status = torch.full((1,), bits, dtype=torch.int32, device="cuda")
     torch.cuda.synchronize()
@@ -49,7 +49,7 @@ print("done")
 
 
 @pytest.mark.parametrize("heads,kv,n,length,seqs", [(8, 2, 1, 4000, 40), (32, 2, 1, 4000, 40), (8, 2, 8, 4000, 40), (8, 2, 1, 200000, 1), (8, 2, 64, 4000, 20), (4, 4, 300, 2000, 20),
-                                                    (8, 2, 100, 40000, 1)])
+                                                    (8, 2, 100, 40000, 1), (4, 1, 1, 12000, 1), (16, 2, 1, 6000, 12), (4, 4, 1, 1500, 74)])
 def test_copies_that_never_arrive(heads, kv, n, length, seqs):
     from paper_2410_16926_b200 import build
     env = dict(os.environ, PVQ_B200_LIB=build.build(debug=True), PYTHONPATH=ROOT)
