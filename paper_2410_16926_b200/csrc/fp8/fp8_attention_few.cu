@@ -9,6 +9,10 @@
 // the weights are relative to the largest of w * scale, whatever the pages' scales are; their sum takes it out again.
 //
 // Warps: one issues the copies, one the products, four hold the tokens (then the dims).
+//
+// What bounds it: memory, up to 16 rows.  A tile of 32 KB in each of 296 blocks takes 1.46 to 1.53 us (1.48 at the copy rate); with 32 rows 2.4, the
+// tokens' warps.  That takes the 4, 8 or 16 columns that there are rows for: computing on all 16 for 4 rows cost 1.7 us a tile of latency, and short
+// calls 2.5 us.  Before the first copy pass 3.5 us (lengths, a scan of the sequences' work, the table), 1.2 less without the scan.
 #include "fp8_attention.cuh"
 
 namespace pvq {

@@ -11,6 +11,10 @@
 // a score.  Sums of V in tensor memory are rescaled only when a row's largest has grown by 2^8 since: fp16 has the room.
 //
 // Warps: eight for the weights, four convert V, one issues the copies, one for each tile of rows the products.
+//
+// What bounds it: the weights' warps, one of each tile of rows in a quarter of the SM.  256 rows by 128 tokens of 128 dims take 2.16 us, about 4000 cycles, two
+// steps of 64 tokens of each row; the exponentials' unit needs 2080 of them, the tensor cores 2200.  128 scores a step: 2.8; one thread for both tiles'
+// products: 2.46, since an answer from a barrier takes it 200 cycles; scores not loaded ahead: 2.32.
 #include "fp8_attention.cuh"
 
 namespace pvq {

@@ -404,7 +404,7 @@ def fp8_cache_write(k, v, cache, table, lengths, starts=None, status=None):
 
 def fp8_cache_read(cache, table, lengths, starts=None, rows=None, dtype=torch.bfloat16, out=(None, None), status=None):
     """(k, v) [rows][heads][dim]: the values of the rows' tokens (whole sequences, with starts the sums of the lengths).  `rows`:
-    how many, where there are starts; those of no sequence are left as they were."""
+    how many, where there are starts; those of no sequence are left as they were (in new tensors: whatever was there)."""
     return (_native or _load_native()).fp8_cache_read(*cache, table, lengths, starts, -1 if rows is None else rows, _value_type(dtype), *out, status)
 
 
@@ -412,6 +412,6 @@ def fp8_attention(q, cache, table, lengths, starts=None, causal=True, window=0, 
     """Attention of q [rows][query heads][dim] bfloat16 to what the sequences hold -> bfloat16 of the same shape.  A row at position i
     sees positions j < lengths[s], j <= i with `causal`, j > i - window with `window`; what sees nothing is zeros.  scale:
     1 / sqrt(dim) if not given.  With `lse` also float32 [rows][query heads], the logarithm of the sum of exp(scale q k).  Rows of no
-    sequence are left as they were.  `status` as above, and STATUS_STAGING_TIMEOUT as for fp8_matmul."""
+    sequence are left as they were (in new tensors: whatever was there).  `status` as above, and STATUS_STAGING_TIMEOUT as for fp8_matmul."""
     return (_native or _load_native()).fp8_attention(q, *cache, table, lengths, starts, causal, window,
                                                      1 / math.sqrt(q.shape[-1]) if scale is None else scale, lse, out, status)
