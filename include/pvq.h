@@ -458,7 +458,7 @@ int pvq_fp8_cache_read(const pvq_fp8_cache* cache, const pvq_fp8_step* step, voi
  *               cache->heads, at most 128 times it.
  *   d_lse       [row][heads] fp32, or NULL: log sum_j exp(scale q . k_j).
  *   scale       positive.
- * Calls whose rows, heads and table would make 2^31 tiles of work or more are refused (PVQ_ERR_UNSUPPORTED).
+ * Calls whose rows, heads and table would make 2^31 tiles of work or more, six added for each block of 256 query rows, are refused (PVQ_ERR_UNSUPPORTED).
  *   d_workspace pvq_fp8_attention_workspace bytes, 16-byte aligned, free again when the call's work is done.  NULL where
  *               that is 0.
  *   d_status    as above, and PVQ_STATUS_STAGING_TIMEOUT when a thread block gave up waiting for its copies (its results are

@@ -99,9 +99,9 @@ int attention(const AttentionArgs& call, cudaStream_t s) {
     const int64_t seqs = a.step.seqs, rows = a.step.rows;
     const Form f = form_of(a.cache, a.step, a.heads);
     a.split = f.split;
-    // (items of all sequences, each of at most as many tiles as a table holds)
-    const int64_t items = rows * a.group / f.rows + seqs, tiles = ((int64_t(a.step.width) << a.cache.page_shift) + kTile - 1) / kTile;
-    if (items * a.cache.heads >= int64_t(1) << 31 || items * a.cache.heads * tiles >= int64_t(1) << 31) return PVQ_ERR_UNSUPPORTED;
+    // (items of all sequences, each of at most as many tiles as a table holds, and its other units)
+    const int64_t items = rows * a.group / f.rows + seqs, units = ((int64_t(a.step.width) << a.cache.page_shift) + kTile - 1) / kTile + (f.rows == 256 ? item_units<256>() : 1);
+    if (items * a.cache.heads >= int64_t(1) << 31 || items * a.cache.heads * units >= int64_t(1) << 31) return PVQ_ERR_UNSUPPORTED;
     a.by_group = division_by(a.group);
     const int threads = 128;  // (the least of a kernel's: a sequence's lanes for all of them, where there are few)
     a.plan_lanes = 1;

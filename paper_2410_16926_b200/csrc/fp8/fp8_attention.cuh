@@ -1,8 +1,8 @@
 // What the attention kernels over the 8-bit cache share: how the work is cut, the pages' way to shared memory, parts of results.
 //
 // An item is a block of a sequence's query rows (query heads of a cache's head side by side, query for query) over one head of the
-// cache; its units are the tiles of 128 tokens that some row of it sees, one at least.  The units of all items in a row are cut into
-// equal shares, one a thread block, whatever the sequences' lengths; an item that is cut leaves parts (sums that are not yet
+// cache; its units are the tiles of 128 tokens that some row of it sees, behind what its beginning and end cost, in tiles (one at least).
+// The units of all items in a row are cut into equal shares, one a thread block, whatever the sequences' lengths; an item that is cut leaves parts (sums that are not yet
 // divided, and what their weights are relative to) in the workspace, which a second kernel adds in the order of the tokens.
 #pragma once
 #include "fp8_cache.cuh"
@@ -14,7 +14,14 @@ struct CacheMaps {
     CUtensorMap k, v;
 };
 
-constexpr int kLeastUnits = 2;   // of a block
+// What an item costs besides its tiles, in tiles: of 256 rows, queries made codes, the first scores, the results, 10 to 20 us by 2.2 a tile.  A causal
+// prompt's first blocks of rows are items of few tiles; thread blocks that got many of them ended last.  32 heads over 8 of 128 dims, in us, with 0, 4, 6
+// and 10: 8192 causal tokens 816, 636, 610, 632; 8 of 1024 236, 215, 212, 219; 4096 seen by all 325, 320, 321, 333.  Few rows begin in a tile's time: 0.
+template <int ROWS>
+__host__ __device__ constexpr int item_units() {
+    return ROWS == 256 ? 6 : 0;
+}
+constexpr int kLeastTiles = 2;   // of a block
 constexpr int kScaleSlots = 8;   // tiles whose scales are on their way
 constexpr float kNone = -INFINITY;
 
@@ -40,7 +47,10 @@ struct Item {
     int lo, hi;          // positions that some row sees
     __device__ __forceinline__ int tile0() const { return lo / kTile; }  // of those
     __device__ __forceinline__ int tiles() const { return hi > lo ? (hi + kTile - 1) / kTile - tile0() : 0; }
-    __device__ __forceinline__ int units() const { return max(tiles(), 1); }
+    template <int ROWS>
+    __device__ __forceinline__ int units() const {
+        return max(item_units<ROWS>() + tiles(), 1);
+    }
 };
 
 template <int ROWS>
@@ -92,7 +102,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
             const int blocks = blocks_of<ROWS>(a, it.q);
             for (it.block = thread & (lanes - 1); it.block < blocks; it.block += lanes) {
                 measure<ROWS>(a, it);
-                units += it.units();
+                units += it.units<ROWS>();
             }
         }
         for (int o = lanes >> 1; o > 0; o >>= 1) units += __shfl_xor_sync(0xffffffffu, units, o);
@@ -119,7 +129,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
     };
     Share r{};
     for (int first = 0; first < seqs; first += per) r.all += chunk(first);
-    r.blocks = min(static_cast<int>(gridDim.x), max(1, r.all / kLeastUnits));
+    r.blocks = min(static_cast<int>(gridDim.x), max(1, r.all / (item_units<ROWS>() + kLeastTiles)));
     const int c = blockIdx.x;
     if (r.all == 0 || c >= r.blocks) return r;
     const int each = static_cast<uint32_t>(r.all) / static_cast<uint32_t>(r.blocks), larger = r.all - each * r.blocks;
@@ -153,7 +163,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
         int sum = 0;
         if (it.block < blocks) {
             measure<ROWS>(a, it);
-            sum = it.units();
+            sum = it.units<ROWS>();
         }
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -190,7 +200,7 @@ struct Walk {
         it.head = rest / blocks, it.block = rest - it.head * blocks;
         it.q = sequence_of(a.step, it.s, a.cache.page_shift);
         measure<ROWS>(a, it);
-        const int units = it.units();
+        const int units = it.template units<ROWS>();
         skip = units * rank / split;
         take = units * (rank + 1) / split - skip;
     }
@@ -200,16 +210,18 @@ struct Walk {
         it.s = sh.s, it.head = sh.head, it.block = sh.block;
         it.q = plan.q;
         measure<ROWS>(a, it);
-        take = min(left, it.units() - skip);
+        take = min(left, it.template units<ROWS>() - skip);
     }
     __device__ __forceinline__ bool there() const { return left > 0 || (left < 0 && !over); }
-    __device__ __forceinline__ int begin() const { return it.tile0() + skip; }  // tiles of this share
-    __device__ __forceinline__ int count() const { return min(take, it.tiles()); }
+    // Tiles of this share (an item's other units are before them).
+    __device__ __forceinline__ int before() const { return max(skip - item_units<ROWS>(), 0); }
+    __device__ __forceinline__ int begin() const { return it.tile0() + before(); }
+    __device__ __forceinline__ int count() const { return max(min(skip + take - item_units<ROWS>(), it.tiles()) - before(), 0); }
     __device__ __forceinline__ bool first() const { return skip == 0; }
-    __device__ __forceinline__ bool last() const { return skip + take == it.units(); }
+    __device__ __forceinline__ bool last() const { return skip + take == it.template units<ROWS>(); }
     // Blocks that the item is shared by, from its first one on (called where first()).
     __device__ __forceinline__ int parts(const PlanShared& plan) const {
-        return share_of(plan.share.all, plan.share.blocks, plan.share.begin + plan.share.left - left + it.units() - 1) - blockIdx.x + 1;
+        return share_of(plan.share.all, plan.share.blocks, plan.share.begin + plan.share.left - left + it.template units<ROWS>() - 1) - blockIdx.x + 1;
     }
     __device__ __forceinline__ void next() {
         over = true;
@@ -227,7 +239,7 @@ struct Walk {
             }
         }
         measure<ROWS>(a, it);
-        take = min(left, it.units());
+        take = min(left, it.template units<ROWS>());
     }
 };
 
