@@ -328,6 +328,15 @@ __device__ __forceinline__ bool warp_waits(uint32_t bar, uint32_t parity, const 
     return false;
 }
 
+// In the bounds-checked build copies may be left out as in the products' kernels, and scales come late instead, each tile's by kLate ns, which
+// the waits have time for: whoever does not wait for them reads those of another tile.
+constexpr unsigned kLate = 10000;
+__device__ __forceinline__ Withheld withheld_in(Bounds& b) {
+    const Withheld w = withheld_of(b, blockIdx.x);
+    if (w.scales && !w.copies) b.polls = kPolls;
+    return w;
+}
+
 // One page of a head to shared memory.
 __device__ __forceinline__ void load_page(uint32_t to, const CUtensorMap* map, int head, int page, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to), "l"(map), "r"(0),

@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
     dependency_wait();
     const uint32_t tensor = tensor_base, sums = tensor + 2 * kWide;
     Bounds bounds{&over, p.status};
-    const Withheld withheld = withheld_of(bounds, blockIdx.x);
+    const Withheld withheld = withheld_in(bounds);
     const int rank = CLUSTER && p.split > 1 ? static_cast<int>(cluster_rank()) : 0;
     Walk<ROWS> walk = [&] {
         if constexpr (CLUSTER) return Walk<ROWS>(p, blockIdx.x / p.split, rank, p.split);
@@ -144,6 +144,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                     turn.next();
                     ++issued;
                 }
+                if (withheld.scales) __nanosleep(kLate);
                 if (t == 0) list.first_scales();
                 const uint32_t word = __shfl_sync(0xffffffffu, list.scales, within + ((lane & 7) * pages >> 3));
                 within += pages;

@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
     dependency_wait();
     const uint32_t tensor = tensor_base;
     Bounds bounds{&over, p.status};
-    const Withheld withheld = withheld_of(bounds, blockIdx.x);
+    const Withheld withheld = withheld_in(bounds);
     const Share share = find_share<kThreads, kRows>(p, plan, 0);
     Walk<kRows> walk(p, share, plan);
 
@@ -196,7 +196,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             float top = kNone, weight = 0.0f;
             float s[2][32];
             if (count > 0) {
-                ok = ok && warp_waits(scales_full + 8 * (tile % kScaleSlots), (tile / kScaleSlots) & 1, bounds) && warp_waits(scores_bar, phase & 1, bounds);
+                // Scores first: when they are there, the slot's scales of eight tiles ago are long past, so that the parity can only mean these.  (Warps
+                // that had no rows in the items before did not wait for those items' scales.)
+                ok = ok && warp_waits(scores_bar, phase & 1, bounds) && warp_waits(scales_full + 8 * (tile % kScaleSlots), (tile / kScaleSlots) & 1, bounds);
                 tensor_fence_after();
                 tensor_load(scores, s[0]);
                 tensor_load(scores + 32, s[1]);
@@ -420,6 +422,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                         __syncwarp();
                         ++loaded[half];
                     }
+                    if (withheld.scales) __nanosleep(kLate);
                     if (t == 0) list.first_scales();
                     const uint32_t word = __shfl_sync(0xffffffffu, list.scales, within + ((lane & 7) * pages >> 3));
                     within += pages;
