@@ -155,9 +155,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             const int position = it.q.first + place.row - it.q.row;
             const int to = p.causal ? min(it.q.held, position + 1) : it.q.held, from = p.window > 0 ? max(0, position - p.window + 1) : 0;
             uint32_t byte = 127u;
-            // The warp's 32 rows of queries: 16 lanes a row, eight dims each.
+            // The warp's 32 rows of queries: 16 lanes a row, eight dims each.  None where the item has no tiles in this share: nothing would hold the warps
+            // together then, so that one could put its results where another's queries are on their way, and a phase of queries_full pass unseen.
 #pragma unroll 1
-            for (int i0 = 0; i0 < 16; i0 += 8) {
+            for (int i0 = count > 0 ? 0 : 16; i0 < 16; i0 += 8) {
                 uint4 w[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             }
             async_fence();
             __syncwarp();
-            if (lane == 0) barrier_arrive(queries_full + 8 * which);
+            if (lane == 0 && count > 0) barrier_arrive(queries_full + 8 * which);
             const bool finite = byte != 255u;
             const float factor = finite ? scale_of(byte) * p.scale : p.scale;
             // what every row of the warp sees
@@ -475,10 +476,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                     }
                     continue;
                 }
-                ok = thread_waits(queries_full + 8 * which, items++ & 1, bounds);
-                if (!ok) break;
                 if (count == 0) continue;
-                ok = keys_wait(tile);
+                ok = thread_waits(queries_full + 8 * which, items++ & 1, bounds) && keys_wait(tile);
                 if (!ok) break;
                 tensor_fence_after();
                 for (int half = 0; half < 2; ++half) {
