@@ -181,12 +181,13 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                 products_done<false>(empty + 8 * (2 * t % kHalves));
                 products_done<false>(scores_full + 8 * (t & 1));
             };
-            for (; walk.there() && ok; walk.next(), ++items) {
+            for (; walk.there() && ok; walk.next()) {
                 const int count = walk.count();
-                ok = barrier_wait(queries_full, items & 1, bounds);
+                if (count == 0) continue;
+                ok = barrier_wait(queries_full, items++ & 1, bounds);
                 if (!ok) break;
                 tensor_fence_after();
-                if (count > 0) score(tile);
+                score(tile);
                 for (int t = 0; t < count && ok; ++t, ++tile) {
                     if (t + 1 < count) score(tile + 1);
                     ok = ok && barrier_wait(weights_full, tile & 1, bounds) && arrived(2 * tile + 1);
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                 }
                 async_fence();
                 __syncwarp();
-                if (lane == 0) barrier_arrive(queries_full);
+                if (lane == 0 && count > 0) barrier_arrive(queries_full);  // (without tiles nothing would hold the next item's back)
             }
             tokens_meet();
             // positions that every row sees, and that any does (a later query sees from later on, and farther)
