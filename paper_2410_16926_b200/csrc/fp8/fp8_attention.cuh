@@ -361,11 +361,11 @@ __device__ __forceinline__ void multiply_codes(uint32_t d, uint64_t a, uint64_t 
 }
 
 // A row's values times 2^-e, |values| at most 448, as two codes each: the nearest one, and the nearest one to what it leaves.
-// Together they are a bf16 value but for 2^-17 of the row's largest.
-__device__ __forceinline__ void two_codes(float x, float y, uint32_t& hi, uint32_t& lo) {
+// Together they are a bf16 value but for 2^-17 of the row's largest.  (`apart`: a power of two by which the second code is larger than what it stands for.)
+__device__ __forceinline__ void two_codes(float x, float y, uint32_t& hi, uint32_t& lo, float apart = 1.0f) {
     hi = codes_of(x, y);
     const float2 h = values_of(hi);
-    lo = codes_of(x - h.x, y - h.y);
+    lo = codes_of((x - h.x) * apart, (y - h.y) * apart);
 }
 
 int cache_maps(const Cache& c, CacheMaps* maps);

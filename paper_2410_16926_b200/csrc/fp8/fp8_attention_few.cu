@@ -3,10 +3,15 @@
 // For each tile of 128 tokens the tokens are the products' 128 lanes and the query rows their columns: S^T = K Q^T, then, with
 // a thread a token, the weights w = 2^(s - m) and P^T, and O^T = V^T P^T with the dims as lanes, added to sums in registers.  Both
 // products take the cache's codes as they lie in memory, the keys along k and the values across it.  What they are multiplied
-// by is split into two codes each (queries to 2^-17 of the row's largest, weights to 2^-8 of themselves).
+// by is split into two codes each (queries to 2^-17 of the row's largest).
 //
 // A page's scales are powers of two: that of the keys multiplies a token's scores, that of the values is added to their exponents, so that
-// the weights are relative to the largest of w * scale, whatever the pages' scales are; their sum takes it out again.
+// what is weighed is w * scale; the weights' sum takes the scale out again.
+//
+// The weights' codes are relative to the tile's own largest (to a power of two of the row's largest so far, so that a tile's sums join the row's
+// by an exact factor): a token that leads by far costs the other tiles nothing, and what many small weights hold together stays.  The
+// second codes, of what the first ones leave, are 2^5 times as large, in columns of their own behind the first ones': one product of twice the columns.
+// Within a tile a weight is off by 2^-8 of itself or 2^-22 of the tile's largest.
 //
 // Warps: one issues the copies, one the products, four hold the tokens (then the dims).
 //
@@ -21,7 +26,8 @@ namespace {
 
 constexpr int kThreads = 192;
 constexpr int kHalf = kTile * 128;       // bytes of a tile's keys or values, rows of 128 bytes
-constexpr float kShift = 8.0f;           // weights are up to 2^8: their smallest code is 2^-9
+constexpr float kShift = 8.0f;           // weights are up to 2^8: the first codes are off by 8 at most
+constexpr float kApart = 32.0f;          // ... and the second ones up to 2^8, too
 
 // ROWS query rows of an item: a product has 16 or 32 columns, of which 4, 8 or all are used.
 template <int ROWS>
@@ -32,8 +38,9 @@ struct Few {
     static constexpr int kWeights = kQueries + 2 * kQueryBytes, kWeightBytes = kWide * kTile;
     static constexpr int kBars = kWeights + 2 * kWeightBytes;
     static constexpr size_t kShared = 1024 + kBars + 256;
-    static constexpr int kColumns = kWide == 16 ? 64 : 128;  // of tensor memory: scores twice, sums
-    static_assert(2 * (kShared + 4096) <= 231424, "two blocks an SM");
+    static constexpr int kColumns = kWide == 16 ? 64 : 128;  // of tensor memory: scores twice, sums of first and of second codes
+    static_assert(kWeightBytes == kWide / 16 * kTile * 16, "the second codes are the next columns");
+    static_assert(2 * (kShared + 1024 + 1200 + 200 * ROWS) <= 233472, "two blocks an SM, with the system's kilobyte each and what else they share");
 };
 
 // Operand across k whose 16 columns of one k lie together: eight k's are 128 bytes, the next 16 columns are `further`.
@@ -82,7 +89,8 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
     __shared__ PlanShared plan;
     __shared__ float page_scales[kScaleSlots][3][8];  // of 16 tokens each: keys', values' exponent, 1 / values'
     __shared__ __align__(16) float factor[ROWS], highs[2][4][ROWS];  // rows' factors; their largest scores, of each warp
-    __shared__ __align__(16) float tops[2][ROWS], ends[4][ROWS], ones[ROWS];  // ... of all tiles so far; their weights' sums, and 1 over them
+    __shared__ float4 tops[2][4][ROWS];         // of each warp: what a tile's weights are relative to, what joins them to the row's, what the row's lose
+    __shared__ float ends[4][ROWS], ones[ROWS];  // the weights' sums, and 1 over them
     __shared__ int64_t places[ROWS];      // of their results
     __shared__ int from[ROWS], to[ROWS];  // positions that a row sees
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -161,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
         if (lane == 0) issued_halves = issued;
     } else if (warp == 1) {
         if (elected()) {
-            constexpr uint32_t scores = product_codes(128, kWide, false, false), results = product_codes(128, kWide, true, true);
+            constexpr uint32_t scores = product_codes(128, kWide, false, false), results = product_codes(128, 2 * kWide, true, true);
             const uint64_t tiles0 = operand(base), queries0 = operand(base + S::kQueries), weights0 = operand_plain(base + S::kWeights, kTile * 16);
             const int steps = (p.cache.dim + 31) / 32;
             uint32_t tile = 0, items = 0;
@@ -195,10 +203,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                     tensor_fence_after();
                     const uint64_t v = half_at(2 * tile + 1);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        multiply_codes(sums, v + 256 * i, weights0 + 32 * i, results, i > 0);
-                        multiply_codes(sums, v + 256 * i, weights0 + (S::kWeightBytes >> 4) + 32 * i, results, true);
-                    }
+                    for (int i = 0; i < 4; ++i) multiply_codes(sums, v + 256 * i, weights0 + 32 * i, results, i > 0);
                     products_done<false>(empty + 8 * ((2 * tile + 1) % kHalves));
                     products_done<false>(sums_full);
                 }
@@ -267,7 +272,6 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                         factor[r] = most < kFiniteEnd ? scale_of(byte) * p.scale : __uint_as_float(0x7fffffffu);
                         to[r] = r < it.rows ? (p.causal ? min(it.q.held, position + 1) : it.q.held) : 0;
                         from[r] = p.window > 0 ? max(0, position - p.window + 1) : 0;
-                        tops[tile & 1][r] = kNone;
                     }
                 }
                 async_fence();
@@ -280,17 +284,19 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
             float weight[ROWS], sum[ROWS];
 #pragma unroll
             for (int n = 0; n < ROWS; ++n) weight[n] = 0.0f, sum[n] = 0.0f;
+            float top = kNone;  // of row `lane`, over all tiles so far
             const auto add_sums = [&](uint32_t t) {
                 ok = ok && warp_wait(sums_full, t & 1, bounds);
                 tensor_fence_after();
 #pragma unroll
                 for (int c = 0; c < ROWS; c += 16) {
                     constexpr int kHere = ROWS < 16 ? ROWS : 16;
-                    float v[kHere];
+                    float v[kHere], w[kHere];
                     load_columns(sums + mine + c, v);
+                    load_columns(sums + mine + kWide + c, w);
                     tensor_wait_loads();
 #pragma unroll
-                    for (int n = 0; n < kHere; ++n) sum[c + n] += v[n];
+                    for (int n = 0; n < kHere; ++n) sum[c + n] = fmaf(fmaf(w[n], 1.0f / kApart, v[n]), tops[t & 1][quarter][c + n].y, sum[c + n]);
                 }
             };
             for (int t = 0; t < count; ++t, ++tile) {
@@ -311,43 +317,45 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                         if (position < from[n] || position >= to[n]) s[n] = kNone;
                 }
                 float (&high)[4][ROWS] = highs[tile & 1];
-                const float (&top)[ROWS] = tops[tile & 1];
-                float (&next_top)[ROWS] = tops[(tile & 1) ^ 1];
+                float4 (&relative)[ROWS] = tops[tile & 1][quarter];
 #pragma unroll
                 for (int n = 0; n < ROWS; n += 4) {
                     const float4 h = make_float4(warp_max(s[n]), warp_max(s[n + 1]), warp_max(s[n + 2]), warp_max(s[n + 3]));
                     if (lane == 0) *reinterpret_cast<float4*>(&high[quarter][n]) = h;
                 }
                 tokens_meet();
+                bool grown = false;
+                if (lane < ROWS) {  // a row each: the tile's weights are relative to 2^-below of the row's largest, which is 1 to 2 times the tile's
+                    const float h = fmaxf(fmaxf(high[0][lane], high[1][lane]), fmaxf(high[2][lane], high[3][lane])), now = fmaxf(top, h);
+                    const int below = __float2int_rd(fminf(now - h, 120.0f));  // (120: nothing seen, or nothing left of it)
+                    grown = now > top;
+                    relative[lane] = make_float4(now == kNone ? 0.0f : now - static_cast<float>(below) - kShift, __uint_as_float(static_cast<uint32_t>(127 - below) << 23),
+                                                 grown ? exp2_of(top - now) : 1.0f, 0.0f);
+                    top = now;
+                }
+                grown = __any_sync(0xffffffffu, grown);
+                __syncwarp();
                 if (t > 0) add_sums(tile - 1);
+                if (grown) {
+#pragma unroll
+                    for (int n = 0; n < ROWS; ++n) {
+                        const float less = relative[n].z;
+                        sum[n] *= less, weight[n] *= less;
+                    }
+                }
                 uint32_t hi[ROWS / 4], lo[ROWS / 4];
 #pragma unroll
                 for (int n = 0; n < ROWS; n += 4) {
-                    const float4 a = *reinterpret_cast<const float4*>(&high[0][n]), b = *reinterpret_cast<const float4*>(&high[1][n]),
-                                 c = *reinterpret_cast<const float4*>(&high[2][n]), d = *reinterpret_cast<const float4*>(&high[3][n]);
-                    const float h[4] = {fmaxf(fmaxf(a.x, b.x), fmaxf(c.x, d.x)), fmaxf(fmaxf(a.y, b.y), fmaxf(c.y, d.y)),
-                                        fmaxf(fmaxf(a.z, b.z), fmaxf(c.z, d.z)), fmaxf(fmaxf(a.w, b.w), fmaxf(c.w, d.w))};
-                    const float4 before = *reinterpret_cast<const float4*>(&top[n]);
-                    const float old[4] = {before.x, before.y, before.z, before.w};
-                    float now[4], w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) now[i] = fmaxf(old[i], h[i]);
-                    if (thread == 0) *reinterpret_cast<float4*>(&next_top[n]) = make_float4(now[0], now[1], now[2], now[3]);
-                    if (now[0] > old[0] || now[1] > old[1] || now[2] > old[2] || now[3] > old[3]) {  // (the same for all threads)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float less = now[i] == kNone ? 1.0f : exp2_of(old[i] - now[i]);
-                            sum[n + i] *= less, weight[n + i] *= less;
-                        }
-                    }
+                    float w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        w[i] = exp2_of(s[n + i] - (now[i] == kNone ? 0.0f : now[i] - kShift));
-                        weight[n + i] = fmaf(w[i], out_of, weight[n + i]);
+                        const float2 r = *reinterpret_cast<const float2*>(&relative[n + i]);
+                        w[i] = exp2_of(s[n + i] - r.x);
+                        weight[n + i] = fmaf(w[i] * out_of, r.y, weight[n + i]);
                     }
                     uint32_t h0, l0, h1, l1;
-                    two_codes(w[0], w[1], h0, l0);
-                    two_codes(w[2], w[3], h1, l1);
+                    two_codes(w[0], w[1], h0, l0, kApart);
+                    two_codes(w[2], w[3], h1, l1, kApart);
                     hi[n / 4] = h0 | h1 << 16, lo[n / 4] = l0 | l1 << 16;
                 }
                 const uint32_t place = base + S::kWeights + thread * 16;
@@ -406,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                 const uint32_t stats = base + ROWS * 512;
                 float all = 0.0f, relative = kNone;
                 if (thread < ROWS) {
-                    all = (ends[0][thread] + ends[1][thread]) + (ends[2][thread] + ends[3][thread]), relative = tops[tile & 1][thread] - kShift;
+                    all = (ends[0][thread] + ends[1][thread]) + (ends[2][thread] + ends[3][thread]), relative = top - kShift;
                     if (over) all = relative = __uint_as_float(0x7fffffffu);
                 }
                 cluster_barrier();
@@ -448,7 +456,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
             const bool whole = walk.first() && walk.last();
             float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<ROWS>();
             if (thread < it.rows) {
-                float all = (ends[0][thread] + ends[1][thread]) + (ends[2][thread] + ends[3][thread]), relative = tops[tile & 1][thread] - kShift;
+                float all = (ends[0][thread] + ends[1][thread]) + (ends[2][thread] + ends[3][thread]), relative = top - kShift;
                 if (over) all = relative = __uint_as_float(0x7fffffffu);
                 if (whole) {
                     const RowPlace place = place_of(p, it.q, it.head, it.q0 + thread);
