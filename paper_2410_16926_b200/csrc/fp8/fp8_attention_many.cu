@@ -8,7 +8,8 @@
 //
 // As in the kernel for few rows, exponents of the pages' scales of V are added to the scores, so that weights are relative to the largest of
 // w * scale; 16 tokens, of one page, share both scales, which are applied to their largest score and inside the exponent, at no cost
-// a score.  Sums of V in tensor memory are rescaled only when a row's largest has grown by 2^8 since: fp16 has the room.
+// a score.  Sums of V in tensor memory are rescaled only when a row's largest has grown by 2^8 since.  The largest gets a weight of 2^7, so that fp16 is used up
+// to 2^15: a weight is off by 2^-11 of itself, or by 2^-32 of the row's largest, where fp16 ends.
 //
 // Warps: eight for the weights, four convert V, one issues the copies, one for each tile of rows the products.
 //
@@ -28,6 +29,7 @@ constexpr int kQueryAt = 0, kKeyAt = 4 * kBytes, kCodeAt = kKeyAt + kKeys * kByt
               kBarAt = kValueAt + kValues * 2 * kBytes;
 constexpr size_t kShared = 1024 + kBarAt + 512;
 constexpr float kRoom = 8.0f;           // exponent by which a row's largest may be behind
+constexpr float kShift = 7.0f;          // ... and of the weight that it gets: up to 2^15 in all
 
 constexpr int kRegisters = 128, kMany = 168, kFew = 88;
 static_assert(2 * kMany + 2 * kFew <= 4 * kRegisters, "a share beyond these would be waited for without end");
@@ -241,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                             tensor_store(sums + c, w);
                         }
                     }
-                    const float against = top == kNone ? 0.0f : top;
+                    const float against = top == kNone ? 0.0f : top - kShift;
                     const float rest[4] = {value.x - against, value.y - against, value.z - against, value.w - against}, back[4] = {out_of.x, out_of.y, out_of.z, out_of.w};
                     const bool more = half == 0 || t + 1 < count;
                     uint32_t w[32];
@@ -292,6 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             const bool whole = walk.first() && walk.last();
             const int rows = it.rows - which * 128 - (warp & 3) * 32;  // of the warp, those that there are
             if (!ok || over) weight = top = __uint_as_float(0x7fffffffu);
+            top -= kShift;  // what the weights are relative to
             if (!finite) weight = __uint_as_float(0x7fffffffu);
             if (!whole && walk.first() && threadIdx.x == 0) *head = {walk.parts(plan), it.q.row, it.q0, it.rows, it.head};
             float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<kRows>();

@@ -89,7 +89,7 @@ SIZES = [(1, 1500, 2), (2, 9000, 2), (64, 8200, 8), (40, 33000, 8)]
 
 @pytest.mark.parametrize("spread", [0.0, 0.5])  # of the others' scores: the same for all, or normal
 @pytest.mark.parametrize("lead", [4.0, 9.0, 12.3125, 13.0, 15.0, 18.0])
-@pytest.mark.parametrize("n", [1, 4])
+@pytest.mark.parametrize("n", [1, 4, 40])
 @pytest.mark.parametrize("seqs,length,kv", SIZES)
 def test_a_token_that_leads(seqs, length, kv, n, lead, spread):
     rng = np.random.default_rng(length + n)
@@ -101,7 +101,7 @@ def test_a_token_that_leads(seqs, length, kv, n, lead, spread):
 
 
 @pytest.mark.parametrize("first", [5000, 8199])  # the row's largest comes late: what was summed before stays
-@pytest.mark.parametrize("n", [1, 2, 8])
+@pytest.mark.parametrize("n", [1, 2, 8, 40])
 def test_a_token_that_leads_late(n, first):
     rng = np.random.default_rng(n)
     cache, table, lengths = led(rng, 40, 8200 + n, 8, 16, 64, 13.0, 0.5, first=first)
@@ -110,7 +110,7 @@ def test_a_token_that_leads_late(n, first):
 
 
 @pytest.mark.parametrize("page", [16, 128])
-@pytest.mark.parametrize("n", [1, 4])
+@pytest.mark.parametrize("n", [1, 4, 40])
 def test_a_channel_that_leads(n, page):
     """One page has one value 2^9 times the others': the other channels, and the other pages, keep theirs."""
     rng = np.random.default_rng(page + n)
