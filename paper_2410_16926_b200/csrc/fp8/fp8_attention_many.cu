@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             const int rows = it.rows - which * 128 - (warp & 3) * 32;  // of the warp, those that there are
             if (!ok || over) weight = top = __uint_as_float(0x7fffffffu);
             top -= kShift;  // what the weights are relative to
-            if (!finite) weight = __uint_as_float(0x7fffffffu);
+            if (!finite && to > from) weight = __uint_as_float(0x7fffffffu);  // (where the row sees something)
             if (!whole && walk.first() && threadIdx.x == 0) *head = {walk.parts(plan), it.q.row, it.q0, it.rows, it.head};
             float* part = p.workspace + (2 * int64_t(blockIdx.x) + (walk.first() ? 1 : 0)) * part_floats<kRows>();
             const float one = whole ? (weight == 0.0f ? 0.0f : 1.0f / weight) : 1.0f;

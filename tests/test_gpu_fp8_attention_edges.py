@@ -73,3 +73,22 @@ def test_sequences_that_hold_nothing(n, empty, causal):
         assert bool((out[nothing] == 0).all()) and bool((lse[nothing] == -float("inf")).all())
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
         assert int(status) == pvq.STATUS_BAD_PAGE  # (lengths below their rows are told)
+
+
+@pytest.mark.parametrize("n,group,length", [(20, 1, 5), (20, 4, 5), (100, 4, 10), (300, 1, 200), (300, 1, 0)])
+def test_rows_that_see_nothing_beside_rows_that_see(n, group, length):
+    """Rows in front of their sequence's beginning get zeros and -inf, whatever their queries hold."""
+    kv, dim, page, seqs = 2, 64, 32, 5
+    rng = np.random.default_rng(n + group)
+    lengths = [length, n, length, 3 * n, length]
+    table, pool = tables(rng, lengths, page)
+    cache = filled(rng, table, lengths, pool, kv, page, dim)
+    starts = [n * i for i in range(seqs + 1)]
+    q = queries(rng, n * seqs, group * kv, dim)
+    first = check(q, cache, table, lengths, starts, page)
+    nothing = torch.cat([torch.arange(n, device="cuda") < n - x for x in lengths])
+    for odd in (float("nan"), -float("inf")):
+        q[nothing] = odd
+        out, lse = pvq.fp8_attention(q, cache, ints(table), ints(lengths), ints(starts), lse=True)
+        assert bool((out[nothing] == 0).all()) and bool((lse[nothing] == -float("inf")).all())
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
