@@ -417,8 +417,9 @@ size_t pvq_fp8_weight_grad_workspace(int64_t rows, int64_t inner, int64_t outer)
  *              holds up to 2^30 tokens.
  *   d_lengths  [seqs] tokens of each sequence, those of this step among them.
  *   d_starts   [seqs + 1] ascending: rows starts[s] .. starts[s + 1] - 1 are the last tokens of sequence
- *              s.  Rows in front of the first and behind the last are neither read nor written.  NULL: one row a
- *              sequence, rows == seqs.
+ *              s.  Rows in front of the first and behind the last are neither read nor written.  Where they descend,
+ *              attention writes nothing (PVQ_STATUS_BAD_PAGE), and what is written to the cache or read from it is not defined.  NULL: one
+ *              row a sequence, rows == seqs.
  * All three are on the device (int32) and only looked at there; what they say is checked there, too: no access
  * leaves the pool, the table or the rows, whatever they hold, and PVQ_STATUS_BAD_PAGE is OR-ed into *d_status (optional) where a
  * position has no place.  Calls keep nothing, and can be captured into graphs.  The same inputs give the same bits. */

@@ -66,7 +66,8 @@ __device__ __forceinline__ int blocks_of(const AttentionArgs& a, const Sequence&
     return (q.n * a.group + ROWS - 1) / ROWS;
 }
 
-// A block's share: it begins `skip` units into an item.  (All units are fewer than 2^31: the host sees to that.)
+// A block's share: it begins `skip` units into an item.  (All units are fewer than 2^31: the host sees to that for sequences that do not
+// overlap.  Where starts descend nobody has a share.)
 struct Share {
     int s, head, block, skip;
     int begin, left;
@@ -90,6 +91,7 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
     const int lanes = a.plan_lanes, per = THREADS / lanes;  // for a sequence; sequences at a time
     const bool leads = (thread & (lanes - 1)) == 0;
     int units = 0, of_head = 0, before = 0;
+    bool descends = false;  // starts of some sequence so far
     Sequence q{};
     const auto chunk = [&](int first) {  // units of a sequence, and of those before it in the chunk; returns those of the chunk
         const int s = first + thread / lanes;
@@ -116,7 +118,8 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
         }
         if (first > 0) __syncthreads();
         if (lane == 31) sh.sums[warp] = sum;
-        __syncthreads();
+        if (a.step.starts) descends |= __syncthreads_or(s < seqs && __ldg(a.step.starts + s + 1) < __ldg(a.step.starts + s));
+        else __syncthreads();
         before = sum - (leads ? units : 0);
         int all = 0;
 #pragma unroll
@@ -128,7 +131,11 @@ __device__ __forceinline__ Share find_share(const AttentionArgs& a, PlanShared& 
         return all;
     };
     Share r{};
-    for (int first = 0; first < seqs; first += per) r.all += chunk(first);
+    for (int first = 0; first < seqs; first += per) r.all = descends ? 0 : r.all + chunk(first);
+    if (descends) {
+        if (a.status && blockIdx.x == 0 && thread == 0) atomicOr(a.status, PVQ_STATUS_BAD_PAGE);
+        r.all = 0;
+    }
     r.blocks = min(static_cast<int>(gridDim.x), max(1, r.all / (item_units<ROWS>() + kLeastTiles)));
     const int c = blockIdx.x;
     if (r.all == 0 || c >= r.blocks) return r;

@@ -92,3 +92,40 @@ def test_rows_that_see_nothing_beside_rows_that_see(n, group, length):
         out, lse = pvq.fp8_attention(q, cache, ints(table), ints(lengths), ints(starts), lse=True)
         assert bool((out[nothing] == 0).all()) and bool((lse[nothing] == -float("inf")).all())
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+
+
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("odd", [[2, 1, 0], [0, 2, 1], [1, 0, 2], [2 ** 31 - 1, 0, 2], [0, 2, -1]])
+def test_starts_that_descend_are_told_and_nothing_is_written(odd, n):
+    kv, dim, page, lengths = 2, 64, 32, [100, 300]
+    rng = np.random.default_rng(n)
+    table, pool = tables(rng, lengths, page)
+    cache = filled(rng, table, lengths, pool, kv, page, dim)
+    q = queries(rng, 2 * n, 8, dim)
+    out = torch.full_like(q, float("nan"))
+    status = torch.zeros(1, dtype=I32, device="cuda")
+    pvq.fp8_attention(q, cache, ints(table), ints(lengths), ints([x * n if abs(x) < 9 else x for x in odd]), out=out, status=status)
+    assert bool(torch.isnan(out).all()) and int(status) == pvq.STATUS_BAD_PAGE
+    status.zero_()
+    for fine in ([0, n, 2 * n], [0, 0, 2 * n], [-5, n, 2 ** 31 - 1]):  # (ends beyond the rows are cut off)
+        out.fill_(float("nan"))
+        pvq.fp8_attention(q, cache, ints(table), ints(lengths), ints(fine), out=out, status=status)
+        assert int(status) == 0 and bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("heads,kv", [(32, 8), (64, 1)])  # few rows and many
+def test_overlapping_sequences_of_more_than_2_to_31_tiles(heads, kv):
+    """Every second sequence claims all rows, over tables of 2^20 tokens: what one sequence after another may have is fewer, all together are not."""
+    dim, page, seqs, rows, width = 64, 128, 1024, 4096, 8192
+    cache = pvq.alloc_fp8_cache(1, kv, page, dim)
+    for c in cache:
+        c.view(torch.uint8).fill_(0x38)
+    table = torch.zeros((seqs, width), dtype=I32, device="cuda")
+    lengths = torch.full((seqs,), width * page, dtype=I32, device="cuda")
+    starts = torch.arange(seqs + 1, dtype=I32, device="cuda") % 2 * rows
+    assert seqs // 2 * (rows * heads // kv // 256) * kv * width >= 2 ** 31
+    q = torch.zeros((rows, heads, dim), dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 3.0)
+    status = torch.zeros(1, dtype=I32, device="cuda")
+    pvq.fp8_attention(q, cache, table, lengths, starts, out=out, status=status)
+    assert bool((out == 3.0).all()) and int(status) == pvq.STATUS_BAD_PAGE
