@@ -24,6 +24,7 @@ __host__ __device__ constexpr int item_units() {
 constexpr int kLeastTiles = 2;   // of a block
 constexpr int kScaleSlots = 8;   // tiles whose scales are on their way
 constexpr float kNone = -INFINITY;
+constexpr float kLargest = 0x1.fffffep127f;
 
 // A part: fp32 sums [rows][128], then what the weights are relative to (as an exponent of 2) and their sum, a row each.
 template <int ROWS>
@@ -374,6 +375,9 @@ __device__ __forceinline__ void two_codes(float x, float y, uint32_t& hi, uint32
     const float2 h = values_of(hi);
     lo = codes_of((x - h.x) * apart, (y - h.y) * apart);
 }
+
+// What a row's scores in codes are times, but for the key's scale.  Finite, so that a score of zero stays zero.
+__device__ __forceinline__ float row_factor(uint32_t byte, float scale) { return fminf(scale_of(byte) * scale, kLargest); }
 
 int cache_maps(const Cache& c, CacheMaps* maps);
 int attention_few(const AttentionArgs& a, int rows, int blocks, cudaStream_t s);  // 4, 8, 16 or 32 rows an item

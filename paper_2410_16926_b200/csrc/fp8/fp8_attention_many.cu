@@ -193,7 +193,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             __syncwarp();
             if (lane == 0 && count > 0) barrier_arrive(queries_full + 8 * which);
             const bool finite = byte != 255u;
-            const float factor = finite ? scale_of(byte) * p.scale : p.scale;
+            // (At least 2^-86, so that no page's scale, 2^-40 at least, makes it 0, times -inf: a score is off by 2^-21 at most, under 2^40.)
+            const float factor = fmaxf(finite ? row_factor(byte, p.scale) : p.scale, 0x1p-86f);
             // what every row of the warp sees
             const int all_to = __reduce_min_sync(0xffffffffu, to), all_from = __reduce_max_sync(0xffffffffu, from);
             float top = kNone, weight = 0.0f;
@@ -213,8 +214,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
                     const int first = (walk.begin() + t) * kTile + 64 * half;
                     const float4 keys = *reinterpret_cast<const float4*>(&page_scales[slot][0][4 * half]), value = *reinterpret_cast<const float4*>(&page_scales[slot][1][4 * half]),
                                  out_of = *reinterpret_cast<const float4*>(&page_scales[slot][2][4 * half]);
-                    const float key[4] = {fmaxf(factor * keys.x, 0x1p-120f), fmaxf(factor * keys.y, 0x1p-120f), fmaxf(factor * keys.z, 0x1p-120f),
-                                          fmaxf(factor * keys.w, 0x1p-120f)};  // (never 0: times -inf)
+                    const float key[4] = {fminf(factor * keys.x, kLargest), fminf(factor * keys.y, kLargest), fminf(factor * keys.z, kLargest),
+                                          fminf(factor * keys.w, kLargest)};  // (never inf: times 0)
                     tensor_wait(s[0]);
                     tensor_wait(s[1]);
                     if (first < all_from || first + 64 > all_to) {

@@ -1,5 +1,6 @@
 // The entry points of the 8-bit cache: argument checks, then the launches.
 #include <cmath>
+#include <limits>
 
 #include "fp8_cache.cuh"
 
@@ -104,7 +105,7 @@ extern "C" int pvq_fp8_attention(const pvq_fp8_cache* cache, const pvq_fp8_step*
     a.heads = heads, a.group = heads / a.cache.heads;
     a.causal = causal;
     a.window = static_cast<int>(window < (int64_t(1) << 30) ? window : 0);  // (no position in a table is farther behind another)
-    a.scale = scale * 1.44269504088896f;
+    a.scale = std::fmin(scale * 1.44269504088896f, std::numeric_limits<float>::max());
     a.status = d_status;
     a.workspace = static_cast<float*>(d_workspace);
     try {  // (the launchers keep small maps of what they asked the driver, and there may be no memory for them)

@@ -129,3 +129,29 @@ def test_overlapping_sequences_of_more_than_2_to_31_tiles(heads, kv):
     status = torch.zeros(1, dtype=I32, device="cuda")
     pvq.fp8_attention(q, cache, table, lengths, starts, out=out, status=status)
     assert bool((out == 3.0).all()) and int(status) == pvq.STATUS_BAD_PAGE
+
+
+@pytest.mark.parametrize("scale", [None, 3e38])
+@pytest.mark.parametrize("size", [1e25, 1e30, 3e38])
+@pytest.mark.parametrize("n", [1, 8, 60])
+def test_keys_of_zero_under_factors_beyond_fp32(n, size, scale):
+    """Query values times the scale times a page's scale beyond fp32: a score of zero stays zero, and one that is far below takes no part."""
+    heads, kv, dim, page, length = 8, 2, 64, 32, 300
+    rng = np.random.default_rng(n)
+    table, pool = tables(rng, [length], page)
+    cache = filled(rng, table, [length], pool, kv, page, dim)
+    keys = cache.k.view(torch.uint8)
+    keys.fill_(0)
+    keys[int(table[0][2])] = 0xb8  # -1
+    cache.k_scales.view(torch.uint8).fill_(127 + 40)
+    q = torch.full((n, heads, dim), size, dtype=torch.bfloat16, device="cuda")
+    out, lse = pvq.fp8_attention(q, cache, ints(table), ints([length]), ints([0, n]), causal=False, lse=True, **({} if scale is None else dict(scale=scale)))
+    kept = [t for t in range(length) if not 2 * page <= t < 3 * page]
+    for h in range(kv):
+        ids = torch.from_numpy(np.ascontiguousarray(table[0])).cuda()
+        v = cache.v.view(torch.uint8)[ids, h].view(torch.float8_e4m3fn).double() * torch.exp2(cache.v_scales.view(torch.uint8)[ids, h].double() - 127)[:, None, None]
+        v = v.flatten(0, 1)[kept]
+        got = out[:, h * 4:h * 4 + 4].double()
+        # equal weights: off by 2^-8 of themselves, the result by as much again
+        assert bool(((got - v.mean(dim=0)).abs() <= 2.0 ** -7 * v.abs().mean(dim=0)).all())
+    assert bool(((lse.double() - np.log(len(kept))).abs() <= 2.0 ** -18).all())
