@@ -54,13 +54,16 @@ struct Item {
     }
 };
 
+// The first position that a row at `position` (negative in front of its sequence) sees.
+__device__ __forceinline__ int first_seen(const AttentionArgs& a, int position) { return a.window > 0 && position >= a.window ? position - a.window + 1 : 0; }
+
 template <int ROWS>
 __device__ __forceinline__ void measure(const AttentionArgs& a, Item& it) {
     it.q0 = it.block * ROWS;
     it.rows = min(ROWS, it.q.n * a.group - it.q0);
     const int i0 = divide(it.q0, a.by_group), i1 = divide(it.q0 + it.rows - 1, a.by_group);
     it.hi = a.causal ? min(it.q.held, it.q.first + i1 + 1) : it.q.held;
-    it.lo = a.window > 0 ? max(0, it.q.first + i0 - a.window + 1) : 0;
+    it.lo = first_seen(a, it.q.first + i0);
 }
 template <int ROWS>
 __device__ __forceinline__ int blocks_of(const AttentionArgs& a, const Sequence& q) {

@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                         const int position = it.q.first + divide(it.q0 + r, p.by_group);
                         factor[r] = most < kFiniteEnd ? row_factor(byte, p.scale) : __uint_as_float(0x7fffffffu);
                         to[r] = r < it.rows ? (p.causal ? min(it.q.held, position + 1) : it.q.held) : 0;
-                        from[r] = p.window > 0 ? max(0, position - p.window + 1) : 0;
+                        from[r] = first_seen(p, position);
                     }
                 }
                 async_fence();

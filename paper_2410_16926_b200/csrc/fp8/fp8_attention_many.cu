@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             }
             const RowPlace place = place_of(p, it.q, it.head, it.q0 + min(which * 128 + row, it.rows - 1));
             const int position = it.q.first + place.row - it.q.row;
-            const int to = p.causal ? min(it.q.held, position + 1) : it.q.held, from = p.window > 0 ? max(0, position - p.window + 1) : 0;
+            const int to = p.causal ? min(it.q.held, position + 1) : it.q.held, from = first_seen(p, position);
             uint32_t byte = 127u;
             // The warp's 32 rows of queries: 16 lanes a row, eight dims each.  None where the item has no tiles in this share: nothing would hold the warps
             // together then, so that one could put its results where another's queries are on their way, and a phase of queries_full pass unseen.

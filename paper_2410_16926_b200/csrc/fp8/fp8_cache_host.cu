@@ -1,5 +1,7 @@
 // The entry points of the 8-bit cache: argument checks, then the launches.
+#include <algorithm>
 #include <cmath>
+#include <cstdint>
 #include <limits>
 
 #include "fp8_cache.cuh"
@@ -104,7 +106,7 @@ extern "C" int pvq_fp8_attention(const pvq_fp8_cache* cache, const pvq_fp8_step*
     a.q_row = q_row, a.q_head = q_head, a.out_row = out_row, a.out_head = out_head;
     a.heads = heads, a.group = heads / a.cache.heads;
     a.causal = causal;
-    a.window = static_cast<int>(window < (int64_t(1) << 30) ? window : 0);  // (no position in a table is farther behind another)
+    a.window = static_cast<int>(std::min<int64_t>(window, INT32_MAX));  // (positions are below that)
     a.scale = std::fmin(scale * 1.44269504088896f, std::numeric_limits<float>::max());
     a.status = d_status;
     a.workspace = static_cast<float*>(d_workspace);

@@ -155,3 +155,29 @@ def test_keys_of_zero_under_factors_beyond_fp32(n, size, scale):
         # equal weights: off by 2^-8 of themselves, the result by as much again
         assert bool(((got - v.mean(dim=0)).abs() <= 2.0 ** -7 * v.abs().mean(dim=0)).all())
     assert bool(((lse.double() - np.log(len(kept))).abs() <= 2.0 ** -18).all())
+
+
+@pytest.mark.parametrize("n", [1, 3, 60])
+@pytest.mark.parametrize("length,window", [(2 ** 31 - 1, 2 ** 30), (2 ** 31 - 1, 2 ** 31 - 200), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31 - 1, 2 ** 40), (2 ** 30 + 200, 2 ** 30),
+                                           (700, 2 ** 30 - 1), (700, 2 ** 31 - 1), (700, 2 ** 62)])
+def test_windows_of_any_size(n, length, window):
+    """Lengths beyond the table: what lies behind the window is not seen, however wide it is."""
+    heads, kv, dim, page, held = 4, 2, 64, 32, 704
+    rng = np.random.default_rng(n)
+    table, pool = tables(rng, [held], page)
+    cache = filled(rng, table, [held], pool, kv, page, dim)
+    q = queries(rng, n, heads, dim)
+    out, lse = pvq.fp8_attention(q, cache, ints(table), ints([length]), ints([0, n]), window=window, lse=True)
+    for i in range(n):
+        at = length - n + i
+        low, high = max(0, at - window + 1), min(held, at + 1)
+        if low >= high:
+            assert bool((out[i] == 0).all()) and bool((lse[i] == -float("inf")).all())
+            continue
+        # the same row as the last of a sequence that ends with it, or with the table, and a window of what it sees
+        want = pvq.fp8_attention(q[i:i + 1], cache, ints(table), ints([high]), window=high - low, lse=True)
+        # each call off by 2^-8 of its result, its weights by 2^-8 of themselves and less for their scores: 2^-7 of the largest value in all, that is
+        # 448 times the largest scale
+        largest = 448.0 * 2.0 ** (int(cache.v_scales.view(torch.uint8).max()) - 127)
+        assert bool(((out[i:i + 1].float() - want[0].float()).abs() <= 2.0 ** -7 * want[0].float().abs() + 2.0 ** -6 * largest).all())
+        assert bool(((lse[i:i + 1] - want[1]).abs() <= 2.0 ** -10).all())
