@@ -488,8 +488,8 @@ size_t pvq_fp8_attention_workspace(const pvq_fp8_cache* cache, const pvq_fp8_ste
 #define PVQ_DEBUG_WITHHOLD 0x80000000u
 /* Set by the caller in the status word of pvq_fp8_matmul and pvq_fp8_weight_grad, as PVQ_DEBUG_WITHHOLD
  * may be there, too: only the copies of every second thread block of a cluster, or the scales (of the
- * weight gradient: the conversion) are withheld, from a few stages into the call on.  In that of pvq_fp8_attention the last
- * bit makes the scales of pages come late. */
+ * weight gradient: the conversion) are withheld, from a few stages into the call on.  In that of pvq_fp8_attention
+ * the first withholds the copies of every second block, of a cluster or not, and the last makes the scales of pages come late. */
 #define PVQ_DEBUG_WITHHOLD_SECOND 0x40000000u
 #define PVQ_DEBUG_WITHHOLD_SCALES 0x20000000u
 

@@ -409,7 +409,8 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
             tokens_meet();
             if (CLUSTER && p.split > 1) {
                 // The parts of the cluster's blocks, in the stages' place, which is free once all are here: those of a share of the dims go to the
-                // block that adds them up, in the order of the ranks: [rank][row][dim of the share], then [rank][largest, weights][row].
+                // block that adds them up, in the order of the ranks: [rank][row][dim of the share], then [rank][largest, weights][row].  (Copies of a block whose
+                // wait ran out may still come over them: its dims are NaN then, as its part makes the others'.)
                 const int split = p.split, share = 128 / split;
                 const uint32_t stats = base + ROWS * 512;
                 float all = 0.0f, relative = kNone;
@@ -429,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_few_kernel(const __grid
                 cluster_barrier();
                 for (int i = thread; i < it.rows * share; i += 128) {
                     const int n = i / share, d = i - n * share;
-                    float m[8], top = kNone;
+                    float m[8], top = over ? __uint_as_float(0x7fffffffu) : kNone;
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
                         m[r] = kNone;
