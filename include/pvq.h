@@ -420,6 +420,7 @@ size_t pvq_fp8_weight_grad_workspace(int64_t rows, int64_t inner, int64_t outer)
  *              s.  Rows in front of the first and behind the last are neither read nor written.  Where they descend,
  *              attention writes nothing (PVQ_STATUS_BAD_PAGE), and what is written to the cache or read from it is not defined.  NULL: one
  *              row a sequence, rows == seqs.
+ * A step has a sequence and a row at least (sequences may have none): others are refused, as matrices of no rows are.
  * All three are on the device (int32) and only looked at there; what they say is checked there, too: no access
  * leaves the pool, the table or the rows, whatever they hold, and PVQ_STATUS_BAD_PAGE is OR-ed into *d_status (optional) where a
  * position has no place.  Calls keep nothing, and can be captured into graphs.  The same inputs give the same bits. */

@@ -384,7 +384,8 @@ def fp8_weight_grad(dy, x, dtype=torch.float32, out=None, status=None, workspace
 # k, v: float8_e4m3fn [pages][heads][page][dim], page 16, 32, 64 or 128, dim a multiple of 16 up to 128; k_scales, v_scales:
 # float8_e8m0fnu [pages][heads].  Views of other orders will do, as long as a token's dims lie together, and keys and values alike.
 # A step's calls share `table` int32 [seqs][pages of the longest], `lengths` int32 [seqs] (with the step's tokens) and `starts` int32
-# [seqs + 1]: rows starts[s] to starts[s + 1] are the last tokens of sequence s; None: one row a sequence.  They stay on the GPU.
+# [seqs + 1]: rows starts[s] to starts[s + 1] are the last tokens of sequence s; None: one row a sequence.  They stay on the GPU.  A sequence may have no rows; a
+# step without any, or without sequences, is refused.
 Fp8Cache = collections.namedtuple("Fp8Cache", "k v k_scales v_scales")
 
 

@@ -181,3 +181,18 @@ def test_windows_of_any_size(n, length, window):
         largest = 448.0 * 2.0 ** (int(cache.v_scales.view(torch.uint8).max()) - 127)
         assert bool(((out[i:i + 1].float() - want[0].float()).abs() <= 2.0 ** -7 * want[0].float().abs() + 2.0 ** -6 * largest).all())
         assert bool(((lse[i:i + 1] - want[1]).abs() <= 2.0 ** -10).all())
+
+
+def test_steps_without_rows_or_sequences_are_refused():
+    cache = pvq.alloc_fp8_cache(2, 2, 16, 32)
+    for c in cache:
+        c.view(torch.uint8).fill_(0x38)
+    kept = [c.view(torch.uint8).clone() for c in cache]
+    x, q = torch.zeros(0, 2, 32, device="cuda"), torch.zeros(0, 4, 32, device="cuda", dtype=torch.bfloat16)
+    nothing = torch.zeros((0, 1), dtype=I32, device="cuda"), ints([])
+    for step in ((ints([[0], [1]]), ints([0, 0]), ints([0, 0, 0])), (*nothing, None), (*nothing, ints([0])), (ints([[], []]), ints([1, 1]), ints([0, 0, 0]))):
+        for call in (lambda: pvq.fp8_cache_write(x, x, cache, *step), lambda: pvq.fp8_cache_read(cache, *step, rows=0), lambda: pvq.fp8_attention(q, cache, *step)):
+            with pytest.raises(pvq.PvqError):
+                call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(c.view(torch.uint8), k) for c, k in zip(cache, kept))
