@@ -145,12 +145,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
         if (threadIdx.x == 0 && gridDim.x > 1) head->parts = 0;
         const uint32_t scores_bar = scores_full + 16 * which, weights_bar = weights_full + 16 * which;
         uint32_t tile = 0, phase = 0;  // tiles of this block; phases of each half's scores
+        int passed = 0;                // tiles of items without rows here since the last that had some
         bool ok = true;
         for (; walk.there(); walk.next()) {
             const Item& it = walk.it;
             const int count = walk.count();
             if (it.rows <= 128 * which) {  // no rows here
                 tile += count;
+                passed += count;
                 continue;
             }
             const RowPlace place = place_of(p, it.q, it.head, it.q0 + min(which * 128 + row, it.rows - 1));
@@ -202,7 +204,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_many_kernel(const __gri
             if (count > 0) {
                 // Scores first: when they are there, the slot's scales of eight tiles ago are long past, so that the parity can only mean these.  (Warps
                 // that had no rows in the items before did not wait for those items' scales.)
-                ok = ok && warp_waits(scores_bar, phase & 1, bounds) && warp_waits(scales_full + 8 * (tile % kScaleSlots), (tile / kScaleSlots) & 1, bounds);
+                // The other tile of rows may have all those items before it: a poll more for each of their tiles, of 2.2 us.
+                Bounds longer = bounds;
+                longer.polls += min(passed, 1 << 24) << 6;
+                passed = 0;
+                ok = ok && warp_waits(scores_bar, phase & 1, longer) && warp_waits(scales_full + 8 * (tile % kScaleSlots), (tile / kScaleSlots) & 1, bounds);
                 tensor_fence_after();
                 tensor_load(scores, s[0]);
                 tensor_load(scores + 32, s[1]);

@@ -196,3 +196,21 @@ def test_steps_without_rows_or_sequences_are_refused():
                 call()
     torch.cuda.synchronize()
     assert all(torch.equal(c.view(torch.uint8), k) for c, k in zip(cache, kept))
+
+
+def test_items_of_few_rows_that_take_long():
+    """Sequences of 2^20 tokens and 100 rows, one after another in a thread block, before one of 300 rows: its second tile of rows has nothing to do for
+    a third of a second, which is no reason to give up.  All values are ones."""
+    page, width, per, dim = 128, 8192, 22, 64
+    new, lengths = [], []
+    for _ in range(150):  # more than there are thread blocks
+        new += [100] * per + [300]
+        lengths += [width * page] * per + [300]
+    cache = pvq.alloc_fp8_cache(1, 1, page, dim)
+    for c, byte in zip(cache, (0x38, 0x38, 127, 127)):
+        c.view(torch.uint8).fill_(byte)
+    table = torch.zeros((len(new), width), dtype=I32, device="cuda")
+    q = queries(np.random.default_rng(1), sum(new), 1, dim)
+    status = torch.zeros(1, dtype=I32, device="cuda")
+    out = pvq.fp8_attention(q, cache, table, ints(lengths), ints([0] + [int(x) for x in np.cumsum(new)]), status=status)
+    assert int(status) == 0 and bool((out == 1).all())
