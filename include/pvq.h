@@ -461,15 +461,17 @@ int pvq_fp8_cache_read(const pvq_fp8_cache* cache, const pvq_fp8_step* step, voi
  *   d_lse       [row][heads] fp32, or NULL: log sum_j exp(scale q . k_j).
  *   scale       positive.
  * Calls whose rows, heads and table would make 2^31 tiles of work or more, six added for each block of 256 query rows, are refused (PVQ_ERR_UNSUPPORTED).
+ * One kernel takes all sequences of a call, by the mean number of their rows: a step of prompts and single tokens is done sooner as two calls.
  *   d_workspace pvq_fp8_attention_workspace bytes, 16-byte aligned, free again when the call's work is done.  NULL where
  *               that is 0.
  *   d_status    as above, and PVQ_STATUS_STAGING_TIMEOUT when a thread block gave up waiting for its copies (its results are
  *               NaN then).
  * Scores and sums are held in fp32, over queries taken to 2^-17 of a row's largest value, and the result rounded once.  Weights
- * (of w_j 2^e, where 2^e is the scale of the values' page) are off by at most 2^-8 of themselves or, where that is more, by 2^-22 of
- * the largest among 128 tokens (positions 128 i to 128 i + 127); or, where steps have more than 32 rows times heads / cache->heads a sequence on
- * average, by 2^-11 of themselves or 2^-32 of the row's largest.  The sum that divides takes them unrounded.  What keys and values hold that no row of a block of rows sees has no
- * influence, NaN or not; a NaN among the values that some row of a sequence sees may reach all of its rows in the call. */
+ * (times the scales of their values' pages) are off by at most 2^-8 of themselves or, where that is more, by 2^-22 of the largest among
+ * their 128 tokens (positions 128 i to 128 i + 127); where sequences have more than 32 rows on average, times heads / cache->heads,
+ * by 2^-11 of themselves or 2^-32 of the row's largest.  The sum that divides takes them unrounded.  What keys and values hold that no
+ * row of a block of rows sees has no influence, NaN or not; a NaN among the values that some row of a sequence sees may reach all of
+ * its rows in the call. */
 int pvq_fp8_attention(const pvq_fp8_cache* cache, const pvq_fp8_step* step, const void* d_q, int heads, int64_t q_row, int64_t q_head, int causal,
                       int64_t window, float scale, void* d_out, int64_t out_row, int64_t out_head, float* d_lse, void* d_workspace,
                       size_t workspace_bytes, uint32_t* d_status, pvq_stream_t stream);

@@ -66,13 +66,15 @@ __global__ void __launch_bounds__(32 * kJoinRows) attention_join_kernel(const __
 struct Form {
     int rows, blocks, split;
 };
+// By the mean: lengths and starts are on the device.  A step of both kinds takes one kernel's time for the other's work (255 single tokens behind 4096
+// and a prompt of 4096 1461 us, apart 328 and 222).
 Form form_of(const Cache& c, const Step& p, int heads) {
     const int group = heads / c.heads;
     const int64_t each = (int64_t(p.rows) * group + p.seqs - 1) / p.seqs;  // rows of a sequence and head
     if (each > 32) return {256, kSms, 0};
     Form f{each <= 4 ? 4 : (each <= 8 ? 8 : (each <= 16 ? 16 : 32)), 2 * kSms, 0};
     // Single tokens of few sequences whose tables are short: an item for a cluster, whose blocks find their work without a scan and join it without
-    // a second kernel.  8 heads, in us, so and with shares: one sequence of 100 tokens 4.6 and 10.3, of 1000 6.0 and 9.5, of 16000 17.2 and 21.8; 37 of 2000
+    // a second kernel.  8 heads, in us, so and with shares: one sequence of 100 tokens 4.6 and 10.3, of 1000 6.2 and 9.5, of 16000 17.2 and 21.8; 37 of 2000
     // (one block an item) 28.8 and 31.4, of a quarter of that and up 21.3 and 25.5; 4 of 8000 20.0 and 18.3.
     const int64_t items = int64_t(p.seqs) * c.heads, tiles = ((int64_t(p.width) << c.page_shift) + kTile - 1) / kTile;
     if (!p.starts && f.rows <= 16 && items <= kAtOnce[0]) {

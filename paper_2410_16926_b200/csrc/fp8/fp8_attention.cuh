@@ -16,7 +16,7 @@ struct CacheMaps {
 
 // What an item costs besides its tiles, in tiles: of 256 rows, queries made codes, the first scores, the results, 10 to 20 us by 2.2 a tile.  A causal
 // prompt's first blocks of rows are items of few tiles; thread blocks that got many of them ended last.  32 heads over 8 of 128 dims, in us, with 0, 4, 6
-// and 10: 8192 causal tokens 816, 636, 610, 632; 8 of 1024 236, 215, 212, 219; 4096 seen by all 325, 320, 321, 333.  Few rows begin in a tile's time: 0.
+// and 10: 8192 causal tokens 829, 655, 640, 651; 8 of 1024 238, 211, 209, 216; 4096 seen by all 333, 324, 324, 332.  Few rows begin in a tile's time: 0.
 template <int ROWS>
 __host__ __device__ constexpr int item_units() {
     return ROWS == 256 ? 6 : 0;

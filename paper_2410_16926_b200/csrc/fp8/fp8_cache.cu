@@ -101,8 +101,8 @@ __device__ __forceinline__ uint2 rescaled(uint2 c, float factor) {
 // A sequence with rows a to b gets b / page - a / page + 2 places for its pages, at least as many as it can touch wherever it
 // begins, from a / page + 2 s on: no sum over the sequences is needed, only a search for the last s with such a beginning.
 //
-// What bounds it: what has to be known one after the other (starts, lengths, the page's number, values) with four blocks an SM, and issue (71 %): 18400
-// rows of 8 heads of 128, bf16, 26.2 us, of which the bytes take 17.9 at the copy rate.  (Comparing values one by one, and holding them as fp32: 78 us.)
+// What bounds it: what has to be known one after the other (starts, lengths, the page's number, values) with four blocks an SM, and issue (69 %): 18400
+// rows of 8 heads of 128, bf16, 27.1 us from a graph (fp32 39.0), of which the bytes take 17.9 at the copy rate.  (Comparing values one by one, and holding them as fp32: 78 us.)
 template <class T>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) cache_write_kernel(const Cache c, const Step p, const Rows x, int64_t units, uint32_t* status) {
     __shared__ uint32_t most[kThreads / 32];
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kThreads) cache_write_few_kernel(const Cache c
 constexpr int kMostRows = 32;  // of a reading block
 
 // 32 bytes of result a thread, of two rows at once.  A warp of the block finds its rows' places first.  Bound by memory: 43500 tokens of 8 heads of
-// 128 to bf16 89 us, of which the bytes take 81.7 at the copy rate.
+// 128 to bf16 89.3 us from a graph, of which the bytes take 81.7 at the copy rate.
 template <class T>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(const Cache c, const Step p, const Rows x, int rows, uint32_t* status) {
     constexpr int kEach = 32 / sizeof(T);
