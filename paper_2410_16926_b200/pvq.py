@@ -412,7 +412,8 @@ def fp8_cache_read(cache, table, lengths, starts=None, rows=None, dtype=torch.bf
 def fp8_attention(q, cache, table, lengths, starts=None, causal=True, window=0, scale=None, lse=False, out=None, status=None):
     """Attention of q [rows][query heads][dim] bfloat16 to what the sequences hold -> bfloat16 of the same shape.  A row at position i
     sees positions j < lengths[s], j <= i with `causal`, j > i - window with `window`; what sees nothing is zeros.  scale:
-    1 / sqrt(dim) if not given.  With `lse` also float32 [rows][query heads], the logarithm of the sum of exp(scale q k).  Rows of no
+    1 / sqrt(dim) if not given.  One kernel takes all sequences, by the mean number of their rows: prompts and single tokens are done sooner in
+    two calls.  With `lse` also float32 [rows][query heads], the logarithm of the sum of exp(scale q k).  Rows of no
     sequence are left as they were (in new tensors: whatever was there).  `status` as above, and STATUS_STAGING_TIMEOUT as for fp8_matmul."""
     return (_native or _load_native()).fp8_attention(q, *cache, table, lengths, starts, causal, window,
                                                      1 / math.sqrt(q.shape[-1]) if scale is None else scale, lse, out, status)
